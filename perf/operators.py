@@ -9,8 +9,10 @@ number of experts that the library routes over.
 Kinds of case
   gate      scores, balance bias, groups, top-K and gates from router logits (fp32 [T, E])
   gate_bwd  the gradient of those gates with respect to the logits
-  mx        quantisation of a matrix to MX blocks and back to the values they stand for
-  experts   the routed and shared experts of one layer on MX weights, given the routing
+  mx        quantisation of a matrix to MX blocks of 4-bit elements (E2M1, 32 to a scale) and back to the
+            values they stand for
+  experts   the routed and shared experts of one layer on MX weights, given the routing; the activations in
+            bf16, or in MX blocks too
 """
 
 import math
@@ -26,12 +28,11 @@ MODELS = {
     "tiny": dict(d=256, F=512, E=8, K=2, ns=0, renorm=True),
 }
 BLOCK = 32
-EMAX = {"e2m1": 2, "e4m3": 8}
 
 
 def _gate(T, E, K, score, **kw):
     c = dict(kind="gate", T=T, E=E, K=K, score=score, groups=1, topk_group=1, rule="max", renorm=True, scale=1.0,
-             bias=False, mask=False, prior=False)
+             bias=False, mask=False, prior=False, spread=1.3)
     c.update(kw)
     return c
 
@@ -51,20 +52,20 @@ def listed():
         # pre-training batch, sigmoid scores renormalised: only the selected experts get a gradient
         dict(_gate(65536, 256, 8, "sigmoid", groups=8, topk_group=4, rule="sum2", bias=True, scale=2.5),
              kind="gate_bwd", name="gate_bwd_t65536_e256"),
-        # activations of a short prompt to 8 bits and back
-        dict(kind="mx", rows=333, cols=2048, fmt="e4m3", src="bf16", name="mx8_act_333"),
+        # activations of a short prompt
+        dict(kind="mx", rows=333, cols=2048, src="bf16", name="mx4_act_333"),
         # one Mixtral-shaped expert's gate / up matrix to 4 bits: the conversion of a checkpoint
-        dict(kind="mx", rows=28672, cols=4096, fmt="e2m1", src="bf16", name="mx4_weight_mixtral"),
+        dict(kind="mx", rows=28672, cols=4096, src="bf16", name="mx4_weight_mixtral"),
         # interactive decode, one token
-        dict(kind="experts", model="mixtral", T=1, act="e4m3", pad=0, name="experts_mixtral_t1"),
+        dict(kind="experts", model="mixtral", T=1, act="bf16", pad=0, spread=1.3, name="experts_mixtral_t1"),
         # few tokens through many small experts
-        dict(kind="experts", model="deepseek", T=5, act="e4m3", pad=0, name="experts_deepseek_t5"),
+        dict(kind="experts", model="deepseek", T=5, act="bf16", pad=0, spread=1.3, name="experts_deepseek_t5"),
         # a serving step with continuous batching: about a hundred sequences, some slots empty
-        dict(kind="experts", model="mixtral", T=96, act="e4m3", pad=5, name="experts_mixtral_t96"),
+        dict(kind="experts", model="mixtral", T=96, act="bf16", pad=5, spread=1.3, name="experts_mixtral_t96"),
         # prefill of the smaller model with 4-bit activations: the matrix units' fastest type
-        dict(kind="experts", model="deepseek", T=4096, act="e2m1", pad=0, name="experts_deepseek_t4096"),
+        dict(kind="experts", model="deepseek", T=4096, act="mx4", pad=0, spread=1.3, name="experts_deepseek_t4096"),
         # a large prefill, 4 x 2048 tokens
-        dict(kind="experts", model="mixtral", T=8192, act="e4m3", pad=0, name="experts_mixtral_t8192"),
+        dict(kind="experts", model="mixtral", T=8192, act="bf16", pad=0, spread=1.3, name="experts_mixtral_t8192"),
     ]
 
 
@@ -80,7 +81,7 @@ def _draw_gate(rng):
     return _gate(_log_int(rng, 1, 131072), E, K, rng.choice(["softmax", "sigmoid"]), groups=groups,
                  topk_group=rng.randint(need, groups), rule=rng.choice(["max", "sum2"]), renorm=rng.random() < 0.6,
                  scale=rng.choice([1.0, 1.0, 2.5, 16.0]), bias=rng.random() < 0.6, mask=rng.random() < 0.3,
-                 prior=rng.random() < 0.3)
+                 prior=rng.random() < 0.3, spread=round(rng.uniform(0.5, 2.5), 2))
 
 
 def draw(rng):
@@ -92,11 +93,11 @@ def draw(rng):
         return dict(c, kind="gate_bwd", T=min(c["T"], 65536))
     if kind == "mx":
         return dict(kind="mx", rows=_log_int(rng, 1, 28000), cols=32 * _log_int(rng, 1, 128),
-                    fmt=rng.choice(["e2m1", "e4m3"]), src=rng.choice(["bf16", "f32"]))
+                    src=rng.choice(["bf16", "f32"]))
     model = rng.choice(["mixtral", "deepseek", "tiny"])
     T = _log_int(rng, 1, 8192)
-    return dict(kind="experts", model=model, T=T, act=rng.choice(["e4m3", "e2m1"]),
-                pad=rng.choice([0, 0, T // 7]))
+    return dict(kind="experts", model=model, T=T, act=rng.choice(["bf16", "mx4"]),
+                pad=rng.choice([0, 0, T // 7]), spread=round(rng.uniform(0.5, 2.5), 2))
 
 
 # ---------------------------------------------------------------- inputs
@@ -113,27 +114,23 @@ def _pow2(byte):
     return torch.where(b == 0, 1 << 22, b << 23).view(torch.float32)
 
 
-def _mx(x, fmt):
+def _mx(x):
     """Blocks of 32 along the last dimension: (element values before scaling, E8M0 bytes), fp32 and uint8."""
     v = x.float().unflatten(-1, (-1, BLOCK))
     amax = v.abs().amax(-1, keepdim=True)
-    e = torch.frexp(amax).exponent - 1 - EMAX[fmt]
+    e = torch.frexp(amax).exponent - 1 - 2
     byte = torch.where(amax > 0, e + 127, 0).clamp(0, 254).to(torch.uint8)
     # two exact steps: the reciprocal of the smallest scales is no finite number
     half = byte.int() // 2
     q = v * _pow2(254 - 127 + 64 - half) * _pow2(127 + 63 - (byte.int() - half))
     mag = q.abs()
-    if fmt == "e2m1":
-        step = torch.where(mag < 2, 0.5, torch.where(mag < 4, 1.0, 2.0))
-        mag = (torch.round(mag / step) * step).clamp(max=6.0)
-    else:
-        step = _pow2((torch.frexp(mag).exponent - 1).clamp(-6, 8) - 3 + 127)
-        mag = (torch.round(mag / step) * step).clamp(max=448.0)
+    step = torch.where(mag < 2, 0.5, torch.where(mag < 4, 1.0, 2.0))
+    mag = (torch.round(mag / step) * step).clamp(max=6.0)
     return torch.copysign(mag, q).flatten(-2), byte.squeeze(-1)
 
 
-def _mx_values(x, fmt):
-    q, byte = _mx(x, fmt)
+def _mx_values(x):
+    q, byte = _mx(x)
     return (q.unflatten(-1, (-1, BLOCK)) * _pow2(byte).unsqueeze(-1)).flatten(-2)
 
 
@@ -155,10 +152,11 @@ def _from_codes(codes, byte):
 
 
 def _gate_inputs(case, seed):
-    """Router logits of unit-variance tokens, the balance bias of a router in training, a learned mask or prior."""
+    """Router logits (spread: their deviation, which decides how uneven the routing is), the balance bias of a
+    router in training, a learned mask or prior."""
     g = _gen(seed)
     T, E, K = case["T"], case["E"], case["K"]
-    s = dict(logits=torch.randn((T, E), generator=g, device="cuda").mul_(1.3))
+    s = dict(logits=torch.randn((T, E), generator=g, device="cuda").mul_(case["spread"]))
     s["bias"] = torch.randn(E, generator=g, device="cuda").mul_(0.05 if case["score"] == "sigmoid" else 0.2 / E) \
         if case["bias"] else None
     rs = np.random.RandomState(seed % (1 << 31))
@@ -181,7 +179,7 @@ def _weights(g, n, rows, cols):
     scales = torch.empty((n, rows, cols // BLOCK), dtype=torch.uint8, device="cuda")
     for i in range(n):
         w = torch.randn((rows, cols), generator=g, device="cuda", dtype=torch.bfloat16).mul_(cols ** -0.5)
-        q, scales[i] = _mx(w, "e2m1")
+        q, scales[i] = _mx(w)
         codes[i] = _to_codes(q)
     return codes, scales
 
@@ -196,7 +194,7 @@ def _expert_inputs(case, seed):
     s = dict(x=(torch.randn((T, d), generator=g, device="cuda") * loud).bfloat16())
     s["gu_codes"], s["gu_scales"] = _weights(g, E + ns, 2 * F, d)
     s["dn_codes"], s["dn_scales"] = _weights(g, E + ns, d, F)
-    p = torch.softmax(1.3 * torch.randn((T, E), generator=g, device="cuda"), -1)
+    p = torch.softmax(case["spread"] * torch.randn((T, E), generator=g, device="cuda"), -1)
     gate, idx = p.topk(K, -1)
     if m["renorm"]:
         gate = gate / gate.sum(-1, keepdim=True)
@@ -224,9 +222,9 @@ def prepare(case, seed):
         if own:   # the handle that a serving program keeps: packed weights, workspace
             from paper_2609_34077_amd import _lib as L
             m = MODELS[case["model"]]
-            s["packed"] = L.maskmoe_mx_pack_experts(s["gu_codes"], s["gu_scales"], s["dn_codes"], s["dn_scales"])
+            s["packed"] = L.maskmoe_mx4_pack_experts(s["gu_codes"], s["gu_scales"], s["dn_codes"], s["dn_scales"])
             s["workspace"] = torch.empty(
-                L.maskmoe_experts_mx_workspace_bytes(case["T"], m["d"], m["E"], m["K"], m["F"], m["ns"]),
+                L.maskmoe_experts_mx4_workspace_bytes(case["T"], m["d"], m["E"], m["K"], m["F"], m["ns"]),
                 dtype=torch.uint8, device="cuda")
     s["case"] = dict(case)
     return s
@@ -294,17 +292,19 @@ def _gate_bwd_plain(case, s):
 
 
 def _ffn(x, wg, ws, dg, dsc, act):
-    """SwiGLU experts on rows x [n, rows, d] (values of MX blocks), weights of n experts."""
+    """SwiGLU experts on rows x [n, rows, d], weights of n experts."""
     ab = torch.bmm(x, _from_codes(wg, ws).transpose(1, 2))
     a, b = ab.chunk(2, -1)
-    h = _mx_values(a / (1 + torch.exp(-a)) * b, act)
+    h = a / (1 + torch.exp(-a)) * b
+    if act == "mx4":
+        h = _mx_values(h)
     return torch.bmm(h, _from_codes(dg, dsc).transpose(1, 2))
 
 
 def _experts_plain(case, s):
     m = MODELS[case["model"]]
     E, K, T, cap = m["E"], m["K"], case["T"], s["cap"]
-    x = _mx_values(s["x"], case["act"])
+    x = _mx_values(s["x"]) if case["act"] == "mx4" else s["x"].float()
     y = torch.zeros_like(x)
     if len(s["active"]):
         act = torch.from_numpy(s["active"]).to(x.device).long()
@@ -338,7 +338,7 @@ def run(state):
         if kind == "gate_bwd":
             return dict(d_logits=_gate_bwd_plain(case, s))
         if kind == "mx":
-            return dict(values=_mx_values(s["x"], case["fmt"]).bfloat16())
+            return dict(values=_mx_values(s["x"]).bfloat16())
         return dict(y=_experts_plain(case, s))
     from paper_2609_34077_amd import _lib as L
     if kind in ("gate", "gate_bwd"):
@@ -352,12 +352,11 @@ def run(state):
             scale=case["scale"], bias=s["bias"], mask=s["mask"], prior=s["prior"], with_load=True)
         return dict(idx=idx, gate=gate, load=load)
     if kind == "mx":
-        fmt = L.MX_E2M1 if case["fmt"] == "e2m1" else L.MX_E4M3
-        codes, scales = L.maskmoe_mx_quantize(s["x"], fmt)
-        return dict(values=L.maskmoe_mx_dequantize(codes, scales, fmt, torch.bfloat16))
-    return dict(y=L.maskmoe_experts_forward_mx(
+        codes, scales = L.maskmoe_mx4_quantize(s["x"])
+        return dict(values=L.maskmoe_mx4_dequantize(codes, scales, torch.bfloat16))
+    return dict(y=L.maskmoe_experts_forward_mx4(
         s["x"], s["idx"], s["gate"], s["packed"], n_shared=MODELS[case["model"]]["ns"],
-        act=L.MX_E2M1 if case["act"] == "e2m1" else L.MX_E4M3, workspace=s["workspace"]))
+        act=L.ACT_MX4 if case["act"] == "mx4" else L.ACT_BF16, workspace=s["workspace"]))
 
 
 def work(case):
@@ -370,8 +369,7 @@ def work(case):
         return dict(bytes=4 * T * E + 4 * T * (E if dense else K) + 8 * T * K, flops=(10 if dense else 1) * T * E)
     if kind == "mx":
         n = case["rows"] * case["cols"]
-        code = (0.5 if case["fmt"] == "e2m1" else 1.0) + 1 / BLOCK
-        return dict(bytes=int(n * ((2 if case["src"] == "bf16" else 4) + 2 * code + 2)), flops=4 * n)
+        return dict(bytes=int(n * ((2 if case["src"] == "bf16" else 4) + 2 * (0.5 + 1 / BLOCK) + 2)), flops=4 * n)
     m = MODELS[case["model"]]
     d, F, E, K, ns = m["d"], m["F"], m["E"], m["K"], m["ns"]
     T, live = case["T"], case["T"] - case["pad"]
@@ -383,23 +381,18 @@ def work(case):
 
 # ---------------------------------------------------------------- the same in 64 bits
 
-def _grid(fmt):
-    """The non-negative values of an element type, in code order."""
-    if fmt == "e2m1":
-        return torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64)
-    return torch.tensor([(m / 8 * 2.0 ** -6) if e == 0 else (1 + m / 8) * 2.0 ** (e - 7)
-                         for e in range(16) for m in range(8)][:127], dtype=torch.float64)
+GRID = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64)   # E2M1 magnitudes in code order
 
 
-def _mx64(x, fmt):
+def _mx64(x):
     """The values of x's MX blocks: nearest on the scaled grid, ties to the even code."""
-    grid = _grid(fmt).to(x.device)
+    grid = GRID.to(x.device)
     mids = (grid[1:] + grid[:-1]) / 2
     v = x.double().reshape(-1, BLOCK)
     amax = v.abs().max(1, keepdim=True).values
     e = torch.where(amax > 0, torch.floor(torch.log2(amax)), -200.0)
     e = torch.where(amax < torch.exp2(e), e - 1, torch.where(amax >= torch.exp2(e + 1), e + 1, e))  # log2 at a border
-    scale = torch.exp2((e - EMAX[fmt]).clamp(min=-127))
+    scale = torch.exp2((e - 2).clamp(min=-127))
     u = (v / scale).abs()
     i = torch.bucketize(u, mids)
     i = i + ((u == mids[i.clamp(max=mids.numel() - 1)]) & (i % 2 == 1) & (i < mids.numel())).long()
@@ -407,7 +400,7 @@ def _mx64(x, fmt):
 
 
 def _weight64(codes, byte):
-    grid = _grid("e2m1").to(codes.device)
+    grid = GRID.to(codes.device)
     lut = torch.cat((grid, -grid))
     c = torch.empty(codes.shape[:-1] + (2 * codes.shape[-1],), dtype=torch.long, device=codes.device)
     c[..., 0::2], c[..., 1::2] = codes % 16, codes // 16
@@ -418,12 +411,12 @@ def exact(case, seed):
     kind = case["kind"]
     if kind == "mx":
         s = prepare(case, seed)
-        return dict(values=_mx64(s["x"], case["fmt"]))
+        return dict(values=_mx64(s["x"]))
     if kind == "experts":
         s = _expert_inputs(case, seed)
         m = MODELS[case["model"]]
         E, F, ns = m["E"], m["F"], m["ns"]
-        x = _mx64(s["x"], case["act"])
+        x = _mx64(s["x"]) if case["act"] == "mx4" else s["x"].double()
         y = torch.zeros_like(x)
         for e in range(E + ns):
             if e < E:
@@ -435,7 +428,9 @@ def exact(case, seed):
             if not t.numel():
                 continue
             ab = x[t] @ _weight64(s["gu_codes"][e], s["gu_scales"][e]).t()
-            h = _mx64(ab[:, :F] * torch.sigmoid(ab[:, :F]) * ab[:, F:], case["act"])
+            h = ab[:, :F] * torch.sigmoid(ab[:, :F]) * ab[:, F:]
+            if case["act"] == "mx4":
+                h = _mx64(h)
             y.index_add_(0, t, g[:, None] * (h @ _weight64(s["dn_codes"][e], s["dn_scales"][e]).t()))
         return dict(y=y)
     s = _gate_inputs(case, seed)
