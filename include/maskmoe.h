@@ -543,6 +543,140 @@ int maskmoe_stage1_backward(const maskmoe_layer_desc* desc, const void* x, const
                             float* d_gate, float* d_mask, float* d_mask_logits, float* d_w_router,
                             float* d_x, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ---- routing by scores, balance bias and expert groups ---- */
+
+/* Score of an expert: softmax p_e over all E experts, or sigmoid s_e = 1 / (1 + e^-z_e). */
+enum { MASKMOE_SCORE_SOFTMAX = 0, MASKMOE_SCORE_SIGMOID = 1 };
+/* Score of a group: its largest key, or the sum of its two largest (one, where only one is eligible). */
+enum { MASKMOE_GROUP_MAX = 0, MASKMOE_GROUP_SUM2 = 1 };
+
+/* T tokens (0 is a no-op), E experts (1..256), K selected per token (1..min(E, 16)); score, group_rule as
+ * above; n_group equal groups of consecutive experts (n_group divides E; 1: no groups), of which the
+ * topk_group best are kept (topk_group * E / n_group >= K); renorm 1: gates are divided by their sum over
+ * the selected experts, 0: not; scale: factor of every gate (finite). */
+typedef struct maskmoe_gate_desc {
+  int32_t T, E, K, score, n_group, topk_group, group_rule, renorm;
+  float scale;
+} maskmoe_gate_desc;
+
+/*
+ * maskmoe_gate_forward -- Top-K selection and gates from router logits z (maskmoe_route's and
+ * maskmoe_layer_forward_train's logits, or any other). With s the score of every expert:
+ *   key_e = s_e * prior_e + bias_e                       (prior 1, bias 0 where not given)
+ *   groups: those with the topk_group largest group scores (of keys) stay
+ *   A = the K experts with the largest keys in them
+ *   gate_k = scale * s_k,   or with renorm scale * s_k / sum_A s      (never of the keys)
+ * The bias balances the experts' load and the prior is Section 3.2's (Eq. 4): both steer the selection and
+ * leave the gates to the scores. The order is that of the real numbers: keys that fp32 cannot tell apart are
+ * compared in fp64, equal ones go to the lower expert (group).
+ * An expert is eligible where its mask is 1 and its logit is neither NaN nor -inf; such logits add nothing
+ * to a softmax, and +inf counts as the largest finite number. A masked expert still counts in the softmax
+ * (Section 3.2 Stage 1: gates of p). Where fewer than K experts are eligible in the kept groups, the entries
+ * that are left over hold index -1 and gate 0.
+ *
+ *  logits      device [T, E] float.
+ *  mask        host [E] uint8 or NULL: 0 excludes an expert for every token (any number may be 0).
+ *  prior       host [E] float or NULL: finite and > 0.
+ *  bias        device [E] float or NULL (finite).
+ *  topk_idx    device [T, K] int32, by decreasing key.   topk_gate  device [T, K] float.
+ *  load        device [E] int32 or NULL: how many entries of topk_idx name each expert (what a balance rule
+ *              updates the bias by). Written also for T = 0.
+ *  Errors: E_INVAL for a desc outside its ranges, a prior that is not finite and > 0, NULL or misaligned
+ *  pointers.
+ */
+int maskmoe_gate_forward(const maskmoe_gate_desc* desc, const float* logits, const uint8_t* mask, const float* prior,
+                         const float* bias, int32_t* topk_idx, float* topk_gate, int32_t* load, hipStream_t stream);
+
+/*
+ * maskmoe_gate_backward -- the gradient of maskmoe_gate_forward's gates with respect to the logits, the
+ * selection held fixed. With dg = d_gate (entries of index -1 or outside [0, E), or of an ineligible logit,
+ * are skipped), w = s_k / sum_A s:
+ *   renorm:      dz_k = scale * w_k (dg_k - sum_A w dg)              (softmax)
+ *                dz_k = scale * w_k (dg_k - sum_A w dg) (1 - s_k)    (sigmoid)
+ *   no renorm:   dz_e = scale * p_e (dg_e [e in A] - sum_A p dg)     (softmax, every expert)
+ *                dz_k = scale * s_k (1 - s_k) dg_k                   (sigmoid)
+ * and zero elsewhere. bias, prior and mask steer the selection only and have no gradient here. An expert
+ * that an entry list names twice gets the sum.
+ *  desc        as given to the forward (T, E, K, score, renorm, scale are used).
+ *  logits, topk_idx: the forward's.   d_gate device [T, K] float.   d_logits device [T, E] float, written whole.
+ *  Errors: E_INVAL as above. T = 0 writes nothing.
+ */
+int maskmoe_gate_backward(const maskmoe_gate_desc* desc, const float* logits, const int32_t* topk_idx,
+                          const float* d_gate, float* d_logits, hipStream_t stream);
+
+/* ---- experts with weights in microscaled 4-bit blocks (MX4) ----
+ * A block is 32 consecutive elements of a row: E2M1 codes (sign, two exponent bits, one mantissa bit:
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6) and one E8M0 scale byte b that stands for 2^(b - 127), 255 for NaN.
+ * Row-major form of a [rows, cols] matrix: codes [rows, cols / 2] bytes, the even element in the low half;
+ * scales [rows, cols / 32] bytes. */
+
+/*
+ * maskmoe_mx4_quantize -- blocks of src: b = floor(log2(max |v|)) - 2 + 127, at least 0 (a block of zeros: 0);
+ * codes = v / 2^(b - 127) rounded to the nearest element, ties to the even mantissa, saturating at 6 (the
+ * largest elements fall in [4, 8)). A block that holds an infinity or NaN gets scale 255 and codes 0.
+ *  rows, cols   cols % 32 == 0.   dtype MASKMOE_BF16 or MASKMOE_F32: type of src.
+ *  src          device [rows, cols], 16-byte aligned.
+ *  codes        device [rows, cols / 2], 16-byte aligned.   scales device [rows, cols / 32].
+ *  Errors: E_INVAL for negative sizes, NULL or misaligned pointers or an unknown dtype; E_UNSUPPORTED for
+ *  cols % 32 != 0 or more than 2^40 elements.
+ */
+int maskmoe_mx4_quantize(int64_t rows, int32_t cols, int32_t dtype, const void* src, uint8_t* codes, uint8_t* scales,
+                         hipStream_t stream);
+
+/* maskmoe_mx4_dequantize -- the values that codes and scales stand for, as bf16 (rounded only where subnormal) or
+ * fp32 (exact). Arguments and errors as maskmoe_mx4_quantize. */
+int maskmoe_mx4_dequantize(int64_t rows, int32_t cols, int32_t dtype, const uint8_t* codes, const uint8_t* scales,
+                           void* dst, hipStream_t stream);
+
+/* MX4 matrices of n experts, gate / up [n, 2F, d] (W_gate rows first) and down [n, d, F]; row-major or packed.
+ * All device memory owned by the caller. */
+typedef struct maskmoe_mx4_experts {
+  const void *gate_up_codes, *gate_up_scales, *down_codes, *down_scales;
+} maskmoe_mx4_experts;
+
+/*
+ * maskmoe_mx4_packed_bytes -- sizes of the packed arrays of n experts in the order of maskmoe_mx4_experts' fields
+ * (d, F of desc are used). maskmoe_mx4_pack_experts -- rewrites row-major blocks into the operand order of the
+ * matrix instructions, once when weights are loaded: the products read every 16 rows x 128 columns as one
+ * contiguous KiB. Columns are filled up to a multiple of 128 with zeros.
+ *  rows, packed  host structs of device pointers, all 16-byte aligned (row-major scales: any); the arrays of
+ *                `packed` are written and must not overlap those of `rows`.
+ *  Errors: E_INVAL for NULL, equal or misaligned pointers, n < 0, d or F < 1; E_UNSUPPORTED for d or F not multiples
+ *  of 64 or 2 F d >= 2^31.
+ */
+int maskmoe_mx4_packed_bytes(const maskmoe_layer_desc* desc, int32_t n, size_t bytes[4]);
+int maskmoe_mx4_pack_experts(const maskmoe_layer_desc* desc, int32_t n, const maskmoe_mx4_experts* rows,
+                             const maskmoe_mx4_experts* packed, hipStream_t stream);
+
+/* Activations of maskmoe_experts_forward_mx4: bf16, or MX4 blocks (x and the SwiGLU rows h, by
+ * maskmoe_mx4_quantize's rule). */
+enum { MASKMOE_ACT_BF16 = 0, MASKMOE_ACT_MX4 = 1 };
+
+/*
+ * maskmoe_experts_forward_mx4 -- the experts of a layer on packed MX4 weights, for a routing that the caller has
+ * (maskmoe_gate_forward's or maskmoe_route's):
+ *     y_t = sum_k gate_{t,k} F_{idx_{t,k}}(x_t) + sum_s F_s(x_t),
+ *     F(x) = W_down h,  h = SiLU(W_gate x) * (W_up x)               (Section 3.1, Eq. 1)
+ *  desc        T, d, E, K, F, n_shared; dtype MASKMOE_BF16; the other fields are ignored.
+ *  act         MASKMOE_ACT_*.
+ *  x           device [T, d] bf16.   y device [T, d] bf16, another buffer than x.
+ *  topk_idx    device [T, K] int32: an index outside [0, E) (the gate's -1, an empty slot of a batch) adds
+ *              nothing; a token without experts gets zeros (the shared experts' sum). An expert named twice
+ *              counts twice.   topk_gate device [T, K] float.
+ *  w           host struct of packed arrays of E + n_shared experts, the shared ones last.
+ *  workspace   device, maskmoe_experts_mx4_workspace_bytes(desc) bytes, 256-byte aligned; contents on entry do not
+ *              matter. Calls that may overlap, and graphs that may run at the same time, must not share it.
+ *  Rounding: sums are fp32; h is rounded once to bf16 (ACT_BF16) or to MX4 blocks (ACT_MX4, as x is); expert outputs
+ *  stay fp32; y is rounded once.
+ *  Errors: E_INVAL for a desc outside its ranges, an unknown act, NULL or misaligned pointers, x == y; E_WORKSPACE;
+ *  E_UNSUPPORTED for MASKMOE_F32, d or F not multiples of 64, or T d, T (K + n_shared) F, T (K + n_shared) d or 2 F d
+ *  at or above 2^31.
+ */
+size_t maskmoe_experts_mx4_workspace_bytes(const maskmoe_layer_desc* desc);
+int maskmoe_experts_forward_mx4(const maskmoe_layer_desc* desc, int32_t act, const void* x, const int32_t* topk_idx,
+                                const float* topk_gate, const maskmoe_mx4_experts* w, void* y, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+
 /* maskmoe_status_string -- static, NUL-terminated description of a status code. */
 const char* maskmoe_status_string(int status);
 

@@ -9,6 +9,9 @@ what the masked MoE hot path computes, written from the paper:
 * ``ffn``      -- the expert FFN (SwiGLU) and the gate-weighted combine with
   shared experts (Eq. 1 and Section 3.1), and the same with the low-rank
   adapters of Stage 2 (Section 3.2, Appendix B);
+* ``gate``     -- selection by scores, balance bias and expert groups, its gates
+  and their gradient;
+* ``mx4``      -- microscaled 4-bit blocks and the expert FFNs on such weights;
 * ``cache``    -- the per-layer expert cache of the trace simulator and the
   hit-rate / fetches-per-token metrics (Section 4.1, Eq. 5);
 * ``offload``  -- a batch-1 offloaded decode of one layer: the experts each
@@ -31,4 +34,4 @@ particular prior strengths have no value printed in the paper to compare
 with; they are pinned only through the cache rules above.
 """
 
-from . import cache, ffn, offload, routing, train  # noqa: F401
+from . import cache, ffn, gate, mx4, offload, routing, train  # noqa: F401

@@ -24,6 +24,9 @@ GATE_P, GATE_RENORM = 0, 1
 BF16, F32 = 0, 1
 CACHE_LRU, CACHE_LFU, CACHE_FIFO = 0, 1, 2
 LAYOUT_ROWS, LAYOUT_PACKED = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_SUM2 = 0, 1
+ACT_BF16, ACT_MX4 = 0, 1
 
 EXPORTS = ("maskmoe_route", "maskmoe_route_workspace_bytes", "maskmoe_layer_workspace_bytes",
            "maskmoe_layer_forward", "maskmoe_layer_forward_profiled", "maskmoe_cache_fetches", "maskmoe_status_string",
@@ -31,7 +34,9 @@ EXPORTS = ("maskmoe_route", "maskmoe_route_workspace_bytes", "maskmoe_layer_work
            "maskmoe_stage1_backward", "maskmoe_layer_train_workspace_bytes",
            "maskmoe_layer_backward_workspace_bytes", "maskmoe_layer_backward", "maskmoe_layer_lora_workspace_bytes",
            "maskmoe_layer_forward_lora", "maskmoe_offload_workspace_bytes", "maskmoe_offload_decode_step",
-           "maskmoe_pack_expert_weights", "maskmoe_layer_forward_noalloc")
+           "maskmoe_pack_expert_weights", "maskmoe_layer_forward_noalloc", "maskmoe_gate_forward",
+           "maskmoe_gate_backward", "maskmoe_mx4_quantize", "maskmoe_mx4_dequantize", "maskmoe_mx4_packed_bytes",
+           "maskmoe_mx4_pack_experts", "maskmoe_experts_mx4_workspace_bytes", "maskmoe_experts_forward_mx4")
 NUM_STAGES = 5
 STAGES = ("route", "permute", "gate_up", "down", "combine")
 
@@ -49,6 +54,19 @@ class Lora(ctypes.Structure):
     _fields_ = [("rank", ctypes.c_int32), ("alpha", ctypes.c_float)] + [
         (n, ctypes.c_void_p) for n in ("a_gate_up", "b_gate_up", "a_down", "b_down",
                                        "as_gate_up", "bs_gate_up", "as_down", "bs_down")]
+
+
+class GateDesc(ctypes.Structure):
+    """``maskmoe_gate_desc``."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("T", "E", "K", "score", "n_group", "topk_group", "group_rule", "renorm")] + [("scale", ctypes.c_float)]
+
+
+class Mx4Experts(ctypes.Structure):
+    """``maskmoe_mx4_experts``."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate_up_codes", "gate_up_scales", "down_codes", "down_scales")]
 
 
 class MaskMoEError(RuntimeError):
@@ -124,6 +142,24 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.maskmoe_offload_decode_step.restype = ctypes.c_int
     lib.maskmoe_pack_expert_weights.argtypes = [ctypes.POINTER(LayerDesc), _i32, _vp, _vp, _vp, _vp, _vp]
     lib.maskmoe_pack_expert_weights.restype = ctypes.c_int
+    lib.maskmoe_gate_forward.argtypes = [ctypes.POINTER(GateDesc), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.maskmoe_gate_forward.restype = ctypes.c_int
+    lib.maskmoe_gate_backward.argtypes = [ctypes.POINTER(GateDesc), _vp, _vp, _vp, _vp, _vp]
+    lib.maskmoe_gate_backward.restype = ctypes.c_int
+    lib.maskmoe_mx4_quantize.argtypes = [ctypes.c_int64, _i32, _i32, _vp, _vp, _vp, _vp]
+    lib.maskmoe_mx4_quantize.restype = ctypes.c_int
+    lib.maskmoe_mx4_dequantize.argtypes = [ctypes.c_int64, _i32, _i32, _vp, _vp, _vp, _vp]
+    lib.maskmoe_mx4_dequantize.restype = ctypes.c_int
+    lib.maskmoe_mx4_packed_bytes.argtypes = [ctypes.POINTER(LayerDesc), _i32, ctypes.POINTER(_sz)]
+    lib.maskmoe_mx4_packed_bytes.restype = ctypes.c_int
+    lib.maskmoe_mx4_pack_experts.argtypes = [ctypes.POINTER(LayerDesc), _i32, ctypes.POINTER(Mx4Experts),
+                                             ctypes.POINTER(Mx4Experts), _vp]
+    lib.maskmoe_mx4_pack_experts.restype = ctypes.c_int
+    lib.maskmoe_experts_mx4_workspace_bytes.argtypes = [ctypes.POINTER(LayerDesc)]
+    lib.maskmoe_experts_mx4_workspace_bytes.restype = _sz
+    lib.maskmoe_experts_forward_mx4.argtypes = [ctypes.POINTER(LayerDesc), _i32, _vp, _vp, _vp,
+                                                ctypes.POINTER(Mx4Experts), _vp, _vp, _sz, _vp]
+    lib.maskmoe_experts_forward_mx4.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -589,3 +625,168 @@ def maskmoe_layer_backward(x, w_gate_up, w_down, K: int, gate_mode: int, topk_ga
                                       _ptr(out["d_w_down"]), _ptr(out["d_ws_gate_up"]), _ptr(out["d_ws_down"]),
                                       _ptr(workspace), workspace.numel(), _stream()))
     return out
+
+
+def _current(t, name: str):
+    """Device tensor ``name`` must be contiguous and on the device that the call enqueues on."""
+    import torch
+    _dev(t, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+
+
+def _want(t, name: str, shape, dtype):
+    """Device tensor ``name`` must be contiguous, on the current device, of this shape and dtype."""
+    _current(t, name)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}")
+
+
+def maskmoe_gate_forward(logits, K: int, score: int, n_group: int = 1, topk_group: int = 1,
+                         group_rule: int = GROUP_MAX, renorm: bool = True, scale: float = 1.0, bias=None, mask=None,
+                         prior=None, with_load: bool = False):
+    """Top-K selection and gates from router logits [T,E] fp32: softmax or sigmoid scores (SCORE_*),
+    keys ``score * prior + bias``, the ``topk_group`` best of ``n_group`` groups by GROUP_MAX or
+    GROUP_SUM2, gates ``scale * score`` (divided by their sum with ``renorm``). bias: device [E] fp32;
+    mask / prior: host [E]. Returns ``(idx [T,K] int32, gate [T,K] fp32, load [E] int32 or None)``;
+    entries without an eligible expert hold index -1 and gate 0."""
+    import torch
+    lib = load()
+    _current(logits, "logits")
+    if logits.dim() != 2 or logits.dtype != torch.float32:
+        raise ValueError("logits must be a 2-d float32 tensor")
+    T, E = logits.shape
+    dev = logits.device
+    if bias is not None:
+        _want(bias, "bias", (E,), torch.float32)
+    m_arr, m_p = _host_u8(mask, E)
+    p_arr, p_p = _host_f32(prior, E)
+    idx = torch.empty((T, K), dtype=torch.int32, device=dev)
+    gate = torch.empty((T, K), dtype=torch.float32, device=dev)
+    ld = torch.empty(E, dtype=torch.int32, device=dev) if with_load else None
+    desc = GateDesc(T, E, K, score, n_group, topk_group, group_rule, int(renorm), scale)
+    _check("maskmoe_gate_forward", lib.maskmoe_gate_forward(ctypes.byref(desc), _ptr(logits), m_p, p_p, _ptr(bias),
+                                                            _ptr(idx), _ptr(gate), _ptr(ld), _stream()))
+    del m_arr, p_arr
+    return idx, gate, ld
+
+
+def maskmoe_gate_backward(logits, topk_idx, d_gate, score: int, renorm: bool = True, scale: float = 1.0):
+    """dL/dlogits [T,E] fp32 of maskmoe_gate_forward's gates for a cotangent d_gate [T,K] fp32 of them, the
+    selection topk_idx [T,K] held fixed."""
+    import torch
+    lib = load()
+    _current(logits, "logits")
+    if logits.dim() != 2 or logits.dtype != torch.float32 or topk_idx.dim() != 2:
+        raise ValueError("logits must be a 2-d float32 tensor, topk_idx 2-d")
+    T, E = logits.shape
+    K = topk_idx.shape[1]
+    _want(topk_idx, "topk_idx", (T, K), torch.int32)
+    _want(d_gate, "d_gate", (T, K), torch.float32)
+    out = torch.empty_like(logits)
+    desc = GateDesc(T, E, K, score, 1, 1, GROUP_MAX, int(renorm), scale)
+    _check("maskmoe_gate_backward", lib.maskmoe_gate_backward(ctypes.byref(desc), _ptr(logits), _ptr(topk_idx),
+                                                              _ptr(d_gate), _ptr(out), _stream()))
+    return out
+
+
+def maskmoe_mx4_quantize(x):
+    """MX4 blocks of x [..., cols] (bf16 or fp32, cols a multiple of 32) along its last dimension: codes
+    [..., cols/2] and scales [..., cols/32], uint8."""
+    import torch
+    lib = load()
+    _current(x, "x")
+    cols = x.shape[-1] if x.dim() else 0
+    if cols == 0 or cols % 32:
+        raise ValueError("the last dimension must be a positive multiple of 32")
+    rows = x.numel() // cols
+    codes = torch.empty(tuple(x.shape[:-1]) + (cols // 2,), dtype=torch.uint8, device=x.device)
+    scales = torch.empty(tuple(x.shape[:-1]) + (cols // 32,), dtype=torch.uint8, device=x.device)
+    _check("maskmoe_mx4_quantize", lib.maskmoe_mx4_quantize(rows, cols, _dtype_code(x), _ptr(x), _ptr(codes),
+                                                            _ptr(scales), _stream()))
+    return codes, scales
+
+
+def maskmoe_mx4_dequantize(codes, scales, dtype):
+    """The values of codes [..., cols/2] and scales [..., cols/32] as a bf16 or fp32 tensor [..., cols]."""
+    import torch
+    lib = load()
+    _current(codes, "codes")
+    cols = 2 * codes.shape[-1] if codes.dim() else 0
+    if cols == 0 or cols % 32 or codes.dtype != torch.uint8:
+        raise ValueError("codes must be uint8, the last dimension a positive multiple of 16")
+    _want(scales, "scales", tuple(codes.shape[:-1]) + (cols // 32,), torch.uint8)
+    out = torch.empty(tuple(codes.shape[:-1]) + (cols,), dtype=dtype, device=codes.device)
+    _check("maskmoe_mx4_dequantize", lib.maskmoe_mx4_dequantize(codes.numel() // (cols // 2), cols, _dtype_code(out),
+                                                                _ptr(codes), _ptr(scales), _ptr(out), _stream()))
+    return out
+
+
+class PackedMx4Experts:
+    """Packed MX4 weights of n experts (maskmoe_mx4_pack_experts) and their sizes; the tensors are only
+    meaningful to the library."""
+
+    def __init__(self, n: int, d: int, F: int, tensors):
+        self.n, self.d, self.F, self.tensors = n, d, F, tuple(tensors)
+
+    def struct(self) -> Mx4Experts:
+        return Mx4Experts(*[t.data_ptr() for t in self.tensors])
+
+
+def maskmoe_mx4_pack_experts(gate_up_codes, gate_up_scales, down_codes, down_scales) -> PackedMx4Experts:
+    """Packs row-major MX4 weights (maskmoe_mx4_quantize of w_gate_up [n,2F,d] and w_down [n,d,F]) for
+    maskmoe_experts_forward_mx4; routed experts first, shared experts last."""
+    import torch
+    lib = load()
+    if gate_up_codes.dim() != 3 or down_codes.dim() != 3:
+        raise ValueError("gate_up_codes and down_codes must be 3-d")
+    n, F2, d2 = gate_up_codes.shape
+    d, F = 2 * d2, F2 // 2
+    for t, name, shape in ((gate_up_codes, "gate_up_codes", (n, 2 * F, d // 2)),
+                           (gate_up_scales, "gate_up_scales", (n, 2 * F, d // 32)),
+                           (down_codes, "down_codes", (n, d, F // 2)), (down_scales, "down_scales", (n, d, F // 32))):
+        _want(t, name, shape, torch.uint8)
+    desc = make_desc(0, d, 1, 1, F)
+    sizes = (_sz * 4)()
+    _check("maskmoe_mx4_packed_bytes", lib.maskmoe_mx4_packed_bytes(ctypes.byref(desc), n, sizes))
+    packed = PackedMx4Experts(n, d, F, [torch.empty(max(int(b), 1), dtype=torch.uint8, device=gate_up_codes.device)
+                                        for b in sizes])
+    src = Mx4Experts(*[t.data_ptr() for t in (gate_up_codes, gate_up_scales, down_codes, down_scales)])
+    dst = packed.struct()
+    _check("maskmoe_mx4_pack_experts", lib.maskmoe_mx4_pack_experts(ctypes.byref(desc), n, ctypes.byref(src),
+                                                                    ctypes.byref(dst), _stream()))
+    return packed
+
+
+def maskmoe_experts_mx4_workspace_bytes(T: int, d: int, E: int, K: int, F: int, n_shared: int = 0) -> int:
+    return int(load().maskmoe_experts_mx4_workspace_bytes(ctypes.byref(make_desc(T, d, E, K, F, n_shared))))
+
+
+def maskmoe_experts_forward_mx4(x, topk_idx, topk_gate, experts: PackedMx4Experts, n_shared: int = 0,
+                                act: int = ACT_BF16, workspace=None, y=None):
+    """The experts of a layer on packed MX4 weights for a given routing: x [T,d] bf16, topk_idx [T,K]
+    int32 (entries outside the routed experts add nothing), topk_gate [T,K] fp32; ``experts`` holds the routed
+    experts and then ``n_shared`` shared ones. ``act``: ACT_BF16 or ACT_MX4 activations. Returns y [T,d]."""
+    import torch
+    lib = load()
+    if x.dim() != 2 or topk_idx.dim() != 2:
+        raise ValueError("x and topk_idx must be 2-d")
+    T, K = topk_idx.shape
+    d, E = experts.d, experts.n - n_shared
+    _want(x, "x", (T, d), torch.bfloat16)
+    _want(topk_idx, "topk_idx", (T, K), torch.int32)
+    _want(topk_gate, "topk_gate", (T, K), torch.float32)
+    desc = make_desc(T, d, E, K, experts.F, n_shared)
+    if workspace is None:
+        workspace = torch.empty(max(int(lib.maskmoe_experts_mx4_workspace_bytes(ctypes.byref(desc))), 1),
+                                dtype=torch.uint8, device=x.device)
+    _current(workspace, "workspace")
+    if y is None:
+        y = torch.empty_like(x)
+    else:
+        _want(y, "y", (T, d), torch.bfloat16)
+    w = experts.struct()
+    _check("maskmoe_experts_forward_mx4", lib.maskmoe_experts_forward_mx4(
+        ctypes.byref(desc), act, _ptr(x), _ptr(topk_idx), _ptr(topk_gate), ctypes.byref(w), _ptr(y), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream()))
+    return y

@@ -1,0 +1,51 @@
+// Microscaled 4-bit blocks: internal launchers (mx4.hip) and the layout of packed expert weights
+// that the products (mx4_experts.hip) read. Arguments are validated by the C-ABI layer.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kernels.hpp"
+
+namespace maskmoe {
+
+constexpr int kMxBlock = 32;    // elements that share a scale
+constexpr int kMxStep = 128;    // reduction elements of one matrix instruction (16 x 16 x 128)
+
+// codes [rows, cols / 2], scales [rows, cols / 32] of src [rows, cols] (bf16 or fp32), cols % 32 == 0.
+hipError_t launch_mx4_quantize(bool bf16, const void* src, int64_t rows, int cols, uint8_t* codes, uint8_t* scales,
+                               hipStream_t stream);
+hipError_t launch_mx4_dequantize(bool bf16, const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
+                                 void* dst, hipStream_t stream);
+
+// Packed expert matrix of R rows and C columns (R % 16 == 0, C % 64 == 0), in the operand order of the
+// 16 x 16 x 128 matrix instructions. Fragment f holds 16 rows, step s 128 columns (the last one filled up
+// with zeros); its 1 KiB at (f * steps + s) is one 16-byte load of a wavefront: lane l the block of row
+// l & 15 and columns 128 s + 32 (l >> 4) ... Scales: dword (f * quads + s / 4) * 64 + l, byte s % 4 the
+// scale of that block. Fragments of a gate / up matrix alternate: 2q rows 16q .. of W_gate, 2q + 1 the
+// same rows of W_up.
+inline __host__ __device__ int mx4_steps(int C) { return (C + kMxStep - 1) / kMxStep; }
+inline __host__ __device__ int mx4_quads(int C) { return (mx4_steps(C) + 3) / 4; }
+inline size_t mx4_code_bytes(int R, int C) { return static_cast<size_t>(R / 16) * mx4_steps(C) * 1024; }
+inline size_t mx4_scale_bytes(int R, int C) { return static_cast<size_t>(R / 16) * mx4_quads(C) * 256; }
+hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, int n, int R, int C, bool gate_up,
+                           uint8_t* p_codes, uint8_t* p_scales, hipStream_t stream);
+
+// Experts on packed MX4 weights.
+struct Mx4Args {
+  const uint16_t* x;       // [T, d] bf16
+  const int32_t* idx;      // [T, K]
+  const float* gate;       // [T, K]
+  const uint8_t *gu_codes, *gu_scales, *dn_codes, *dn_scales;   // E + n_shared experts
+  uint16_t* y;             // [T, d] bf16
+  int T, d, F, E, K, n_shared;
+  bool mx_act;             // activations in MX4 blocks; else bf16
+};
+struct Mx4Layout {         // byte offsets into the workspace
+  size_t idx, gate, offsets, tile_off, active, n_active, perm, inv, row_tok, pcount, xq, xs, h, hs, o, total;
+};
+Mx4Layout mx4_layout(int T, int d, int F, int E, int K, int n_shared);
+hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t stream);
+
+}  // namespace maskmoe

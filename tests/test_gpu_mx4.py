@@ -1,0 +1,241 @@
+"""MX4 conversion bit for bit, and the experts on MX4 weights within the bound that the oracle derives from
+every rounding on the way (oracle/mx4.py)."""
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import say
+from oracle import mx4 as M
+from paper_2609_34077_amd import _lib as L
+
+pytestmark = pytest.mark.gpu
+
+
+def bf16(a):
+    return torch.from_numpy(np.asarray(a, np.float32)).bfloat16()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols", [(1, 32), (3, 64), (7, 96), (33, 416), (130, 2048), (1, 4096)])
+def test_quantize_and_back(rows, cols, dtype):
+    say(f"mx4 {rows} x {cols} {dtype}")
+    g = np.random.default_rng(rows * cols)
+    v = g.standard_normal((rows, cols)) * 10.0 ** g.integers(-44, 38, (rows, cols // 32)).repeat(32, 1)
+    v[0, :32] = 0
+    v[-1, -32:] = g.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -5.0, 6.0, 7.99], 32)   # rounding borders
+    v[-1, -1] = 7
+    x = torch.from_numpy(np.clip(v, -3e38, 3e38).astype(np.float32)).to(dtype)
+    codes, scales = L.maskmoe_mx4_quantize(x.cuda())
+    co, eo = M.quantize(x.double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), eo + 127)
+    assert np.array_equal(codes.cpu().numpy(), M.pack_codes(co))
+    want = torch.from_numpy(M.values(co, eo))
+    for dt in (torch.float32, torch.bfloat16):
+        back = L.maskmoe_mx4_dequantize(codes, scales, dt).cpu()
+        assert torch.equal(back, want.to(dt))
+
+
+def test_every_bf16_value():
+    """Each finite bf16 number as the largest of a block, beside one, three quarters and a half of it."""
+    bits = torch.arange(0, 0x7F80, dtype=torch.int32).to(torch.int16)
+    top = bits.view(torch.bfloat16).float()
+    x = (top[:, None] * torch.linspace(-1, 1, 32)).bfloat16()
+    x[:, 31] = top.bfloat16()
+    codes, scales = L.maskmoe_mx4_quantize(x.cuda())
+    co, eo = M.quantize(x.double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), eo + 127) and np.array_equal(codes.cpu().numpy(), M.pack_codes(co))
+
+
+def test_infinities_and_nan_stay_in_their_block():
+    x = torch.ones((4, 96))
+    x[0, 5], x[1, 40], x[2, 95] = float("inf"), float("nan"), float("-inf")
+    codes, scales = L.maskmoe_mx4_quantize(x.cuda())
+    back = L.maskmoe_mx4_dequantize(codes, scales, torch.float32).cpu()
+    bad = torch.zeros((4, 3), dtype=torch.bool)
+    bad[0, 0] = bad[1, 1] = bad[2, 2] = True
+    assert torch.equal(back.isnan().view(4, 3, 32).all(-1), bad) and torch.equal(back.isnan().view(4, 3, 32).any(-1), bad)
+    assert torch.equal(scales.cpu() == 255, bad) and (codes.cpu().view(4, 3, 16)[bad] == 0).all()
+
+
+def make(T, d, F, E, K, ns, seed, pad=0):
+    g = np.random.default_rng(seed)
+    n = E + ns
+    x = bf16(g.standard_normal((T, d)) * np.where(g.random(d) < 0.05, 6, 1))
+    wq, dev = [], []
+    for shape in ((n, 2 * F, d), (n, d, F)):
+        c, e = M.quantize(g.standard_normal(shape) * shape[-1] ** -0.5 * 2.0 ** g.integers(-1, 2, shape[:2] + (1,)))
+        wq.append(M.values(c, e))
+        dev += [torch.from_numpy(M.pack_codes(c)).cuda(), torch.from_numpy((e + 127).astype(np.uint8)).cuda()]
+    idx = np.argsort(-(g.standard_normal((T, E)) + np.linspace(0, 2, E)), 1)[:, :K].astype(np.int32)
+    gate = g.random((T, K)).astype(np.float32)
+    if pad:
+        idx[T - pad:] = -1
+    return x, wq, dev, idx, gate
+
+
+def call(x, dev, idx, gate, ns, act, **kw):
+    packed = L.maskmoe_mx4_pack_experts(*dev)
+    return L.maskmoe_experts_forward_mx4(x.cuda(), torch.from_numpy(idx).cuda(), torch.from_numpy(gate).cuda(), packed,
+                                         n_shared=ns, act=act, **kw)
+
+
+def check(x, wq, dev, idx, gate, ns, act):
+    y = call(x, dev, idx, gate, ns, act).double().cpu().numpy()
+    want, bound = M.experts(x.double().numpy(), idx, gate, *wq, ns, act == L.ACT_MX4)
+    worst = (np.abs(y - want) / (bound + 1e-300)).max()
+    assert worst <= 1, worst
+    return y
+
+
+# T, d, F, E, K, shared, empty slots at the end
+LAYERS = [(1, 64, 64, 1, 1, 0, 0), (1, 128, 192, 8, 2, 0, 0), (2, 192, 64, 4, 2, 1, 1), (5, 256, 320, 64, 6, 2, 0),
+          (16, 320, 128, 8, 2, 0, 3), (17, 64, 576, 3, 3, 0, 0), (33, 512, 256, 5, 2, 0, 2), (64, 128, 128, 2, 1, 1, 0),
+          (65, 192, 64, 2, 2, 0, 0), (100, 256, 512, 8, 2, 0, 7), (130, 64, 64, 256, 16, 0, 0), (200, 384, 448, 4, 2, 2, 0),
+          (300, 128, 1408, 16, 4, 1, 11), (700, 640, 192, 3, 2, 0, 0), (1100, 192, 256, 8, 2, 1, 50)]
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T,d,F,E,K,ns,pad", LAYERS)
+def test_experts(T, d, F, E, K, ns, pad, act):
+    say(f"mx4 experts T={T} d={d} F={F} E={E} K={K} shared={ns} pad={pad} act={act}")
+    x, wq, dev, idx, gate = make(T, d, F, E, K, ns, T + d + F, pad)
+    y = check(x, wq, dev, idx, gate, ns, act)
+    if pad and not ns:
+        assert (y[T - pad:] == 0).all()
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T", [1, 7, 40, 300])
+def test_uneven_and_odd_routing(T, act):
+    """All tokens to one expert; experts named twice; indices outside the experts; no expert at all."""
+    say(f"mx4 experts routing T={T} act={act}")
+    x, wq, dev, idx, gate = make(T, 128, 192, 6, 2, 0, T)
+    idx[:] = [4, 4]
+    check(x, wq, dev, idx, gate, 0, act)
+    idx[:, 0], idx[:, 1] = np.arange(T) % 9 - 2, 2 ** 31 - 1 - np.arange(T) % 3
+    check(x, wq, dev, idx, gate, 0, act)
+    idx[:] = np.iinfo(np.int32).min
+    assert (check(x, wq, dev, idx, gate, 0, act) == 0).all()
+    x2, wq2, dev2, idx2, gate2 = make(T, 128, 192, 4, 2, 2, T)
+    idx2[:] = -1
+    check(x2, wq2, dev2, idx2, gate2, 2, act)
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T", [3, 16, 90, 600])
+def test_nan_and_infinity_stay_in_their_token(T, act):
+    x, wq, dev, idx, gate = make(T, 192, 128, 4, 2, 0, T + 1)
+    clean = call(x, dev, idx, gate, 0, act).cpu()
+    x[1, 7], x[T - 1, 100] = float("nan"), float("inf")
+    y = call(x, dev, idx, gate, 0, act).cpu()
+    rows = torch.ones(T, dtype=torch.bool)
+    rows[1] = rows[T - 1] = False
+    assert torch.equal(y[rows], clean[rows]) and y[1].isnan().all() and not y[T - 1].isfinite().any()
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T", [2, 40, 520])
+def test_scales_at_their_ends(T, act):
+    """Weight blocks with the smallest scales (bytes 0 and 1), a large one, and NaN scales of one expert."""
+    x, wq, dev, idx, gate = make(T, 128, 64, 4, 1, 0, T + 2)
+    idx[:, 0] = np.arange(T) % 4
+    gu, sc = dev[0].cpu().numpy(), dev[1].cpu().numpy()
+    sc[0, :, 0], sc[0, :, 1], sc[1, :, 2] = 0, 1, 150
+    sc[3, 0, 0] = 255
+    dev[1] = torch.from_numpy(sc).cuda()
+    codes = np.empty((4, 128, 128), np.int64)
+    codes[..., 0::2], codes[..., 1::2] = gu & 15, gu >> 4
+    wq[0] = M.values(codes, sc.astype(np.int64) - 127)
+    y = call(x, dev, idx, gate, 0, act).double().cpu().numpy()
+    want, bound = M.experts(x.double().numpy()[idx[:, 0] < 3], idx[idx[:, 0] < 3], gate[idx[:, 0] < 3], *wq, 0, act == L.ACT_MX4)
+    assert (np.abs(y[idx[:, 0] < 3] - want) <= bound + 1e-37).all()
+    assert np.isnan(y[idx[:, 0] == 3]).all()
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T", [4, 100, 900])
+def test_dirty_workspace_streams_and_graphs(T, act):
+    """The workspace's contents do not matter; calls on two streams with a workspace each; captured and replayed
+    with other work between; the same bits every time."""
+    say(f"mx4 experts graph T={T} act={act}")
+    E, K, ns, d, F = 8, 2, 1, 256, 320
+    x, wq, dev, idx, gate = make(T, d, F, E, K, ns, T + 3)
+    packed = L.maskmoe_mx4_pack_experts(*dev)
+    xs, it, gt = x.cuda(), torch.from_numpy(idx).cuda(), torch.from_numpy(gate).cuda()
+    n = L.maskmoe_experts_mx4_workspace_bytes(T, d, E, K, F, ns)
+    ws = [torch.full((n,), fill, dtype=torch.uint8, device="cuda") for fill in (0xFF, 0x7F)]
+    f = lambda w, v=xs: L.maskmoe_experts_forward_mx4(v, it, gt, packed, n_shared=ns, act=act, workspace=w)
+    ref = f(None)
+    assert torch.equal(f(ws[0]), ref) and torch.equal(f(ws[1]), ref)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = []
+    torch.cuda.synchronize()
+    for s, w in zip(streams, ws):
+        with torch.cuda.stream(s):
+            outs.append([f(w) for _ in range(5)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, ref) for o in outs for y in o)
+    buf = xs.clone()
+    y = torch.empty_like(buf)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.maskmoe_experts_forward_mx4(buf, it, gt, packed, n_shared=ns, act=act, workspace=ws[0], y=y)
+    for i in range(4):
+        buf.copy_(xs.roll(i, 0))
+        want = f(None, buf)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+
+
+def test_gate_to_experts():
+    """As a serving step runs them: logits, gates, the experts on quantised weights, an empty slot in the batch; the
+    bf16 layer on the values of the same weights agrees within the bf16 layer's bound."""
+    say("mx4 gate -> experts")
+    T, d, F, E, K = 50, 256, 192, 64, 6
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w_gu = torch.randn((E, 2 * F, d), generator=g, device="cuda").mul_(d ** -0.5).bfloat16()
+    w_dn = torch.randn((E, d, F), generator=g, device="cuda").mul_(F ** -0.5).bfloat16()
+    x = torch.randn((T, d), generator=g, device="cuda").bfloat16()
+    wr = torch.randn((E, d), generator=g, device="cuda").mul_(0.1).bfloat16()
+    q = L.maskmoe_mx4_quantize(w_gu) + L.maskmoe_mx4_quantize(w_dn)
+    packed = L.maskmoe_mx4_pack_experts(*q)
+    z = x.float() @ wr.float().t()
+    z[T - 1] = float("nan")
+    idx, gate, load = L.maskmoe_gate_forward(z, K, L.SCORE_SIGMOID, n_group=8, topk_group=3, group_rule=L.GROUP_SUM2,
+                                             bias=0.02 * torch.randn(E, generator=g, device="cuda"), scale=2.5, with_load=True)
+    assert int(load.sum()) == (T - 1) * K and (idx[T - 1] == -1).all()
+    y = L.maskmoe_experts_forward_mx4(x, idx, gate, packed)
+    vals = [L.maskmoe_mx4_dequantize(*q[i:i + 2], torch.float32).double().cpu().numpy() for i in (0, 2)]
+    want, bound = M.experts(x.double().cpu().numpy(), idx.cpu().numpy(), gate.cpu().numpy(), *vals, 0, False)
+    assert (np.abs(y.double().cpu().numpy() - want) <= bound).all() and (y[T - 1] == 0).all()
+    # maskmoe_route's routing drives the same experts; the bf16 layer runs on the values of the blocks
+    ri, rg, _ = L.maskmoe_route(x, wr, 2, L.ROUTE_PLAIN, L.GATE_RENORM)
+    dense = [L.maskmoe_mx4_dequantize(*q[i:i + 2], torch.bfloat16) for i in (0, 2)]
+    yd = L.maskmoe_layer_forward(x, wr, *dense, 2, L.ROUTE_PLAIN, L.GATE_RENORM).float()
+    ym = L.maskmoe_experts_forward_mx4(x, ri, rg, packed).float()
+    assert (yd - ym).abs().max() <= 2e-2 * yd.abs().max()
+
+
+def test_python_refusals():
+    x = torch.zeros((4, 64), device="cuda")
+    for bad in (x[:, :48], x.half(), x.cpu(), x.t()):
+        with pytest.raises((ValueError, TypeError)):
+            L.maskmoe_mx4_quantize(bad)
+    codes, scales = L.maskmoe_mx4_quantize(x)
+    with pytest.raises(ValueError):
+        L.maskmoe_mx4_dequantize(codes, scales[:, :1].contiguous(), torch.float32)
+    xq, wq, dev, idx, gate = make(4, 64, 64, 2, 1, 0, 0)
+    with pytest.raises(ValueError):
+        L.maskmoe_mx4_pack_experts(dev[0], dev[1], dev[2][:1].contiguous(), dev[3])
+    packed = L.maskmoe_mx4_pack_experts(*dev)
+    it, gt = torch.from_numpy(idx).cuda(), torch.from_numpy(gate).cuda()
+    with pytest.raises(ValueError):
+        L.maskmoe_experts_forward_mx4(xq.cuda().float(), it, gt, packed)
+    with pytest.raises(ValueError):
+        L.maskmoe_experts_forward_mx4(xq.cuda(), it.long(), gt, packed)
+    with pytest.raises(L.MaskMoEError):
+        L.maskmoe_experts_forward_mx4(xq.cuda(), it, gt, packed, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(L.MaskMoEError):
+        L.maskmoe_experts_forward_mx4(xq.cuda(), it, gt, packed, act=3)
