@@ -42,6 +42,23 @@ struct Mx4Args {
   int T, d, F, E, K, n_shared;
   bool mx_act;             // activations in MX4 blocks; else bf16
 };
+struct Mx4Params {
+  Mx4Args a;
+  int32_t* idx;      // [T, K + n_shared] experts of every entry, -1 for none
+  float* gate;       // [T, K + n_shared]
+  PermBuffers pb;
+  uint8_t* xq;       // [T, d / 2] codes
+  uint8_t* xs;       // [T, quads of d, 16]: the scale of block b at byte 16 (b / 16) + 4 (b % 4) + b / 4 % 4, so that
+                     // dword g of a quad holds the scales of columns 32 g .. of its four steps
+  void* h;           // [rows, F] bf16, or codes
+  uint8_t* hs;       // [rows, quads of F, 16]
+  float* o;          // [rows, d]
+  int G;             // E + n_shared
+};
+// Many rows per expert (mx4_tile.hip): both products on 256 x 256 tiles, the permutation in tiles of kMx4TileRows.
+constexpr int kMx4TileRows = 256;
+hipError_t launch_mx4_wide(const Mx4Params& p, int max_tiles, hipStream_t stream);
+
 struct Mx4Layout {         // byte offsets into the workspace
   size_t idx, gate, offsets, tile_off, active, n_active, perm, inv, row_tok, pcount, xq, xs, h, hs, o, total;
 };

@@ -40,15 +40,19 @@ __device__ __forceinline__ u32x4 mx4_to_bf16(uint32_t codes, float scale) {
   return r;
 }
 
-// D = A(16x128) * B(128x16) + C on E2M1 codes with block scales (the low byte of sa / sb), fp32 sums.
+// Byte of block b's scale in a row of activation scales (Mx4Params::xs).
+__device__ __forceinline__ int mx4_scale_at(int b) { return 16 * (b >> 4) + 4 * (b & 3) + (b >> 2 & 3); }
+
+// D = A(16x128) * B(128x16) + C on E2M1 codes with block scales (byte S of sa / sb), fp32 sums.
 // Lane l: row (column) l & 15, the block of columns (rows) 32 (l >> 4) ..; result as mfma_16x16x32.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+template <int S = 0>
 __device__ __forceinline__ f32x4 mfma_mx4(const u32x4& a, const u32x4& b, f32x4 c, uint32_t sa, uint32_t sb) {
   const i32x8 av = {static_cast<int>(a[0]), static_cast<int>(a[1]), static_cast<int>(a[2]), static_cast<int>(a[3]),
                     0, 0, 0, 0};
   const i32x8 bv = {static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3]),
                     0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4, 4, 0, static_cast<int>(sa), 0,
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4, 4, S, static_cast<int>(sa), S,
                                                           static_cast<int>(sb));
 }
 

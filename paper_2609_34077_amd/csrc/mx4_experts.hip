@@ -13,19 +13,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-struct Mx4Params {
-  Mx4Args a;
-  int32_t* idx;      // [T, K + n_shared] experts of every entry, -1 for none
-  float* gate;       // [T, K + n_shared]
-  PermBuffers pb;
-  uint32_t* xq;      // [T, d / 8] codes
-  uint8_t* xs;       // [T, d / 32]
-  void* h;           // [rows, F] bf16, or codes
-  uint8_t* hs;       // [rows, F / 32]
-  float* o;          // [rows, d]
-  int G;             // E + n_shared
-};
-
 // Entries of routed and shared experts in one list; x in blocks (four lanes a block).
 __global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p, int entry_blocks) {
   const Mx4Args& a = p.a;
@@ -61,8 +48,12 @@ __global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p
   m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0xB1, 0xF, 0xF, true)));
   m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0x4E, 0xF, 0xF, true)));
   const uint32_t byte = mx4_scale_byte(m);
-  p.xq[i] = byte == 255 ? 0 : mx4_codes(v, mx4_scale(byte));
-  if ((i & 3) == 0) p.xs[i >> 2] = static_cast<uint8_t>(byte);
+  reinterpret_cast<uint32_t*>(p.xq)[i] = byte == 255 ? 0 : mx4_codes(v, mx4_scale(byte));
+  if ((i & 3) == 0) {
+    const int blocks = a.d / kMxBlock;
+    const int64_t b = i >> 2, t = b / blocks;
+    p.xs[t * 16 * mx4_quads(a.d) + mx4_scale_at(static_cast<int>(b - t * blocks))] = static_cast<uint8_t>(byte);
+  }
 }
 
 // Group that holds row tile `tile` (tile < tile_off[G]): the groups that end at or before it, counted by
@@ -121,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void mx4_tile_kernel(const Mx4Params p) {
       ws[i] = *reinterpret_cast<const uint32_t*>(scales + ((f * quads + (s >> 2)) * 64 + lane) * 4) >> (8 * (s & 3));
     }
     if constexpr (MX) {
-      const uint8_t* xq = EPI == 0 ? reinterpret_cast<const uint8_t*>(p.xq) : static_cast<const uint8_t*>(p.h);
+      const uint8_t* xq = EPI == 0 ? p.xq : static_cast<const uint8_t*>(p.h);
       const uint8_t* xs = EPI == 0 ? p.xs : p.hs;
 #pragma unroll
       for (int n = 0; n < NF; ++n) {
@@ -130,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void mx4_tile_kernel(const Mx4Params p) {
         if (live[n] && in) {
           const size_t blk = row[n] * blocks + 4 * s + lg;
           b = *reinterpret_cast<const u32x4*>(xq + blk * 16);
-          bs = xs[blk];
+          bs = xs[row[n] * 16 * quads + mx4_scale_at(4 * s + lg)];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i][n] = mfma_mx4(w[i], b, acc[i][n], ws[i], bs);
@@ -195,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void mx4_tile_kernel(const Mx4Params p) {
           uint16_t* q = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(p.h) + rr * (a.F / 2) + 16 * cx + 2 * lg);
           q[0] = static_cast<uint16_t>(c);
           q[4] = static_cast<uint16_t>(c >> 16);
-          if (lg == 0) p.hs[rr * (a.F / 32) + cx] = static_cast<uint8_t>(byte);
+          if (lg == 0) p.hs[rr * 16 * mx4_quads(a.F) + mx4_scale_at(cx)] = static_cast<uint8_t>(byte);
         }
       } else if (ok) {
         uint2* q = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.h) + rr * a.F + 32 * cx + 4 * lg);
@@ -256,9 +247,9 @@ Mx4Layout mx4_layout(int T, int d, int F, int E, int K, int n_shared) {
   w.row_tok = take(rows * 4);
   w.pcount = take(static_cast<size_t>(permute_chunks(T, K + n_shared)) * G * 4);
   w.xq = take(static_cast<size_t>(T) * d / 2);
-  w.xs = take(static_cast<size_t>(T) * d / kMxBlock);
+  w.xs = take(static_cast<size_t>(T) * mx4_quads(d) * 16);
   w.h = take(rows * F * 2);
-  w.hs = take(rows * F / kMxBlock);
+  w.hs = take(rows * mx4_quads(F) * 16);
   w.o = take(rows * d * 4);
   w.total = off;
   return w;
@@ -279,7 +270,7 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   p.pb.perm = reinterpret_cast<int32_t*>(ws + w.perm);
   p.pb.inv = reinterpret_cast<int32_t*>(ws + w.inv);
   p.pb.row_tok = reinterpret_cast<int32_t*>(ws + w.row_tok);
-  p.xq = reinterpret_cast<uint32_t*>(ws + w.xq);
+  p.xq = reinterpret_cast<uint8_t*>(ws + w.xq);
   p.xs = reinterpret_cast<uint8_t*>(ws + w.xs);
   p.h = ws + w.h;
   p.hs = reinterpret_cast<uint8_t*>(ws + w.hs);
@@ -292,11 +283,13 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const bool few = a.T <= 16;
-  const int tile_rows = few ? 16 : 64;
+  const bool wide = rows >= 100 * p.G;
+  const int tile_rows = few ? 16 : wide ? kMx4TileRows : 64;
   err = launch_permute(p.idx, a.T, KS, p.G, 0, tile_rows, p.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
   if (err != hipSuccess) return err;
   const int max_tiles = std::min(rows, rows / tile_rows + p.G);
-  if (a.mx_act) err = few ? launch_tiles<true, 1>(p, max_tiles, stream) : launch_tiles<true, 4>(p, max_tiles, stream);
+  if (wide) err = launch_mx4_wide(p, max_tiles, stream);
+  else if (a.mx_act) err = few ? launch_tiles<true, 1>(p, max_tiles, stream) : launch_tiles<true, 4>(p, max_tiles, stream);
   else err = few ? launch_tiles<false, 1>(p, max_tiles, stream) : launch_tiles<false, 4>(p, max_tiles, stream);
   if (err != hipSuccess) return err;
   const int64_t cn = static_cast<int64_t>(a.T) * a.d / 4;

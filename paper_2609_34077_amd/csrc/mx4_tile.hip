@@ -1,0 +1,339 @@
+// Both products of experts on MX4 weights for many rows per expert: 256 weight rows x 256 token rows a
+// workgroup on the matrix units' 16 x 16 tiles.
+//
+// Eight wavefronts: wave w owns weight fragments 8 (w / 4) .. + 7 (16 rows each) and token fragments w % 4,
+// + 4, + 8, + 12, so that a last tile with few rows leaves every wavefront equally little to multiply. Weight rows
+// are the instruction's row operand: a lane holds four neighbouring output columns of one token, and the gate and
+// up rows of a column, which alternate in the packed layout, meet in one lane.
+//   bf16 activations  stages of 128 columns. Weights go from global memory to the registers of the four wavefronts
+//                     that share them (4 bits a value: a quarter of the bytes that LDS would have to pass), half a stage
+//                     ahead, and are widened to bf16 there, beside the products (v_mfma_f32_16x16x32_bf16); tokens
+//                     go straight to LDS, double-buffered (2 x 64 KB).
+//   MX4 activations   stages of 256 columns on v_mfma_scale_f32_16x16x128_f8f6f4; both operands go straight to LDS
+//                     (2 x 64 KB), the scales to registers, four steps a dword.
+// Token loads are buffer loads: rows past the tile's end and columns past a row's end read as zeros.
+
+#include "gemm_tile.hpp"
+#include "mx4.hpp"
+#include "mx4_block.hpp"
+
+namespace maskmoe {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kFrags = 16;               // weight fragments of a tile
+constexpr int kWF = 8, kTF = 4;          // a wavefront's fragments
+constexpr uint32_t kNoRow = 0xfffffff0u; // past any operand (fewer than 2^32 - 256 bytes)
+
+// 16 bytes per lane at rsrc + voff + soff straight into LDS at m0v + 16 * lane; zeros past the buffer's end.
+__device__ __forceinline__ void dma16s(uint32_t m0v, i32x4 rsrc, uint32_t voff, uint32_t soff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(m0v), "v"(voff), "s"(rsrc),
+               "s"(soff)
+               : "memory", "m0");
+}
+
+struct Tile {
+  int g, row0, nrows, f0;   // expert, its first row and rows here, first weight fragment
+};
+
+template <bool MX, int EPI, int NL>
+__device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x4* lds) {
+  const Mx4Args& a = p.a;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const int C = EPI == 0 ? a.d : a.F, R = EPI == 0 ? 2 * a.F : a.d;
+  const int steps = mx4_steps(C), quads = mx4_quads(C);
+  const uint8_t* wc = (EPI == 0 ? a.gu_codes : a.dn_codes) + static_cast<size_t>(t.g) * (R / 16) * steps * 1024;
+  const uint8_t* wsc = (EPI == 0 ? a.gu_scales : a.dn_scales) + static_cast<size_t>(t.g) * (R / 16) * quads * 256;
+  const __amdgpu_buffer_rsrc_t cr = make_rsrc(wc, static_cast<uint32_t>(R / 16) * steps * 1024);
+  const __amdgpu_buffer_rsrc_t sr = make_rsrc(wsc, static_cast<uint32_t>(R / 16) * quads * 256);
+  uint32_t frag[kWF];   // fragments past the matrix repeat its last one and are not stored
+#pragma unroll
+  for (int i = 0; i < kWF; ++i) frag[i] = min(t.f0 + kWF * wm + i, R / 16 - 1);
+  const int src_rows = EPI == 0 ? a.T : a.T * (a.K + a.n_shared);
+  const void* x = EPI == 0 ? (MX ? static_cast<const void*>(p.xq) : a.x) : p.h;
+  const uint32_t row_bytes = MX ? C / 2 : 2 * C;
+  const i32x4 xr = buffer_rsrc(x, static_cast<uint32_t>(src_rows) * row_bytes);
+  const uint32_t lds0 = lds_offset(lds);
+  auto source = [&](int r) { return EPI == 0 ? p.pb.row_tok[t.row0 + r] : t.row0 + r; };
+
+  f32x4 acc[kWF][NL];
+#pragma unroll
+  for (int i = 0; i < kWF; ++i)
+#pragma unroll
+    for (int n = 0; n < NL; ++n) acc[i][n] = f32x4{0, 0, 0, 0};
+
+  if constexpr (!MX) {
+    // token pieces: instruction i of this wave fills stage rows 4 (8 wave + i) .. + 3, 256 bytes each; the piece at
+    // slot s of row r is logical piece s ^ (r & 15), so that 16 rows at one logical piece fall on all banks
+    uint32_t off[8];
+    bool upper[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * (8 * wave + i) + (lane >> 4);
+      const int piece = (lane & 15) ^ (r & 15);
+      off[i] = r < t.nrows ? source(r) * row_bytes + piece * 16 : kNoRow;
+      upper[i] = piece >= 8;
+    }
+    const bool half = C % kMxStep != 0;   // the last step holds 64 columns
+    auto dma = [&](int s, int buf) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (4 * (8 * wave + i) >= 64 * NL) break;   // rows that no wavefront multiplies
+        const uint32_t o = half && s == steps - 1 && upper[i] ? kNoRow : off[i];
+        const uint32_t so = static_cast<uint32_t>(s) * 256;
+        dma16s(lds0 + buf * 65536 + (8 * wave + i) * 1024, xr, o, so);
+      }
+    };
+    // Weights of a half of the fragments are loaded again, for the next step, as soon as its products are done.
+    constexpr int kHalf = kWF / 2;
+    u32x4 w[2][kHalf];
+    uint32_t ws[2][kHalf];
+    auto load_w = [&](int s, int hf) {
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i) {
+        const uint32_t f = frag[kHalf * hf + i];
+        w[hf][i] = __builtin_amdgcn_raw_buffer_load_b128(cr, lane * 16, (f * steps + s) * 1024, 0);
+        ws[hf][i] = __builtin_amdgcn_raw_buffer_load_b32(sr, lane * 4, (f * quads + (s >> 2)) * 256, 0);
+      }
+    };
+    // token row 16 (4 n + wn) + l16 of the stage, logical piece 4 lg + j
+    auto compute = [&](int s, int hf) {
+      float sc[kHalf];
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i) sc[i] = mx4_scale(ws[hf][i] >> (8 * (s & 3)) & 255);
+      const u32x4* b0 = lds + (s & 1) * 4096 + (16 * wn + l16) * 16;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        u32x4 b[NL];
+#pragma unroll
+        for (int n = 0; n < NL; ++n) b[n] = b0[n * 1024 + ((4 * lg + j) ^ l16)];
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+          const u32x4 wa = mx4_to_bf16(w[hf][i][j], sc[i]);
+#pragma unroll
+          for (int n = 0; n < NL; ++n) acc[kHalf * hf + i][n] = mfma_16x16x32(wa, b[n], acc[kHalf * hf + i][n]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto settle = [&](int hf) {   // in registers: the compiler waits here, not behind the next stage's loads
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i) asm volatile("" : "+v"(w[hf][i]), "+v"(ws[hf][i]));
+    };
+    dma(0, 0);
+    load_w(0, 0);
+    load_w(0, 1);
+    for (int s = 0; s < steps; ++s) {
+      // all but the second half's loads; the stage is whole when every wavefront has waited for its part
+      wait_vmcnt<2 * kHalf>();
+      settle(0);
+      lds_sync();
+      const int nx = min(s + 1, steps - 1);   // past the end: a buffer that nothing reads again
+      dma(nx, (s + 1) & 1);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(s, 0);
+      load_w(nx, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(s, 1);
+      load_w(nx, 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    wait_vmcnt<0>();
+  } else {
+    // stage: 16 fragments x 2 steps of weights (32 KB, operand order), 256 rows x 128 bytes of tokens (32 KB; the
+    // piece at slot s of row r is logical piece s ^ (r / 2 & 7))
+    const int stages = (steps + 1) / 2;
+    uint32_t off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * (4 * wave + i) + (lane >> 3);
+      off[i] = r < t.nrows ? source(r) * row_bytes + ((lane & 7) ^ (r >> 1 & 7)) * 16 : kNoRow;
+    }
+    const i32x4 wr = buffer_rsrc(wc, static_cast<uint32_t>(R / 16) * steps * 1024);
+    auto dma = [&](int st, int buf) {
+      const uint32_t base = lds0 + buf * 65536;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {   // fragments 2 wave, + 1, both steps of each
+        const int f = min(t.f0 + 2 * wave + (i >> 1), R / 16 - 1), s = min(2 * st + (i & 1), steps - 1);
+        dma16s(base + (4 * wave + i) * 1024, wr, lane * 16, (static_cast<uint32_t>(f) * steps + s) * 1024);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (8 * (4 * wave + i) >= 64 * NL) break;
+        dma16s(base + 32768 + (4 * wave + i) * 1024, xr, off[i], static_cast<uint32_t>(st) * 128);
+      }
+    };
+    // scales: a dword of four steps per fragment; tokens [row, quad, 16]
+    const uint8_t* xs = EPI == 0 ? p.xs : p.hs;
+    const __amdgpu_buffer_rsrc_t xsr = make_rsrc(xs, static_cast<uint32_t>(src_rows) * quads * 16);
+    uint32_t soff[NL];
+#pragma unroll
+    for (int n = 0; n < NL; ++n) {
+      const int r = 16 * (4 * n + wn) + l16;
+      soff[n] = r < t.nrows ? source(r) * quads * 16 + 4 * lg : kNoRow;
+    }
+    uint32_t ws[2][kWF], ts[2][NL];
+    auto load_s = [&](int q, uint32_t (&w)[kWF], uint32_t (&b)[NL]) {
+#pragma unroll
+      for (int i = 0; i < kWF; ++i) w[i] = __builtin_amdgcn_raw_buffer_load_b32(sr, lane * 4, (frag[i] * quads + q) * 256, 0);
+#pragma unroll
+      for (int n = 0; n < NL; ++n) b[n] = __builtin_amdgcn_raw_buffer_load_b32(xsr, soff[n], q * 16, 0);
+    };
+    // the last step of a C of an odd number of 64 columns: its upper blocks have no token scales
+    const int cut = C % kMxStep != 0 ? steps - 1 : -1;
+    auto compute = [&](auto sub_c, int s, int buf, const uint32_t (&w)[kWF], const uint32_t (&b)[NL]) {
+      constexpr int S = decltype(sub_c)::value;   // step within the quad
+      const u32x4* wa = lds + buf * 4096 + kWF * wm * 128 + (S & 1) * 64 + lane;
+      const u32x4* xa = lds + buf * 4096 + 2048 + (16 * wn + l16) * 8 + ((4 * (S & 1) + lg) ^ (l16 >> 1));
+      u32x4 xv[NL];
+      uint32_t bs[NL];
+#pragma unroll
+      for (int n = 0; n < NL; ++n) {
+        xv[n] = xa[n * 512];
+        bs[n] = s == cut && lg >= 2 ? 0 : b[n];
+      }
+#pragma unroll
+      for (int i = 0; i < kWF; ++i) {
+        const u32x4 wv = wa[i * 128];
+#pragma unroll
+        for (int n = 0; n < NL; ++n) acc[i][n] = mfma_mx4<S>(wv, xv[n], acc[i][n], w[i], bs[n]);
+      }
+    };
+    auto arrive = [&]() {
+      wait_vmcnt<0>();
+      lds_sync();
+    };
+    auto settle = [&](uint32_t (&w)[kWF], uint32_t (&b)[NL]) {
+#pragma unroll
+      for (int i = 0; i < kWF; ++i) asm volatile("" : "+v"(w[i]));
+#pragma unroll
+      for (int n = 0; n < NL; ++n) asm volatile("" : "+v"(b[n]));
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+    dma(0, 0);
+    load_s(0, ws[0], ts[0]);
+    arrive();
+    settle(ws[0], ts[0]);
+    // a quad of steps: stage 2 q in buffer 0, stage 2 q + 1 in buffer 1
+    auto quad = [&](int q, uint32_t (&w)[kWF], uint32_t (&b)[NL], uint32_t (&wn_)[kWF], uint32_t (&bn)[NL]) {
+      const int s = 4 * q;
+      dma(min(2 * q + 1, stages - 1), 1);
+      load_s(min(q + 1, quads - 1), wn_, bn);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(I0{}, s, 0, w, b);
+      if (s + 1 < steps) compute(I1{}, s + 1, 0, w, b);
+      __builtin_amdgcn_sched_barrier(0);
+      arrive();
+      settle(wn_, bn);
+      if (s + 2 >= steps) return;
+      dma(min(2 * q + 2, stages - 1), 0);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(I2{}, s + 2, 1, w, b);
+      if (s + 3 < steps) compute(I3{}, s + 3, 1, w, b);
+      __builtin_amdgcn_sched_barrier(0);
+      arrive();
+    };
+    for (int q = 0; q < quads; q += 2) {
+      quad(q, ws[0], ts[0], ws[1], ts[1]);
+      if (q + 1 < quads) quad(q + 1, ws[1], ts[1], ws[0], ts[0]);
+    }
+  }
+
+  // acc[i][n][e]: weight row 4 lg + e of fragment i, token l16 of fragment 4 n + wn
+#pragma unroll
+  for (int n = 0; n < NL; ++n) {
+    const int r = 16 * (4 * n + wn) + l16;
+    const bool ok = r < t.nrows;
+    const size_t row = t.row0 + r;
+    if constexpr (EPI == 1) {
+#pragma unroll
+      for (int i = 0; i < kWF; ++i) {
+        const int f = t.f0 + kWF * wm + i;
+        if (ok && f < R / 16) *reinterpret_cast<f32x4*>(p.o + row * a.d + 16 * f + 4 * lg) = acc[i][n];
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kWF / 4; ++q) {   // 32 columns: two gate and two up fragments
+        const int cb = (t.f0 + kWF * wm) / 4 + q;   // their block of h
+        float h[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          h[e] = silu(acc[4 * q][n][e]) * acc[4 * q + 1][n][e];
+          h[4 + e] = silu(acc[4 * q + 2][n][e]) * acc[4 * q + 3][n][e];
+        }
+        if constexpr (MX) {
+          uint32_t m = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(h[e]) & 0x7fffffffu);
+          m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, kWave)));
+          m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32, kWave)));
+          const uint32_t byte = mx4_scale_byte(m);
+          const uint32_t c = byte == 255 ? 0 : mx4_codes(h, mx4_scale(byte));
+          if (ok && cb < a.F / 32) {
+            uint16_t* o = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(p.h) + row * (a.F / 2) + 16 * cb + 2 * lg);
+            o[0] = static_cast<uint16_t>(c);
+            o[4] = static_cast<uint16_t>(c >> 16);
+            if (lg == 0) p.hs[row * 16 * mx4_quads(a.F) + mx4_scale_at(cb)] = static_cast<uint8_t>(byte);
+          }
+        } else if (ok && cb < a.F / 32) {
+          uint2* o = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.h) + row * a.F + 32 * cb + 4 * lg);
+          o[0] = make_uint2(f32x2_to_bf16x2(h[0], h[1]), f32x2_to_bf16x2(h[2], h[3]));
+          o[4] = make_uint2(f32x2_to_bf16x2(h[4], h[5]), f32x2_to_bf16x2(h[6], h[7]));
+        }
+      }
+    }
+  }
+}
+
+template <bool MX, int EPI>
+__global__ __launch_bounds__(kThreads, 2) void mx4_wide_kernel(const Mx4Params p) {
+  __shared__ u32x4 lds[8192];
+  const int R = EPI == 0 ? 2 * p.a.F : p.a.d;
+  const int wt = (R / 16 + kFrags - 1) / kFrags;   // weight tiles
+  const int live = p.pb.tile_off[p.G] * wt;
+  if (static_cast<int>(blockIdx.x) >= live) return;
+  const int lid = xcd_tile_id(live);
+  int mt, nt;
+  grouped_tile_coords(lid, p.pb.tile_off[p.G], wt, mt, nt);
+  int g = 0;
+  {
+    const int lane = threadIdx.x & 63;
+    for (int g0 = 0; g0 < p.G; g0 += kWave) {
+      const int i = g0 + lane;
+      g += __popcll(__ballot(i < p.G && p.pb.tile_off[i + 1] <= mt));
+    }
+  }
+  Tile t;
+  t.g = g;
+  t.row0 = p.pb.offsets[g] + (mt - p.pb.tile_off[g]) * kMx4TileRows;
+  t.nrows = min(kMx4TileRows, p.pb.offsets[g + 1] - t.row0);
+  t.f0 = nt * kFrags;
+  const int nl = __builtin_amdgcn_readfirstlane((t.nrows + 63) / 64);   // token fragments per wavefront
+  if (nl == 4) run_tile<MX, EPI, 4>(p, t, lds);
+  else if (nl == 3) run_tile<MX, EPI, 3>(p, t, lds);
+  else if (nl == 2) run_tile<MX, EPI, 2>(p, t, lds);
+  else run_tile<MX, EPI, 1>(p, t, lds);
+}
+
+template <bool MX>
+hipError_t launch(const Mx4Params& p, int max_tiles, hipStream_t stream) {
+  auto grid = [&](int R) { return dim3(static_cast<unsigned>(max_tiles) * ((R / 16 + kFrags - 1) / kFrags)); };
+  hipLaunchKernelGGL((mx4_wide_kernel<MX, 0>), grid(2 * p.a.F), dim3(kThreads), 0, stream, p);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL((mx4_wide_kernel<MX, 1>), grid(p.a.d), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mx4_wide(const Mx4Params& p, int max_tiles, hipStream_t stream) {
+  return p.a.mx_act ? launch<true>(p, max_tiles, stream) : launch<false>(p, max_tiles, stream);
+}
+
+}  // namespace maskmoe
