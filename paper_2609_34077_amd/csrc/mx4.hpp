@@ -55,6 +55,18 @@ struct Mx4Params {
   float* o;          // [rows, d]
   int G;             // E + n_shared
 };
+// Up to kMx4FewT tokens (mx4_few.hip): both products without prepare and permutation; p.o holds kMx4FewSplits x T rows.
+constexpr int kMx4FewT = 16, kMx4FewSplits = 32;
+// Parts of the down projection's reductions: about four workgroups (64 columns each) a CU, a multiple of 8.
+inline int mx4_few_splits(int d) {
+  const int s = (1024 / (d / 64) + 7) / 8 * 8;
+  return s < 8 ? 8 : s > kMx4FewSplits ? kMx4FewSplits : s;
+}
+hipError_t launch_mx4_few(const Mx4Params& p, hipStream_t stream);
+// Few rows per expert (mx4_batch.hip), the permutation in tiles of kMx4BatchRows; the down projection's reduction in
+// `splits` parts, each with its own rows of o.
+constexpr int kMx4BatchRows = 64, kMx4BatchSplits = 8, kMx4BatchSplitRows = 8192;
+hipError_t launch_mx4_batch(const Mx4Params& p, int max_tiles, int splits, hipStream_t stream);
 // Many rows per expert (mx4_tile.hip): both products on 256 x 256 tiles, the permutation in tiles of kMx4TileRows.
 constexpr int kMx4TileRows = 256;
 hipError_t launch_mx4_wide(const Mx4Params& p, int max_tiles, hipStream_t stream);

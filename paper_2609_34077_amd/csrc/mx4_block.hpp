@@ -40,6 +40,29 @@ __device__ __forceinline__ u32x4 mx4_to_bf16(uint32_t codes, float scale) {
   return r;
 }
 
+// A block of 32 bf16 values in one lane (v) to its 16 bytes of codes; returns the scale byte.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t mx4_block_codes(const u32x4 (&v)[4], u32x4& codes) {
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i][j] & 0x7fff7fffu));
+  const uint32_t byte = mx4_scale_byte(static_cast<uint32_t>(m.x > m.y ? m.x : m.y) << 16);
+  const float s = mx4_scale(byte);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = v[i][0], b = v[i][1], c = v[i][2], d = v[i][3];
+    uint32_t r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2_t, a), s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2_t, b), s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2_t, c), s, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2_t, d), s, 3);
+    codes[i] = byte == 255 ? 0 : r;
+  }
+  return byte;
+}
+
 // Byte of block b's scale in a row of activation scales (Mx4Params::xs).
 __device__ __forceinline__ int mx4_scale_at(int b) { return 16 * (b >> 4) + 4 * (b & 3) + (b >> 2 & 3); }
 

@@ -56,149 +56,9 @@ __global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p
   }
 }
 
-// Group that holds row tile `tile` (tile < tile_off[G]): the groups that end at or before it, counted by
-// all lanes in one round trip.
-__device__ __forceinline__ int group_of_tile(const int32_t* tile_off, int G, int tile) {
-  const int lane = threadIdx.x & 63;
-  int g = 0;
-  for (int g0 = 0; g0 < G; g0 += kWave) {
-    const int i = g0 + lane;
-    g += __popcll(__ballot(i < G && tile_off[i + 1] <= tile));
-  }
-  return g;
-}
-
-// A tile of 16 NF rows of one expert times 64 weight rows (EPI 0: 32 gate rows and their up rows, then the
-// SwiGLU; EPI 1: rows of W_down). Four wavefronts split the reduction and join in LDS.
-template <bool MX, int NF, int EPI>
-__global__ __launch_bounds__(kThreads) void mx4_tile_kernel(const Mx4Params p) {
-  __shared__ f32x4 red[4][4][NF][kWave];
-  const Mx4Args& a = p.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, lg = lane >> 4;
-  const int cols = EPI == 0 ? a.F / 32 : a.d / 64;
-  const int tile = blockIdx.x / cols, cx = blockIdx.x % cols;
-  if (tile >= p.pb.tile_off[p.G]) return;
-  const int g = group_of_tile(p.pb.tile_off, p.G, tile);
-  const int r0 = p.pb.offsets[g] + (tile - p.pb.tile_off[g]) * 16 * NF;
-  const int nrows = min(16 * NF, p.pb.offsets[g + 1] - r0);
-  const int C = EPI == 0 ? a.d : a.F, R = EPI == 0 ? 2 * a.F : a.d;
-  const int steps = mx4_steps(C), quads = mx4_quads(C), blocks = C / kMxBlock;
-  const uint8_t* codes = (EPI == 0 ? a.gu_codes : a.dn_codes) + static_cast<size_t>(g) * (R / 16) * steps * 1024;
-  const uint8_t* scales = (EPI == 0 ? a.gu_scales : a.dn_scales) + static_cast<size_t>(g) * (R / 16) * quads * 256;
-  size_t row[NF];
-  bool live[NF];
-#pragma unroll
-  for (int n = 0; n < NF; ++n) {
-    const int r = 16 * n + l16;
-    live[n] = r < nrows;
-    row[n] = !live[n] ? 0 : EPI == 0 ? p.pb.row_tok[r0 + r] : r0 + r;
-  }
-  f32x4 acc[4][NF];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int n = 0; n < NF; ++n) acc[i][n] = f32x4{0, 0, 0, 0};
-  const int per = (steps + 3) / 4;
-  const int s1 = min((wave + 1) * per, steps);
-#pragma unroll 2
-  for (int s = wave * per; s < s1; ++s) {
-    const bool in = 4 * s + lg < blocks;
-    u32x4 w[4];
-    uint32_t ws[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const size_t f = 4 * cx + i;
-      w[i] = *reinterpret_cast<const u32x4*>(codes + (f * steps + s) * 1024 + lane * 16);
-      ws[i] = *reinterpret_cast<const uint32_t*>(scales + ((f * quads + (s >> 2)) * 64 + lane) * 4) >> (8 * (s & 3));
-    }
-    if constexpr (MX) {
-      const uint8_t* xq = EPI == 0 ? p.xq : static_cast<const uint8_t*>(p.h);
-      const uint8_t* xs = EPI == 0 ? p.xs : p.hs;
-#pragma unroll
-      for (int n = 0; n < NF; ++n) {
-        u32x4 b = {0, 0, 0, 0};
-        uint32_t bs = 0;
-        if (live[n] && in) {
-          const size_t blk = row[n] * blocks + 4 * s + lg;
-          b = *reinterpret_cast<const u32x4*>(xq + blk * 16);
-          bs = xs[row[n] * 16 * quads + mx4_scale_at(4 * s + lg)];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][n] = mfma_mx4(w[i], b, acc[i][n], ws[i], bs);
-      }
-    } else {
-      const uint16_t* x = EPI == 0 ? a.x : static_cast<const uint16_t*>(p.h);
-      u32x4 b[NF][4];
-#pragma unroll
-      for (int n = 0; n < NF; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          b[n][j] = u32x4{0, 0, 0, 0};
-          if (live[n] && in)
-            b[n][j] = *reinterpret_cast<const u32x4*>(x + row[n] * C + kMxStep * s + 32 * lg + 8 * j);
-        }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float sc = mx4_scale(ws[i] & 255);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x4 wa = mx4_to_bf16(w[i][j], sc);
-#pragma unroll
-          for (int n = 0; n < NF; ++n) acc[i][n] = mfma_16x16x32(wa, b[n][j], acc[i][n]);
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int n = 0; n < NF; ++n) red[wave][i][n][lane] = acc[i][n];
-  lds_sync();
-  for (int n = wave; n < NF; n += 4) {
-    f32x4 v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = red[0][i][n][lane] + red[1][i][n][lane] + red[2][i][n][lane] + red[3][i][n][lane];
-    const bool ok = 16 * n + l16 < nrows;
-    const size_t rr = r0 + 16 * n + l16;
-    if constexpr (EPI == 1) {
-      if (ok) {
-        f32x4* o = reinterpret_cast<f32x4*>(p.o + rr * a.d + 64 * cx + 4 * lg);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[4 * i] = v[i];
-      }
-    } else {
-      // lane: rows 4 lg + i of both 16-row halves of the 32, one token
-      float h[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        h[i] = silu(v[0][i]) * v[1][i];
-        h[4 + i] = silu(v[2][i]) * v[3][i];
-      }
-      if constexpr (MX) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(h[i]) & 0x7fffffffu);
-        m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, kWave)));
-        m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32, kWave)));
-        const uint32_t byte = mx4_scale_byte(m);
-        const uint32_t c = byte == 255 ? 0 : mx4_codes(h, mx4_scale(byte));
-        if (ok) {
-          uint16_t* q = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(p.h) + rr * (a.F / 2) + 16 * cx + 2 * lg);
-          q[0] = static_cast<uint16_t>(c);
-          q[4] = static_cast<uint16_t>(c >> 16);
-          if (lg == 0) p.hs[rr * 16 * mx4_quads(a.F) + mx4_scale_at(cx)] = static_cast<uint8_t>(byte);
-        }
-      } else if (ok) {
-        uint2* q = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.h) + rr * a.F + 32 * cx + 4 * lg);
-        q[0] = make_uint2(f32x2_to_bf16x2(h[0], h[1]), f32x2_to_bf16x2(h[2], h[3]));
-        q[4] = make_uint2(f32x2_to_bf16x2(h[4], h[5]), f32x2_to_bf16x2(h[6], h[7]));
-      }
-    }
-  }
-}
-
-// y = sum of the gate-weighted expert outputs in entry order, fp32, rounded once; a thread per 4 columns.
-__global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p) {
+// y = sum of the gate-weighted expert outputs (each the sum of its parts) in entry order, fp32, rounded once; a thread
+// per 4 columns.
+__global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p, int splits) {
   const Mx4Args& a = p.a;
   const int KS = a.K + a.n_shared, c4 = a.d / 4;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
@@ -209,20 +69,13 @@ __global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p
     const int j = t * KS + k;
     if (p.idx[j] < 0) continue;
     const float g = p.gate[j];
-    const f32x4 o = reinterpret_cast<const f32x4*>(p.o)[static_cast<size_t>(p.pb.inv[j]) * c4 + c];
+    const f32x4* src = reinterpret_cast<const f32x4*>(p.o) + static_cast<size_t>(p.pb.inv[j]) * c4 + c;
+    f32x4 o = src[0];
+    for (int z = 1; z < splits; ++z) o += src[static_cast<size_t>(z) * a.T * KS * c4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) s[q] += g * o[q];
   }
   reinterpret_cast<uint2*>(a.y)[i] = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
-}
-
-template <bool MX, int NF>
-hipError_t launch_tiles(const Mx4Params& p, int max_tiles, hipStream_t stream) {
-  hipLaunchKernelGGL((mx4_tile_kernel<MX, NF, 0>), dim3(p.a.F / 32 * max_tiles), dim3(kThreads), 0, stream, p);
-  const hipError_t err = hipGetLastError();
-  if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((mx4_tile_kernel<MX, NF, 1>), dim3(p.a.d / 64 * max_tiles), dim3(kThreads), 0, stream, p);
-  return hipGetLastError();
 }
 
 }  // namespace
@@ -250,7 +103,10 @@ Mx4Layout mx4_layout(int T, int d, int F, int E, int K, int n_shared) {
   w.xs = take(static_cast<size_t>(T) * mx4_quads(d) * 16);
   w.h = take(rows * F * 2);
   w.hs = take(rows * mx4_quads(F) * 16);
-  w.o = take(rows * d * 4);
+  // rows of o: one per entry; the parts of the few-token and batch paths' reductions
+  const size_t few = static_cast<size_t>(kMx4FewSplits) * std::min(T, kMx4FewT);
+  const size_t batch = std::min<size_t>(kMx4BatchSplits * rows, kMx4BatchSplitRows);
+  w.o = take(std::max({rows, few, batch}) * d * 4);
   w.total = off;
   return w;
 }
@@ -275,6 +131,7 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   p.h = ws + w.h;
   p.hs = reinterpret_cast<uint8_t*>(ws + w.hs);
   p.o = reinterpret_cast<float*>(ws + w.o);
+  if (a.T <= kMx4FewT) return launch_mx4_few(p, stream);
   const int KS = a.K + a.n_shared, rows = a.T * KS;
   const int entry_blocks = (rows + kThreads - 1) / kThreads;
   const int64_t quant_blocks = a.mx_act ? (static_cast<int64_t>(a.T) * a.d / 8 + kThreads - 1) / kThreads : 0;
@@ -282,19 +139,26 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
                      stream, p, entry_blocks);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  const bool few = a.T <= 16;
   const bool wide = rows >= 100 * p.G;
-  const int tile_rows = few ? 16 : wide ? kMx4TileRows : 64;
+  const int tile_rows = wide ? kMx4TileRows : kMx4BatchRows;
   err = launch_permute(p.idx, a.T, KS, p.G, 0, tile_rows, p.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
   if (err != hipSuccess) return err;
   const int max_tiles = std::min(rows, rows / tile_rows + p.G);
-  if (wide) err = launch_mx4_wide(p, max_tiles, stream);
-  else if (a.mx_act) err = few ? launch_tiles<true, 1>(p, max_tiles, stream) : launch_tiles<true, 4>(p, max_tiles, stream);
-  else err = few ? launch_tiles<false, 1>(p, max_tiles, stream) : launch_tiles<false, 4>(p, max_tiles, stream);
+  int splits = 1;
+  if (wide) {
+    err = launch_mx4_wide(p, max_tiles, stream);
+  } else {
+    // two workgroups a CU for the down projection, each with eight steps or more
+    const int jobs = std::min(rows, p.G) * ((a.d + 255) / 256);
+    while (splits < kMx4BatchSplits && jobs * splits < 512 && mx4_steps(a.F) >= 16 * splits &&
+           2 * splits * rows <= kMx4BatchSplitRows)
+      splits *= 2;
+    err = launch_mx4_batch(p, max_tiles, splits, stream);
+  }
   if (err != hipSuccess) return err;
   const int64_t cn = static_cast<int64_t>(a.T) * a.d / 4;
   hipLaunchKernelGGL(mx4_combine_kernel, dim3(static_cast<unsigned>((cn + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                     stream, p);
+                     stream, p, splits);
   return hipGetLastError();
 }
 
