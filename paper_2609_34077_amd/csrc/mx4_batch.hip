@@ -146,22 +146,21 @@ __device__ __forceinline__ void run_job(const Mx4Params& p, const Job& t, u32x4*
     wait_vmcnt<kOps*(kDepth - 1)>();
     lds_sync();
     dma(min(s + kDepth, t.s1 - 1), (s + kDepth) % (kDepth + 1));
-    multiply(s, s % (kDepth + 1), q);
+    __builtin_amdgcn_sched_barrier(0);
+    if (s < t.s1) multiply(s, s % (kDepth + 1), q);
+    __builtin_amdgcn_sched_barrier(0);
     load(min(s + kDepth, t.s1 - 1), q);
+    __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll
   for (int i = 0; i < kDepth; ++i) {
     dma(min(t.s0 + i, t.s1 - 1), (t.s0 + i) % (kDepth + 1));
     load(min(t.s0 + i, t.s1 - 1), st[i]);
   }
-  int s = t.s0;
-  for (; s + kDepth <= t.s1; s += kDepth) {
+  for (int s = t.s0; s < t.s1; s += kDepth) {
 #pragma unroll
     for (int i = 0; i < kDepth; ++i) step(s + i, st[i]);
   }
-#pragma unroll
-  for (int i = 0; i + 1 < kDepth; ++i)
-    if (s + i < t.s1) step(s + i, st[i]);
   wait_vmcnt<0>();   // nothing may arrive in LDS after the workgroup's end
 
   // acc[i][n][e]: weight row 4 lg + e of fragment i, token l16 of fragment n
