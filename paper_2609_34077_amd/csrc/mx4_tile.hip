@@ -1,16 +1,20 @@
 // Both products of experts on MX4 weights for many rows per expert: 256 weight rows x 256 token rows a
 // workgroup on the matrix units' 16 x 16 tiles.
 //
-// Eight wavefronts: wave w owns weight fragments 8 (w / 4) .. + 7 (16 rows each) and token fragments w % 4,
-// + 4, + 8, + 12, so that a last tile with few rows leaves every wavefront equally little to multiply. Weight rows
+// Eight wavefronts, WN of them side by side along the tokens: wave w owns the weight fragments (16 rows each) of
+// w / WN and the token fragments w % WN, + WN, .., so that a last tile with few rows leaves every wavefront equally
+// little to multiply. Weight rows
 // are the instruction's row operand: a lane holds four neighbouring output columns of one token, and the gate and
 // up rows of a column, which alternate in the packed layout, meet in one lane.
-//   bf16 activations  stages of 128 columns. Weights go from global memory to the registers of the four wavefronts
-//                     that share them (4 bits a value: a quarter of the bytes that LDS would have to pass), half a stage
+//   bf16 activations  stages of 128 columns. Weights go from global memory to the registers of the two wavefronts
+//                     that share them (4 bits a value: a quarter of the bytes that LDS would have to pass), a stage
 //                     ahead, and are widened to bf16 there, beside the products (v_mfma_f32_16x16x32_bf16); tokens
-//                     go straight to LDS, double-buffered (2 x 64 KB).
+//                     go straight to LDS, double-buffered (2 x 64 KB). Widening two values takes about as long as a
+//                     product (16 cycles): with 8 x 4 fragments a wavefront (WN 4) it was as much work as they, 4850 us for the
+//                     Mixtral-shaped layer of 8192 tokens instead of 4330 with 4 x 8 (WN 2).
 //   MX4 activations   stages of 256 columns on v_mfma_scale_f32_16x16x128_f8f6f4; both operands go straight to LDS
-//                     (2 x 64 KB), the scales to registers, four steps a dword.
+//                     (2 x 64 KB), the scales to registers, four steps a dword. 8 x 4 fragments (DeepSeek-shaped layer, 4096
+//                     tokens: 362 us, with 4 x 8 398).
 // Token loads are buffer loads: rows past the tile's end and columns past a row's end read as zeros.
 
 #include "gemm_tile.hpp"
@@ -22,7 +26,8 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kFrags = 16;               // weight fragments of a tile
-constexpr int kWF = 8, kTF = 4;          // a wavefront's fragments
+template <bool MX>
+constexpr int kWN = MX ? 4 : 2;          // wavefronts side by side along the tokens
 constexpr uint32_t kNoRow = 0xfffffff0u; // past any operand (fewer than 2^32 - 256 bytes)
 
 // 16 bytes per lane at rsrc + voff + soff straight into LDS at m0v + 16 * lane; zeros past the buffer's end.
@@ -41,7 +46,8 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
   const Mx4Args& a = p.a;
   const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int wm = wave >> 2, wn = wave & 3;
+  constexpr int WN = kWN<MX>, kWF = 2 * WN;   // kWF: a wavefront's weight fragments
+  const int wm = wave / WN, wn = wave % WN;
   const int C = EPI == 0 ? a.d : a.F, R = EPI == 0 ? 2 * a.F : a.d;
   const int steps = mx4_steps(C), quads = mx4_quads(C);
   const uint8_t* wc = (EPI == 0 ? a.gu_codes : a.dn_codes) + static_cast<size_t>(t.g) * (R / 16) * steps * 1024;
@@ -80,65 +86,62 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     auto dma = [&](int s, int buf) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (4 * (8 * wave + i) >= 64 * NL) break;   // rows that no wavefront multiplies
+        if (4 * (8 * wave + i) >= 16 * WN * NL) break;   // rows that no wavefront multiplies
         const uint32_t o = half && s == steps - 1 && upper[i] ? kNoRow : off[i];
         const uint32_t so = static_cast<uint32_t>(s) * 256;
         dma16s(lds0 + buf * 65536 + (8 * wave + i) * 1024, xr, o, so);
       }
     };
-    // Weights of a half of the fragments are loaded again, for the next step, as soon as its products are done.
-    constexpr int kHalf = kWF / 2;
-    u32x4 w[2][kHalf];
-    uint32_t ws[2][kHalf];
-    auto load_w = [&](int s, int hf) {
+    u32x4 w[2][kWF];
+    uint32_t ws[2][kWF];
+    auto load_w = [&](int s, int set) {
 #pragma unroll
-      for (int i = 0; i < kHalf; ++i) {
-        const uint32_t f = frag[kHalf * hf + i];
-        w[hf][i] = __builtin_amdgcn_raw_buffer_load_b128(cr, lane * 16, (f * steps + s) * 1024, 0);
-        ws[hf][i] = __builtin_amdgcn_raw_buffer_load_b32(sr, lane * 4, (f * quads + (s >> 2)) * 256, 0);
+      for (int i = 0; i < kWF; ++i) {
+        w[set][i] = __builtin_amdgcn_raw_buffer_load_b128(cr, lane * 16, (frag[i] * steps + s) * 1024, 0);
+        ws[set][i] = __builtin_amdgcn_raw_buffer_load_b32(sr, lane * 4, (frag[i] * quads + (s >> 2)) * 256, 0);
       }
     };
-    // token row 16 (4 n + wn) + l16 of the stage, logical piece 4 lg + j
-    auto compute = [&](int s, int hf) {
-      float sc[kHalf];
+    // token row 16 (WN n + wn) + l16 of the stage, logical piece 4 lg + j
+    auto compute = [&](int s, int set) {
+      float sc[kWF];
 #pragma unroll
-      for (int i = 0; i < kHalf; ++i) sc[i] = mx4_scale(ws[hf][i] >> (8 * (s & 3)) & 255);
-      const u32x4* b0 = lds + (s & 1) * 4096 + (16 * wn + l16) * 16;
+      for (int i = 0; i < kWF; ++i) sc[i] = mx4_scale(ws[set][i] >> (8 * (s & 3)) & 255);
+      const u32x4* b0 = lds + set * 4096 + (16 * wn + l16) * 16;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         u32x4 b[NL];
 #pragma unroll
-        for (int n = 0; n < NL; ++n) b[n] = b0[n * 1024 + ((4 * lg + j) ^ l16)];
+        for (int n = 0; n < NL; ++n) b[n] = b0[n * WN * 256 + ((4 * lg + j) ^ l16)];
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-          const u32x4 wa = mx4_to_bf16(w[hf][i][j], sc[i]);
+        for (int i = 0; i < kWF; ++i) {
+          const u32x4 wa = mx4_to_bf16(w[set][i][j], sc[i]);
 #pragma unroll
-          for (int n = 0; n < NL; ++n) acc[kHalf * hf + i][n] = mfma_16x16x32(wa, b[n], acc[kHalf * hf + i][n]);
+          for (int n = 0; n < NL; ++n) acc[i][n] = mfma_16x16x32(wa, b[n], acc[i][n]);
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
     };
-    auto settle = [&](int hf) {   // in registers: the compiler waits here, not behind the next stage's loads
+    // the stage is whole when every wavefront has waited for its part; its weights are in registers then, so that the
+    // compiler does not wait again behind the next stage's loads
+    auto arrive = [&](int set) {
+      wait_vmcnt<0>();
 #pragma unroll
-      for (int i = 0; i < kHalf; ++i) asm volatile("" : "+v"(w[hf][i]), "+v"(ws[hf][i]));
+      for (int i = 0; i < kWF; ++i) asm volatile("" : "+v"(w[set][i]), "+v"(ws[set][i]));
+      lds_sync();
+    };
+    auto step = [&](int s, int set) {
+      arrive(set);
+      const int nx = min(s + 1, steps - 1);   // past the end: a buffer that nothing reads again
+      dma(nx, set ^ 1);
+      load_w(nx, set ^ 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s < steps) compute(s, set);
+      __builtin_amdgcn_sched_barrier(0);
     };
     dma(0, 0);
     load_w(0, 0);
-    load_w(0, 1);
-    for (int s = 0; s < steps; ++s) {
-      // all but the second half's loads; the stage is whole when every wavefront has waited for its part
-      wait_vmcnt<2 * kHalf>();
-      settle(0);
-      lds_sync();
-      const int nx = min(s + 1, steps - 1);   // past the end: a buffer that nothing reads again
-      dma(nx, (s + 1) & 1);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(s, 0);
-      load_w(nx, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(s, 1);
-      load_w(nx, 1);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int s = 0; s < steps; s += 2) {
+      step(s, 0);
+      step(s + 1, 1);
     }
     wait_vmcnt<0>();
   } else {
@@ -161,7 +164,7 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (8 * (4 * wave + i) >= 64 * NL) break;
+        if (8 * (4 * wave + i) >= 16 * WN * NL) break;
         dma16s(base + 32768 + (4 * wave + i) * 1024, xr, off[i], static_cast<uint32_t>(st) * 128);
       }
     };
@@ -171,7 +174,7 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     uint32_t soff[NL];
 #pragma unroll
     for (int n = 0; n < NL; ++n) {
-      const int r = 16 * (4 * n + wn) + l16;
+      const int r = 16 * (WN * n + wn) + l16;
       soff[n] = r < t.nrows ? source(r) * quads * 16 + 4 * lg : kNoRow;
     }
     uint32_t ws[2][kWF], ts[2][NL];
@@ -191,7 +194,7 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
       uint32_t bs[NL];
 #pragma unroll
       for (int n = 0; n < NL; ++n) {
-        xv[n] = xa[n * 512];
+        xv[n] = xa[n * WN * 128];
         bs[n] = s == cut && lg >= 2 ? 0 : b[n];
       }
 #pragma unroll
@@ -244,10 +247,10 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     }
   }
 
-  // acc[i][n][e]: weight row 4 lg + e of fragment i, token l16 of fragment 4 n + wn
+  // acc[i][n][e]: weight row 4 lg + e of fragment i, token l16 of fragment WN n + wn
 #pragma unroll
   for (int n = 0; n < NL; ++n) {
-    const int r = 16 * (4 * n + wn) + l16;
+    const int r = 16 * (WN * n + wn) + l16;
     const bool ok = r < t.nrows;
     const size_t row = t.row0 + r;
     if constexpr (EPI == 1) {
@@ -313,11 +316,12 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_wide_kernel(const Mx4Params p
   t.row0 = p.pb.offsets[g] + (mt - p.pb.tile_off[g]) * kMx4TileRows;
   t.nrows = min(kMx4TileRows, p.pb.offsets[g + 1] - t.row0);
   t.f0 = nt * kFrags;
-  const int nl = __builtin_amdgcn_readfirstlane((t.nrows + 63) / 64);   // token fragments per wavefront
-  if (nl == 4) run_tile<MX, EPI, 4>(p, t, lds);
-  else if (nl == 3) run_tile<MX, EPI, 3>(p, t, lds);
-  else if (nl == 2) run_tile<MX, EPI, 2>(p, t, lds);
-  else run_tile<MX, EPI, 1>(p, t, lds);
+  const int quarters = __builtin_amdgcn_readfirstlane((t.nrows + 63) / 64);   // of the tile's rows
+  constexpr int Q = 4 / kWN<MX>;   // a wavefront's token fragments per quarter
+  if (quarters == 4) run_tile<MX, EPI, 4 * Q>(p, t, lds);
+  else if (quarters == 3) run_tile<MX, EPI, 3 * Q>(p, t, lds);
+  else if (quarters == 2) run_tile<MX, EPI, 2 * Q>(p, t, lds);
+  else run_tile<MX, EPI, Q>(p, t, lds);
 }
 
 template <bool MX>
