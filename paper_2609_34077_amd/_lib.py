@@ -174,8 +174,9 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream():
+    """Handle of torch's current stream on the current device."""
     import torch
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def _dtype_code(t) -> int:
@@ -627,18 +628,17 @@ def maskmoe_layer_backward(x, w_gate_up, w_down, K: int, gate_mode: int, topk_ga
     return out
 
 
-def _current(t, name: str):
-    """Device tensor ``name`` must be contiguous and on the device that the call enqueues on."""
-    import torch
+def _refuse(t, name: str):
     _dev(t, name)
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current device")
+    raise ValueError(f"{name} must be on the current device")
 
 
-def _want(t, name: str, shape, dtype):
-    """Device tensor ``name`` must be contiguous, on the current device, of this shape and dtype."""
-    _current(t, name)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+def _want(t, name: str, shape, dtype, device: int):
+    """Device tensor ``name`` must be contiguous, on device ``device`` (the current one, which the call
+    enqueues on), of this shape and dtype."""
+    if t.get_device() != device or not t.is_contiguous():
+        _refuse(t, name)
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}")
 
 
@@ -652,21 +652,21 @@ def maskmoe_gate_forward(logits, K: int, score: int, n_group: int = 1, topk_grou
     entries without an eligible expert hold index -1 and gate 0."""
     import torch
     lib = load()
-    _current(logits, "logits")
-    if logits.dim() != 2 or logits.dtype != torch.float32:
-        raise ValueError("logits must be a 2-d float32 tensor")
+    here = torch.cuda.current_device()
+    if logits.dim() != 2:
+        raise ValueError("logits must be 2-d")
     T, E = logits.shape
-    dev = logits.device
+    _want(logits, "logits", (T, E), torch.float32, here)
     if bias is not None:
-        _want(bias, "bias", (E,), torch.float32)
+        _want(bias, "bias", (E,), torch.float32, here)
     m_arr, m_p = _host_u8(mask, E)
     p_arr, p_p = _host_f32(prior, E)
-    idx = torch.empty((T, K), dtype=torch.int32, device=dev)
-    gate = torch.empty((T, K), dtype=torch.float32, device=dev)
-    ld = torch.empty(E, dtype=torch.int32, device=dev) if with_load else None
+    idx = logits.new_empty((T, K), dtype=torch.int32)
+    gate = logits.new_empty((T, K))
+    ld = logits.new_empty(E, dtype=torch.int32) if with_load else None
     desc = GateDesc(T, E, K, score, n_group, topk_group, group_rule, int(renorm), scale)
-    _check("maskmoe_gate_forward", lib.maskmoe_gate_forward(ctypes.byref(desc), _ptr(logits), m_p, p_p, _ptr(bias),
-                                                            _ptr(idx), _ptr(gate), _ptr(ld), _stream()))
+    _check("maskmoe_gate_forward", lib.maskmoe_gate_forward(ctypes.byref(desc), logits.data_ptr(), m_p, p_p, _ptr(bias),
+                                                            idx.data_ptr(), gate.data_ptr(), _ptr(ld), _stream()))
     del m_arr, p_arr
     return idx, gate, ld
 
@@ -676,17 +676,18 @@ def maskmoe_gate_backward(logits, topk_idx, d_gate, score: int, renorm: bool = T
     selection topk_idx [T,K] held fixed."""
     import torch
     lib = load()
-    _current(logits, "logits")
-    if logits.dim() != 2 or logits.dtype != torch.float32 or topk_idx.dim() != 2:
-        raise ValueError("logits must be a 2-d float32 tensor, topk_idx 2-d")
+    here = torch.cuda.current_device()
+    if logits.dim() != 2 or topk_idx.dim() != 2:
+        raise ValueError("logits and topk_idx must be 2-d")
     T, E = logits.shape
     K = topk_idx.shape[1]
-    _want(topk_idx, "topk_idx", (T, K), torch.int32)
-    _want(d_gate, "d_gate", (T, K), torch.float32)
+    _want(logits, "logits", (T, E), torch.float32, here)
+    _want(topk_idx, "topk_idx", (T, K), torch.int32, here)
+    _want(d_gate, "d_gate", (T, K), torch.float32, here)
     out = torch.empty_like(logits)
     desc = GateDesc(T, E, K, score, 1, 1, GROUP_MAX, int(renorm), scale)
-    _check("maskmoe_gate_backward", lib.maskmoe_gate_backward(ctypes.byref(desc), _ptr(logits), _ptr(topk_idx),
-                                                              _ptr(d_gate), _ptr(out), _stream()))
+    _check("maskmoe_gate_backward", lib.maskmoe_gate_backward(ctypes.byref(desc), logits.data_ptr(), topk_idx.data_ptr(),
+                                                              d_gate.data_ptr(), out.data_ptr(), _stream()))
     return out
 
 
@@ -695,15 +696,15 @@ def maskmoe_mx4_quantize(x):
     [..., cols/2] and scales [..., cols/32], uint8."""
     import torch
     lib = load()
-    _current(x, "x")
-    cols = x.shape[-1] if x.dim() else 0
+    shape = x.shape
+    cols = shape[-1] if shape else 0
     if cols == 0 or cols % 32:
         raise ValueError("the last dimension must be a positive multiple of 32")
-    rows = x.numel() // cols
-    codes = torch.empty(tuple(x.shape[:-1]) + (cols // 2,), dtype=torch.uint8, device=x.device)
-    scales = torch.empty(tuple(x.shape[:-1]) + (cols // 32,), dtype=torch.uint8, device=x.device)
-    _check("maskmoe_mx4_quantize", lib.maskmoe_mx4_quantize(rows, cols, _dtype_code(x), _ptr(x), _ptr(codes),
-                                                            _ptr(scales), _stream()))
+    _want(x, "x", shape, x.dtype, torch.cuda.current_device())
+    codes = x.new_empty(shape[:-1] + (cols // 2,), dtype=torch.uint8)
+    scales = x.new_empty(shape[:-1] + (cols // 32,), dtype=torch.uint8)
+    _check("maskmoe_mx4_quantize", lib.maskmoe_mx4_quantize(x.numel() // cols, cols, _dtype_code(x), x.data_ptr(),
+                                                            codes.data_ptr(), scales.data_ptr(), _stream()))
     return codes, scales
 
 
@@ -711,14 +712,17 @@ def maskmoe_mx4_dequantize(codes, scales, dtype):
     """The values of codes [..., cols/2] and scales [..., cols/32] as a bf16 or fp32 tensor [..., cols]."""
     import torch
     lib = load()
-    _current(codes, "codes")
-    cols = 2 * codes.shape[-1] if codes.dim() else 0
-    if cols == 0 or cols % 32 or codes.dtype != torch.uint8:
-        raise ValueError("codes must be uint8, the last dimension a positive multiple of 16")
-    _want(scales, "scales", tuple(codes.shape[:-1]) + (cols // 32,), torch.uint8)
-    out = torch.empty(tuple(codes.shape[:-1]) + (cols,), dtype=dtype, device=codes.device)
+    here = torch.cuda.current_device()
+    shape = codes.shape
+    cols = 2 * shape[-1] if shape else 0
+    if cols == 0 or cols % 32:
+        raise ValueError("the last dimension of codes must be a positive multiple of 16")
+    _want(codes, "codes", shape, torch.uint8, here)
+    _want(scales, "scales", shape[:-1] + (cols // 32,), torch.uint8, here)
+    out = codes.new_empty(shape[:-1] + (cols,), dtype=dtype)
     _check("maskmoe_mx4_dequantize", lib.maskmoe_mx4_dequantize(codes.numel() // (cols // 2), cols, _dtype_code(out),
-                                                                _ptr(codes), _ptr(scales), _ptr(out), _stream()))
+                                                                codes.data_ptr(), scales.data_ptr(), out.data_ptr(),
+                                                                _stream()))
     return out
 
 
@@ -728,9 +732,7 @@ class PackedMx4Experts:
 
     def __init__(self, n: int, d: int, F: int, tensors):
         self.n, self.d, self.F, self.tensors = n, d, F, tuple(tensors)
-
-    def struct(self) -> Mx4Experts:
-        return Mx4Experts(*[t.data_ptr() for t in self.tensors])
+        self.struct = Mx4Experts(*[t.data_ptr() for t in self.tensors])
 
 
 def maskmoe_mx4_pack_experts(gate_up_codes, gate_up_scales, down_codes, down_scales) -> PackedMx4Experts:
@@ -738,6 +740,7 @@ def maskmoe_mx4_pack_experts(gate_up_codes, gate_up_scales, down_codes, down_sca
     maskmoe_experts_forward_mx4; routed experts first, shared experts last."""
     import torch
     lib = load()
+    here = torch.cuda.current_device()
     if gate_up_codes.dim() != 3 or down_codes.dim() != 3:
         raise ValueError("gate_up_codes and down_codes must be 3-d")
     n, F2, d2 = gate_up_codes.shape
@@ -745,16 +748,15 @@ def maskmoe_mx4_pack_experts(gate_up_codes, gate_up_scales, down_codes, down_sca
     for t, name, shape in ((gate_up_codes, "gate_up_codes", (n, 2 * F, d // 2)),
                            (gate_up_scales, "gate_up_scales", (n, 2 * F, d // 32)),
                            (down_codes, "down_codes", (n, d, F // 2)), (down_scales, "down_scales", (n, d, F // 32))):
-        _want(t, name, shape, torch.uint8)
+        _want(t, name, shape, torch.uint8, here)
     desc = make_desc(0, d, 1, 1, F)
     sizes = (_sz * 4)()
     _check("maskmoe_mx4_packed_bytes", lib.maskmoe_mx4_packed_bytes(ctypes.byref(desc), n, sizes))
     packed = PackedMx4Experts(n, d, F, [torch.empty(max(int(b), 1), dtype=torch.uint8, device=gate_up_codes.device)
                                         for b in sizes])
     src = Mx4Experts(*[t.data_ptr() for t in (gate_up_codes, gate_up_scales, down_codes, down_scales)])
-    dst = packed.struct()
     _check("maskmoe_mx4_pack_experts", lib.maskmoe_mx4_pack_experts(ctypes.byref(desc), n, ctypes.byref(src),
-                                                                    ctypes.byref(dst), _stream()))
+                                                                    ctypes.byref(packed.struct), _stream()))
     return packed
 
 
@@ -769,24 +771,27 @@ def maskmoe_experts_forward_mx4(x, topk_idx, topk_gate, experts: PackedMx4Expert
     experts and then ``n_shared`` shared ones. ``act``: ACT_BF16 or ACT_MX4 activations. Returns y [T,d]."""
     import torch
     lib = load()
-    if x.dim() != 2 or topk_idx.dim() != 2:
-        raise ValueError("x and topk_idx must be 2-d")
+    here = torch.cuda.current_device()
+    if topk_idx.dim() != 2:
+        raise ValueError("topk_idx must be 2-d")
     T, K = topk_idx.shape
-    d, E = experts.d, experts.n - n_shared
-    _want(x, "x", (T, d), torch.bfloat16)
-    _want(topk_idx, "topk_idx", (T, K), torch.int32)
-    _want(topk_gate, "topk_gate", (T, K), torch.float32)
-    desc = make_desc(T, d, E, K, experts.F, n_shared)
+    d = experts.d
+    _want(x, "x", (T, d), torch.bfloat16, here)
+    _want(topk_idx, "topk_idx", (T, K), torch.int32, here)
+    _want(topk_gate, "topk_gate", (T, K), torch.float32, here)
+    if experts.tensors[0].get_device() != here:
+        _refuse(experts.tensors[0], "experts")
+    desc = make_desc(T, d, experts.n - n_shared, K, experts.F, n_shared)
     if workspace is None:
         workspace = torch.empty(max(int(lib.maskmoe_experts_mx4_workspace_bytes(ctypes.byref(desc))), 1),
                                 dtype=torch.uint8, device=x.device)
-    _current(workspace, "workspace")
+    elif workspace.get_device() != here or not workspace.is_contiguous():
+        _refuse(workspace, "workspace")
     if y is None:
         y = torch.empty_like(x)
     else:
-        _want(y, "y", (T, d), torch.bfloat16)
-    w = experts.struct()
+        _want(y, "y", (T, d), torch.bfloat16, here)
     _check("maskmoe_experts_forward_mx4", lib.maskmoe_experts_forward_mx4(
-        ctypes.byref(desc), act, _ptr(x), _ptr(topk_idx), _ptr(topk_gate), ctypes.byref(w), _ptr(y), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream()))
+        ctypes.byref(desc), act, x.data_ptr(), topk_idx.data_ptr(), topk_gate.data_ptr(), ctypes.byref(experts.struct),
+        y.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
     return y
