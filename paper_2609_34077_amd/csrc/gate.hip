@@ -1,18 +1,21 @@
 // Routing by scores, balance bias and expert groups (include/maskmoe.h, maskmoe_gate_forward), and
 // the gradient of its gates.
 //
-// A token takes a segment of W lanes (16, 32 or 64), each of which holds V consecutive experts in
+// A token takes a segment of W lanes (16; above 64 experts 64), each of which holds V consecutive experts in
 // registers, so that a row of logits is read once, in order, and lower lanes hold lower experts:
 //   scores    softmax or sigmoid of the registers, row maximum and sum by lane exchanges;
 //   groups    the two largest keys of a group by lane exchanges, its rank by comparing it with every other; a
 //             group stays if fewer than topk_group groups beat it;
-//   top-K     every lane sorts its V keys; each round takes the largest first key of the segment and
-//             the lowest lane that holds it, which drops it.
+//   top-K     up to 64 experts: every lane sorts its V keys; each round takes the largest first key of the segment
+//             and the lowest lane that holds it, which drops it, four tokens at once. Above: the K-th largest of
+//             the lanes' largest keys is a bound that the K best keys reach; the few that do go to LDS, and
+//             four tokens' candidates are ranked at once, a lane each (rounds over 64 lanes took 45 instructions each for
+//             one token: 131072 tokens x 256 experts 157 us instead of 120).
 // Keys travel as integers that order as the numbers do (0: no eligible expert), so that a step of an
 // exchange is one instruction.
-// Selection goes by real numbers: keys are compared in fp32, and where two keys that the result
+// Selection goes by real numbers: keys are compared in fp32, and where two keys (groups) that the result
 // depends on come closer than fp32 can tell apart (a bound on its errors, below), the wavefront
-// selects again with keys in fp64 from LDS (select_exact, plain loops: about one token in 300 with 256 experts).
+// selects again with keys in fp64 (select_exact).
 // Without bias, prior and group sums the keys are the logits, which order as their scores do and need neither.
 
 #include <float.h>
@@ -112,7 +115,7 @@ constexpr float kKeyTol = 4e-6f;
 
 // e^x for x <= 0 in fp64: x = k ln 2 + r with |r| <= ln 2 / 2, the Taylor polynomial of degree 13 in r (its
 // remainder is 4e-18), times 2^k. Coefficients come from memory one at a time: the library's exp keeps its own in
-// registers through the loops below, which left room for half the wavefronts (113 registers instead of 62).
+// registers through the loops around it, which leaves room for half the wavefronts.
 __constant__ double kInvFactorial[14] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040,
                                          1.0 / 40320, 1.0 / 362880, 1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600,
                                          1.0 / 6227020800.0};
@@ -126,45 +129,113 @@ __device__ __forceinline__ double exp_neg(double x) {
   return ldexp(p, static_cast<int>(k));
 }
 
-// Selection of one segment's token (logits zr) with fp64 keys, in LDS: `keys` of E experts, -inf where
-// ineligible, `leads` of the groups. out receives the selected experts, -1 where none is left. Plain loops that
-// read everything again and hold little: rarely run, or run for groups whose size is no multiple of V.
-template <int W>
-__device__ __forceinline__ void select_exact(const GateArgs& a, const float* zr, int sl, bool by_key, double* keys,
-                                             double* leads, int* out) {
+// How the keys order and the groups lie: keys that are the logits; keys s * prior + bias.
+enum { kByLogit = 0, kByKey = 1 };
+// no groups; groups of a power of two of lanes; of another number of lanes; of no whole lanes
+enum { kNoGroups = 0, kLaneGroups = 1, kOddGroups = 2, kOtherGroups = 3 };
+
+// What a lane knows of its V experts, the same for every token.
+template <int V>
+struct LaneExperts {
+  float bias[V], prior[V];
+  bool allowed[V];
+};
+template <int V, int KEYS>
+__device__ __forceinline__ LaneExperts<V> lane_experts(const GateArgs& a, int e0) {
+  LaneExperts<V> x;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int e = e0 + v;
+    const bool in = e < a.E;
+    x.bias[v] = KEYS == kByKey && in && a.bias ? a.bias[e] : 0.0f;
+    x.prior[v] = KEYS == kByKey && in && a.has_prior ? a.prior[e] : 1.0f;
+    x.allowed[v] = in && (!a.has_mask || (a.mask[e >> 5] >> (e & 31) & 1));
+  }
+  return x;
+}
+
+template <int V, bool VEC>
+__device__ __forceinline__ void load_row(const GateArgs& a, int t, int e0, float (&z)[V]) {
+  const float* zr = a.logits + static_cast<size_t>(t) * a.E;
+  if constexpr (VEC && V == 4) {
+    f32x4 q = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (e0 < a.E) q = *reinterpret_cast<const f32x4*>(zr + e0);
+#pragma unroll
+    for (int v = 0; v < V; ++v) z[v] = q[v];
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) z[v] = e0 + v < a.E ? zr[e0 + v] : -INFINITY;
+  }
+}
+
+template <int S>
+__device__ __forceinline__ double other(double v) {
+  return __hiloint2double(static_cast<int>(other<S>(static_cast<uint32_t>(__double2hiint(v)))),
+                          static_cast<int>(other<S>(static_cast<uint32_t>(__double2loint(v)))));
+}
+template <int W, int S = 1>
+__device__ __forceinline__ double seg_max(double v) {
+  if constexpr (S < W) return seg_max<W, 2 * S>(fmax(v, other<S>(v)));
+  else return v;
+}
+template <int W, int S = 1>
+__device__ __forceinline__ double seg_sum(double v) {
+  if constexpr (S < W) return seg_sum<W, 2 * S>(v + other<S>(v));
+  else return v;
+}
+
+// Score of a logit in fp64; softmax: relative to the row's largest logit, before the division by the sum.
+__device__ __forceinline__ double exact_score(bool soft, float z, float zmax) {
+  const double x = exp_neg(soft ? static_cast<double>(z) - zmax : -fabs(static_cast<double>(z)));
+  return soft ? x : (z >= 0.0f ? 1.0 : x) / (1.0 + x);
+}
+
+// Selection of one segment's token t with fp64 keys: lane r < K gets the r-th expert, -1 where none is left. keys and
+// leads: LDS for the segment's W * V experts (leads: of their groups). Runs where fp32 keys came too close, or for
+// groups whose size is no multiple of V.
+template <int W, int V, bool VEC, int KEYS, int GROUPS>
+__device__ __forceinline__ int select_exact(const GateArgs& a, const LaneExperts<V>& x, int t, int seg, int sl, double* keys,
+                                            double* leads) {
   const double ninf = -INFINITY;
-  const bool soft = by_key && a.score == 0;
-  float top = -FLT_MAX;
-  double sum = 0.0;
-  if (soft) {
-#pragma unroll 1
-    for (int e = sl; e < a.E; e += W) top = fmaxf(top, clamp_logit(zr[e] > -INFINITY ? zr[e] : -FLT_MAX));
-    top = seg_fmax<W>(top);
-#pragma unroll 1
-    for (int e = sl; e < a.E; e += W)
-      if (zr[e] > -INFINITY) sum += exp_neg(static_cast<double>(clamp_logit(zr[e])) - top);
-#pragma unroll 1
-    for (int m = 1; m < W; m *= 2) sum += __shfl_xor(sum, m, kWave);
+  const bool soft = a.score == 0;
+  const int e0 = sl * V;
+  float z[V];
+  load_row<V, VEC>(a, t, e0, z);
+  float zmax = -FLT_MAX;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    z[v] = z[v] > -INFINITY ? clamp_logit(z[v]) : -INFINITY;
+    zmax = fmaxf(zmax, z[v]);
   }
-#pragma unroll 1
-  for (int e = sl; e < a.E; e += W) {
-    double k = clamp_logit(zr[e]);
-    const bool ok = zr[e] > -INFINITY && (!a.has_mask || (a.mask[e >> 5] >> (e & 31) & 1));
-    if (by_key) {
-      const double x = exp_neg(soft ? k - top : -fabs(k));
-      k = soft ? x / sum : (k >= 0 ? 1.0 : x) / (1.0 + x);
-      if (a.has_prior) k *= a.prior[e];
-      if (a.bias) k += a.bias[e];
+  zmax = seg_fmax<W>(zmax);
+  double key[V], sum = 0.0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    key[v] = z[v];
+    if constexpr (KEYS == kByKey) {
+      key[v] = exact_score(soft, z[v], zmax);
+      if (z[v] > -INFINITY) sum += key[v];
+      __builtin_amdgcn_sched_barrier(0);   // one exponential's registers at a time
     }
-    keys[e] = ok ? k : ninf;
   }
-  lds_order();
-  if (a.n_group > 1) {
+  if constexpr (KEYS == kByKey) {
+    sum = soft ? seg_sum<W>(sum) : 1.0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = key[v] / sum * x.prior[v] + x.bias[v];
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (!(z[v] > -INFINITY) || !x.allowed[v]) key[v] = ninf;
+  if constexpr (GROUPS != kNoGroups) {
     const int n = a.E / a.n_group;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (e0 + v < a.E) keys[e0 + v] = key[v];
+    lds_order();
 #pragma unroll 1
     for (int g = sl; g < a.n_group; g += W) {
       double t1 = ninf, t2 = ninf;
-#pragma unroll 1
+#pragma unroll 4
       for (int i = 0; i < n; ++i) {
         const double k = keys[g * n + i];
         t2 = fmax(t2, fmin(t1, k));
@@ -174,174 +245,240 @@ __device__ __forceinline__ void select_exact(const GateArgs& a, const float* zr,
     }
     lds_order();
 #pragma unroll 1
-    for (int e = sl; e < a.E; e += W) {
-      const int own = e / n;
-      const double lead = leads[own];
+    for (int g = sl; g < a.n_group; g += W) {   // a group that is beaten too often loses its experts
+      const double lead = leads[g];
       int ahead = 0;
+#pragma unroll 4
+      for (int o = 0; o < a.n_group; ++o) ahead += leads[o] > lead || (leads[o] == lead && o < g) ? 1 : 0;
+      if (ahead >= a.topk_group)
 #pragma unroll 1
-      for (int g = 0; g < a.n_group; ++g) ahead += leads[g] > lead || (leads[g] == lead && g < own) ? 1 : 0;
-      if (ahead >= a.topk_group) keys[e] = ninf;
+        for (int i = 0; i < n; ++i) keys[g * n + i] = ninf;
     }
     lds_order();
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (e0 + v < a.E) key[v] = keys[e0 + v];
   }
+  const uint64_t segbits = (W == 64 ? ~0ull : (1ull << W) - 1) << (seg * W);
+  int mine = -1;
 #pragma unroll 1
   for (int r = 0; r < a.K; ++r) {
-    double best = ninf;
-    int at = 0x7fffffff;
-#pragma unroll 1
-    for (int e = sl; e < a.E; e += W) {
-      const double k = keys[e];
-      if (k > best) best = k, at = e;
+    double head = key[0];
+    int at = e0;
+#pragma unroll
+    for (int v = 1; v < V; ++v)
+      if (key[v] > head) head = key[v], at = e0 + v;
+    const double m = seg_max<W>(head);
+    const uint64_t who = __ballot(head == m && m > ninf) & segbits;
+    const int first = who ? __ffsll(static_cast<unsigned long long>(who)) - 1 : seg * W;
+    const int e = who ? __shfl(at, first, kWave) : -1;
+    if (sl == r) mine = e;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (e0 + v == e) key[v] = ninf;
+  }
+  return mine;
+}
+
+// The largest value that at least `need` and, where no equal values prevent it, at most `enough` of the lanes in
+// `open` reach (found by comparing all with one that is still in question; with how many reach it), for a value per
+// lane of a whole wavefront; 1 where fewer lanes hold one at all (kNone: none).
+__device__ __forceinline__ uint32_t reached_by(uint32_t value, uint64_t open, int need, int enough, uint32_t& reach) {
+  const uint64_t all = open;
+  open &= __ballot(value != kNone);
+  reach = static_cast<uint32_t>(__popcll(open));
+  if (static_cast<int>(reach) <= need) return 1;
+  for (;;) {
+    const uint32_t pivot = static_cast<uint32_t>(
+        __builtin_amdgcn_readlane(static_cast<int>(value), __ffsll(static_cast<unsigned long long>(open)) - 1));
+    const uint64_t upto = __ballot(value >= pivot) & all;
+    reach = static_cast<uint32_t>(__popcll(upto));
+    if (static_cast<int>(reach) < need) {
+      open &= ~upto;
+    } else {
+      if (static_cast<int>(reach) <= enough) return pivot;
+      const uint64_t above = __ballot(value > pivot) & all;
+      if (__popcll(above) < need) return pivot;
+      open &= above;
     }
-#pragma unroll 1
-    for (int m = 1; m < W; m *= 2) {
-      const double ok = __shfl_xor(best, m, kWave);
-      const int oe = __shfl_xor(at, m, kWave);
-      if (ok > best || (ok == best && oe < at)) best = ok, at = oe;
-    }
-    lds_order();
-    if (sl == 0) {
-      out[r] = best > ninf ? at : -1;
-      if (best > ninf) keys[at] = ninf;
-    }
-    lds_order();
   }
 }
 
-// How the keys order and the groups lie: keys that are the logits; keys s * prior + bias.
-enum { kByLogit = 0, kByKey = 1 };
-// no groups; groups of a power of two of lanes; of another number of lanes; of no whole lanes
-enum { kNoGroups = 0, kLaneGroups = 1, kOddGroups = 2, kOtherGroups = 3 };
+struct Row {
+  float zmax, total;   // softmax: largest logit and sum of e^(z - zmax) (where the gates or keys need them)
+  float tol;           // how close two keys may come
+  bool close;          // group scores came too close
+};
 
-template <int W, int V, bool VEC, int KEYS, int GROUPS>
+// Keys of a row's logits z (overwritten) with the experts outside the kept groups dropped.
+template <int W, int V, int KEYS, int GROUPS>
+__device__ __forceinline__ Row row_keys(const GateArgs& a, const LaneExperts<V>& x, int seg, int e0, float pmax, float bmax,
+                                        float (&z)[V], uint32_t (&key)[V]) {
+  const float ninf = -INFINITY;
+  const bool soft = a.score == 0;
+  Row r{-FLT_MAX, 1.0f, 0.0f, GROUPS == kOtherGroups};
+  bool ok[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const bool live = z[v] > ninf;   // false for NaN too
+    z[v] = live ? clamp_logit(z[v]) : ninf;
+    ok[v] = live && x.allowed[v];
+  }
+  if (soft && (KEYS == kByKey || !a.renorm)) {   // renormalised gates need no row sum
+#pragma unroll
+    for (int v = 0; v < V; ++v) r.zmax = fmaxf(r.zmax, z[v]);
+    r.zmax = seg_fmax<W>(r.zmax);
+    r.total = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) r.total += fast_exp(z[v] - r.zmax);   // 0 for -inf
+    r.total = seg_sum<W>(r.total);
+  }
+  if constexpr (KEYS == kByLogit) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = ok[v] ? order(z[v]) : kNone;
+  } else {
+    const float inv = fast_rcp(r.total);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float s = soft ? fast_exp(z[v] - r.zmax) * inv : fast_sigmoid(z[v]);
+      key[v] = ok[v] ? order(s * x.prior[v] + x.bias[v]) : kNone;
+    }
+    r.tol = kKeyTol * (pmax * (soft ? inv : 1.0f) + bmax);   // inv: the largest softmax score
+  }
+  if constexpr (GROUPS == kLaneGroups || GROUPS == kOddGroups) {
+    const int n = a.E / a.n_group, glanes = n / V, own = e0 / n;
+    const bool sum2 = KEYS == kByKey && a.group_rule == 1;
+    uint32_t t1 = key[0], t2 = kNone;
+#pragma unroll
+    for (int v = 1; v < V; ++v) {
+      t2 = umax(t2, umin(t1, key[v]));
+      t1 = umax(t1, key[v]);
+    }
+    auto join = [&](uint32_t b1, uint32_t b2) {
+      t2 = umax(umin(t1, b1), umax(t2, b2));
+      t1 = umax(t1, b1);
+    };
+    if constexpr (GROUPS == kLaneGroups) {
+      if (glanes > 1) join(other<1>(t1), other<1>(t2));
+      if (glanes > 2) join(other<2>(t1), other<2>(t2));
+      if (glanes > 4) join(other<4>(t1), other<4>(t2));
+      if (glanes > 8) join(other<8>(t1), other<8>(t2));
+      if (W > 16 && glanes > 16) join(other<16>(t1), other<16>(t2));
+    } else {
+      const uint32_t m1 = t1, m2 = t2;
+      t1 = t2 = kNone;
+      for (int i = 0; i < glanes; ++i) {
+        const int from = seg * W + min(own, a.n_group - 1) * glanes + i;
+        join(__shfl(m1, from, kWave), __shfl(m2, from, kWave));
+      }
+    }
+    const uint32_t lead = sum2 && t2 != kNone ? order(number(t1) + number(t2)) : t1;
+    bool kept;
+    if constexpr (W == 64) {   // the first lane of every group stands for it
+      const int lane = threadIdx.x & 63;
+      const uint64_t firsts = __ballot(lane == own * glanes && own < a.n_group);
+      uint32_t most;
+      const uint32_t bound = reached_by(lead, firsts, a.topk_group, a.topk_group, most);
+      kept = lead >= bound && own < a.n_group;
+      // equal group scores at the bound, or (the keys being rounded) scores that come too close to it
+      const uint32_t low = KEYS == kByKey && bound > kNone + 1 ? umax(order(number(bound) - 2.0f * r.tol), 1u) : bound;
+      r.close = most > static_cast<uint32_t>(a.topk_group) ||
+                __popcll(__ballot(lead >= low) & firsts) > static_cast<int>(most);
+    } else {
+      int ahead = 0;
+      for (int g = 0; g < a.n_group; ++g) {
+        const uint32_t o = __shfl(lead, seg * W + g * glanes, kWave);
+        ahead += o > lead || (o == lead && g < own) ? 1 : 0;
+      }
+      kept = ahead < a.topk_group && own < a.n_group;
+      if constexpr (KEYS == kByKey) {   // the last group kept and the first one left out
+        const float in = number(~seg_max<W>(kept ? ~lead : 0u)), out = number(seg_max<W>(kept ? kNone : lead));
+        r.close = in - out < 2.0f * r.tol;   // no group left out, or none with an expert: NaN, not close
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = kept ? key[v] : kNone;
+  }
+  return r;
+}
+
+// The largest prior and |bias| of the experts (for the keys' errors), over the W lanes of a segment.
+template <int W, int V>
+__device__ __forceinline__ void key_bounds(const LaneExperts<V>& x, float& pmax, float& bmax) {
+  pmax = bmax = 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    pmax = fmaxf(pmax, x.prior[v]);
+    bmax = fmaxf(bmax, fabsf(x.bias[v]));
+  }
+  pmax = seg_fmax<W>(pmax);
+  bmax = seg_fmax<W>(bmax);
+}
+
+// The W lanes of a token write its entries: this lane entry r (if r < K), expert e (-1: none) and its gate.
+template <int W>
+__device__ __forceinline__ void write_gate(const GateArgs& a, int t, bool real, int r, int e, float zmax, float total,
+                                           int* hist) {
+  const bool has = e >= 0, soft = a.score == 0;
+  const float zs = has ? clamp_logit(a.logits[static_cast<size_t>(t) * a.E + e]) : -INFINITY;
+  float g;
+  if (a.renorm) {
+    // ratios of scores, from logits relative to the largest selected one: exp(z_k - z_max) for
+    // softmax, and for sigmoid where every score is e^z to fp32's precision; no score underflows
+    const float top = seg_fmax<W>(fmaxf(zs, -FLT_MAX));
+    const float w = !has ? 0.0f : soft || top < -30.0f ? fast_exp(zs - top) : fast_sigmoid(zs);
+    g = a.scale * (w / seg_sum<W>(w));
+  } else {
+    g = a.scale * (soft ? fast_exp(zs - zmax) / total : fast_sigmoid(zs));
+  }
+  if (real && r < a.K) {
+    a.idx[static_cast<size_t>(t) * a.K + r] = e;
+    a.gate[static_cast<size_t>(t) * a.K + r] = has ? g : 0.0f;
+    if (a.load && has) atomicAdd(&hist[e], 1);   // integer counts: order-independent
+  }
+}
+__device__ __forceinline__ void clear_hist(const GateArgs& a, int* hist) {
+  if (!a.load) return;
+  for (int e = threadIdx.x; e < a.E; e += kThreads) hist[e] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ void add_hist(const GateArgs& a, const int* hist) {
+  if (!a.load) return;
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kThreads) {
+    if (gridDim.x == 1) a.load[e] = hist[e];
+    else if (hist[e]) atomicAdd(&a.load[e], hist[e]);
+  }
+}
+
+// Up to 64 experts: four tokens per wavefront, 16 lanes each.
+template <int V, bool VEC, int KEYS, int GROUPS>
 __global__ __launch_bounds__(kThreads) void gate_kernel(const GateArgs a) {
-  constexpr int SEGS = kWave / W;        // tokens per wavefront
-  constexpr int PER = SEGS * kWaves;     // tokens per workgroup and round
+  constexpr int W = 16, SEGS = kWave / W, PER = SEGS * kWaves;   // tokens per wavefront and workgroup
   constexpr bool EXACT = KEYS == kByKey || GROUPS == kOtherGroups;   // may select in fp64
   __shared__ uint2 sel[PER][kGateMaxK];  // selected experts and their keys
-  __shared__ int exact_sel[EXACT ? PER : 1][kGateMaxK];
-  __shared__ double rows[EXACT ? PER : 1][W * V], leads[EXACT && GROUPS != kNoGroups ? PER : 1][W * V];
+  constexpr bool GROUPED = EXACT && GROUPS != kNoGroups;
+  __shared__ double rows[GROUPED ? PER : 1][W * V], leads[GROUPED ? PER : 1][W * V];
   __shared__ int hist[kGateMaxE];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int seg = lane / W, sl = lane % W, e0 = sl * V;
   const int slot = wave * SEGS + seg;
-  if (a.load) {
-    for (int e = tid; e < a.E; e += kThreads) hist[e] = 0;
-    __syncthreads();
-  }
-  float bias[V], prior[V];
-  bool allowed[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int e = e0 + v;
-    const bool in = e < a.E;
-    bias[v] = KEYS == kByKey && in && a.bias ? a.bias[e] : 0.0f;
-    prior[v] = KEYS == kByKey && in && a.has_prior ? a.prior[e] : 1.0f;
-    allowed[v] = in && (!a.has_mask || (a.mask[e >> 5] >> (e & 31) & 1));
-  }
-  const bool soft = a.score == 0;
-  const float ninf = -INFINITY;
-  const int n = a.E / a.n_group, glanes = n / V, own = e0 / n;   // group of this lane (kLaneGroups, kOddGroups)
-  const uint32_t below = (1u << (lane & (W < 32 ? W - 1 : 31))) - 1;   // W < 64: lower lanes of the segment
-  auto load = [&](int t, float (&z)[V]) {
-    const float* zr = a.logits + static_cast<size_t>(t) * a.E;
-    if constexpr (VEC) {
-      f32x4 q = {ninf, ninf, ninf, ninf};
-      if (e0 < a.E) q = *reinterpret_cast<const f32x4*>(zr + e0);
-#pragma unroll
-      for (int v = 0; v < V; ++v) z[v] = q[v];
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) z[v] = e0 + v < a.E ? zr[e0 + v] : ninf;
-    }
-  };
+  clear_hist(a, hist);
+  const LaneExperts<V> x = lane_experts<V, KEYS>(a, e0);
+  float pmax, bmax;
+  key_bounds<W>(x, pmax, bmax);
+  const uint32_t below = (1u << sl) - 1;   // lower lanes of the segment
   float next[V];
   const int stride = gridDim.x * PER;
-  const int first = blockIdx.x * PER + slot;
-  load(min(first, a.T - 1), next);
+  load_row<V, VEC>(a, min(static_cast<int>(blockIdx.x) * PER + slot, a.T - 1), e0, next);
   for (int t0 = blockIdx.x * PER; t0 < a.T; t0 += stride) {
     const int t = min(t0 + slot, a.T - 1);   // segments past the last token repeat it, unwritten
-    const bool real = t0 + slot < a.T;
     float z[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) z[v] = next[v];
-    load(min(t0 + slot + stride, a.T - 1), next);   // the next round's row, behind this one's work
-    float zmax = -FLT_MAX, total = 1.0f;
-    bool live[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      live[v] = z[v] > ninf;   // false for NaN too
-      z[v] = live[v] ? clamp_logit(z[v]) : ninf;
-    }
-    if (soft && (KEYS == kByKey || !a.renorm)) {   // renormalised gates need no row sum
-#pragma unroll
-      for (int v = 0; v < V; ++v) zmax = fmaxf(zmax, z[v]);
-      zmax = seg_fmax<W>(zmax);
-      total = 0.0f;
-#pragma unroll
-      for (int v = 0; v < V; ++v) total += fast_exp(z[v] - zmax);   // 0 for -inf
-      total = seg_sum<W>(total);
-    }
+    load_row<V, VEC>(a, min(t0 + slot + stride, a.T - 1), e0, next);   // the next round's row, behind this one's work
     uint32_t key[V];
-    float mag = 0.0f;
-    if constexpr (KEYS == kByLogit) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) key[v] = live[v] && allowed[v] ? order(z[v]) : kNone;
-    } else {
-      const float inv = fast_rcp(total);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const bool ok = live[v] && allowed[v];
-        const float s = (soft ? fast_exp(z[v] - zmax) * inv : fast_sigmoid(z[v])) * prior[v];
-        key[v] = ok ? order(s + bias[v]) : kNone;
-        mag = fmaxf(mag, ok ? s + fabsf(bias[v]) : 0.0f);
-      }
-      mag = seg_fmax<W>(mag);
-    }
-    const float tol = kKeyTol * mag;
-    bool close = GROUPS == kOtherGroups;
-    if constexpr (GROUPS == kLaneGroups || GROUPS == kOddGroups) {
-      const bool sum2 = KEYS == kByKey && a.group_rule == 1;
-      uint32_t t1 = key[0], t2 = kNone;
-#pragma unroll
-      for (int v = 1; v < V; ++v) {
-        t2 = umax(t2, umin(t1, key[v]));
-        t1 = umax(t1, key[v]);
-      }
-      auto join = [&](uint32_t b1, uint32_t b2) {
-        t2 = umax(umin(t1, b1), umax(t2, b2));
-        t1 = umax(t1, b1);
-      };
-      if constexpr (GROUPS == kLaneGroups) {
-        if (glanes > 1) join(other<1>(t1), other<1>(t2));
-        if (glanes > 2) join(other<2>(t1), other<2>(t2));
-        if (glanes > 4) join(other<4>(t1), other<4>(t2));
-        if (glanes > 8) join(other<8>(t1), other<8>(t2));
-        if (W > 16 && glanes > 16) join(other<16>(t1), other<16>(t2));
-      } else {
-        const uint32_t m1 = t1, m2 = t2;
-        t1 = t2 = kNone;
-        for (int i = 0; i < glanes; ++i) {
-          const int from = seg * W + min(own, a.n_group - 1) * glanes + i;
-          join(__shfl(m1, from, kWave), __shfl(m2, from, kWave));
-        }
-      }
-      const uint32_t lead = sum2 && t2 != kNone ? order(number(t1) + number(t2)) : t1;
-      int ahead = 0;
-      for (int g = 0; g < a.n_group; ++g) {
-        uint32_t o;
-        if constexpr (W == 64) o = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(lead), g * glanes));
-        else o = __shfl(lead, seg * W + g * glanes, kWave);
-        ahead += o > lead || (o == lead && g < own) ? 1 : 0;
-      }
-      const bool kept = ahead < a.topk_group && own < a.n_group;
-      if constexpr (KEYS == kByKey) {   // the last group kept and the first one left out
-        const float in = number(~seg_max<W>(kept ? ~lead : 0u)), out = number(seg_max<W>(kept ? kNone : lead));
-        close |= in - out < 2.0f * tol;   // no group left out, or none with an expert: NaN, not close
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v) key[v] = kept ? key[v] : kNone;
-    }
+    Row row = row_keys<W, V, KEYS, GROUPS>(a, x, seg, e0, pmax, bmax, z, key);
     // the lane's keys by decreasing key, equal ones by increasing expert
     int id[V];
 #pragma unroll
@@ -352,22 +489,17 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(const GateArgs a) {
       for (int j = 0; j + 1 < V - i; ++j) {
         const bool sw = key[j + 1] > key[j];   // strict: a lower expert stays ahead of its equal
         const uint32_t k = key[j];
-        const int x = id[j];
+        const int y = id[j];
         key[j] = sw ? key[j + 1] : k;
         key[j + 1] = sw ? k : key[j + 1];
-        id[j] = sw ? id[j + 1] : x;
-        id[j + 1] = sw ? x : id[j + 1];
+        id[j] = sw ? id[j + 1] : y;
+        id[j + 1] = sw ? y : id[j + 1];
       }
     uint32_t m = seg_max<W>(key[0]);
     for (int r = 0; r < a.K; ++r) {
-      bool mine;
-      if constexpr (W == 64) {
-        mine = lane == __ffsll(static_cast<unsigned long long>(__ballot(key[0] == m))) - 1;
-      } else {
-        const uint64_t at = __ballot(key[0] == m);
-        const uint32_t half = static_cast<uint32_t>(lane < 32 ? at : at >> 32) >> (W == 16 ? lane & 16 : 0);
-        mine = key[0] == m && (half & below) == 0;
-      }
+      const uint64_t at = __ballot(key[0] == m);
+      const uint32_t half = static_cast<uint32_t>(lane < 32 ? at : at >> 32) >> (lane & 16);
+      const bool mine = key[0] == m && (half & below) == 0;
       if (mine) sel[slot][r] = make_uint2(m == kNone ? 0xffffffffu : static_cast<uint32_t>(id[0]), m);
 #pragma unroll
       for (int v = 0; v + 1 < V; ++v) {
@@ -378,73 +510,207 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(const GateArgs a) {
       m = seg_max<W>(key[0]);
     }
     lds_order();
-    // lane r of the first 16 holds the r-th selected expert (K <= 16 <= W)
     int e = -1;
     uint32_t ke = kNone;
     if (sl < a.K) {
-      const uint2 x = sel[slot][sl];
-      e = static_cast<int>(x.x);
-      ke = x.y;
+      const uint2 q = sel[slot][sl];
+      e = static_cast<int>(q.x);
+      ke = q.y;
     }
     if constexpr (EXACT) {
       if constexpr (KEYS == kByKey) {   // m: the best key left out
         uint32_t after = dpp<0x101>(ke);   // the next lane's (row_shl:1)
         after = sl == a.K - 1 ? m : after;
-        close |= sl < a.K && number(ke) - number(after) < tol;   // kNone: NaN, not close
+        row.close |= sl < a.K && number(ke) - number(after) < row.tol;   // kNone: NaN, not close
       }
-      if (__any(close)) {
-        select_exact<W>(a, a.logits + static_cast<size_t>(t) * a.E, sl, KEYS == kByKey, rows[slot],
-                        leads[GROUPS != kNoGroups ? slot : 0], exact_sel[slot]);
-        if (sl < a.K) e = exact_sel[slot][sl];
+      if (__any(row.close)) {
+        e = select_exact<W, V, VEC, KEYS, GROUPS>(a, x, t, seg, sl, rows[GROUPED ? slot : 0], leads[GROUPED ? slot : 0]);
       }
     }
     lds_order();
-    const bool has = e >= 0;
-    const float zs = has ? clamp_logit(a.logits[static_cast<size_t>(t) * a.E + e]) : ninf;
-    float g;
-    if (a.renorm) {
-      // ratios of scores, from logits relative to the largest selected one: exp(z_k - z_max) for
-      // softmax, and for sigmoid where every score is e^z to fp32's precision; no score underflows
-      const float top = seg_fmax<16>(fmaxf(zs, -FLT_MAX));
-      const float w = !has ? 0.0f : soft || top < -30.0f ? fast_exp(zs - top) : fast_sigmoid(zs);
-      g = a.scale * (w / seg_sum<16>(w));
+    write_gate<W>(a, t, t0 + slot < a.T, sl, e, row.zmax, row.total, hist);
+  }
+  add_hist(a, hist);
+}
+
+// More than 64 experts: a wavefront finds the candidates of `batch` (up to 64 / C) tokens one after the other, a row over
+// its 64 lanes, and then ranks them all at once, C lanes a token, by fp64 keys of the candidates alone. Bound by the
+// instructions of the first part (300 vector and 270 scalar ones a token: 131072 tokens x 256 experts in 8 groups
+// 120 us, of which the 142 MB would take 30); six wavefronts a SIMD.
+template <int V, bool VEC, int KEYS, int GROUPS, int C>
+__global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a, int batch) {
+  constexpr int TB = kWave / C;
+  constexpr bool GROUPED = GROUPS != kNoGroups;
+  struct Found {
+    float zmax, total, tol;
+    int again;                             // select in fp64: group scores too close, or more candidates than C
+  };
+  __shared__ uint2 cand[kWaves][TB][C];    // (key, expert)
+  __shared__ double cand64[KEYS == kByKey ? kWaves : 1][TB][C];
+  __shared__ Found found[kWaves][TB];
+  __shared__ double rows[GROUPED ? kWaves : 1][64 * V], leads[GROUPED ? kWaves : 1][64 * V];
+  __shared__ int hist[kGateMaxE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e0 = lane * V;
+  const int seg = lane / C, sl = lane % C;
+  clear_hist(a, hist);
+  const LaneExperts<V> x = lane_experts<V, KEYS>(a, e0);
+  float pmax, bmax;
+  key_bounds<kWave>(x, pmax, bmax);
+  const int stride = gridDim.x * kWaves * batch;
+  int t0 = (blockIdx.x * kWaves + wave) * batch;
+  float next[V];
+  load_row<V, VEC>(a, min(t0, a.T - 1), e0, next);
+  for (; t0 < a.T; t0 += stride) {
+    cand[wave][seg][sl] = make_uint2(kNone, 0xffffffffu);
+    lds_order();
+    const int count = min(batch, a.T - t0);
+    for (int k = 0; k < count; ++k) {
+      float z[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) z[v] = next[v];
+      load_row<V, VEC>(a, min(k + 1 < count ? t0 + k + 1 : t0 + stride, a.T - 1), e0, next);
+      uint32_t key[V];
+      const Row row = row_keys<kWave, V, KEYS, GROUPS>(a, x, 0, e0, pmax, bmax, z, key);
+      uint32_t head = key[0], reach;
+#pragma unroll
+      for (int v = 1; v < V; ++v) head = umax(head, key[v]);
+      // a bound that the heads of K lanes or two more reach: so do the K best keys, and some others
+      uint32_t bound = reached_by(head, ~0ull, a.K, a.K + 2, reach);
+      uint64_t at[V];
+      int n;
+      // The candidates: keys that reach the bound; rounded ones also where their real values might
+      auto candidates = [&](uint32_t b) {
+        if constexpr (KEYS == kByKey)
+          if (b > 1) b = umax(order(number(b) - row.tol), 1u);
+        n = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          at[v] = __ballot(key[v] >= b);
+          n += __popcll(at[v]);
+        }
+      };
+      candidates(bound);
+      if (n > C) {   // several large keys in one lane: a higher bound, as long as K keys reach it
+        uint32_t high = 0xffffffffu;
+        for (;;) {
+          const uint64_t open = __ballot(head > bound && head < high);
+          if (open == 0) break;
+          const uint32_t pivot = static_cast<uint32_t>(
+              __builtin_amdgcn_readlane(static_cast<int>(head), __ffsll(static_cast<unsigned long long>(open)) - 1));
+          int reach_all = 0;
+#pragma unroll
+          for (int v = 0; v < V; ++v) reach_all += __popcll(__ballot(key[v] >= pivot));
+          if (reach_all < a.K) {
+            high = pivot;
+          } else {
+            bound = pivot;
+            candidates(bound);
+            if (n <= C) break;
+          }
+        }
+      }
+      if (n <= C) {
+        int base = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int pos = static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(at[v] >> 32),
+                                                                     __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(at[v]), base)));
+          if (at[v] >> lane & 1) cand[wave][k][pos] = make_uint2(key[v], e0 + v);
+          base += __popcll(at[v]);
+        }
+      }
+      if (lane == 0) found[wave][k] = Found{row.zmax, row.total, row.tol, row.close || n > C ? 1 : 0};
+    }
+    lds_order();
+    // lane (token seg, candidate sl): its rank among the token's candidates, by fp64 keys
+    const int t = min(t0 + seg, a.T - 1);
+    const bool real = seg < count;
+    const Found f = found[wave][real ? seg : 0];
+    const uint2 own = cand[wave][seg][sl];
+    const bool has = own.x != kNone;
+    int rank = 0;
+    bool close = real && f.again;
+    if constexpr (KEYS == kByKey) {
+      double k = -INFINITY;
+      if (has) {
+        k = exact_score(a.score == 0, clamp_logit(a.logits[static_cast<size_t>(t) * a.E + own.y]), f.zmax);
+        if (a.score == 0 && a.bias) k /= f.total;   // without bias the order does not depend on the sum
+        if (a.has_prior) k *= a.prior[own.y];
+        if (a.bias) k += a.bias[own.y];
+      }
+      cand64[wave][seg][sl] = k;
+      lds_order();
+      double gap = INFINITY;
+#pragma unroll 4
+      for (int j = 0; j < C; ++j) {
+        const double o = cand64[wave][seg][j];
+        rank += o > k || (o == k && cand[wave][seg][j].y < own.y) ? 1 : 0;
+        gap = j == sl ? gap : fmin(gap, fabs(o - k));
+      }
+      // a sum in fp32 beside a bias: the keys are no better than fp32
+      if (a.score == 0 && a.bias) close |= real && has && rank < a.K && gap < f.tol;
     } else {
-      g = a.scale * (soft ? fast_exp(zs - zmax) / total : fast_sigmoid(zs));
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        const uint2 o = cand[wave][seg][j];
+        rank += o.x > own.x || (o.x == own.x && o.y < own.y) ? 1 : 0;
+      }
     }
-    if (real && sl < a.K) {
-      a.idx[static_cast<size_t>(t) * a.K + sl] = e;
-      a.gate[static_cast<size_t>(t) * a.K + sl] = has ? g : 0.0f;
-      if (a.load && has) atomicAdd(&hist[e], 1);   // integer counts: order-independent
+    // a selected candidate's lane writes its entry; lanes without a candidate the entries that are left over
+    int r = rank, e = has && rank < a.K ? static_cast<int>(own.y) : -1;
+    if (!has) {
+      const uint32_t filled = static_cast<uint32_t>(__ballot(has) >> (C * seg)) & static_cast<uint32_t>((1ull << C) - 1);
+      r = __popc(filled) + __popc(~filled & ((1u << sl) - 1));
     }
+    const uint64_t again = __ballot(close);
+    if (again != 0) {
+#pragma unroll 1
+      for (int k = 0; k < count; ++k) {
+        if ((again >> (C * k) & ((1ull << C) - 1)) == 0) continue;
+        const int ex = select_exact<kWave, V, VEC, KEYS, GROUPS>(a, x, t0 + k, 0, lane, rows[GROUPED ? wave : 0],
+                                                                 leads[GROUPED ? wave : 0]);
+        const int mine = __shfl(ex, sl, kWave);   // entry sl, for the token's lanes
+        if (seg == k) e = sl < a.K ? mine : -1, r = sl;
+      }
+    }
+    lds_order();
+    write_gate<C>(a, t, real, r, e, f.zmax, f.total, hist);
   }
-  if (a.load) {
-    __syncthreads();
-    for (int e = tid; e < a.E; e += kThreads) {
-      if (gridDim.x == 1) a.load[e] = hist[e];
-      else if (hist[e]) atomicAdd(&a.load[e], hist[e]);
-    }
-  }
+  add_hist(a, hist);
 }
 
 __global__ void gate_zero_kernel(int32_t* load, int E) {
   if (static_cast<int>(threadIdx.x) < E) load[threadIdx.x] = 0;
 }
 
-template <int W, int V, bool VEC, int KEYS>
-void launch_groups(const GateArgs& a, dim3 grid, hipStream_t stream) {
+constexpr int kRowsK = 10;   // experts up to which 16 candidates of a token nearly always suffice
+
+template <int V, bool ROWS, bool VEC, int KEYS, int GROUPS>
+void launch_one(const GateArgs& a, int blocks, int batch, hipStream_t stream) {
+  if constexpr (ROWS) {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, stream, a, batch); };
+    if (a.K <= kRowsK) go(gate_rows_kernel<V, VEC, KEYS, GROUPS, 16>);
+    else go(gate_rows_kernel<V, VEC, KEYS, GROUPS, 32>);
+  } else {
+    hipLaunchKernelGGL((gate_kernel<V, VEC, KEYS, GROUPS>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  }
+}
+template <int V, bool ROWS, bool VEC, int KEYS>
+void launch_groups(const GateArgs& a, int blocks, int batch, hipStream_t stream) {
   const int n = a.E / a.n_group, lanes = n / V;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
-  if (a.n_group == 1 || a.topk_group == a.n_group) go(gate_kernel<W, V, VEC, KEYS, kNoGroups>);
-  else if (n % V != 0) go(gate_kernel<W, V, VEC, KEYS, kOtherGroups>);
-  else if ((lanes & (lanes - 1)) == 0) go(gate_kernel<W, V, VEC, KEYS, kLaneGroups>);
-  else go(gate_kernel<W, V, VEC, KEYS, kOddGroups>);
+  if (a.n_group == 1 || a.topk_group == a.n_group) launch_one<V, ROWS, VEC, KEYS, kNoGroups>(a, blocks, batch, stream);
+  else if (n % V != 0) launch_one<V, ROWS, VEC, KEYS, kOtherGroups>(a, blocks, batch, stream);
+  else if ((lanes & (lanes - 1)) == 0) launch_one<V, ROWS, VEC, KEYS, kLaneGroups>(a, blocks, batch, stream);
+  else launch_one<V, ROWS, VEC, KEYS, kOddGroups>(a, blocks, batch, stream);
 }
 
-template <int W, int V>
+template <int V, bool ROWS>
 hipError_t launch_gate(const GateArgs& a, hipStream_t stream) {
-  constexpr int PER = kWave / W * kWaves;
   if (a.T == 0 && !a.load) return hipSuccess;
-  const int blocks = std::max(1, std::min((a.T + PER - 1) / PER, 256 * 8));
+  // rows over a wavefront: one token each while the chip holds a wavefront for every token (8192), else as many as
+  // are ranked at once
+  const int batch = !ROWS ? 4 : a.T <= 8192 ? 1 : a.K <= kRowsK ? 4 : 2;
+  const int per = batch * kWaves, blocks = std::max(1, std::min((a.T + per - 1) / per, 256 * 8));
   if (a.load && (blocks > 1 || a.T == 0)) {
     hipLaunchKernelGGL(gate_zero_kernel, dim3(1), dim3(kGateMaxE), 0, stream, a.load, a.E);
     const hipError_t err = hipGetLastError();
@@ -453,10 +719,10 @@ hipError_t launch_gate(const GateArgs& a, hipStream_t stream) {
   const bool by_key = a.bias || a.has_prior || (a.n_group > 1 && a.group_rule == 1);
   const bool vec = V == 4 && a.E % 4 == 0 && (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0;
   constexpr bool VEC = V == 4;
-  if (vec && by_key) launch_groups<W, V, VEC, kByKey>(a, dim3(blocks), stream);
-  else if (vec) launch_groups<W, V, VEC, kByLogit>(a, dim3(blocks), stream);
-  else if (by_key) launch_groups<W, V, false, kByKey>(a, dim3(blocks), stream);
-  else launch_groups<W, V, false, kByLogit>(a, dim3(blocks), stream);
+  if (vec && by_key) launch_groups<V, ROWS, VEC, kByKey>(a, blocks, batch, stream);
+  else if (vec) launch_groups<V, ROWS, VEC, kByLogit>(a, blocks, batch, stream);
+  else if (by_key) launch_groups<V, ROWS, false, kByKey>(a, blocks, batch, stream);
+  else launch_groups<V, ROWS, false, kByLogit>(a, blocks, batch, stream);
   return hipGetLastError();
 }
 
@@ -617,10 +883,10 @@ void launch_dense(const GateBwdArgs& a, bool vec, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_gate_forward(const GateArgs& a, hipStream_t stream) {
-  if (a.E <= 16) return launch_gate<16, 1>(a, stream);
-  if (a.E <= 64) return launch_gate<16, 4>(a, stream);
-  if (a.E <= 128) return launch_gate<32, 4>(a, stream);
-  return launch_gate<64, 4>(a, stream);
+  if (a.E <= 16) return launch_gate<1, false>(a, stream);
+  if (a.E <= 64) return launch_gate<4, false>(a, stream);
+  if (a.E <= 128) return launch_gate<2, true>(a, stream);
+  return launch_gate<4, true>(a, stream);
 }
 
 hipError_t launch_gate_backward(const GateBwdArgs& a, hipStream_t stream) {
