@@ -12,8 +12,8 @@
 //                     go straight to LDS, double-buffered (2 x 64 KB). Widening two values takes about as long as a
 //                     product (16 cycles): with 8 x 4 fragments a wavefront (WN 4) it was as much work as they, 4850 us for the
 //                     Mixtral-shaped layer of 8192 tokens instead of 4330 with 4 x 8 (WN 2).
-//   MX4 activations   stages of 256 columns on v_mfma_scale_f32_16x16x128_f8f6f4; both operands go straight to LDS
-//                     (2 x 64 KB), the scales to registers, four steps a dword. 8 x 4 fragments (DeepSeek-shaped layer, 4096
+//   MX4 activations   stages of 128 columns on v_mfma_scale_f32_16x16x128_f8f6f4; both operands and their scales go
+//                     straight to LDS, three stages ahead (4 x 32 KB and 2 x 8 KB). 8 x 4 fragments (DeepSeek-shaped layer, 4096
 //                     tokens: 362 us, with 4 x 8 398).
 // Token loads are buffer loads: rows past the tile's end and columns past a row's end read as zeros.
 
@@ -145,106 +145,94 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     }
     wait_vmcnt<0>();
   } else {
-    // stage: 16 fragments x 2 steps of weights (32 KB, operand order), 256 rows x 128 bytes of tokens (32 KB; the
-    // piece at slot s of row r is logical piece s ^ (r / 2 & 7))
-    const int stages = (steps + 1) / 2;
-    uint32_t off[4];
+    // A stage is one step: 16 fragments of weights (16 KB, operand order), 256 rows x 64 bytes of tokens (16 KB; the
+    // piece at slot s of row r is logical piece s ^ (r / 4 & 3)). Four stages; the scales of four steps, a dword per
+    // fragment lane and token block, in two buffers of 8 KB behind them. Every wavefront issues the same number of
+    // loads a step (rows past the end read as zeros), so that it can wait for the oldest alone.
+    uint32_t off[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 8 * (4 * wave + i) + (lane >> 3);
-      off[i] = r < t.nrows ? source(r) * row_bytes + ((lane & 7) ^ (r >> 1 & 7)) * 16 : kNoRow;
+    for (int i = 0; i < 2; ++i) {
+      const int r = 16 * (2 * wave + i) + (lane >> 2);
+      off[i] = r < t.nrows ? source(r) * row_bytes + ((lane & 3) ^ (r >> 2 & 3)) * 16 : kNoRow;
     }
     const i32x4 wr = buffer_rsrc(wc, static_cast<uint32_t>(R / 16) * steps * 1024);
-    auto dma = [&](int st, int buf) {
-      const uint32_t base = lds0 + buf * 65536;
+    auto dma = [&](int ahead) {
+      const int s = min(ahead, steps - 1);   // past the end: a stage that nothing reads again
+      const uint32_t base = lds0 + (ahead & 3) * 32768;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {   // fragments 2 wave, + 1, both steps of each
-        const int f = min(t.f0 + 2 * wave + (i >> 1), R / 16 - 1), s = min(2 * st + (i & 1), steps - 1);
-        dma16s(base + (4 * wave + i) * 1024, wr, lane * 16, (static_cast<uint32_t>(f) * steps + s) * 1024);
+      for (int i = 0; i < 2; ++i) {
+        const int f = min(t.f0 + 2 * wave + i, R / 16 - 1);
+        dma16s(base + (2 * wave + i) * 1024, wr, lane * 16, (static_cast<uint32_t>(f) * steps + s) * 1024);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (8 * (4 * wave + i) >= 16 * WN * NL) break;
-        dma16s(base + 32768 + (4 * wave + i) * 1024, xr, off[i], static_cast<uint32_t>(st) * 128);
-      }
+      for (int i = 0; i < 2; ++i) dma16s(base + 16384 + (2 * wave + i) * 1024, xr, off[i], static_cast<uint32_t>(s) * 64);
     };
-    // scales: a dword of four steps per fragment; tokens [row, quad, 16]
-    const uint8_t* xs = EPI == 0 ? p.xs : p.hs;
-    const __amdgpu_buffer_rsrc_t xsr = make_rsrc(xs, static_cast<uint32_t>(src_rows) * quads * 16);
-    uint32_t soff[NL];
-#pragma unroll
-    for (int n = 0; n < NL; ++n) {
-      const int r = 16 * (WN * n + wn) + l16;
-      soff[n] = r < t.nrows ? source(r) * quads * 16 + 4 * lg : kNoRow;
+    // scales: waves 0 to 3 four fragments each, 4 to 7 64 token rows each
+    const bool of_w = wave < 4;
+    const i32x4 scr = of_w ? buffer_rsrc(wsc, static_cast<uint32_t>(R / 16) * quads * 256)
+                           : buffer_rsrc(EPI == 0 ? p.xs : p.hs, static_cast<uint32_t>(src_rows) * quads * 16);
+    uint32_t sc_off, sc_step;
+    if (of_w) {
+      sc_off = static_cast<uint32_t>(min(t.f0 + 4 * wave + (lane >> 4), R / 16 - 1)) * quads * 256 + (lane & 15) * 16;
+      sc_step = 256;
+    } else {
+      const int r = 64 * (wave - 4) + lane;
+      sc_off = r < t.nrows ? source(r) * quads * 16 : kNoRow;
+      sc_step = 16;
     }
-    uint32_t ws[2][kWF], ts[2][NL];
-    auto load_s = [&](int q, uint32_t (&w)[kWF], uint32_t (&b)[NL]) {
-#pragma unroll
-      for (int i = 0; i < kWF; ++i) w[i] = __builtin_amdgcn_raw_buffer_load_b32(sr, lane * 4, (frag[i] * quads + q) * 256, 0);
-#pragma unroll
-      for (int n = 0; n < NL; ++n) b[n] = __builtin_amdgcn_raw_buffer_load_b32(xsr, soff[n], q * 16, 0);
+    auto dma_scales = [&](int q) {
+      dma16s(lds0 + 131072 + (q & 1) * 8192 + wave * 1024, scr, sc_off, min(q, quads - 1) * sc_step);
     };
     // the last step of a C of an odd number of 64 columns: its upper blocks have no token scales
     const int cut = C % kMxStep != 0 ? steps - 1 : -1;
-    auto compute = [&](auto sub_c, int s, int buf, const uint32_t (&w)[kWF], const uint32_t (&b)[NL]) {
+    uint32_t ws[kWF], ts[NL];
+    auto compute = [&](auto sub_c, int s) {
       constexpr int S = decltype(sub_c)::value;   // step within the quad
-      const u32x4* wa = lds + buf * 4096 + kWF * wm * 128 + (S & 1) * 64 + lane;
-      const u32x4* xa = lds + buf * 4096 + 2048 + (16 * wn + l16) * 8 + ((4 * (S & 1) + lg) ^ (l16 >> 1));
+      const u32x4* wa = lds + S * 2048 + kWF * wm * 64 + lane;
+      const u32x4* xa = lds + S * 2048 + 1024 + (16 * wn + l16) * 4 + (lg ^ (l16 >> 2));
+      if constexpr (S == 0) {
+        const uint32_t* sc = reinterpret_cast<const uint32_t*>(lds + 8192 + (s >> 2 & 1) * 512);
+#pragma unroll
+        for (int i = 0; i < kWF; ++i) ws[i] = sc[(kWF * wm + i) * 64 + lane];
+#pragma unroll
+        for (int n = 0; n < NL; ++n) ts[n] = sc[1024 + (16 * (WN * n + wn) + l16) * 4 + lg];
+      }
       u32x4 xv[NL];
       uint32_t bs[NL];
 #pragma unroll
       for (int n = 0; n < NL; ++n) {
-        xv[n] = xa[n * WN * 128];
-        bs[n] = s == cut && lg >= 2 ? 0 : b[n];
+        xv[n] = xa[n * WN * 64];
+        bs[n] = s == cut && lg >= 2 ? 0 : ts[n];
       }
 #pragma unroll
       for (int i = 0; i < kWF; ++i) {
-        const u32x4 wv = wa[i * 128];
+        const u32x4 wv = wa[i * 64];
 #pragma unroll
-        for (int n = 0; n < NL; ++n) acc[i][n] = mfma_mx4<S>(wv, xv[n], acc[i][n], w[i], bs[n]);
+        for (int n = 0; n < NL; ++n) acc[i][n] = mfma_mx4<S>(wv, xv[n], acc[i][n], ws[i], bs[n]);
       }
     };
-    auto arrive = [&]() {
-      wait_vmcnt<0>();
+    auto step = [&](auto sub_c, int s) {
+      constexpr int S = decltype(sub_c)::value;
+      // behind step s's loads are those of two more steps, and a quad's scales where they were issued since
+      wait_vmcnt<S == 0 ? 8 : 9>();
       lds_sync();
+      dma(s + 3);
+      if constexpr (S == 0) dma_scales((s >> 2) + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s < steps) compute(sub_c, s);
+      __builtin_amdgcn_sched_barrier(0);
     };
-    auto settle = [&](uint32_t (&w)[kWF], uint32_t (&b)[NL]) {
-#pragma unroll
-      for (int i = 0; i < kWF; ++i) asm volatile("" : "+v"(w[i]));
-#pragma unroll
-      for (int n = 0; n < NL; ++n) asm volatile("" : "+v"(b[n]));
-    };
-    using I0 = std::integral_constant<int, 0>;
-    using I1 = std::integral_constant<int, 1>;
-    using I2 = std::integral_constant<int, 2>;
-    using I3 = std::integral_constant<int, 3>;
-    dma(0, 0);
-    load_s(0, ws[0], ts[0]);
-    arrive();
-    settle(ws[0], ts[0]);
-    // a quad of steps: stage 2 q in buffer 0, stage 2 q + 1 in buffer 1
-    auto quad = [&](int q, uint32_t (&w)[kWF], uint32_t (&b)[NL], uint32_t (&wn_)[kWF], uint32_t (&bn)[NL]) {
-      const int s = 4 * q;
-      dma(min(2 * q + 1, stages - 1), 1);
-      load_s(min(q + 1, quads - 1), wn_, bn);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(I0{}, s, 0, w, b);
-      if (s + 1 < steps) compute(I1{}, s + 1, 0, w, b);
-      __builtin_amdgcn_sched_barrier(0);
-      arrive();
-      settle(wn_, bn);
-      if (s + 2 >= steps) return;
-      dma(min(2 * q + 2, stages - 1), 0);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(I2{}, s + 2, 1, w, b);
-      if (s + 3 < steps) compute(I3{}, s + 3, 1, w, b);
-      __builtin_amdgcn_sched_barrier(0);
-      arrive();
-    };
-    for (int q = 0; q < quads; q += 2) {
-      quad(q, ws[0], ts[0], ws[1], ts[1]);
-      if (q + 1 < quads) quad(q + 1, ws[1], ts[1], ws[0], ts[0]);
+    dma_scales(0);
+    dma(0);
+    dma(1);
+    dma(2);
+    for (int s = 0; s < steps; s += 4) {
+      step(std::integral_constant<int, 0>{}, s);
+      step(std::integral_constant<int, 1>{}, s + 1);
+      step(std::integral_constant<int, 2>{}, s + 2);
+      step(std::integral_constant<int, 3>{}, s + 3);
     }
+    wait_vmcnt<0>();   // nothing may arrive in LDS after the workgroup's end
   }
 
   // acc[i][n][e]: weight row 4 lg + e of fragment i, token l16 of fragment WN n + wn
@@ -295,7 +283,7 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
 
 template <bool MX, int EPI>
 __global__ __launch_bounds__(kThreads, 2) void mx4_wide_kernel(const Mx4Params p) {
-  __shared__ u32x4 lds[8192];
+  __shared__ u32x4 lds[MX ? 9216 : 8192];
   const int R = EPI == 0 ? 2 * p.a.F : p.a.d;
   const int wt = (R / 16 + kFrags - 1) / kFrags;   // weight tiles
   const int live = p.pb.tile_off[p.G] * wt;
