@@ -44,15 +44,16 @@ struct Mx4Args {
 };
 struct Mx4Params {
   Mx4Args a;
-  int32_t* idx;      // [T, K + n_shared] experts of every entry, -1 for none
-  float* gate;       // [T, K + n_shared]
+  const int32_t* idx;   // [T, K + n_shared] experts of every entry; outside [0, G): none
+  const float* gate;    // [T, K + n_shared]
   PermBuffers pb;
   uint8_t* xq;       // [T, d / 2] codes
   uint8_t* xs;       // [T, quads of d, 16]: the scale of block b at byte 16 (b / 16) + 4 (b % 4) + b / 4 % 4, so that
                      // dword g of a quad holds the scales of columns 32 g .. of its four steps
   void* h;           // [rows, F] bf16, or codes
   uint8_t* hs;       // [rows, quads of F, 16]
-  float* o;          // [rows, d]
+  void* o;           // [rows, d] fp32; bf16 where o_bf16
+  bool o_bf16;       // wide tiles with MX4 activations: expert outputs rounded once more (see mx4_experts.hip)
   int G;             // E + n_shared
 };
 // Up to kMx4FewT tokens (mx4_few.hip): both products without prepare and permutation; p.o holds kMx4FewSplits x T rows.

@@ -14,7 +14,8 @@ namespace {
 constexpr int kThreads = 256;
 
 // Entries of routed and shared experts in one list; x in blocks (four lanes a block).
-__global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p, int entry_blocks) {
+__global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p, int32_t* idx, float* gate,
+                                                              int entry_blocks) {
   const Mx4Args& a = p.a;
   const int KS = a.K + a.n_shared;
   if (static_cast<int>(blockIdx.x) < entry_blocks) {
@@ -28,8 +29,8 @@ __global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p
       if (e < 0 || e >= a.E) e = -1;
       g = a.gate[t * a.K + k];
     }
-    p.idx[j] = e;
-    p.gate[j] = g;
+    idx[j] = e;
+    gate[j] = g;
     return;
   }
   const int64_t n = static_cast<int64_t>(a.T) * a.d / 8;
@@ -57,7 +58,9 @@ __global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p
 }
 
 // y = sum of the gate-weighted expert outputs (each the sum of its parts) in entry order, fp32, rounded once; a thread
-// per 4 columns.
+// per 4 columns. OB: expert outputs in bf16. Bound by their bytes (268 MB in fp32, 4096 tokens of the
+// DeepSeek-shaped layer: 70 us).
+template <bool OB>
 __global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p, int splits) {
   const Mx4Args& a = p.a;
   const int KS = a.K + a.n_shared, c4 = a.d / 4;
@@ -67,15 +70,34 @@ __global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p
   f32x4 s = {0, 0, 0, 0};
   for (int k = 0; k < KS; ++k) {
     const int j = t * KS + k;
-    if (p.idx[j] < 0) continue;
+    if (static_cast<uint32_t>(p.idx[j]) >= static_cast<uint32_t>(p.G)) continue;
     const float g = p.gate[j];
-    const f32x4* src = reinterpret_cast<const f32x4*>(p.o) + static_cast<size_t>(p.pb.inv[j]) * c4 + c;
-    f32x4 o = src[0];
-    for (int z = 1; z < splits; ++z) o += src[static_cast<size_t>(z) * a.T * KS * c4];
+    const size_t at = static_cast<size_t>(p.pb.inv[j]) * c4 + c;
+    f32x4 o;
+    if constexpr (OB) {
+      const uint2 b = static_cast<const uint2*>(p.o)[at];
+      o = f32x4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16),
+                __uint_as_float(b.y & 0xffff0000u)};
+    } else {
+      const f32x4* src = static_cast<const f32x4*>(p.o) + at;
+      o = src[0];
+      for (int z = 1; z < splits; ++z) o += src[static_cast<size_t>(z) * a.T * KS * c4];
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) s[q] += g * o[q];
   }
   reinterpret_cast<uint2*>(a.y)[i] = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
+}
+
+// Whether the wide tiles are taken: by the rows per expert from which they are faster, and their number, which must
+// cover the chip (small layers: F 512, 8 experts, bf16, 1000 / 4000 tokens 42 / 48 us, batch tiles 28 / 40).
+//   bf16: the batch tiles' weight stream hides the widening, which the wide ones pay with the products; whole call,
+//     batch / wide: Mixtral-shaped 450 tokens (112 rows an expert) 336 / 429 us, 1000 (250) 666 / 697, 1500 (375)
+//     927 / 907; DeepSeek-shaped 1600 (194 with the shared experts) 297 / 323, 2500 (303) 420 / 395.
+//   MX4: Mixtral-shaped 64 tokens (16) 150 / 159, 128 (32) 173 / 165; DeepSeek-shaped 100 (12) 91 / 96, 333 (40) 112 / 108.
+bool mx4_takes_wide(int rows, int G, int F, bool mx_act) {
+  const int64_t tiles = (static_cast<int64_t>(rows) / kMx4TileRows + G / 2) * ((2 * F + 255) / 256);
+  return rows >= (mx_act ? 25 : 280) * G && tiles >= 256;
 }
 
 }  // namespace
@@ -117,8 +139,8 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   Mx4Params p;
   p.a = a;
   p.G = a.E + a.n_shared;
-  p.idx = reinterpret_cast<int32_t*>(ws + w.idx);
-  p.gate = reinterpret_cast<float*>(ws + w.gate);
+  p.idx = a.idx;
+  p.gate = a.gate;
   p.pb.offsets = reinterpret_cast<int32_t*>(ws + w.offsets);
   p.pb.tile_off = reinterpret_cast<int32_t*>(ws + w.tile_off);
   p.pb.active = reinterpret_cast<int32_t*>(ws + w.active);
@@ -130,22 +152,36 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   p.xs = reinterpret_cast<uint8_t*>(ws + w.xs);
   p.h = ws + w.h;
   p.hs = reinterpret_cast<uint8_t*>(ws + w.hs);
-  p.o = reinterpret_cast<float*>(ws + w.o);
+  p.o = ws + w.o;
+  p.o_bf16 = false;
   if (a.T <= kMx4FewT) return launch_mx4_few(p, stream);
   const int KS = a.K + a.n_shared, rows = a.T * KS;
-  const int entry_blocks = (rows + kThreads - 1) / kThreads;
-  const int64_t quant_blocks = a.mx_act ? (static_cast<int64_t>(a.T) * a.d / 8 + kThreads - 1) / kThreads : 0;
-  hipLaunchKernelGGL(mx4_prepare_kernel, dim3(static_cast<unsigned>(entry_blocks + quant_blocks)), dim3(kThreads), 0,
-                     stream, p, entry_blocks);
-  hipError_t err = hipGetLastError();
-  if (err != hipSuccess) return err;
-  const bool wide = rows >= 100 * p.G;
+  hipError_t err;
+  if (a.n_shared > 0 || a.mx_act) {   // else the caller's entries are all there is
+    const int entry_blocks = a.n_shared > 0 ? (rows + kThreads - 1) / kThreads : 0;
+    const int64_t quant_blocks = a.mx_act ? (static_cast<int64_t>(a.T) * a.d / 8 + kThreads - 1) / kThreads : 0;
+    int32_t* idx = reinterpret_cast<int32_t*>(ws + w.idx);
+    float* gate = reinterpret_cast<float*>(ws + w.gate);
+    hipLaunchKernelGGL(mx4_prepare_kernel, dim3(static_cast<unsigned>(entry_blocks + quant_blocks)), dim3(kThreads), 0,
+                       stream, p, idx, gate, entry_blocks);
+    err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    if (a.n_shared > 0) {
+      p.idx = idx;
+      p.gate = gate;
+    }
+  }
+  const bool wide = mx4_takes_wide(rows, p.G, a.F, a.mx_act);
   const int tile_rows = wide ? kMx4TileRows : kMx4BatchRows;
   err = launch_permute(p.idx, a.T, KS, p.G, 0, tile_rows, p.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
   if (err != hipSuccess) return err;
   const int max_tiles = std::min(rows, rows / tile_rows + p.G);
   int splits = 1;
   if (wide) {
+    // With MX4 activations the bytes of fp32 outputs take as long as the products that make them; in bf16 (the layer's
+    // type; y is off by 2.3e-3 instead of 1.7e-3 then) they take half: DeepSeek-shaped layer, 4096 tokens, down and
+    // combine 121 + 70 -> 112 + 40 us. With bf16 activations, whose h is rounded to bf16 already, they stay fp32.
+    p.o_bf16 = a.mx_act;
     err = launch_mx4_wide(p, max_tiles, stream);
   } else {
     // two workgroups a CU for the down projection, each with eight steps or more
@@ -157,8 +193,9 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   }
   if (err != hipSuccess) return err;
   const int64_t cn = static_cast<int64_t>(a.T) * a.d / 4;
-  hipLaunchKernelGGL(mx4_combine_kernel, dim3(static_cast<unsigned>((cn + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                     stream, p, splits);
+  const dim3 cgrid(static_cast<unsigned>((cn + kThreads - 1) / kThreads));
+  if (p.o_bf16) hipLaunchKernelGGL(mx4_combine_kernel<true>, cgrid, dim3(kThreads), 0, stream, p, splits);
+  else hipLaunchKernelGGL(mx4_combine_kernel<false>, cgrid, dim3(kThreads), 0, stream, p, splits);
   return hipGetLastError();
 }
 

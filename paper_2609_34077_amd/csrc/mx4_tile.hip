@@ -245,7 +245,13 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
 #pragma unroll
       for (int i = 0; i < kWF; ++i) {
         const int f = t.f0 + kWF * wm + i;
-        if (ok && f < R / 16) *reinterpret_cast<f32x4*>(p.o + row * a.d + 16 * f + 4 * lg) = acc[i][n];
+        if (!ok || f >= R / 16) continue;
+        const size_t at = row * a.d + 16 * f + 4 * lg;
+        const f32x4 v = acc[i][n];
+        if constexpr (MX)
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + at) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
+        else
+          *reinterpret_cast<f32x4*>(static_cast<float*>(p.o) + at) = v;
       }
     } else {
 #pragma unroll

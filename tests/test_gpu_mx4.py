@@ -105,6 +105,28 @@ def test_experts(T, d, F, E, K, ns, pad, act):
         assert (y[T - pad:] == 0).all()
 
 
+# the same with enough rows and columns that 256 x 256 tiles cover the chip (the last: with MX4 activations alone)
+WIDE = [(2100, 64, 4096, 1, 1, 0, 0), (900, 192, 4160, 2, 2, 1, 37), (700, 320, 4160, 3, 2, 1, 0), (1500, 448, 4160, 2, 1, 0, 1),
+        (210, 128, 4160, 16, 2, 0, 5)]
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T,d,F,E,K,ns,pad", WIDE)
+def test_experts_on_wide_tiles(T, d, F, E, K, ns, pad, act):
+    say(f"mx4 wide T={T} d={d} F={F} E={E} K={K} shared={ns} pad={pad} act={act}")
+    x, wq, dev, idx, gate = make(T, d, F, E, K, ns, T + d + F, pad)
+    bad = (T // 3, T - pad - 1)
+    y = check(x, wq, dev, idx, gate, ns, act)
+    if pad and not ns:
+        assert (y[T - pad:] == 0).all()
+    clean = torch.from_numpy(y)
+    x[bad[0], 7], x[bad[1], d - 1] = float("nan"), float("inf")     # they stay in their tokens
+    y2 = call(x, dev, idx, gate, ns, act).cpu().double()
+    rows = torch.ones(T, dtype=torch.bool)
+    rows[list(bad)] = False
+    assert torch.equal(y2[rows], clean[rows]) and not y2[~rows].isfinite().any()
+
+
 @pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
 @pytest.mark.parametrize("T", [1, 7, 40, 300])
 def test_uneven_and_odd_routing(T, act):
@@ -154,12 +176,12 @@ def test_scales_at_their_ends(T, act):
 
 
 @pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
-@pytest.mark.parametrize("T", [4, 100, 900])
-def test_dirty_workspace_streams_and_graphs(T, act):
+@pytest.mark.parametrize("T,F", [(4, 320), (100, 320), (900, 320), (1400, 4160)])
+def test_dirty_workspace_streams_and_graphs(T, F, act):
     """The workspace's contents do not matter; calls on two streams with a workspace each; captured and replayed
     with other work between; the same bits every time."""
     say(f"mx4 experts graph T={T} act={act}")
-    E, K, ns, d, F = 8, 2, 1, 256, 320
+    E, K, ns, d = 8, 2, 1, 256
     x, wq, dev, idx, gate = make(T, d, F, E, K, ns, T + 3)
     packed = L.maskmoe_mx4_pack_experts(*dev)
     xs, it, gt = x.cuda(), torch.from_numpy(idx).cuda(), torch.from_numpy(gate).cuda()
