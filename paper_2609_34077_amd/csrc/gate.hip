@@ -415,12 +415,13 @@ __device__ __forceinline__ void key_bounds(const LaneExperts<V>& x, float& pmax,
   bmax = seg_fmax<W>(bmax);
 }
 
-// The W lanes of a token write its entries: this lane entry r (if r < K), expert e (-1: none) and its gate.
+// The W lanes of a token write its entries: this lane entry r (if r < K), expert e (-1: none), whose (clamped) logit is
+// given, and its gate.
 template <int W>
-__device__ __forceinline__ void write_gate(const GateArgs& a, int t, bool real, int r, int e, float zmax, float total,
-                                           int* hist) {
+__device__ __forceinline__ void write_gate(const GateArgs& a, int t, bool real, int r, int e, float logit, float zmax,
+                                           float total, int* hist) {
   const bool has = e >= 0, soft = a.score == 0;
-  const float zs = has ? clamp_logit(a.logits[static_cast<size_t>(t) * a.E + e]) : -INFINITY;
+  const float zs = has ? logit : -INFINITY;
   float g;
   if (a.renorm) {
     // ratios of scores, from logits relative to the largest selected one: exp(z_k - z_max) for
@@ -463,14 +464,14 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(const GateArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int seg = lane / W, sl = lane % W, e0 = sl * V;
   const int slot = wave * SEGS + seg;
-  clear_hist(a, hist);
-  const LaneExperts<V> x = lane_experts<V, KEYS>(a, e0);
-  float pmax, bmax;
-  key_bounds<W>(x, pmax, bmax);
-  const uint32_t below = (1u << sl) - 1;   // lower lanes of the segment
   float next[V];
   const int stride = gridDim.x * PER;
   load_row<V, VEC>(a, min(static_cast<int>(blockIdx.x) * PER + slot, a.T - 1), e0, next);
+  const LaneExperts<V> x = lane_experts<V, KEYS>(a, e0);
+  clear_hist(a, hist);
+  float pmax, bmax;
+  key_bounds<W>(x, pmax, bmax);
+  const uint32_t below = (1u << sl) - 1;   // lower lanes of the segment
   for (int t0 = blockIdx.x * PER; t0 < a.T; t0 += stride) {
     const int t = min(t0 + slot, a.T - 1);   // segments past the last token repeat it, unwritten
     float z[V];
@@ -528,7 +529,8 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(const GateArgs a) {
       }
     }
     lds_order();
-    write_gate<W>(a, t, t0 + slot < a.T, sl, e, row.zmax, row.total, hist);
+    const float logit = e >= 0 ? clamp_logit(a.logits[static_cast<size_t>(t) * a.E + e]) : 0.0f;
+    write_gate<W>(a, t, t0 + slot < a.T, sl, e, logit, row.zmax, row.total, hist);
   }
   add_hist(a, hist);
 }
@@ -545,23 +547,27 @@ __global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a
     float zmax, total, tol;
     int again;                             // select in fp64: group scores too close, or more candidates than C
   };
-  __shared__ uint2 cand[kWaves][TB][C];    // (key, expert)
+  struct Candidate {
+    uint32_t key, expert;
+    float logit, bias;
+  };
+  __shared__ __align__(16) Candidate cand[kWaves][TB][C];
   __shared__ double cand64[KEYS == kByKey ? kWaves : 1][TB][C];
   __shared__ Found found[kWaves][TB];
   __shared__ double rows[GROUPED ? kWaves : 1][64 * V], leads[GROUPED ? kWaves : 1][64 * V];
   __shared__ int hist[kGateMaxE];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e0 = lane * V;
   const int seg = lane / C, sl = lane % C;
-  clear_hist(a, hist);
-  const LaneExperts<V> x = lane_experts<V, KEYS>(a, e0);
-  float pmax, bmax;
-  key_bounds<kWave>(x, pmax, bmax);
   const int stride = gridDim.x * kWaves * batch;
   int t0 = (blockIdx.x * kWaves + wave) * batch;
   float next[V];
   load_row<V, VEC>(a, min(t0, a.T - 1), e0, next);
+  const LaneExperts<V> x = lane_experts<V, KEYS>(a, e0);
+  clear_hist(a, hist);
+  float pmax, bmax;
+  key_bounds<kWave>(x, pmax, bmax);
   for (; t0 < a.T; t0 += stride) {
-    cand[wave][seg][sl] = make_uint2(kNone, 0xffffffffu);
+    cand[wave][seg][sl] = Candidate{kNone, 0xffffffffu, 0.0f, 0.0f};
     lds_order();
     const int count = min(batch, a.T - t0);
     for (int k = 0; k < count; ++k) {
@@ -615,7 +621,7 @@ __global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a
         for (int v = 0; v < V; ++v) {
           const int pos = static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(at[v] >> 32),
                                                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(at[v]), base)));
-          if (at[v] >> lane & 1) cand[wave][k][pos] = make_uint2(key[v], e0 + v);
+          if (at[v] >> lane & 1) cand[wave][k][pos] = Candidate{key[v], static_cast<uint32_t>(e0 + v), z[v], x.bias[v]};
           base += __popcll(at[v]);
         }
       }
@@ -626,17 +632,18 @@ __global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a
     const int t = min(t0 + seg, a.T - 1);
     const bool real = seg < count;
     const Found f = found[wave][real ? seg : 0];
-    const uint2 own = cand[wave][seg][sl];
-    const bool has = own.x != kNone;
+    const Candidate own = cand[wave][seg][sl];
+    const bool has = own.key != kNone;
+    float logit = own.logit;
     int rank = 0;
     bool close = real && f.again;
     if constexpr (KEYS == kByKey) {
       double k = -INFINITY;
       if (has) {
-        k = exact_score(a.score == 0, clamp_logit(a.logits[static_cast<size_t>(t) * a.E + own.y]), f.zmax);
+        k = exact_score(a.score == 0, own.logit, f.zmax);
         if (a.score == 0 && a.bias) k /= f.total;   // without bias the order does not depend on the sum
-        if (a.has_prior) k *= a.prior[own.y];
-        if (a.bias) k += a.bias[own.y];
+        if (a.has_prior) k *= a.prior[own.expert];
+        k += own.bias;
       }
       cand64[wave][seg][sl] = k;
       lds_order();
@@ -644,7 +651,7 @@ __global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a
 #pragma unroll 4
       for (int j = 0; j < C; ++j) {
         const double o = cand64[wave][seg][j];
-        rank += o > k || (o == k && cand[wave][seg][j].y < own.y) ? 1 : 0;
+        rank += o > k || (o == k && cand[wave][seg][j].expert < own.expert) ? 1 : 0;
         gap = j == sl ? gap : fmin(gap, fabs(o - k));
       }
       // a sum in fp32 beside a bias: the keys are no better than fp32
@@ -652,12 +659,12 @@ __global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a
     } else {
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        const uint2 o = cand[wave][seg][j];
-        rank += o.x > own.x || (o.x == own.x && o.y < own.y) ? 1 : 0;
+        const uint32_t o = cand[wave][seg][j].key;
+        rank += o > own.key || (o == own.key && cand[wave][seg][j].expert < own.expert) ? 1 : 0;
       }
     }
     // a selected candidate's lane writes its entry; lanes without a candidate the entries that are left over
-    int r = rank, e = has && rank < a.K ? static_cast<int>(own.y) : -1;
+    int r = rank, e = has && rank < a.K ? static_cast<int>(own.expert) : -1;
     if (!has) {
       const uint32_t filled = static_cast<uint32_t>(__ballot(has) >> (C * seg)) & static_cast<uint32_t>((1ull << C) - 1);
       r = __popc(filled) + __popc(~filled & ((1u << sl) - 1));
@@ -670,11 +677,15 @@ __global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a
         const int ex = select_exact<kWave, V, VEC, KEYS, GROUPS>(a, x, t0 + k, 0, lane, rows[GROUPED ? wave : 0],
                                                                  leads[GROUPED ? wave : 0]);
         const int mine = __shfl(ex, sl, kWave);   // entry sl, for the token's lanes
-        if (seg == k) e = sl < a.K ? mine : -1, r = sl;
+        if (seg == k) {
+          e = sl < a.K ? mine : -1;
+          r = sl;
+          logit = e >= 0 ? clamp_logit(a.logits[static_cast<size_t>(t) * a.E + e]) : 0.0f;
+        }
       }
     }
     lds_order();
-    write_gate<C>(a, t, real, r, e, f.zmax, f.total, hist);
+    write_gate<C>(a, t, real, r, e, logit, f.zmax, f.total, hist);
   }
   add_hist(a, hist);
 }

@@ -22,7 +22,9 @@ constexpr int kMaxExperts = 256, kMaxSlots = 256 + 8;
 constexpr int kThreads = 256;
 constexpr int kUpDepth = 2, kDownDepth = 2;   // steps in flight per wavefront, 4 KiB of weights each
 
-constexpr uint32_t kNowhere = 0xfffffff0u;   // an offset past every buffer: reads as zeros, without a branch
+// An offset past every buffer (fewer than 2^31 bf16 values of whole 128-byte pieces), with room for the 48 bytes that
+// are added to it: reads as zeros, without a branch.
+constexpr uint32_t kNowhere = 0xffffffc0u;
 constexpr int kNt = 2;                       // the load's non-temporal bit: weights that one workgroup reads once
 
 // The selected experts as bits, and the entries themselves (T * K <= 256), in LDS.

@@ -157,6 +157,20 @@ def test_nan_and_infinity_stay_in_their_token(T, act):
 
 
 @pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T", [2, 5, 16, 17, 130])
+@pytest.mark.parametrize("at", [0, -1])
+def test_a_token_of_nan_beside_rows_of_odd_length(T, at, act):
+    """Rows that end inside a 128-column step: nothing of the first or last token's is read in place of their rest."""
+    x, wq, dev, idx, gate = make(T, 192, 192, 3, 2, 1, T + 5)
+    clean = call(x, dev, idx, gate, 1, act).cpu()
+    x[at] = float("nan")
+    y = call(x, dev, idx, gate, 1, act).cpu()
+    rows = torch.ones(T, dtype=torch.bool)
+    rows[at] = False
+    assert torch.equal(y[rows], clean[rows]) and y[at].isnan().all()
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
 @pytest.mark.parametrize("T", [2, 40, 520])
 def test_scales_at_their_ends(T, act):
     """Weight blocks with the smallest scales (bytes 0 and 1), a large one, and NaN scales of one expert."""
