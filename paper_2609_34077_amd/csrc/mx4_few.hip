@@ -5,7 +5,9 @@
 //         to end: each expert's sum is weighed by the tokens' gates and added, so that y comes out;
 //   sum   of the parts, in order.
 // A wavefront multiplies 64 weight rows at a time, so that the tokens' operand, which takes as many registers as
-// theirs, is used four times, and has two steps (8 KiB of weights) in flight.
+// theirs, is used four times. It keeps no ring of steps: in 64 to 84 registers six to eight wavefronts a SIMD have their
+// loads in flight together (Mixtral-shaped layer, one token, up / down: 25.3 / 14.3 us; with rings of two steps in 156
+// registers 27.0 / 17.1, and rings of one, whose registers the compiler keeps apart, 26.4 / 16.1).
 // Tokens are the 16 columns of the matrix instructions as they are; a token that an expert is not selected for
 // loads nothing there. Weights go from memory straight to registers, 1 KiB of 16 rows x 128 columns a load.
 
@@ -20,7 +22,6 @@ namespace {
 
 constexpr int kMaxExperts = 256, kMaxSlots = 256 + 8;
 constexpr int kThreads = 256;
-constexpr int kUpDepth = 2, kDownDepth = 2;   // steps in flight per wavefront, 4 KiB of weights each
 
 // An offset past every buffer (fewer than 2^31 bf16 values of whole 128-byte pieces), with room for the 48 bytes that
 // are added to it: reads as zeros, without a branch.
@@ -100,15 +101,11 @@ __global__ __launch_bounds__(kThreads, 4) void mx4_few_up_kernel(const Mx4Params
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc[i] = f32x4{0, 0, 0, 0};
   const int s0 = steps * wave / 4, s1 = steps * (wave + 1) / 4;
-  // kUpDepth steps in flight, weights and tokens together (loads return in order, so tokens loaded later would wait
-  // for the weights behind them): step s sits in set (s - s0) % kUpDepth, which takes step s + kUpDepth
   struct Step {
     u32x4 w[4], b[4];
     uint32_t ws[4];
   };
-  Step st[kUpDepth];
-  auto load = [&](int ahead, Step& q) {
-    const int s = min(ahead, s1 - 1);   // past the end: loaded again and not used, so that every wait is the same
+  auto load = [&](int s, Step& q) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       q.w[i] = __builtin_amdgcn_raw_buffer_load_b128(codes, lane * 16, (i * steps + s) * 1024, kNt);
@@ -134,20 +131,10 @@ __global__ __launch_bounds__(kThreads, 4) void mx4_few_up_kernel(const Mx4Params
       }
     }
   };
-  if (s0 < s1) {
-#pragma unroll
-    for (int q = 0; q < kUpDepth; ++q) load(s0 + q, st[q]);
-    int s = s0;
-    for (; s + kUpDepth <= s1; s += kUpDepth) {
-#pragma unroll
-      for (int q = 0; q < kUpDepth; ++q) {
-        multiply(s + q, st[q]);
-        load(s + q + kUpDepth, st[q]);
-      }
-    }
-#pragma unroll
-    for (int q = 0; q + 1 < kUpDepth; ++q)
-      if (s + q < s1) multiply(s + q, st[q]);
+  for (int s = s0; s < s1; ++s) {
+    Step q;
+    load(s, q);
+    multiply(s, q);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) red[wave][i][lane] = acc[i];
@@ -185,13 +172,16 @@ __global__ __launch_bounds__(kThreads, 4) void mx4_few_up_kernel(const Mx4Params
 }
 
 template <bool MX>
-__global__ __launch_bounds__(kThreads, 4) void mx4_few_down_kernel(const Mx4Params p, int splits) {
+__global__ __launch_bounds__(kThreads, 4) void mx4_few_down_kernel(const Mx4Params p, int splits, int max_slots) {
   __shared__ Routing rt;
   __shared__ uint16_t expert[kMaxSlots];
   __shared__ uint16_t slot_of[kMaxExperts];
-  __shared__ float gates[kMaxSlots][kMx4FewT];   // of the slot's expert and a token: the sum over its entries
-  __shared__ int16_t hrow[kMaxSlots][kMx4FewT];  // row of h, -1 where the token did not select the expert
   __shared__ f32x4 red[4][4][kWave];
+  // for each of max_slots slots and a token: the gate (the sum over the token's entries that name the expert) and the row
+  // of h, -1 where none does. As large as the launch needs, so that four workgroups fit a CU.
+  extern __shared__ float tables[];
+  float(*gates)[kMx4FewT] = reinterpret_cast<float(*)[kMx4FewT]>(tables);
+  int16_t(*hrow)[kMx4FewT] = reinterpret_cast<int16_t(*)[kMx4FewT]>(tables + max_slots * kMx4FewT);
   const Mx4Args& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -247,7 +237,6 @@ __global__ __launch_bounds__(kThreads, 4) void mx4_few_down_kernel(const Mx4Para
   f32x4 y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = f32x4{0, 0, 0, 0};
-  Unit un[kDownDepth];
   auto load = [&](const Place& at, Unit& q) {
     const int s = at.step;
     const size_t f = static_cast<size_t>(__builtin_amdgcn_readfirstlane(expert[at.slot])) * (R / 16) + 4 * cx;
@@ -288,29 +277,13 @@ __global__ __launch_bounds__(kThreads, 4) void mx4_few_down_kernel(const Mx4Para
         y[i][e] += q.row >= 0 ? q.gate * acc[e] : 0.0f;
     }
   };
-  if (u0 < u1) {
-    const Place last{(u1 - 1) / steps, (u1 - 1) % steps};
-    Place ahead{u0 / steps, u0 % steps};
-    auto load_next = [&](Unit& q) {   // past the end: the last unit again, not used, so that every wait is the same
-      load(ahead, q);
-      if (ahead.slot != last.slot || ahead.step != last.step) {
-        const bool wrap = ahead.step + 1 == steps;
-        ahead = Place{wrap ? ahead.slot + 1 : ahead.slot, wrap ? 0 : ahead.step + 1};
-      }
-    };
-#pragma unroll
-    for (int q = 0; q < kDownDepth; ++q) load_next(un[q]);
-    int u = u0;
-    for (; u + kDownDepth <= u1; u += kDownDepth) {
-#pragma unroll
-      for (int q = 0; q < kDownDepth; ++q) {
-        multiply(un[q]);
-        load_next(un[q]);
-      }
-    }
-#pragma unroll
-    for (int q = 0; q + 1 < kDownDepth; ++q)
-      if (u + q < u1) multiply(un[q]);
+  Place at{u0 / steps, u0 % steps};
+  for (int u = u0; u < u1; ++u) {
+    Unit q;
+    load(at, q);
+    multiply(q);
+    const bool wrap = at.step + 1 == steps;
+    at = Place{wrap ? at.slot + 1 : at.slot, wrap ? 0 : at.step + 1};
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) red[wave][i][lane] = y[i];
@@ -346,7 +319,8 @@ hipError_t launch(const Mx4Params& p, hipStream_t stream) {
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const int splits = mx4_few_splits(a.d);
-  hipLaunchKernelGGL(mx4_few_down_kernel<MX>, dim3(a.d / 64 * splits), dim3(kThreads), 0, stream, p, splits);
+  hipLaunchKernelGGL(mx4_few_down_kernel<MX>, dim3(a.d / 64 * splits), dim3(kThreads), slots * kMx4FewT * 6, stream, p,
+                     splits, slots);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   const int n = a.T * a.d / 4;
