@@ -576,13 +576,13 @@ typedef struct maskmoe_gate_desc {
  *
  *  logits      device [T, E] float.
  *  mask        host [E] uint8 or NULL: 0 excludes an expert for every token (any number may be 0).
- *  prior       host [E] float or NULL: finite and > 0.
- *  bias        device [E] float or NULL (finite).
+ *  prior       host [E] float or NULL: 2^-100 to 2^100.
+ *  bias        device [E] float or NULL: finite, at most 2^100 in magnitude.
  *  topk_idx    device [T, K] int32, by decreasing key.   topk_gate  device [T, K] float.
  *  load        device [E] int32 or NULL: how many entries of topk_idx name each expert (what a balance rule
  *              updates the bias by). Written also for T = 0.
- *  Errors: E_INVAL for a desc outside its ranges, a prior that is not finite and > 0, NULL or misaligned
- *  pointers.
+ *  Errors: E_INVAL for a desc or a prior outside its ranges, NULL or misaligned pointers; E_UNSUPPORTED for T
+ *  above 2^30.
  */
 int maskmoe_gate_forward(const maskmoe_gate_desc* desc, const float* logits, const uint8_t* mask, const float* prior,
                          const float* bias, int32_t* topk_idx, float* topk_gate, int32_t* load, hipStream_t stream);
@@ -598,8 +598,9 @@ int maskmoe_gate_forward(const maskmoe_gate_desc* desc, const float* logits, con
  * and zero elsewhere. bias, prior and mask steer the selection only and have no gradient here. An expert
  * that an entry list names twice gets the sum.
  *  desc        as given to the forward (T, E, K, score, renorm, scale are used).
- *  logits, topk_idx: the forward's.   d_gate device [T, K] float.   d_logits device [T, E] float, written whole.
- *  Errors: E_INVAL as above. T = 0 writes nothing.
+ *  logits, topk_idx: the forward's.   d_gate device [T, K] float.   d_logits device [T, E] float, written whole,
+ *  another buffer than logits.
+ *  Errors: as above, and E_INVAL for d_logits == logits. T = 0 writes nothing.
  */
 int maskmoe_gate_backward(const maskmoe_gate_desc* desc, const float* logits, const int32_t* topk_idx,
                           const float* d_gate, float* d_logits, hipStream_t stream);
@@ -669,8 +670,8 @@ enum { MASKMOE_ACT_BF16 = 0, MASKMOE_ACT_MX4 = 1 };
  *  Rounding: sums are fp32; h is rounded once to bf16 (ACT_BF16) or to MX4 blocks (ACT_MX4, as x is); expert outputs
  *  stay fp32 (ACT_MX4 with 25 rows per expert or more: rounded once to bf16); y is rounded once.
  *  Errors: E_INVAL for a desc outside its ranges, an unknown act, NULL or misaligned pointers, x == y; E_WORKSPACE;
- *  E_UNSUPPORTED for MASKMOE_F32, d or F not multiples of 64, or T d, T (K + n_shared) F, T (K + n_shared) d or 2 F d
- *  at or above 2^31.
+ *  E_UNSUPPORTED for MASKMOE_F32, d or F not multiples of 64, T d, T (K + n_shared) F, T (K + n_shared) d or 2 F d
+ *  at or above 2^31, or up to 16 tokens with T (K + n_shared) F at or above 2^29.
  */
 size_t maskmoe_experts_mx4_workspace_bytes(const maskmoe_layer_desc* desc);
 int maskmoe_experts_forward_mx4(const maskmoe_layer_desc* desc, int32_t act, const void* x, const int32_t* topk_idx,

@@ -23,7 +23,7 @@ int check_gate(const maskmoe_gate_desc* d) {
   if (d->score != MASKMOE_SCORE_SOFTMAX && d->score != MASKMOE_SCORE_SIGMOID) return MASKMOE_E_INVAL;
   if (d->renorm != 0 && d->renorm != 1) return MASKMOE_E_INVAL;
   if (!isfinite(d->scale)) return MASKMOE_E_INVAL;
-  if (static_cast<int64_t>(d->T) * d->E >= int64_t{1} << 38) return MASKMOE_E_INVAL;
+  if (d->T > 1 << 30) return MASKMOE_E_UNSUPPORTED;   // token numbers and a grid's stride past them fit 32 bits
   return MASKMOE_OK;
 }
 
@@ -38,6 +38,7 @@ int check_mx4(const maskmoe_layer_desc* d) {
   if (static_cast<int64_t>(d->T) * d->d >= kLim || rows * d->F >= kLim || int64_t{2} * d->F * d->d >= kLim ||
       rows * d->d >= kLim)
     return MASKMOE_E_UNSUPPORTED;
+  if (d->T <= maskmoe::kMx4FewT && rows * d->F >= kLim / 4) return MASKMOE_E_UNSUPPORTED;   // a launch's 2^32 threads
   return MASKMOE_OK;
 }
 
@@ -54,9 +55,9 @@ int maskmoe_gate_forward(const maskmoe_gate_desc* desc, const float* logits, con
       static_cast<int64_t>(d.topk_group) * (d.E / d.n_group) < d.K)
     return MASKMOE_E_INVAL;
   if (d.group_rule != MASKMOE_GROUP_MAX && d.group_rule != MASKMOE_GROUP_SUM2) return MASKMOE_E_INVAL;
-  if (prior)
+  if (prior)   // in between, neither a key nor its error bound leaves fp32's range
     for (int e = 0; e < d.E; ++e)
-      if (!(prior[e] > 0.0f) || !isfinite(prior[e])) return MASKMOE_E_INVAL;
+      if (!(prior[e] >= 0x1p-100f && prior[e] <= 0x1p100f)) return MASKMOE_E_INVAL;
   if (d.T > 0 && (!logits || !topk_idx || !topk_gate)) return MASKMOE_E_INVAL;
   if (!aligned(logits, 4) || !aligned(bias, 4) || !aligned(topk_idx, 4) || !aligned(topk_gate, 4) || !aligned(load, 4))
     return MASKMOE_E_INVAL;
@@ -84,7 +85,7 @@ int maskmoe_gate_backward(const maskmoe_gate_desc* desc, const float* logits, co
   const maskmoe_gate_desc& d = *desc;
   if (d.T == 0) return MASKMOE_OK;
   if (!logits || !topk_idx || !d_gate || !d_logits) return MASKMOE_E_INVAL;
-  if (!aligned(logits, 4) || !aligned(topk_idx, 4) || !aligned(d_gate, 4) || !aligned(d_logits, 4))
+  if (!aligned(logits, 4) || !aligned(topk_idx, 4) || !aligned(d_gate, 4) || !aligned(d_logits, 4) || d_logits == logits)
     return MASKMOE_E_INVAL;
   const maskmoe::GateBwdArgs a{logits, topk_idx, d_gate, d_logits, d.T, d.E, d.K, d.score, d.renorm, d.scale};
   return hip_status(maskmoe::launch_gate_backward(a, stream));

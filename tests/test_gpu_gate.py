@@ -116,6 +116,19 @@ def test_infinities_nan_and_rows_without_experts(E, score):
             assert (idx == -1).all() and (gate == 0).all()
 
 
+@pytest.mark.parametrize("score", [G.SOFTMAX, G.SIGMOID])
+@pytest.mark.parametrize("E", [32, 256])
+def test_largest_and_smallest_priors_and_biases(E, score):
+    g = np.random.default_rng(E)
+    z, _ = make(60, E, E, {}, score)
+    low = (2.0 ** -100 * g.uniform(1, 2, E)).astype(np.float32)
+    high = (2.0 ** 100 * g.uniform(0.5, 1, E)).astype(np.float32)
+    for prior in (low, high, np.where(g.random(E) < 0.5, low, high)):
+        check(z, 6, score, prior=prior)
+        check(z, 6, score, prior=prior, bias=np.where(g.random(E) < 0.1, 2.0 ** 100, -1.0).astype(np.float32), n_group=8,
+              topk_group=4, group_rule=G.GROUP_SUM2)
+
+
 def check_special(z, K, score, **kw):
     """As check, with the gates' bound by the row's own finite range."""
     idx, gate, load = run(z, K, score, **kw)
@@ -176,6 +189,32 @@ def test_many_tokens_and_unaligned_rows():
     assert np.array_equal(a[0][::97].cpu().numpy(), io)
     assert int(a[2].sum()) == 20011 * 6
     assert torch.equal(a[2], torch.bincount(a[0].reshape(-1).long(), minlength=64).int())
+
+
+@pytest.mark.parametrize("score", [G.SOFTMAX, G.SIGMOID])
+@pytest.mark.parametrize("E,K,ng,tg", [(65, 12, 5, 3), (100, 10, 10, 5), (160, 6, 8, 3), (256, 8, 8, 4), (256, 16, 1, 1),
+                                       (256, 11, 1, 1), (255, 16, 51, 40), (256, 16, 128, 12)])
+def test_many_tokens_above_64_experts(E, K, ng, tg, score):
+    """Several tokens of a wavefront ranked at once, the last ones fewer: as in batches too small for that, and as
+    the oracle for a sample and the last rows. Rows without a finite logit, and rows of equal ones, among them."""
+    T = 9001
+    for i, rule in enumerate((RULES[0], RULES[3], RULES[5])):
+        say(f"gate T={T} E={E} K={K} groups {ng}/{tg} score {score} rule {i}")
+        z, kw = make(T, E, E + K + i, rule, score)
+        z[5::1000] = -np.inf
+        z[6::1000, E // 4:] = np.nan
+        z[7::1000] = 0.25
+        kw.update(n_group=ng, topk_group=tg)
+        idx, gate, load = run(z, K, score, **kw)
+        parts = [run(z[at:at + 4000], K, score, **kw) for at in (0, 4000, 8000)]
+        assert np.array_equal(idx, np.concatenate([p[0] for p in parts]))
+        assert np.array_equal(gate, np.concatenate([p[1] for p in parts]))
+        assert np.array_equal(load, sum(p[2] for p in parts))
+        pick = np.unique(np.r_[np.arange(0, T, 211), 1005:1008, T - 5:T])
+        io, go, _ = G.forward(z[pick], K, score, **kw)
+        assert np.array_equal(idx[pick], io)
+        fin = np.where(np.isfinite(z), z, 0)
+        assert (np.abs(gate[pick] - go) <= (fin.max() - fin.min() + 16) * U * np.abs(go) + 1e-37).all()
 
 
 def test_captured_and_replayed_with_other_work():

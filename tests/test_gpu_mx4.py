@@ -105,6 +105,20 @@ def test_experts(T, d, F, E, K, ns, pad, act):
         assert (y[T - pad:] == 0).all()
 
 
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T", [1, 16, 17, 40])
+def test_most_experts_entries_and_shared_experts(T, act):
+    """E = 256, K = 16 and 8 shared experts; then no token with an expert, with and without shared ones."""
+    say(f"mx4 limits T={T} act={act}")
+    x, wq, dev, idx, gate = make(T, 64, 64, 256, 16, 8, T)
+    idx = np.random.default_rng(T).permuted(np.tile(np.arange(256, dtype=np.int32), (T, 1)), axis=1)[:, :16].copy()
+    check(x, wq, dev, idx, gate, 8, act)
+    idx[:] = -1
+    check(x, wq, dev, idx, gate, 8, act)
+    routed = [t[:256].contiguous() for t in dev]
+    assert (call(x, routed, idx, gate, 0, act) == 0).all()
+
+
 # the same with enough rows and columns that 256 x 256 tiles cover the chip (the last: with MX4 activations alone)
 WIDE = [(2100, 64, 4096, 1, 1, 0, 0), (900, 192, 4160, 2, 2, 1, 37), (700, 320, 4160, 3, 2, 1, 0), (1500, 448, 4160, 2, 1, 0, 1),
         (210, 128, 4160, 16, 2, 0, 5)]

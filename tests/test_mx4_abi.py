@@ -58,6 +58,25 @@ def test_gate_rejects_pointers_and_priors():
     assert fwd(gate_desc(T=0), logits=None, idx=None, gate=None) == L.OK
 
 
+def test_gate_rejects_more_tokens_than_it_counts_and_gradients_in_place():
+    d = gate_desc(T=(1 << 30) + 1, E=1, K=1)
+    assert fwd(d) == L.E_UNSUPPORTED and bwd(d, out=FAKE + 64) == L.E_UNSUPPORTED
+    assert bwd(gate_desc(), logits=FAKE, out=FAKE) == L.E_INVAL
+
+
+@pytest.mark.parametrize("v", [2.0 ** -101, 2.0 ** 101])
+def test_gate_rejects_priors_that_leave_the_range_of_keys(v):
+    p = np.ones(64, np.float32)
+    p[5] = v
+    assert fwd(gate_desc(), prior=p.ctypes.data_as(ctypes.c_void_p)) == L.E_INVAL
+
+
+def test_experts_mx4_rejects_launches_above_the_limit():
+    for T, want in ((16, L.E_UNSUPPORTED), (17, L.E_WORKSPACE)):
+        d = L.make_desc(T=T, d=64, E=256, K=16, F=1 << 21, n_shared=0)
+        assert experts(d, ws=None) == want
+
+
 @pytest.mark.parametrize("fn", ["maskmoe_mx4_quantize", "maskmoe_mx4_dequantize"])
 def test_mx4_conversion_rejects(fn):
     f = getattr(L.load(), fn)
