@@ -68,8 +68,9 @@ hipError_t launch_mx4_few(const Mx4Params& p, hipStream_t stream);
 // `splits` parts, each with its own rows of o.
 constexpr int kMx4BatchRows = 64, kMx4BatchSplits = 8, kMx4BatchSplitRows = 8192;
 hipError_t launch_mx4_batch(const Mx4Params& p, int max_tiles, int splits, hipStream_t stream);
-// Many rows per expert (mx4_tile.hip): both products on 256 x 256 tiles, the permutation in tiles of kMx4TileRows.
-constexpr int kMx4TileRows = 256;
+// Many rows per expert (mx4_tile.hip): both products on tiles of 256 weight rows, the permutation in tiles of
+// mx4_tile_rows rows.
+constexpr int mx4_tile_rows(bool mx_act) { return mx_act ? 128 : 256; }
 hipError_t launch_mx4_wide(const Mx4Params& p, int max_tiles, hipStream_t stream);
 
 struct Mx4Layout {         // byte offsets into the workspace

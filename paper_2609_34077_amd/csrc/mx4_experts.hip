@@ -58,35 +58,62 @@ __global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p
 }
 
 // y = sum of the gate-weighted expert outputs (each the sum of its parts) in entry order, fp32, rounded once; a thread
-// per 4 columns. OB: expert outputs in bf16. Bound by their bytes (268 MB in fp32, 4096 tokens of the
-// DeepSeek-shaped layer: 70 us).
+// per 16 bytes of a row. OB: expert outputs in bf16. Bound by their bytes, with the loads of U entries in flight
+// (DeepSeek-shaped layer, 4096 tokens, 151 MB: 25 us, one entry at a time 40).
 template <bool OB>
 __global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p, int splits) {
+  constexpr int COLS = OB ? 8 : 4, U = 4;
   const Mx4Args& a = p.a;
-  const int KS = a.K + a.n_shared, c4 = a.d / 4;
+  const int KS = a.K + a.n_shared, cn = a.d / COLS;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= static_cast<int64_t>(a.T) * c4) return;
-  const int t = static_cast<int>(i / c4), c = static_cast<int>(i % c4);
-  f32x4 s = {0, 0, 0, 0};
-  for (int k = 0; k < KS; ++k) {
-    const int j = t * KS + k;
-    if (static_cast<uint32_t>(p.idx[j]) >= static_cast<uint32_t>(p.G)) continue;
-    const float g = p.gate[j];
-    const size_t at = static_cast<size_t>(p.pb.inv[j]) * c4 + c;
-    f32x4 o;
-    if constexpr (OB) {
-      const uint2 b = static_cast<const uint2*>(p.o)[at];
-      o = f32x4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16),
-                __uint_as_float(b.y & 0xffff0000u)};
-    } else {
-      const f32x4* src = static_cast<const f32x4*>(p.o) + at;
-      o = src[0];
-      for (int z = 1; z < splits; ++z) o += src[static_cast<size_t>(z) * a.T * KS * c4];
-    }
+  if (i >= static_cast<int64_t>(a.T) * cn) return;
+  const int t = static_cast<int>(i / cn), c = static_cast<int>(i % cn);
+  const u32x4* src = static_cast<const u32x4*>(p.o) + c;
+  const size_t part = static_cast<size_t>(a.T) * KS * cn;
+  float s[COLS];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) s[q] += g * o[q];
+  for (int q = 0; q < COLS; ++q) s[q] = 0.0f;
+  for (int k0 = 0; k0 < KS; k0 += U) {
+    bool live[U];
+    float g[U];
+    size_t at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = t * KS + min(k0 + u, KS - 1);
+      live[u] = k0 + u < KS && static_cast<uint32_t>(p.idx[j]) < static_cast<uint32_t>(p.G);
+      g[u] = p.gate[j];
+      at[u] = static_cast<size_t>(p.pb.inv[j]) * cn;
+    }
+    u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (live[u]) v[u] = src[at[u]];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!live[u]) continue;
+      if constexpr (OB) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t w = v[u][q];
+          s[2 * q] += g[u] * __uint_as_float(w << 16);
+          s[2 * q + 1] += g[u] * __uint_as_float(w & 0xffff0000u);
+        }
+      } else {
+        f32x4 o = __builtin_bit_cast(f32x4, v[u]);
+        for (int z = 1; z < splits; ++z) o += __builtin_bit_cast(f32x4, src[at[u] + z * part]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s[q] += g[u] * o[q];
+      }
+    }
   }
-  reinterpret_cast<uint2*>(a.y)[i] = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
+  if constexpr (OB) {
+    u32x4 y;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = f32x2_to_bf16x2(s[2 * q], s[2 * q + 1]);
+    reinterpret_cast<u32x4*>(a.y)[i] = y;
+  } else {
+    reinterpret_cast<uint2*>(a.y)[i] = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
+  }
 }
 
 // Whether the wide tiles are taken: by the rows per expert from which they are faster, and their number, which must
@@ -94,10 +121,11 @@ __global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p
 //   bf16: the batch tiles' weight stream hides the widening, which the wide ones pay with the products; whole call,
 //     batch / wide: Mixtral-shaped 450 tokens (112 rows an expert) 336 / 429 us, 1000 (250) 666 / 697, 1500 (375)
 //     927 / 907; DeepSeek-shaped 1600 (194 with the shared experts) 297 / 323, 2500 (303) 420 / 395.
-//   MX4: Mixtral-shaped 64 tokens (16) 150 / 159, 128 (32) 173 / 165; DeepSeek-shaped 100 (12) 91 / 96, 333 (40) 112 / 108.
+//   MX4: Mixtral-shaped 40 tokens (10 rows) 142 / 156, 64 (16) 149 / 157, 90 (22) 158 / 159, 128 (32) 173 / 163;
+//     DeepSeek-shaped 100 (12) 91 / 88, 200 (24) 103 / 90.
 bool mx4_takes_wide(int rows, int G, int F, bool mx_act) {
-  const int64_t tiles = (static_cast<int64_t>(rows) / kMx4TileRows + G / 2) * ((2 * F + 255) / 256);
-  return rows >= (mx_act ? 25 : 280) * G && tiles >= 256;
+  const int64_t tiles = (static_cast<int64_t>(rows) / mx4_tile_rows(mx_act) + G / 2) * ((2 * F + 255) / 256);
+  return rows >= (mx_act ? 22 : 280) * G && tiles >= 256;
 }
 
 }  // namespace
@@ -172,7 +200,7 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
     }
   }
   const bool wide = mx4_takes_wide(rows, p.G, a.F, a.mx_act);
-  const int tile_rows = wide ? kMx4TileRows : kMx4BatchRows;
+  const int tile_rows = wide ? mx4_tile_rows(a.mx_act) : kMx4BatchRows;
   err = launch_permute(p.idx, a.T, KS, p.G, 0, tile_rows, p.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
   if (err != hipSuccess) return err;
   const int max_tiles = std::min(rows, rows / tile_rows + p.G);
@@ -180,7 +208,7 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   if (wide) {
     // With MX4 activations the bytes of fp32 outputs take as long as the products that make them; in bf16 (the layer's
     // type; y is off by 2.3e-3 instead of 1.7e-3 then) they take half: DeepSeek-shaped layer, 4096 tokens, down and
-    // combine 121 + 70 -> 112 + 40 us. With bf16 activations, whose h is rounded to bf16 already, they stay fp32.
+    // combine 121 + 70 -> 112 + 40 us (the latter 25 since, see there). With bf16 activations, whose h is rounded to bf16 already, they stay fp32.
     p.o_bf16 = a.mx_act;
     err = launch_mx4_wide(p, max_tiles, stream);
   } else {
@@ -192,7 +220,7 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
     err = launch_mx4_batch(p, max_tiles, splits, stream);
   }
   if (err != hipSuccess) return err;
-  const int64_t cn = static_cast<int64_t>(a.T) * a.d / 4;
+  const int64_t cn = static_cast<int64_t>(a.T) * a.d / (p.o_bf16 ? 8 : 4);
   const dim3 cgrid(static_cast<unsigned>((cn + kThreads - 1) / kThreads));
   if (p.o_bf16) hipLaunchKernelGGL(mx4_combine_kernel<true>, cgrid, dim3(kThreads), 0, stream, p, splits);
   else hipLaunchKernelGGL(mx4_combine_kernel<false>, cgrid, dim3(kThreads), 0, stream, p, splits);

@@ -1,20 +1,22 @@
-// Both products of experts on MX4 weights for many rows per expert: 256 weight rows x 256 token rows a
-// workgroup on the matrix units' 16 x 16 tiles.
+// Both products of experts on MX4 weights for many rows per expert: 256 weight rows a workgroup on the matrix
+// units' 16 x 16 tiles.
 //
-// Eight wavefronts, WN of them side by side along the tokens: wave w owns the weight fragments (16 rows each) of
-// w / WN and the token fragments w % WN, + WN, .., so that a last tile with few rows leaves every wavefront equally
-// little to multiply. Weight rows
-// are the instruction's row operand: a lane holds four neighbouring output columns of one token, and the gate and
-// up rows of a column, which alternate in the packed layout, meet in one lane.
-//   bf16 activations  stages of 128 columns. Weights go from global memory to the registers of the two wavefronts
-//                     that share them (4 bits a value: a quarter of the bytes that LDS would have to pass), a stage
-//                     ahead, and are widened to bf16 there, beside the products (v_mfma_f32_16x16x32_bf16); tokens
-//                     go straight to LDS, double-buffered (2 x 64 KB). Widening two values takes about as long as a
-//                     product (16 cycles): with 8 x 4 fragments a wavefront (WN 4) it was as much work as they, 4850 us for the
-//                     Mixtral-shaped layer of 8192 tokens instead of 4330 with 4 x 8 (WN 2).
-//   MX4 activations   stages of 128 columns on v_mfma_scale_f32_16x16x128_f8f6f4; both operands and their scales go
-//                     straight to LDS, three stages ahead (4 x 32 KB and 2 x 8 KB). 8 x 4 fragments (DeepSeek-shaped layer, 4096
-//                     tokens: 362 us, with 4 x 8 398).
+// Wavefronts lie two side by side along the tokens: wave w owns the weight fragments (16 rows each) of w / 2 and the
+// token fragments w % 2, + 2, .., so that a last tile with few rows leaves every wavefront equally little to multiply.
+// Weight rows are the instruction's row operand: a lane holds four neighbouring output columns of one token, and the
+// gate and up rows of a column, which alternate in the packed layout, meet in one lane.
+//   bf16 activations  256 token rows, eight wavefronts of 4 x 8 fragments, stages of 128 columns. Weights go from global
+//                     memory to the registers of the two wavefronts that share them (4 bits a value: a quarter of the
+//                     bytes that LDS would have to pass), a stage ahead, and are widened to bf16 there, beside the
+//                     products (v_mfma_f32_16x16x32_bf16); tokens go straight to LDS, double-buffered (2 x 64 KB).
+//                     Widening two values takes about as long as a product (16 cycles): with 8 x 4 fragments it was as
+//                     much work as they, 4850 us for the Mixtral-shaped layer of 8192 tokens instead of 4330.
+//   MX4 activations   128 token rows, four wavefronts of 8 x 4 fragments, stages of 128 columns on
+//                     v_mfma_scale_f32_16x16x128_f8f6f4; both operands and their scales go straight to LDS, two stages
+//                     ahead (3 x 24 KB and 6 KB), two workgroups a CU, whose starts and ends overlap. Workgroups of
+//                     256 rows and eight wavefronts were slower for few steps and rows (both products, DeepSeek-shaped
+//                     1200 / 4096 / 8192 tokens 128 / 290 / 479 us, now 106 / 285 / 460) and faster for many
+//                     (Mixtral-shaped 1500 / 8192 tokens 373 / 1589 us, now 393 / 1632). 3.6 PFLOP/s at the last.
 // Token loads are buffer loads: rows past the tile's end and columns past a row's end read as zeros.
 
 #include "gemm_tile.hpp"
@@ -24,10 +26,10 @@
 namespace maskmoe {
 namespace {
 
-constexpr int kThreads = 512;
 constexpr int kFrags = 16;               // weight fragments of a tile
+constexpr int kWN = 2;                   // wavefronts side by side along the tokens
 template <bool MX>
-constexpr int kWN = MX ? 4 : 2;          // wavefronts side by side along the tokens
+constexpr int kThreads = MX ? 256 : 512;
 constexpr uint32_t kNoRow = 0xfffffff0u; // past any operand (fewer than 2^32 - 256 bytes)
 
 // 16 bytes per lane at rsrc + voff + soff straight into LDS at m0v + 16 * lane; zeros past the buffer's end.
@@ -36,6 +38,8 @@ __device__ __forceinline__ void dma16s(uint32_t m0v, i32x4 rsrc, uint32_t voff, 
                "s"(soff)
                : "memory", "m0");
 }
+
+constexpr uint32_t kStage = 24576;       // of MX4 operands in LDS
 
 struct Tile {
   int g, row0, nrows, f0;   // expert, its first row and rows here, first weight fragment
@@ -46,7 +50,7 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
   const Mx4Args& a = p.a;
   const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  constexpr int WN = kWN<MX>, kWF = 2 * WN;   // kWF: a wavefront's weight fragments
+  constexpr int WN = kWN, kWF = MX ? 8 : 4;   // kWF: a wavefront's weight fragments
   const int wm = wave / WN, wn = wave % WN;
   const int C = EPI == 0 ? a.d : a.F, R = EPI == 0 ? 2 * a.F : a.d;
   const int steps = mx4_steps(C), quads = mx4_quads(C);
@@ -145,10 +149,10 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     }
     wait_vmcnt<0>();
   } else {
-    // A stage is one step: 16 fragments of weights (16 KB, operand order), 256 rows x 64 bytes of tokens (16 KB; the
-    // piece at slot s of row r is logical piece s ^ (r / 4 & 3)). Four stages; the scales of four steps, a dword per
-    // fragment lane and token block, in two buffers of 8 KB behind them. Every wavefront issues the same number of
-    // loads a step (rows past the end read as zeros), so that it can wait for the oldest alone.
+    // A stage is one step: 16 fragments of weights (16 KB, operand order), 128 rows x 64 bytes of tokens (8 KB; the
+    // piece at slot s of row r is logical piece s ^ (r / 4 & 3)). Three stages; the scales of four steps, a dword per
+    // fragment lane and token block, in 6 KB behind them. Every wavefront issues the same number of loads a step (rows
+    // past the end read as zeros), so that it can wait for the oldest alone.
     uint32_t off[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -156,42 +160,40 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
       off[i] = r < t.nrows ? source(r) * row_bytes + ((lane & 3) ^ (r >> 2 & 3)) * 16 : kNoRow;
     }
     const i32x4 wr = buffer_rsrc(wc, static_cast<uint32_t>(R / 16) * steps * 1024);
+    uint32_t in = 0;   // where the next stage goes
     auto dma = [&](int ahead) {
       const int s = min(ahead, steps - 1);   // past the end: a stage that nothing reads again
-      const uint32_t base = lds0 + (ahead & 3) * 32768;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int f = min(t.f0 + 2 * wave + i, R / 16 - 1);
-        dma16s(base + (2 * wave + i) * 1024, wr, lane * 16, (static_cast<uint32_t>(f) * steps + s) * 1024);
+      for (int i = 0; i < 4; ++i) {
+        const int f = min(t.f0 + 4 * wave + i, R / 16 - 1);
+        dma16s(lds0 + in + (4 * wave + i) * 1024, wr, lane * 16, (static_cast<uint32_t>(f) * steps + s) * 1024);
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) dma16s(base + 16384 + (2 * wave + i) * 1024, xr, off[i], static_cast<uint32_t>(s) * 64);
+      for (int i = 0; i < 2; ++i) dma16s(lds0 + in + 16384 + (2 * wave + i) * 1024, xr, off[i], static_cast<uint32_t>(s) * 64);
+      in = in == 2 * kStage ? 0 : in + kStage;
     };
-    // scales: waves 0 to 3 four fragments each, 4 to 7 64 token rows each
-    const bool of_w = wave < 4;
-    const i32x4 scr = of_w ? buffer_rsrc(wsc, static_cast<uint32_t>(R / 16) * quads * 256)
-                           : buffer_rsrc(EPI == 0 ? p.xs : p.hs, static_cast<uint32_t>(src_rows) * quads * 16);
-    uint32_t sc_off, sc_step;
-    if (of_w) {
-      sc_off = static_cast<uint32_t>(min(t.f0 + 4 * wave + (lane >> 4), R / 16 - 1)) * quads * 256 + (lane & 15) * 16;
-      sc_step = 256;
-    } else {
-      const int r = 64 * (wave - 4) + lane;
-      sc_off = r < t.nrows ? source(r) * quads * 16 : kNoRow;
-      sc_step = 16;
-    }
-    auto dma_scales = [&](int q) {
-      dma16s(lds0 + 131072 + (q & 1) * 8192 + wave * 1024, scr, sc_off, min(q, quads - 1) * sc_step);
+    // scales: a wavefront four fragments and 64 token rows (both pairs of wavefronts the same ones)
+    const i32x4 wscr = buffer_rsrc(wsc, static_cast<uint32_t>(R / 16) * quads * 256);
+    const i32x4 xscr = buffer_rsrc(EPI == 0 ? p.xs : p.hs, static_cast<uint32_t>(src_rows) * quads * 16);
+    const uint32_t wsc_off = static_cast<uint32_t>(min(t.f0 + 4 * wave + (lane >> 4), R / 16 - 1)) * quads * 256 + (lane & 15) * 16;
+    const int sr_row = 64 * (wave & 1) + lane;
+    const uint32_t xsc_off = sr_row < t.nrows ? source(sr_row) * quads * 16 : kNoRow;
+    auto dma_scales = [&](int ahead) {
+      const uint32_t q = min(ahead, quads - 1);
+      dma16s(lds0 + 3 * kStage + wave * 1024, wscr, wsc_off, q * 256);
+      dma16s(lds0 + 3 * kStage + 4096 + (wave & 1) * 1024, xscr, xsc_off, q * 16);
     };
     // the last step of a C of an odd number of 64 columns: its upper blocks have no token scales
     const int cut = C % kMxStep != 0 ? steps - 1 : -1;
     uint32_t ws[kWF], ts[NL];
+    int out = 0;   // the stage multiplied, in 16 bytes
     auto compute = [&](auto sub_c, int s) {
       constexpr int S = decltype(sub_c)::value;   // step within the quad
-      const u32x4* wa = lds + S * 2048 + kWF * wm * 64 + lane;
-      const u32x4* xa = lds + S * 2048 + 1024 + (16 * wn + l16) * 4 + (lg ^ (l16 >> 2));
+      const u32x4* wa = lds + out + kWF * wm * 64 + lane;
+      const u32x4* xa = lds + out + 1024 + (16 * wn + l16) * 4 + (lg ^ (l16 >> 2));
+      out = out == 2 * kStage / 16 ? 0 : out + kStage / 16;
       if constexpr (S == 0) {
-        const uint32_t* sc = reinterpret_cast<const uint32_t*>(lds + 8192 + (s >> 2 & 1) * 512);
+        const uint32_t* sc = reinterpret_cast<const uint32_t*>(lds + 3 * kStage / 16);
 #pragma unroll
         for (int i = 0; i < kWF; ++i) ws[i] = sc[(kWF * wm + i) * 64 + lane];
 #pragma unroll
@@ -213,11 +215,11 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     };
     auto step = [&](auto sub_c, int s) {
       constexpr int S = decltype(sub_c)::value;
-      // behind step s's loads are those of two more steps, and a quad's scales where they were issued since
-      wait_vmcnt<S == 0 ? 8 : 9>();
+      // behind step s's loads are the next step's, and in S 2 the scales issued between them
+      wait_vmcnt<S == 2 ? 8 : 6>();
       lds_sync();
-      dma(s + 3);
-      if constexpr (S == 0) dma_scales((s >> 2) + 1);
+      if constexpr (S == 1) dma_scales((s >> 2) + 1);   // every wavefront has read this quad's
+      dma(s + 2);
       __builtin_amdgcn_sched_barrier(0);
       if (s < steps) compute(sub_c, s);
       __builtin_amdgcn_sched_barrier(0);
@@ -225,7 +227,6 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     dma_scales(0);
     dma(0);
     dma(1);
-    dma(2);
     for (int s = 0; s < steps; s += 4) {
       step(std::integral_constant<int, 0>{}, s);
       step(std::integral_constant<int, 1>{}, s + 1);
@@ -288,8 +289,9 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
 }
 
 template <bool MX, int EPI>
-__global__ __launch_bounds__(kThreads, 2) void mx4_wide_kernel(const Mx4Params p) {
-  __shared__ u32x4 lds[MX ? 9216 : 8192];
+__global__ __launch_bounds__(kThreads<MX>, 2) void mx4_wide_kernel(const Mx4Params p) {
+  __shared__ u32x4 lds[MX ? (3 * kStage + 6144) / 16 : 8192];
+  constexpr int kRows = mx4_tile_rows(MX);
   const int R = EPI == 0 ? 2 * p.a.F : p.a.d;
   const int wt = (R / 16 + kFrags - 1) / kFrags;   // weight tiles
   const int live = p.pb.tile_off[p.G] * wt;
@@ -307,11 +309,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_wide_kernel(const Mx4Params p
   }
   Tile t;
   t.g = g;
-  t.row0 = p.pb.offsets[g] + (mt - p.pb.tile_off[g]) * kMx4TileRows;
-  t.nrows = min(kMx4TileRows, p.pb.offsets[g + 1] - t.row0);
+  t.row0 = p.pb.offsets[g] + (mt - p.pb.tile_off[g]) * kRows;
+  t.nrows = min(kRows, p.pb.offsets[g + 1] - t.row0);
   t.f0 = nt * kFrags;
-  const int quarters = __builtin_amdgcn_readfirstlane((t.nrows + 63) / 64);   // of the tile's rows
-  constexpr int Q = 4 / kWN<MX>;   // a wavefront's token fragments per quarter
+  const int quarters = __builtin_amdgcn_readfirstlane((t.nrows + kRows / 4 - 1) / (kRows / 4));   // of the tile's rows
+  constexpr int Q = kRows / 4 / 16 / kWN;   // a wavefront's token fragments per quarter
   if (quarters == 4) run_tile<MX, EPI, 4 * Q>(p, t, lds);
   else if (quarters == 3) run_tile<MX, EPI, 3 * Q>(p, t, lds);
   else if (quarters == 2) run_tile<MX, EPI, 2 * Q>(p, t, lds);
@@ -321,10 +323,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_wide_kernel(const Mx4Params p
 template <bool MX>
 hipError_t launch(const Mx4Params& p, int max_tiles, hipStream_t stream) {
   auto grid = [&](int R) { return dim3(static_cast<unsigned>(max_tiles) * ((R / 16 + kFrags - 1) / kFrags)); };
-  hipLaunchKernelGGL((mx4_wide_kernel<MX, 0>), grid(2 * p.a.F), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((mx4_wide_kernel<MX, 0>), grid(2 * p.a.F), dim3(kThreads<MX>), 0, stream, p);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((mx4_wide_kernel<MX, 1>), grid(p.a.d), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((mx4_wide_kernel<MX, 1>), grid(p.a.d), dim3(kThreads<MX>), 0, stream, p);
   return hipGetLastError();
 }
 
