@@ -217,6 +217,24 @@ def test_many_tokens_above_64_experts(E, K, ng, tg, score):
         assert (np.abs(gate[pick] - go) <= (fin.max() - fin.min() + 16) * U * np.abs(go) + 1e-37).all()
 
 
+def test_logits_past_32_bit_offsets():
+    """More than 2^32 bytes of logits, forward and both gradients: the last rows as they are alone."""
+    T, E, K, last = (1 << 24) + 77, 72, 6, 300
+    say(f"gate T={T} E={E}")
+    z = torch.randn((1 << 16, E), device="cuda").repeat(257, 1)[:T].contiguous()
+    z[-last:] = torch.randn((last, E), device="cuda")
+    idx, gate, load = L.maskmoe_gate_forward(z, K, L.SCORE_SIGMOID, with_load=True)
+    tail = z[-last:].contiguous()
+    i, g, _ = L.maskmoe_gate_forward(tail, K, L.SCORE_SIGMOID)
+    assert torch.equal(idx[-last:], i) and torch.equal(gate[-last:], g)
+    assert int(load.sum()) == T * K and torch.equal(idx[: 1 << 16], idx[1 << 23:(1 << 23) + (1 << 16)])
+    for score, renorm in ((L.SCORE_SIGMOID, True), (L.SCORE_SOFTMAX, False)):
+        dz = L.maskmoe_gate_backward(z, idx, gate, score, renorm=renorm)
+        assert torch.equal(dz[-last:], L.maskmoe_gate_backward(tail, i, g, score, renorm=renorm))
+        assert torch.equal(dz[: 1 << 16], dz[1 << 23:(1 << 23) + (1 << 16)])
+        del dz
+
+
 def test_captured_and_replayed_with_other_work():
     say("gate graph")
     z, kw = make(3000, 256, 9, dict(bias=True), G.SIGMOID)

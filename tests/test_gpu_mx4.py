@@ -268,6 +268,47 @@ def test_gate_to_experts():
     assert (yd - ym).abs().max() <= 2e-2 * yd.abs().max()
 
 
+def test_blocks_past_32_bit_offsets():
+    """More than 2^32 elements: the rows at the end are converted as they are alone."""
+    rows, cols = (1 << 17) + 3, 1 << 15
+    say(f"mx4 quantize {rows} x {cols}")
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    x[:] = torch.randn(cols, device="cuda").bfloat16()
+    x[-3:] = torch.randn((3, cols), device="cuda").bfloat16()
+    codes, scales = L.maskmoe_mx4_quantize(x)
+    c, e = L.maskmoe_mx4_quantize(x[-3:].contiguous())
+    assert torch.equal(codes[-3:], c) and torch.equal(scales[-3:], e)
+    assert torch.equal(codes[: rows - 3], codes[:1].expand(rows - 3, -1))
+    back = L.maskmoe_mx4_dequantize(codes, scales, torch.bfloat16)
+    assert torch.equal(back[-3:], L.maskmoe_mx4_dequantize(c, e, torch.bfloat16))
+    assert torch.equal(back[: rows - 3], back[:1].expand(rows - 3, -1))
+
+
+def test_experts_past_32_bit_offsets():
+    """Weights of more than 2^32 bytes: the last of 256 experts give the bits that the first ones give, which are
+    copies of them (with fewer experts in all, a reduction may be split into other parts)."""
+    E, d, F, at = 256, 4096, 4096, 250
+    say("mx4 experts past 4 GiB")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    dev = []
+    for shape in ((E, 2 * F, d), (E, d, F)):
+        dev += [torch.randint(0, 256, shape[:2] + (shape[2] // 2,), dtype=torch.uint8, generator=g, device="cuda"),
+                torch.randint(118, 121, shape[:2] + (shape[2] // 32,), dtype=torch.uint8, generator=g, device="cuda")]
+    for t in dev:
+        t[:E - at] = t[at:]
+    packed = L.maskmoe_mx4_pack_experts(*dev)
+    del dev
+    # few tokens; a batch; wide tiles (rows per expert of all: 6000 / 256 = 23.4)
+    for T, act in ((1, L.ACT_BF16), (5, L.ACT_MX4), (40, L.ACT_BF16), (40, L.ACT_MX4), (6000, L.ACT_MX4)):
+        say(f"  T={T} act={act}")
+        x = torch.randn((T, d), generator=g, device="cuda").bfloat16()
+        idx = torch.randint(at, E, (T, 1), dtype=torch.int32, generator=g, device="cuda")
+        gate = torch.rand((T, 1), generator=g, device="cuda")
+        y = L.maskmoe_experts_forward_mx4(x, idx, gate, packed, act=act)
+        assert y.float().abs().max() > 0 and y.isfinite().all()
+        assert torch.equal(y, L.maskmoe_experts_forward_mx4(x, idx - at, gate, packed, act=act))
+
+
 def test_python_refusals():
     x = torch.zeros((4, 64), device="cuda")
     for bad in (x[:, :48], x.half(), x.cpu(), x.t()):
