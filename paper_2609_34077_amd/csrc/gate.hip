@@ -391,8 +391,12 @@ __device__ __forceinline__ Row row_keys(const GateArgs& a, const LaneExperts<V>&
         ahead += o > lead || (o == lead && g < own) ? 1 : 0;
       }
       kept = ahead < a.topk_group && own < a.n_group;
-      if constexpr (KEYS == kByKey) {   // the last group kept and the first one left out
-        const float in = number(~seg_max<W>(kept ? ~lead : 0u)), out = number(seg_max<W>(kept ? kNone : lead));
+      if constexpr (KEYS == kByKey) {
+        // the last group kept and the first one left out; lanes past the last expert hold no group (a copy of the last
+        // one's score among those left out sent every row that keeps it to fp64: 65536 tokens x 24 experts in 2 groups
+        // 34 us instead of 17)
+        const float in = number(~seg_max<W>(kept ? ~lead : 0u));
+        const float out = number(seg_max<W>(kept || own >= a.n_group ? kNone : lead));
         r.close = in - out < 2.0f * r.tol;   // no group left out, or none with an expert: NaN, not close
       }
     }

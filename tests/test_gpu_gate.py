@@ -269,3 +269,50 @@ def test_python_refusals():
         L.maskmoe_gate_forward(z, 17, L.SCORE_SOFTMAX)
     with pytest.raises(ValueError):
         L.maskmoe_gate_backward(z, torch.zeros((4, 2), dtype=torch.int64, device="cuda"), z[:, :2].contiguous(), 0)
+
+
+def fastest(calls, reps=9, n=20):
+    """Shortest mean time (us) of n calls of each, the calls timed in turn."""
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    best = [float("inf")] * len(calls)
+    for f in calls:
+        f()
+    for _ in range(reps):
+        for i, f in enumerate(calls):
+            torch.cuda.synchronize()
+            start.record()
+            for _ in range(n):
+                f()
+            end.record()
+            end.synchronize()
+            best[i] = min(best[i], start.elapsed_time(end) / n * 1e3)
+    return best
+
+
+# groups of 3, 5, 6 or 7 lanes (V experts each: 1 up to 16 experts, 4 up to 64), with lanes past the last expert
+ODD_GROUPS = [(6, 2, 2, 1), (9, 3, 3, 2), (12, 2, 4, 1), (12, 4, 4, 2), (14, 3, 2, 1), (15, 4, 3, 2), (24, 4, 2, 1), (36, 6, 3, 2),
+              (40, 8, 2, 1), (48, 4, 4, 2), (56, 4, 2, 1), (60, 6, 5, 2), (60, 16, 5, 4)]
+
+
+@pytest.mark.parametrize("score", [G.SOFTMAX, G.SIGMOID])
+@pytest.mark.parametrize("E,K,ng,tg", ODD_GROUPS)
+def test_groups_of_odd_numbers_of_lanes(E, K, ng, tg, score):
+    for i, rule in enumerate(RULES):
+        say(f"gate odd groups E={E} K={K} groups {ng}/{tg} score {score} rule {i}")
+        z, kw = make((37, 200)[i % 2], E, 10 * E + i, rule, score)
+        check(z, K, score, n_group=ng, topk_group=tg, **kw)
+
+
+@pytest.mark.parametrize("score", [G.SOFTMAX, G.SIGMOID])
+@pytest.mark.parametrize("E,K,ng", [(24, 2, 2), (48, 4, 4), (60, 4, 5)])
+def test_keeping_the_last_group_costs_no_more_than_the_first(E, K, ng, score):
+    """The row's own work is the same whichever group leads; selecting every row again in fp64 takes 1.5 to 2.1
+    times as long."""
+    say(f"gate time of the last group E={E} groups {ng} score {score}")
+    z = torch.from_numpy(make(65536, E, E, {}, score)[0]).cuda()
+    bias = torch.zeros((2, E), device="cuda")
+    bias[0, : E // ng] = bias[1, E - E // ng:] = 1.0
+    calls = [lambda b=b: L.maskmoe_gate_forward(z, K, score, n_group=ng, topk_group=1, group_rule=L.GROUP_SUM2, bias=b)
+             for b in bias]
+    first, last = fastest(calls)
+    assert last <= 1.25 * first, (first, last)
