@@ -668,7 +668,7 @@ enum { MASKMOE_ACT_BF16 = 0, MASKMOE_ACT_MX4 = 1 };
  *  workspace   device, maskmoe_experts_mx4_workspace_bytes(desc) bytes, 256-byte aligned; contents on entry do not
  *              matter. Calls that may overlap, and graphs that may run at the same time, must not share it.
  *  Rounding: sums are fp32; h is rounded once to bf16 (ACT_BF16) or to MX4 blocks (ACT_MX4, as x is); expert outputs
- *  stay fp32 (ACT_MX4 with 22 rows per expert or more: rounded once to bf16); y is rounded once.
+ *  stay fp32; y is rounded once.
  *  Errors: E_INVAL for a desc outside its ranges, an unknown act, NULL or misaligned pointers, x == y; E_WORKSPACE;
  *  E_UNSUPPORTED for MASKMOE_F32, d or F not multiples of 64, T d, T (K + n_shared) F, T (K + n_shared) d or 2 F d
  *  at or above 2^31, or up to 16 tokens with T (K + n_shared) F at or above 2^29.

@@ -57,7 +57,7 @@ def silu(a):
 def experts(x, idx, gate, w_gate_up, w_down, n_shared, mx_act, u32=2.0 ** -24, half=2.0 ** -8):
     """y [T,d] of experts with weights w_gate_up [n,2F,d], w_down [n,d,F] (values; the last n_shared are shared)
     and a bound on |y' - y| for a computation with fp32 sums (u32: relative error of an addition), h rounded
-    to bf16 (half: half a bf16 step) or to MX4 blocks, expert outputs rounded to bf16 where mx_act, and y rounded to bf16.
+    to bf16 (half: half a bf16 step) or to MX4 blocks, and y rounded to bf16.
 
     The bound follows each rounding through the sums with absolute values: a sum of n products is off by at
     most n u32 times the sum of their magnitudes; SiLU has slope at most 1.1; MX4 elements of h that come within
@@ -101,7 +101,5 @@ def experts(x, idx, gate, w_gate_up, w_down, n_shared, mx_act, u32=2.0 ** -24, h
         o = h @ wd.T
         eo = eh @ np.abs(wd).T + (F + 8) * u32 * ((np.abs(h) + eh) @ np.abs(wd).T)
         np.add.at(y, t, g[:, None] * o)
-        if mx_act:
-            eo = eo + half * (np.abs(o) + eo)
         np.add.at(bound, t, np.abs(g)[:, None] * (eo + 32 * u32 * np.abs(o)))
     return y, bound + half * (np.abs(y) + bound)

@@ -52,8 +52,7 @@ struct Mx4Params {
                      // dword g of a quad holds the scales of columns 32 g .. of its four steps
   void* h;           // [rows, F] bf16, or codes
   uint8_t* hs;       // [rows, quads of F, 16]
-  void* o;           // [rows, d] fp32; bf16 where o_bf16
-  bool o_bf16;       // wide tiles with MX4 activations: expert outputs rounded once more (see mx4_experts.hip)
+  float* o;          // [rows, d] expert outputs, in as many parts as the down projection's reduction
   int G;             // E + n_shared
 };
 // Up to kMx4FewT tokens (mx4_few.hip): both products without prepare and permutation; p.o holds kMx4FewSplits x T rows.

@@ -171,7 +171,7 @@ __device__ __forceinline__ void run_job(const Mx4Params& p, const Job& t, u32x4*
     const bool ok = r < t.nrows;
     if constexpr (EPI == 1) {
       if (ok) {
-        f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p.o) + (t.out0 + r) * a.d + 16 * f + 4 * lg);
+        f32x4* o = reinterpret_cast<f32x4*>(p.o + (t.out0 + r) * a.d + 16 * f + 4 * lg);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[4 * i] = acc[i][n];
       }

@@ -58,21 +58,19 @@ __global__ __launch_bounds__(kThreads) void mx4_prepare_kernel(const Mx4Params p
 }
 
 // y = sum of the gate-weighted expert outputs (each the sum of its parts) in entry order, fp32, rounded once; a thread
-// per 16 bytes of a row. OB: expert outputs in bf16. Bound by their bytes, with the loads of U entries in flight
-// (DeepSeek-shaped layer, 4096 tokens, 151 MB: 25 us, one entry at a time 40).
-template <bool OB>
+// per four columns. Bound by their bytes, with the loads of U entries in flight (DeepSeek-shaped layer, 4096 tokens, 285 MB:
+// 50 us). Outputs in bf16 took half the time there and 30 us off the down projection, but left an error of half a bf16
+// step in every term of the sum: y was off by 2.3e-3 (relative, RMS) instead of the 1.7e-3 of its own rounding.
 __global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p, int splits) {
-  constexpr int COLS = OB ? 8 : 4, U = 4;
+  constexpr int U = 4;
   const Mx4Args& a = p.a;
-  const int KS = a.K + a.n_shared, cn = a.d / COLS;
+  const int KS = a.K + a.n_shared, c4 = a.d / 4;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= static_cast<int64_t>(a.T) * cn) return;
-  const int t = static_cast<int>(i / cn), c = static_cast<int>(i % cn);
-  const u32x4* src = static_cast<const u32x4*>(p.o) + c;
-  const size_t part = static_cast<size_t>(a.T) * KS * cn;
-  float s[COLS];
-#pragma unroll
-  for (int q = 0; q < COLS; ++q) s[q] = 0.0f;
+  if (i >= static_cast<int64_t>(a.T) * c4) return;
+  const int t = static_cast<int>(i / c4), c = static_cast<int>(i % c4);
+  const f32x4* src = reinterpret_cast<const f32x4*>(p.o) + c;
+  const size_t part = static_cast<size_t>(a.T) * KS * c4;
+  f32x4 s = {0, 0, 0, 0};
   for (int k0 = 0; k0 < KS; k0 += U) {
     bool live[U];
     float g[U];
@@ -82,47 +80,33 @@ __global__ __launch_bounds__(kThreads) void mx4_combine_kernel(const Mx4Params p
       const int j = t * KS + min(k0 + u, KS - 1);
       live[u] = k0 + u < KS && static_cast<uint32_t>(p.idx[j]) < static_cast<uint32_t>(p.G);
       g[u] = p.gate[j];
-      at[u] = static_cast<size_t>(p.pb.inv[j]) * cn;
+      at[u] = static_cast<size_t>(p.pb.inv[j]) * c4;
     }
-    u32x4 v[U];
+    f32x4 o[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (live[u]) v[u] = src[at[u]];
+      if (live[u]) o[u] = src[at[u]];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (!live[u]) continue;
-      if constexpr (OB) {
+      for (int z = 1; z < splits; ++z) o[u] += src[at[u] + z * part];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t w = v[u][q];
-          s[2 * q] += g[u] * __uint_as_float(w << 16);
-          s[2 * q + 1] += g[u] * __uint_as_float(w & 0xffff0000u);
-        }
-      } else {
-        f32x4 o = __builtin_bit_cast(f32x4, v[u]);
-        for (int z = 1; z < splits; ++z) o += __builtin_bit_cast(f32x4, src[at[u] + z * part]);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) s[q] += g[u] * o[q];
-      }
+      for (int q = 0; q < 4; ++q) s[q] += g[u] * o[u][q];
     }
   }
-  if constexpr (OB) {
-    u32x4 y;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) y[q] = f32x2_to_bf16x2(s[2 * q], s[2 * q + 1]);
-    reinterpret_cast<u32x4*>(a.y)[i] = y;
-  } else {
-    reinterpret_cast<uint2*>(a.y)[i] = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
-  }
+  reinterpret_cast<uint2*>(a.y)[i] = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
 }
 
-// Whether the wide tiles are taken: by the rows per expert from which they are faster, and their number, which must
-// cover the chip (small layers: F 512, 8 experts, bf16, 1000 / 4000 tokens 42 / 48 us, batch tiles 28 / 40).
-//   bf16: the batch tiles' weight stream hides the widening, which the wide ones pay with the products; whole call,
-//     batch / wide: Mixtral-shaped 450 tokens (112 rows an expert) 336 / 429 us, 1000 (250) 666 / 697, 1500 (375)
-//     927 / 907; DeepSeek-shaped 1600 (194 with the shared experts) 297 / 323, 2500 (303) 420 / 395.
-//   MX4: Mixtral-shaped 40 tokens (10 rows) 142 / 156, 64 (16) 149 / 157, 90 (22) 158 / 159, 128 (32) 173 / 163;
-//     DeepSeek-shaped 100 (12) 91 / 88, 200 (24) 103 / 90.
+// Whether the wide tiles are taken: by the rows per expert from which they are faster, averaged over all experts, and
+// their number, which must cover the chip (small layers: F 512, 8 experts, bf16, 1000 / 4000 tokens 42 / 48 us, batch tiles
+// 28 / 40). Whole call, batch / wide, in us; "of half": the routing leaves out every other expert, as a hard mask does, so
+// that the experts it reads have twice the average rows:
+//   bf16: the batch tiles' weight stream hides the widening, which the wide ones pay with the products. Mixtral-shaped
+//     400 tokens (100 rows an expert) 317 / 423, 1000 (250) 680 / 740, 1300 (325) 852 / 872, 1700 (425) 1079 / 992; of half
+//     1000 tokens 642 / 679, 1300 829 / 801. DeepSeek-shaped 1600 (194 with the shared experts) 285 / 319, 2500 (303)
+//     405 / 387, 3500 (424) 540 / 576; of half 1600 tokens 263 / 288, 2500 391 / 370.
+//   MX4: Mixtral-shaped 64 tokens (16 rows) 150 / 156, 90 (22) 160 / 159, 128 (32) 181 / 163; of half 64 tokens 92 / 111,
+//     90 103 / 115, 128 173 / 124. DeepSeek-shaped 100 (12) 87 / 81, 200 (24) 99 / 84; of half 100 65 / 55.
 bool mx4_takes_wide(int rows, int G, int F, bool mx_act) {
   const int64_t tiles = (static_cast<int64_t>(rows) / mx4_tile_rows(mx_act) + G / 2) * ((2 * F + 255) / 256);
   return rows >= (mx_act ? 22 : 280) * G && tiles >= 256;
@@ -180,8 +164,7 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   p.xs = reinterpret_cast<uint8_t*>(ws + w.xs);
   p.h = ws + w.h;
   p.hs = reinterpret_cast<uint8_t*>(ws + w.hs);
-  p.o = ws + w.o;
-  p.o_bf16 = false;
+  p.o = reinterpret_cast<float*>(ws + w.o);
   if (a.T <= kMx4FewT) return launch_mx4_few(p, stream);
   const int KS = a.K + a.n_shared, rows = a.T * KS;
   hipError_t err;
@@ -206,10 +189,6 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
   const int max_tiles = std::min(rows, rows / tile_rows + p.G);
   int splits = 1;
   if (wide) {
-    // With MX4 activations the bytes of fp32 outputs take as long as the products that make them; in bf16 (the layer's
-    // type; y is off by 2.3e-3 instead of 1.7e-3 then) they take half: DeepSeek-shaped layer, 4096 tokens, down and
-    // combine 121 + 70 -> 112 + 40 us (the latter 25 since, see there). With bf16 activations, whose h is rounded to bf16 already, they stay fp32.
-    p.o_bf16 = a.mx_act;
     err = launch_mx4_wide(p, max_tiles, stream);
   } else {
     // two workgroups a CU for the down projection, each with eight steps or more
@@ -220,10 +199,9 @@ hipError_t launch_mx4_experts(const Mx4Args& a, void* workspace, hipStream_t str
     err = launch_mx4_batch(p, max_tiles, splits, stream);
   }
   if (err != hipSuccess) return err;
-  const int64_t cn = static_cast<int64_t>(a.T) * a.d / (p.o_bf16 ? 8 : 4);
-  const dim3 cgrid(static_cast<unsigned>((cn + kThreads - 1) / kThreads));
-  if (p.o_bf16) hipLaunchKernelGGL(mx4_combine_kernel<true>, cgrid, dim3(kThreads), 0, stream, p, splits);
-  else hipLaunchKernelGGL(mx4_combine_kernel<false>, cgrid, dim3(kThreads), 0, stream, p, splits);
+  const int64_t cn = static_cast<int64_t>(a.T) * a.d / 4;
+  hipLaunchKernelGGL(mx4_combine_kernel, dim3(static_cast<unsigned>((cn + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                     stream, p, splits);
   return hipGetLastError();
 }
 

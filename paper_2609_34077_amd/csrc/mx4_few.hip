@@ -291,7 +291,7 @@ __global__ __launch_bounds__(kThreads, 4) void mx4_few_down_kernel(const Mx4Para
   // wave w joins fragment w
   const f32x4 v = red[0][wave][lane] + red[1][wave][lane] + red[2][wave][lane] + red[3][wave][lane];
   if (l16 < a.T)
-    *reinterpret_cast<f32x4*>(static_cast<float*>(p.o) + (static_cast<size_t>(split) * a.T + l16) * a.d + 64 * cx + 16 * wave + 4 * lg) = v;
+    *reinterpret_cast<f32x4*>(p.o + (static_cast<size_t>(split) * a.T + l16) * a.d + 64 * cx + 16 * wave + 4 * lg) = v;
 }
 
 // y = the sum of the parts [splits, T, d] in order; four columns a thread.

@@ -16,8 +16,8 @@
 //                     ahead (3 x 24 KB and 6 KB), two workgroups a CU, whose starts and ends overlap. Workgroups of
 //                     256 rows and eight wavefronts were slower for few steps and rows (both products, DeepSeek-shaped
 //                     1200 / 4096 / 8192 tokens 128 / 290 / 479 us, these 106 / 285 / 460) and faster for many
-//                     (Mixtral-shaped 1500 / 8192 tokens 373 / 1589 us, these 393 / 1632). With whole stores (join_pieces)
-//                     now 101 / 262 and, Mixtral-shaped 8192 tokens, 1540: 3.7 PFLOP/s.
+//                     (Mixtral-shaped 1500 / 8192 tokens 373 / 1589 us, these 393 / 1632; all with expert outputs in bf16).
+//                     In fp32, as they are, 109 / 278 to 301 / 499 and 400 / 1650, the latter 3.5 PFLOP/s.
 // Token loads are buffer loads: rows past the tile's end and columns past a row's end read as zeros.
 
 #include "gemm_tile.hpp"
@@ -41,15 +41,6 @@ __device__ __forceinline__ void dma16s(uint32_t m0v, i32x4 rsrc, uint32_t voff, 
 }
 
 constexpr uint32_t kStage = 24576;       // of MX4 operands in LDS
-
-// Two 8-byte pieces a and b that lane 16 lg + t holds of two 32-byte runs of row t (piece lg of each): the lane gets the
-// 16 bytes 2 (lg / 2) and 2 (lg / 2) + 1 of run lg % 2 (rows of 16 lanes 1 and 0, 3 and 2 change places between the two). Stores
-// of 64 bytes a row instead of 32: the down projection with MX4 activations, DeepSeek-shaped, 4096 tokens, 117 -> 101 us.
-__device__ __forceinline__ u32x4 join_pieces(uint2 a, uint2 b) {
-  const auto x = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false);
-  const auto y = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
-  return u32x4{x[0], y[0], x[1], y[1]};
-}
 
 struct Tile {
   int g, row0, nrows, f0;   // expert, its first row and rows here, first weight fragment
@@ -252,21 +243,11 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
     const int r = 16 * (WN * n + wn) + l16;
     const bool ok = r < t.nrows;
     const size_t row = t.row0 + r;
-    if constexpr (EPI == 1 && MX) {
-#pragma unroll
-      for (int i = 0; i < kWF; i += 2) {   // R is a multiple of 64: both fragments are in or out
-        const int f = t.f0 + kWF * wm + i;
-        const f32x4 v = acc[i][n], w = acc[i + 1][n];
-        const u32x4 o = join_pieces(make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])),
-                                    make_uint2(f32x2_to_bf16x2(w[0], w[1]), f32x2_to_bf16x2(w[2], w[3])));
-        if (ok && f < R / 16)
-          *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.o) + row * a.d + 16 * (f + (lg & 1)) + 8 * (lg >> 1)) = o;
-      }
-    } else if constexpr (EPI == 1) {
+    if constexpr (EPI == 1) {
 #pragma unroll
       for (int i = 0; i < kWF; ++i) {
         const int f = t.f0 + kWF * wm + i;
-        if (ok && f < R / 16) *reinterpret_cast<f32x4*>(static_cast<float*>(p.o) + row * a.d + 16 * f + 4 * lg) = acc[i][n];
+        if (ok && f < R / 16) *reinterpret_cast<f32x4*>(p.o + row * a.d + 16 * f + 4 * lg) = acc[i][n];
       }
     } else {
 #pragma unroll
@@ -294,10 +275,11 @@ __device__ __forceinline__ void run_tile(const Mx4Params& p, const Tile& t, u32x
             if (lg == 0) p.hs[row * 16 * mx4_quads(a.F) + mx4_scale_at(cb)] = static_cast<uint8_t>(byte);
           }
         } else {
-          const u32x4 o = join_pieces(make_uint2(f32x2_to_bf16x2(h[0], h[1]), f32x2_to_bf16x2(h[2], h[3])),
-                                      make_uint2(f32x2_to_bf16x2(h[4], h[5]), f32x2_to_bf16x2(h[6], h[7])));
-          if (ok && cb < a.F / 32)
-            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.h) + row * a.F + 32 * cb + 16 * (lg & 1) + 8 * (lg >> 1)) = o;
+          if (ok && cb < a.F / 32) {
+            uint2* o = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.h) + row * a.F + 32 * cb + 4 * lg);
+            o[0] = make_uint2(f32x2_to_bf16x2(h[0], h[1]), f32x2_to_bf16x2(h[2], h[3]));
+            o[4] = make_uint2(f32x2_to_bf16x2(h[4], h[5]), f32x2_to_bf16x2(h[6], h[7]));
+          }
         }
       }
     }

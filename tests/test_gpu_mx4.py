@@ -330,3 +330,31 @@ def test_python_refusals():
         L.maskmoe_experts_forward_mx4(xq.cuda(), it, gt, packed, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
     with pytest.raises(L.MaskMoEError):
         L.maskmoe_experts_forward_mx4(xq.cuda(), it, gt, packed, act=3)
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T", [4, 40, 1300])
+def test_expert_outputs_stay_fp32(T, act):
+    """Two experts whose outputs 257 v and -256 v leave v: exact in fp32, 0 where they were rounded to bf16 (257 lies
+    between 256 and 258), for few tokens, a batch and enough rows for the wide tiles (2 T / 128 + 1 or 2 T / 256 + 1
+    row tiles of 33: 700 and 363). Every step is exact: a = 128 s, SiLU(a) = a to fp32 from 128 on, b = s, so that
+    h = 128 s^2 in every column, a block of equal powers of two; v = 128 s^2."""
+    say(f"mx4 experts fp32 outputs T={T} act={act}")
+    d, F = 128, 4160
+    gu = np.zeros((2, 2 * F, d), np.int64)
+    gu[:, :, 0] = 2                                            # the code of 1
+    eg = np.zeros((2, 2 * F, d // 32), np.int64)
+    eg[:, F:] = -7
+    dn = np.zeros((2, d, F), np.int64)
+    dn[0, :, 5:5 + 128 * 32:32], dn[0, :, F - 1] = 4, 2        # 128 twos and a one
+    dn[1, :, 7:7 + 128 * 32:32] = 12                           # 128 times -2
+    ed = np.zeros((2, d, F // 32), np.int64)
+    dev = []
+    for c, e in ((gu, eg), (dn, ed)):
+        dev += [torch.from_numpy(M.pack_codes(c)).cuda(), torch.from_numpy((e + 127).astype(np.uint8)).cuda()]
+    s = 2.0 ** (np.arange(T) % 3)
+    x = np.zeros((T, d))
+    x[:, 0] = 128 * s
+    idx, gate = np.tile(np.array([0, 1], np.int32), (T, 1)), np.ones((T, 2), np.float32)
+    y = call(bf16(x), dev, idx, gate, 0, act).double().cpu().numpy()
+    assert (y == (128 * s * s)[:, None]).all()
