@@ -628,6 +628,12 @@ def maskmoe_layer_backward(x, w_gate_up, w_down, K: int, gate_mode: int, topk_ga
     return out
 
 
+def _fits(*sizes: int):
+    """ctypes keeps the low 32 bits of a size that int32 does not hold."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError("sizes must be below 2^31")
+
+
 def _refuse(t, name: str):
     _dev(t, name)
     raise ValueError(f"{name} must be on the current device")
@@ -652,10 +658,11 @@ def maskmoe_gate_forward(logits, K: int, score: int, n_group: int = 1, topk_grou
     entries without an eligible expert hold index -1 and gate 0."""
     import torch
     lib = load()
-    here = torch.cuda.current_device()
     if logits.dim() != 2:
         raise ValueError("logits must be 2-d")
     T, E = logits.shape
+    _fits(T, E, K, n_group, topk_group)
+    here = torch.cuda.current_device()
     _want(logits, "logits", (T, E), torch.float32, here)
     if bias is not None:
         _want(bias, "bias", (E,), torch.float32, here)
@@ -676,11 +683,12 @@ def maskmoe_gate_backward(logits, topk_idx, d_gate, score: int, renorm: bool = T
     selection topk_idx [T,K] held fixed."""
     import torch
     lib = load()
-    here = torch.cuda.current_device()
     if logits.dim() != 2 or topk_idx.dim() != 2:
         raise ValueError("logits and topk_idx must be 2-d")
     T, E = logits.shape
     K = topk_idx.shape[1]
+    _fits(T, E, K)
+    here = torch.cuda.current_device()
     _want(logits, "logits", (T, E), torch.float32, here)
     _want(topk_idx, "topk_idx", (T, K), torch.int32, here)
     _want(d_gate, "d_gate", (T, K), torch.float32, here)
@@ -700,6 +708,7 @@ def maskmoe_mx4_quantize(x):
     cols = shape[-1] if shape else 0
     if cols == 0 or cols % 32:
         raise ValueError("the last dimension must be a positive multiple of 32")
+    _fits(cols)
     _want(x, "x", shape, x.dtype, torch.cuda.current_device())
     codes = x.new_empty(shape[:-1] + (cols // 2,), dtype=torch.uint8)
     scales = x.new_empty(shape[:-1] + (cols // 32,), dtype=torch.uint8)
@@ -712,11 +721,12 @@ def maskmoe_mx4_dequantize(codes, scales, dtype):
     """The values of codes [..., cols/2] and scales [..., cols/32] as a bf16 or fp32 tensor [..., cols]."""
     import torch
     lib = load()
-    here = torch.cuda.current_device()
     shape = codes.shape
     cols = 2 * shape[-1] if shape else 0
     if cols == 0 or cols % 32:
         raise ValueError("the last dimension of codes must be a positive multiple of 16")
+    _fits(cols)
+    here = torch.cuda.current_device()
     _want(codes, "codes", shape, torch.uint8, here)
     _want(scales, "scales", shape[:-1] + (cols // 32,), torch.uint8, here)
     out = codes.new_empty(shape[:-1] + (cols,), dtype=dtype)
@@ -771,11 +781,12 @@ def maskmoe_experts_forward_mx4(x, topk_idx, topk_gate, experts: PackedMx4Expert
     experts and then ``n_shared`` shared ones. ``act``: ACT_BF16 or ACT_MX4 activations. Returns y [T,d]."""
     import torch
     lib = load()
-    here = torch.cuda.current_device()
     if topk_idx.dim() != 2:
         raise ValueError("topk_idx must be 2-d")
     T, K = topk_idx.shape
     d = experts.d
+    _fits(T, K, n_shared)
+    here = torch.cuda.current_device()
     _want(x, "x", (T, d), torch.bfloat16, here)
     _want(topk_idx, "topk_idx", (T, K), torch.int32, here)
     _want(topk_gate, "topk_gate", (T, K), torch.float32, here)

@@ -6,6 +6,7 @@ import os
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2609_34077_amd import _lib as L
 
@@ -155,3 +156,22 @@ def test_experts_mx4_workspace_is_monotone_in_tokens():
     f = lambda T: L.maskmoe_experts_mx4_workspace_bytes(T, 192, 64, 6, 320, 2)
     sizes = [f(T) for T in (0, 1, 16, 17, 100, 1000, 5000)]
     assert sizes == sorted(sizes)
+
+
+def test_sizes_that_int32_does_not_hold():
+    """ctypes would pass their low 32 bits: a batch of 2^32 + 5 rows as one of 5, whose other results nothing writes."""
+    meta = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device="meta")
+    i32, u8 = torch.int32, torch.uint8
+    few = meta(4, 64)
+    calls = [lambda: L.maskmoe_gate_forward(meta(2 ** 32 + 5, 1), 1, L.SCORE_SOFTMAX),
+             lambda: L.maskmoe_gate_forward(few, 2 ** 32 + 2, L.SCORE_SOFTMAX),
+             lambda: L.maskmoe_gate_forward(few, 2, L.SCORE_SOFTMAX, n_group=2 ** 32 + 8, topk_group=2),
+             lambda: L.maskmoe_gate_backward(meta(2 ** 32 + 5, 1), meta(2 ** 32 + 5, 1, dtype=i32), meta(2 ** 32 + 5, 1), 0),
+             lambda: L.maskmoe_gate_backward(meta(1, 8), meta(1, 2 ** 32 + 2, dtype=i32), meta(1, 2 ** 32 + 2), 0),
+             lambda: L.maskmoe_mx4_quantize(meta(2 ** 32 + 32)),
+             lambda: L.maskmoe_mx4_dequantize(meta(2 ** 31 + 16, dtype=u8), meta(2 ** 27 + 1, dtype=u8), torch.bfloat16)]
+    packed = L.PackedMx4Experts(4, 64, 64, [torch.empty(1, dtype=u8)] * 4)
+    calls.append(lambda: L.maskmoe_experts_forward_mx4(meta(4, 64), meta(4, 2, dtype=i32), meta(4, 2), packed, n_shared=2 ** 32))
+    for f in calls:
+        with pytest.raises(ValueError, match="below 2"):
+            f()
