@@ -355,3 +355,44 @@ def test_what_has_no_key_costs_no_second_selection(E):
     us = fastest(calls)
     for f in (0, 2, 4):
         assert us[f + 1] <= 1.25 * us[f], us
+
+
+@pytest.mark.parametrize("score", [G.SOFTMAX, G.SIGMOID])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("E", [8, 64, 100, 256])
+def test_backward_of_infinities_nan_and_saturated_scores(E, renorm, score):
+    """The forward's special rows. An unnormalised weight e^-v is off by (v + 2) 2^-23 relative, so by at most 4 U of the
+    largest weight whatever v; its sum (256 terms, 8 levels), the division and the sums over K = 4 entries stay within
+    16 U more, for each of three factors: (3 * 16 + 16) U of scale * sum |d_gate|, as test_backward's for a range of 0.
+    Renormalised sigmoids are not relative to the largest one above -30, where e^-z is off by (30 + 2) 2^-23 = 64 U: 80."""
+    say(f"gate backward special rows E={E} renorm={renorm} score={score}")
+    K, scale = 4, 2.5
+    g = np.random.default_rng(E)
+    z = (1.3 * g.standard_normal((40, E))).astype(np.float32)
+    z[0] = -np.inf
+    z[1] = np.nan
+    z[2] = np.finfo(np.float32).min
+    z[3, 1:] = -np.inf
+    z[4, : E // 2] = np.nan
+    z[5, 3] = np.inf
+    z[6, [2, 5]] = np.inf
+    z[7] = -200.0 - np.arange(E) / 64       # every sigmoid underflows
+    z[8] = 200.0 + np.arange(E) / 64
+    z[9, 0] = np.finfo(np.float32).max
+    z[10:20, 1] = np.inf
+    z[20:30, 4] = np.nan
+    z[30:34] *= 30
+    z[34] = -29.9 - np.arange(E) / 16       # across the border below which sigmoids are taken as e^z
+    chosen = G.forward(z, K, score)[0]
+    any4 = np.argsort(g.random((40, E)), 1)[:, :K]             # entries without a logit among them
+    dg = g.standard_normal((40, K)).astype(np.float32)
+    for idx in (chosen, any4, np.repeat(any4[:, :1], K, 1)):
+        dz = L.maskmoe_gate_backward(torch.from_numpy(z).cuda(), torch.from_numpy(idx.astype(np.int32)).cuda(),
+                                     torch.from_numpy(dg).cuda(), score, renorm=renorm, scale=scale).cpu().numpy()
+        with np.errstate(over="ignore", invalid="ignore"):
+            want = G.backward(z, idx, dg, score, renorm, scale)
+        assert np.isfinite(want).all() and np.isfinite(dz).all()
+        factor = 80 if renorm and score == G.SIGMOID else 16
+        tol = (3 * factor + 16) * U * scale * np.abs(dg).sum(1, keepdims=True)
+        assert (np.abs(dz - want) <= tol + 1e-37).all(), np.abs(dz - want).max()
+        assert (dz[:2] == 0).all()
