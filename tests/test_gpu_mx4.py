@@ -358,3 +358,79 @@ def test_expert_outputs_stay_fp32(T, act):
     idx, gate = np.tile(np.array([0, 1], np.int32), (T, 1)), np.ones((T, 2), np.float32)
     y = call(bf16(x), dev, idx, gate, 0, act).double().cpu().numpy()
     assert (y == (128 * s * s)[:, None]).all()
+
+
+def taken(T, d, F, E, K, ns, act):
+    """The kernels that a call takes, by the rules of csrc/mx4_experts.hip: "few", "wide", or the parts that the batch
+    kernels split the down projection's reduction into."""
+    rows, G, mx = T * (K + ns), E + ns, act == L.ACT_MX4
+    if T <= 16:
+        return "few"
+    tiles = (rows // (128 if mx else 256) + G // 2) * ((2 * F + 255) // 256)
+    if rows >= (22 if mx else 280) * G and tiles >= 256:
+        return "wide"
+    splits, steps = 1, (F + 127) // 128
+    while splits < 8 and min(rows, G) * ((d + 255) // 256) * splits < 512 and steps >= 16 * splits and 2 * splits * rows <= 8192:
+        splits *= 2
+    return splits
+
+
+# T, d, F, E, K, shared, empty slots, parts: reductions of 16, 17, 33 and 65 steps, of which the parts start at any step
+# and the last one may hold 64 columns
+SPLIT = [(17, 64, 2048, 2, 1, 0, 0, 2), (33, 192, 2112, 3, 2, 0, 4, 2), (80, 64, 2112, 2, 2, 1, 5, 2), (24, 320, 2112, 5, 2, 2, 0, 2),
+         (40, 192, 4160, 3, 2, 0, 0, 4), (61, 64, 4160, 4, 1, 1, 9, 4), (18, 64, 8256, 2, 1, 0, 1, 8), (70, 128, 8256, 3, 1, 1, 6, 8),
+         (80, 64, 8256, 4, 2, 0, 0, 8)]
+
+
+@pytest.mark.parametrize("act", [L.ACT_BF16, L.ACT_MX4])
+@pytest.mark.parametrize("T,d,F,E,K,ns,pad,parts", SPLIT)
+def test_batches_with_split_reductions(T, d, F, E, K, ns, pad, parts, act):
+    say(f"mx4 split T={T} d={d} F={F} E={E} K={K} shared={ns} pad={pad} parts={parts} act={act}")
+    assert taken(T, d, F, E, K, ns, act) == parts
+    x, wq, dev, idx, gate = make(T, d, F, E, K, ns, T + d + F, pad)
+    y = check(x, wq, dev, idx, gate, ns, act)
+    if pad and not ns:
+        assert (y[T - pad:] == 0).all()
+    x[T // 2, 3] = float("nan")                                # stays in its token
+    y2 = call(x, dev, idx, gate, ns, act).cpu().double()
+    rows = torch.ones(T, dtype=torch.bool)
+    rows[T // 2] = False
+    assert torch.equal(y2[rows], torch.from_numpy(y)[rows]) and y2[T // 2].isnan().all()
+
+
+@pytest.mark.parametrize("T,d,F,E,K,ns,pad,act", [(2100, 448, 4160, 2, 1, 0, 1, L.ACT_BF16), (2300, 576, 2112, 1, 1, 1, 3, L.ACT_BF16),
+                                                  (500, 448, 4160, 2, 2, 0, 1, L.ACT_MX4)])
+def test_wide_tiles_past_the_matrix(T, d, F, E, K, ns, pad, act):
+    """Weight tiles of 256 rows that the matrix ends in, both products."""
+    say(f"mx4 wide T={T} d={d} F={F} E={E} K={K} shared={ns} pad={pad} act={act}")
+    assert taken(T, d, F, E, K, ns, act) == "wide"
+    x, wq, dev, idx, gate = make(T, d, F, E, K, ns, T + d + F, pad)
+    y = check(x, wq, dev, idx, gate, ns, act)
+    if not ns:
+        assert (y[T - pad:] == 0).all()
+
+
+@pytest.mark.parametrize("n,d,F", [(1, 64, 64), (3, 192, 320), (2, 640, 1088)])
+def test_packed_layout(n, d, F):
+    """Operand order: fragment f of 16 rows, step s of 128 columns, lane l the block of row l % 16 and columns 128 s +
+    32 (l / 16); scales of four steps a dword; gate and up fragments alternate; zeros past the columns."""
+    g = np.random.default_rng(n + d + F)
+    dev, want = [], []
+    for R, C, gate_up in ((2 * F, d, True), (d, F, False)):
+        codes = g.integers(0, 256, (n, R, C // 2), dtype=np.uint8)
+        scales = g.integers(0, 256, (n, R, C // 32), dtype=np.uint8)
+        dev += [torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()]
+        steps = (C + 127) // 128
+        quads = (steps + 3) // 4
+        cb = np.zeros((n, R, 4 * steps, 16), np.uint8)
+        cb[:, :, : C // 32] = codes.reshape(n, R, C // 32, 16)
+        sb = np.zeros((n, R, 16 * quads), np.uint8)
+        sb[:, :, : C // 32] = scales
+        if gate_up:   # fragments 2q of W_gate, 2q + 1 of W_up
+            order = np.arange(R).reshape(2, R // 32, 16).transpose(1, 0, 2).reshape(-1)
+            cb, sb = cb[:, order], sb[:, order]
+        want.append(cb.reshape(n, R // 16, 16, steps, 4, 16).transpose(0, 1, 3, 4, 2, 5).reshape(-1))
+        want.append(sb.reshape(n, R // 16, 16, quads, 4, 4).transpose(0, 1, 3, 5, 2, 4).reshape(-1))
+    packed = L.maskmoe_mx4_pack_experts(*dev)
+    for t, w in zip(packed.tensors, want):
+        assert np.array_equal(t.cpu().numpy(), w)
