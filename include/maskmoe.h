@@ -625,7 +625,8 @@ int maskmoe_mx4_quantize(int64_t rows, int32_t cols, int32_t dtype, const void* 
                          hipStream_t stream);
 
 /* maskmoe_mx4_dequantize -- the values that codes and scales stand for, as bf16 (rounded only where subnormal) or
- * fp32 (exact). Arguments and errors as maskmoe_mx4_quantize. */
+ * fp32 (exact). Scales of 2^126 and 2^127, which maskmoe_mx4_quantize never gives, can stand for magnitudes past both
+ * types' ranges: these are infinite. Arguments and errors as maskmoe_mx4_quantize. */
 int maskmoe_mx4_dequantize(int64_t rows, int32_t cols, int32_t dtype, const uint8_t* codes, const uint8_t* scales,
                            void* dst, hipStream_t stream);
 

@@ -434,3 +434,15 @@ def test_packed_layout(n, d, F):
     packed = L.maskmoe_mx4_pack_experts(*dev)
     for t, w in zip(packed.tensors, want):
         assert np.array_equal(t.cpu().numpy(), w)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_code_and_scale(dtype):
+    """All 16 codes under all 256 scales; values past the type's range are infinite."""
+    byte = np.arange(256)
+    codes = np.tile(np.arange(16), (256, 2))
+    want = torch.from_numpy(M.values(codes, np.where(byte == 255, 128, byte - 127)[:, None])).to(dtype)
+    got = L.maskmoe_mx4_dequantize(torch.from_numpy(M.pack_codes(codes)).cuda(),
+                                   torch.from_numpy(byte.astype(np.uint8)[:, None]).cuda(), dtype).cpu()
+    assert got[255].isnan().all() and torch.equal(got[:255], want[:255])
+    assert got[253:255].isinf().any() and got[:253].isfinite().all()
