@@ -114,15 +114,17 @@ __device__ __forceinline__ float clamp_logit(float z) { return fminf(z, FLT_MAX)
 constexpr float kKeyTol = 4e-6f;
 
 // e^x for x <= 0 in fp64: x = k ln 2 + r with |r| <= ln 2 / 2, the Taylor polynomial of degree 13 in r (its
-// remainder is 4e-18), times 2^k. Coefficients come from memory one at a time: the library's exp keeps its own in
+// remainder is 4e-18), times 2^k. The reduction is Cody and Waite's: ln 2 as its first 32 binary places, of which k (11 bits)
+// times is exact, and the rest. Coefficients come from memory one at a time: the library's exp keeps its own in
 // registers through the loops around it, which leaves room for half the wavefronts.
 __constant__ double kInvFactorial[14] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040,
                                          1.0 / 40320, 1.0 / 362880, 1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600,
                                          1.0 / 6227020800.0};
 __device__ __forceinline__ double exp_neg(double x) {
   x = fmax(x, -800.0);   // 0 in fp64
-  const double k = rint(x * 1.4426950408889634);
-  const double r = fma(-k, 1.9082149292705877e-10, fma(-k, 0.6931471803691238, x));   // ln 2 in two parts
+  constexpr double kLn2First = 0x1.62e42feep-1, kLn2Rest = 0x1.a39ef35793c76p-33, kLog2E = 0x1.71547652b82fep+0;
+  const double k = rint(x * kLog2E);
+  const double r = fma(-k, kLn2Rest, fma(-k, kLn2First, x));
   double p = kInvFactorial[13];
 #pragma unroll 1
   for (int i = 12; i >= 0; --i) p = fma(p, r, kInvFactorial[i]);
