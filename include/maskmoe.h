@@ -560,8 +560,8 @@ typedef struct maskmoe_gate_desc {
 } maskmoe_gate_desc;
 
 /*
- * maskmoe_gate_forward -- Top-K selection and gates from router logits z (maskmoe_route's and
- * maskmoe_layer_forward_train's logits, or any other). With s the score of every expert:
+ * maskmoe_gate_forward -- Top-K selection and gates from router logits z that the caller has: x W_router^T of its own, or
+ * maskmoe_layer_forward_train's (maskmoe_route writes none). With s the score of every expert:
  *   key_e = s_e * prior_e + bias_e                       (prior 1, bias 0 where not given)
  *   groups: those with the topk_group largest group scores (of keys) stay
  *   A = the K experts with the largest keys in them
