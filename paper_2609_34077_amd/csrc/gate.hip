@@ -545,8 +545,11 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(const GateArgs a) {
 
 // More than 64 experts: a wavefront finds the candidates of `batch` (up to 64 / C) tokens one after the other, a row over
 // its 64 lanes, and then ranks them all at once, C lanes a token, by fp64 keys of the candidates alone. Bound by the
-// instructions of the first part (300 vector and 270 scalar ones a token: 131072 tokens x 256 experts in 8 groups
-// 120 us, of which the 142 MB would take 30); six wavefronts a SIMD.
+// first part: 131072 tokens x 256 experts in 8 groups take 112 to 117 us, of which the 142 MB would be 30. Its 300 vector
+// instructions a token are 64 us of issue over the chip; the rest is the chain of ballots, counts and lane reads of one token's
+// bound, and a loop over tokens that the compiler does not know to be uniform (`wave` is no scalar to it), which puts
+// counters and row addresses in vector registers. Six wavefronts a SIMD leave 80 registers, of which some 16 are stored and
+// reloaded once a batch.
 template <int V, bool VEC, int KEYS, int GROUPS, int C>
 __global__ __launch_bounds__(kThreads, 6) void gate_rows_kernel(const GateArgs a, int batch) {
   constexpr int TB = kWave / C;

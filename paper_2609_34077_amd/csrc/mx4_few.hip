@@ -5,9 +5,10 @@
 //         to end: each expert's sum is weighed by the tokens' gates and added, so that y comes out;
 //   sum   of the parts, in order.
 // A wavefront multiplies 64 weight rows at a time, so that the tokens' operand, which takes as many registers as
-// theirs, is used four times. It keeps no ring of steps: in 64 to 84 registers six to eight wavefronts a SIMD have their
-// loads in flight together (Mixtral-shaped layer, one token, up / down: 25.3 / 14.3 us; with rings of two steps in 156
-// registers 27.0 / 17.1, and rings of one, whose registers the compiler keeps apart, 26.4 / 16.1).
+// theirs, is used four times. It keeps no ring of steps: in 56 to 84 registers all of a small launch's wavefronts are on
+// the chip at once, each with one step's loads in flight (Mixtral-shaped layer, one token: 896 and 1024 workgroups, 3.5 and 4
+// wavefronts a SIMD, up / down 25.3 / 14.3 us; with rings of two steps in 156 registers 27.0 / 17.1, and rings of one, whose
+// registers the compiler keeps apart, 26.4 / 16.1).
 // Tokens are the 16 columns of the matrix instructions as they are; a token that an expert is not selected for
 // loads nothing there. Weights go from memory straight to registers, 1 KiB of 16 rows x 128 columns a load.
 
