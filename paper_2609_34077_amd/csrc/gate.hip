@@ -104,6 +104,15 @@ __device__ __forceinline__ float fast_exp(float v) { return __builtin_amdgcn_exp
 __device__ __forceinline__ float fast_rcp(float v) { return __builtin_amdgcn_rcpf(v); }
 __device__ __forceinline__ float fast_sigmoid(float z) { return fast_rcp(1.0f + fast_exp(-z)); }
 
+// Numbers in the ratio of the scores of a token's entries, of which top is the largest logit: e^z for softmax, e^z / (1 + e^z)
+// for sigmoid, times e^-top where that is needed to keep them in fp32's range (a sigmoid of -90 is 0 in fp32, beside one of
+// -29 it is 3e-27).
+__device__ __forceinline__ float ratio_weight(bool soft, float z, float top) {
+  const bool low = top < 0.0f;
+  const float rel = soft || low ? fast_exp(z - top) : 1.0f;
+  return soft ? rel : rel * fast_rcp(1.0f + fast_exp(low ? z : -z));
+}
+
 // +inf counts as the largest finite logit; NaN and -inf leave the row (see live below).
 __device__ __forceinline__ float clamp_logit(float z) { return fminf(z, FLT_MAX); }
 
@@ -432,10 +441,8 @@ __device__ __forceinline__ void write_gate(const GateArgs& a, int t, bool real, 
   const float zs = has ? logit : -INFINITY;
   float g;
   if (a.renorm) {
-    // ratios of scores, from logits relative to the largest selected one: exp(z_k - z_max) for
-    // softmax, and for sigmoid where every score is e^z to fp32's precision; no score underflows
     const float top = seg_fmax<W>(fmaxf(zs, -FLT_MAX));
-    const float w = !has ? 0.0f : soft || top < -30.0f ? fast_exp(zs - top) : fast_sigmoid(zs);
+    const float w = has ? ratio_weight(soft, zs, top) : 0.0f;
     g = a.scale * (w / seg_sum<W>(w));
   } else {
     g = a.scale * (soft ? fast_exp(zs - zmax) / total : fast_sigmoid(zs));
@@ -855,7 +862,7 @@ __global__ __launch_bounds__(kThreads) void gate_bwd_sparse_kernel(const GateBwd
     float d;
     if (a.renorm) {
       const float top = seg_fmax<16>(fmaxf(x.zs, -FLT_MAX));
-      float w = !has ? 0.0f : soft || top < -30.0f ? fast_exp(x.zs - top) : fast_sigmoid(x.zs);
+      float w = has ? ratio_weight(soft, x.zs, top) : 0.0f;
       const float s = seg_sum<16>(w);
       w = has ? w / s : 0.0f;
       const float mean = seg_sum<16>(w * x.dg);

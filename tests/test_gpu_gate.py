@@ -396,3 +396,29 @@ def test_backward_of_infinities_nan_and_saturated_scores(E, renorm, score):
         tol = (3 * factor + 16) * U * scale * np.abs(dg).sum(1, keepdims=True)
         assert (np.abs(dz - want) <= tol + 1e-37).all(), np.abs(dz - want).max()
         assert (dz[:2] == 0).all()
+
+
+@pytest.mark.parametrize("E", [8, 256])
+def test_renormalised_sigmoids_far_below_the_largest(E):
+    """Gates are ratios of scores, e^-60 as well as 1/2, where a score by itself is 0 in fp32. Relative bounds: a weight is
+    off by (range + 16) U as in the forward's tests; a gradient w (dg - mean) (1 - s) by three such factors."""
+    say(f"gate ratios of sigmoids E={E}")
+    K, scale = 4, 2.5
+    T = 64
+    z = np.full((T, E), -np.inf, np.float32)
+    z[:, :4] = np.array([0.0, -1.0, -70.0, -86.0]) + np.linspace(-31, 1, T)[:, None]
+    z[::2, 2] = -89.0
+    z[:, 3] = np.minimum(z[:, 3], -90.0)
+    idx, gate, _ = run(z, K, G.SIGMOID, scale=scale)
+    io, go, _ = G.forward(z, K, G.SIGMOID, scale=scale)
+    fin = z[:, :4].astype(np.float64)
+    rel = (fin.max(1, keepdims=True) - fin.min(1, keepdims=True) + 16) * U
+    assert np.array_equal(idx, io)
+    assert (np.abs(gate - go) <= rel * np.abs(go) + 1e-37).all()
+    dg = np.random.default_rng(E).standard_normal((T, K)).astype(np.float32)
+    dz = L.maskmoe_gate_backward(torch.from_numpy(z).cuda(), torch.from_numpy(io.astype(np.int32)).cuda(),
+                                 torch.from_numpy(dg).cuda(), G.SIGMOID, scale=scale).cpu().numpy()
+    want = G.backward(z, io, dg, G.SIGMOID, True, scale)
+    t = np.arange(T)[:, None]
+    part = np.abs(go) * (np.abs(dg) + (np.abs(go) / scale * np.abs(dg)).sum(1, keepdims=True))
+    assert (np.abs(dz - want)[t, io] <= (3 * rel + 16 * U) * part + 1e-37).all()
