@@ -679,6 +679,135 @@ int maskmoe_experts_forward_mx4(const maskmoe_layer_desc* desc, int32_t act, con
                                 const float* topk_gate, const maskmoe_mx4_experts* w, void* y, void* workspace,
                                 size_t workspace_bytes, hipStream_t stream);
 
+/* ---- microscaled 8-bit blocks (MX8) ----
+ * A block is 32 consecutive elements of a row: int8 codes c in -127..127 and one E8M0 scale byte b; the values are
+ * c / 64 * 2^(b - 127), b = 255 standing for NaN. codes [rows, cols], scales [rows, cols / 32], row-major. */
+
+/*
+ * maskmoe_mx8_quantize -- blocks of src: b = floor(log2(max |v|)) + 127, at least 0 (a block of zeros: 0);
+ * c = 64 v / 2^(b - 127) rounded to the nearest integer, ties to even, saturating at 127 (the largest elements fall in
+ * [64, 128)). An element is off by at most 2^-7 of the block's largest one, 2^-6 where it saturates. A block that
+ * holds an infinity or NaN gets scale 255 and codes 0.
+ * maskmoe_mx8_dequantize -- the values that codes and scales stand for; exact in both types.
+ *  rows, cols   cols % 32 == 0.   dtype MASKMOE_BF16 or MASKMOE_F32: type of src / dst.
+ *  src, dst     device [rows, cols].   codes device [rows, cols].   All three 16-byte aligned.
+ *  scales       device [rows, cols / 32].
+ *  Errors: E_INVAL for negative rows, cols < 1, NULL or misaligned pointers or an unknown dtype; E_UNSUPPORTED for
+ *  cols % 32 != 0 or more than 2^40 elements.
+ */
+int maskmoe_mx8_quantize(int64_t rows, int32_t cols, int32_t dtype, const void* src, int8_t* codes, uint8_t* scales,
+                         hipStream_t stream);
+int maskmoe_mx8_dequantize(int64_t rows, int32_t cols, int32_t dtype, const int8_t* codes, const uint8_t* scales,
+                           void* dst, hipStream_t stream);
+
+/* ---- the norm before a layer ---- */
+
+/*
+ * maskmoe_norm_forward -- root-mean-square norm of T rows, with the residual's addition:
+ *     s = x + residual,   hidden = s,   y_j = s_j (mean_j s_j^2 + eps)^-1/2 weight_j
+ * hidden is the stream that the next residual comes from; y what a router or expert reads (maskmoe_layer_forward's,
+ * maskmoe_experts_forward_train's x); codes and scales are y's 8-bit blocks, which a training step keeps instead of y
+ * (maskmoe_experts_backward reads them).
+ *  T >= 0 (0 is a no-op), 1 <= d <= 32768, eps finite and >= 0 (a row of zeros with eps 0 gives NaN).
+ *  dtype     MASKMOE_BF16 or MASKMOE_F32: type of x, residual, weight, hidden and y.
+ *  x         device [T, d].   residual device [T, d] or NULL (s = x).   weight device [d].
+ *  hidden    device [T, d] or NULL; x or residual itself to add in place.
+ *  y         device [T, d] or NULL; may be x or residual itself (another buffer than hidden).
+ *  codes     device [T, d], scales device [T, d / 32]: both or neither; d % 32 == 0 then.
+ *  Any alignment of the elements' own will do; rows of a multiple of 16 bytes in 16-byte aligned tensors are faster.
+ *  Buffers other than those named above must not overlap.
+ *  Rounding: s, the mean and y are fp32 (the norm is that of the unrounded s); hidden, y and the blocks are each rounded
+ *  once from those. Rows whose squares pass fp32's range give 0, an infinity or NaN in a row NaN in all of it that an
+ *  infinity or NaN reaches by the formula.
+ *  Errors: E_INVAL for sizes, eps or dtype outside their ranges, NULL required or misaligned pointers, no output at all,
+ *  codes without scales (or the reverse), y == hidden; E_UNSUPPORTED for d > 32768 or codes with d % 32 != 0.
+ */
+int maskmoe_norm_forward(int32_t T, int32_t d, int32_t dtype, float eps, const void* x, const void* residual,
+                         const void* weight, void* hidden, void* y, int8_t* codes, uint8_t* scales, hipStream_t stream);
+
+/*
+ * maskmoe_norm_backward -- the gradient of maskmoe_norm_forward from the hidden it stored (without a residual: x).
+ * With n = hidden (mean hidden^2 + eps)^-1/2, the sum taken again from hidden:
+ *     d_x = d_hidden + (mean hidden^2 + eps)^-1/2 (weight dy - n mean_j(weight dy n)),    d_weight = sum_t dy n
+ * d_x is the gradient of x and of the residual alike.
+ *  hidden, dy  device [T, d] (dtype).   weight device [d] (dtype).
+ *  d_hidden    device [T, d] (dtype) or NULL: what reaches hidden along the stream.
+ *  d_x         device [T, d] (dtype); may be dy, d_hidden or hidden itself.
+ *  d_weight    device [d] float or NULL (weight not trained). Written also for T = 0: zeros.
+ *  workspace   device, maskmoe_norm_backward_workspace_bytes(T, d) bytes, 256-byte aligned; unused without d_weight.
+ *              Calls that may overlap, and graphs that may run at the same time, must not share it.
+ *  Sums are fp32 in a fixed order; d_x is rounded once.
+ *  Errors: as above; E_WORKSPACE for a missing, small or misaligned workspace. The size query gives 0 for sizes out of
+ *  range.
+ */
+size_t maskmoe_norm_backward_workspace_bytes(int32_t T, int32_t d);
+int maskmoe_norm_backward(int32_t T, int32_t d, int32_t dtype, float eps, const void* hidden, const void* weight,
+                          const void* dy, const void* d_hidden, void* d_x, float* d_weight, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
+/* ---- the experts' training pass at a given routing, activations kept in 8 bits ---- */
+
+/*
+ * maskmoe_experts_forward_train -- the routed and shared experts of a layer for a routing that the caller has
+ * (maskmoe_gate_forward's or maskmoe_route's), keeping what maskmoe_experts_backward reads:
+ *     y_t = sum_k gate_{t,k} F_{idx_{t,k}}(x_t) + sum_s F_s(x_t),
+ *     F(x) = W_down h,  h = SiLU(a) b,  a = W_gate x,  b = W_up x                   (Section 3.1, Eq. 1)
+ * a and b are kept in 8-bit blocks, from which the backward takes h too: 2.06 F bytes for each (token, expert) row
+ * where the bf16 workspace of maskmoe_layer_forward_train keeps 6 F.
+ *  desc        T, d, E, K, F, n_shared; dtype MASKMOE_BF16; the other fields are ignored.
+ *  x           device [T, d] bf16.   y device [T, d] bf16, another buffer than x.
+ *  topk_idx    device [T, K] int32: an index outside [0, E) adds nothing and has no row; an expert named twice counts
+ *              twice.   topk_gate device [T, K] float.
+ *  w_gate_up, w_down, ws_gate_up, ws_down: as maskmoe_layer_forward (LAYOUT_ROWS).
+ *  codes       device [T (K + n_shared), 2F] int8, 16-byte aligned: a in columns 0..F-1, b in F..2F-1. Rows in order of
+ *              experts (shared ones last), those of an expert by token and slot; rows behind the last one, as many as
+ *              topk_idx has entries outside [0, E), are left as they were.
+ *  scales      device [T (K + n_shared), 2F / 32], likewise.
+ *  workspace   device, maskmoe_experts_train_workspace_bytes(desc) bytes, 256-byte aligned, free again once the call has
+ *              run; contents on entry do not matter. Calls that may overlap, and graphs that may run at the same time,
+ *              must not share it.
+ *  Rounding: sums are fp32; h and each expert's output are rounded to bf16, y once; codes are those of the unrounded
+ *  a and b.
+ *  Errors: E_INVAL for a desc outside its ranges, NULL or misaligned pointers, x == y; E_WORKSPACE; E_UNSUPPORTED for
+ *  MASKMOE_F32, d or F not multiples of 64, and T d, T (K + n_shared) 2F, T (K + n_shared) d or 2 F d at or above 2^31.
+ *  T = 0 writes nothing.
+ */
+size_t maskmoe_experts_train_workspace_bytes(const maskmoe_layer_desc* desc);
+int maskmoe_experts_forward_train(const maskmoe_layer_desc* desc, const void* x, const int32_t* topk_idx,
+                                  const float* topk_gate, const void* w_gate_up, const void* w_down,
+                                  const void* ws_gate_up, const void* ws_down, void* y, int8_t* codes, uint8_t* scales,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * maskmoe_experts_backward -- the gradients of maskmoe_experts_forward_train for a cotangent dy of y, the selection held
+ * fixed. With a, b the values of the kept blocks, h = SiLU(a) b, and for each row (token t, expert e, gate g; 1 for
+ * shared experts) u = W_down^T dy_t:
+ *     d_gate = <u, h>,   da = g u b SiLU'(a),  db = g u SiLU(a),
+ *     d_x_t = sum over t's rows of W_gate^T da + W_up^T db,
+ *     dW_down = sum over e's rows of dy (g h)^T,   dW_gate = da x^T,  dW_up = db x^T  likewise.
+ * d_gate continues in maskmoe_gate_backward.
+ *  desc, topk_idx, topk_gate, weights: as given to the forward.   codes, scales: as it left them.
+ *  x           device [T, d] bf16 as given to the forward, or, with x_scales, the codes [T, d] of its 8-bit blocks
+ *              (maskmoe_norm_forward's): x then enters dW_gate and dW_up with those values.
+ *  x_scales    device [T, d / 32] or NULL.
+ *  dy          device [T, d] bf16.
+ *  d_x         device [T, d] bf16, another buffer than dy and x; tokens without experts get zeros.
+ *  d_gate      device [T, K] float or NULL; 0 for entries without an expert.
+ *  d_w_gate_up device [E, 2F, d] bf16, d_w_down device [E, d, F] bf16: zero for experts that no entry names.
+ *  d_ws_gate_up, d_ws_down: the shared experts', [n_shared, ...]; NULL when n_shared == 0.
+ *  workspace   device, maskmoe_experts_backward_workspace_bytes(desc) bytes, as above.
+ *  Rounding: sums, d_gate and the rows' shares of d_x are fp32; da, db and g h are rounded to bf16 before their products;
+ *  outputs are rounded once.
+ *  Errors: as the forward's; E_INVAL for a missing gradient buffer too. T = 0 writes zero weight gradients.
+ */
+size_t maskmoe_experts_backward_workspace_bytes(const maskmoe_layer_desc* desc);
+int maskmoe_experts_backward(const maskmoe_layer_desc* desc, const void* x, const uint8_t* x_scales,
+                             const int32_t* topk_idx, const float* topk_gate, const void* w_gate_up, const void* w_down,
+                             const void* ws_gate_up, const void* ws_down, const int8_t* codes, const uint8_t* scales,
+                             const void* dy, void* d_x, float* d_gate, void* d_w_gate_up, void* d_w_down,
+                             void* d_ws_gate_up, void* d_ws_down, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
 /* maskmoe_status_string -- static, NUL-terminated description of a status code. */
 const char* maskmoe_status_string(int status);
 

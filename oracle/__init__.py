@@ -12,6 +12,10 @@ what the masked MoE hot path computes, written from the paper:
 * ``gate``     -- selection by scores, balance bias and expert groups, its gates
   and their gradient;
 * ``mx4``      -- microscaled 4-bit blocks and the expert FFNs on such weights;
+* ``mx8``      -- microscaled 8-bit blocks and the experts' training pass that keeps
+  its pre-activations in them;
+* ``norm``     -- the root-mean-square norm with the residual's addition, and its
+  gradient;
 * ``cache``    -- the per-layer expert cache of the trace simulator and the
   hit-rate / fetches-per-token metrics (Section 4.1, Eq. 5);
 * ``offload``  -- a batch-1 offloaded decode of one layer: the experts each
@@ -34,4 +38,4 @@ particular prior strengths have no value printed in the paper to compare
 with; they are pinned only through the cache rules above.
 """
 
-from . import cache, ffn, gate, mx4, offload, routing, train  # noqa: F401
+from . import cache, ffn, gate, mx4, mx8, norm, offload, routing, train  # noqa: F401

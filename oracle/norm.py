@@ -1,0 +1,37 @@
+"""Root-mean-square norm with the residual's addition, and its gradient, in float64, with bounds on what a computation in
+fp32 that rounds its outputs once may be off by. ``u32`` is the relative error of one fp32 operation, ``half`` that of the
+output's rounding (2^-24 for fp32, 2^-8 for bf16)."""
+
+import numpy as np
+
+U32 = 2.0 ** -24
+
+
+def forward(x, residual, weight, eps, half):
+    """(s, bound on hidden, y, bound on fp32 y, bound on y)."""
+    s = x if residual is None else x + residual
+    d = s.shape[-1]
+    rstd = 1 / np.sqrt((s * s).mean(-1, keepdims=True) + eps)
+    y = s * rstd * weight
+    # s one rounding; each of the d squares and d - 1 additions another, the mean, eps and the root a few more: half of
+    # a relative error of the sum reaches rstd
+    e_y = np.abs(y) * ((d + 8) / 2 + 8) * U32
+    return s, np.abs(s) * (U32 + half), y, e_y, e_y + (np.abs(y) + e_y) * half
+
+
+def backward(h, weight, dy, d_hidden, eps, half):
+    """(d_x, bound, d_weight, bound): the derivative of <dy, y(h)> + <d_hidden, h>."""
+    T, d = h.shape
+    rstd = 1 / np.sqrt((h * h).mean(-1, keepdims=True) + eps)
+    n, wg = h * rstd, weight * dy
+    c = (wg * n).mean(-1, keepdims=True)
+    dx = rstd * (wg - n * c)
+    rel = (d + 16) * U32                       # of n, of c's terms, of rstd
+    e_c = (np.abs(wg) * np.abs(n)).mean(-1, keepdims=True) * 2 * rel
+    e = rstd * (np.abs(wg) * rel + np.abs(n) * (e_c + np.abs(c) * 2 * rel)) + np.abs(dx) * rel
+    if d_hidden is not None:
+        dx = dx + d_hidden
+        e = e + (np.abs(dx) + np.abs(d_hidden)) * 2 * U32
+    dw = (dy * n).sum(0)
+    e_w = (np.abs(dy) * np.abs(n)).sum(0) * (rel + (T + 4) * U32)
+    return dx, e + (np.abs(dx) + e) * half, dw, e_w

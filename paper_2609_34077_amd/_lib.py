@@ -36,7 +36,10 @@ EXPORTS = ("maskmoe_route", "maskmoe_route_workspace_bytes", "maskmoe_layer_work
            "maskmoe_layer_forward_lora", "maskmoe_offload_workspace_bytes", "maskmoe_offload_decode_step",
            "maskmoe_pack_expert_weights", "maskmoe_layer_forward_noalloc", "maskmoe_gate_forward",
            "maskmoe_gate_backward", "maskmoe_mx4_quantize", "maskmoe_mx4_dequantize", "maskmoe_mx4_packed_bytes",
-           "maskmoe_mx4_pack_experts", "maskmoe_experts_mx4_workspace_bytes", "maskmoe_experts_forward_mx4")
+           "maskmoe_mx4_pack_experts", "maskmoe_experts_mx4_workspace_bytes", "maskmoe_experts_forward_mx4",
+           "maskmoe_mx8_quantize", "maskmoe_mx8_dequantize", "maskmoe_norm_forward",
+           "maskmoe_norm_backward_workspace_bytes", "maskmoe_norm_backward", "maskmoe_experts_train_workspace_bytes",
+           "maskmoe_experts_forward_train", "maskmoe_experts_backward_workspace_bytes", "maskmoe_experts_backward")
 NUM_STAGES = 5
 STAGES = ("route", "permute", "gate_up", "down", "combine")
 
@@ -160,6 +163,24 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.maskmoe_experts_forward_mx4.argtypes = [ctypes.POINTER(LayerDesc), _i32, _vp, _vp, _vp,
                                                 ctypes.POINTER(Mx4Experts), _vp, _vp, _sz, _vp]
     lib.maskmoe_experts_forward_mx4.restype = ctypes.c_int
+    lib.maskmoe_mx8_quantize.argtypes = [ctypes.c_int64, _i32, _i32, _vp, _vp, _vp, _vp]
+    lib.maskmoe_mx8_quantize.restype = ctypes.c_int
+    lib.maskmoe_mx8_dequantize.argtypes = [ctypes.c_int64, _i32, _i32, _vp, _vp, _vp, _vp]
+    lib.maskmoe_mx8_dequantize.restype = ctypes.c_int
+    lib.maskmoe_norm_forward.argtypes = [_i32, _i32, _i32, ctypes.c_float] + [_vp] * 8
+    lib.maskmoe_norm_forward.restype = ctypes.c_int
+    lib.maskmoe_norm_backward_workspace_bytes.argtypes = [_i32, _i32]
+    lib.maskmoe_norm_backward_workspace_bytes.restype = _sz
+    lib.maskmoe_norm_backward.argtypes = [_i32, _i32, _i32, ctypes.c_float] + [_vp] * 7 + [_sz, _vp]
+    lib.maskmoe_norm_backward.restype = ctypes.c_int
+    lib.maskmoe_experts_train_workspace_bytes.argtypes = [ctypes.POINTER(LayerDesc)]
+    lib.maskmoe_experts_train_workspace_bytes.restype = _sz
+    lib.maskmoe_experts_forward_train.argtypes = [ctypes.POINTER(LayerDesc)] + [_vp] * 11 + [_sz, _vp]
+    lib.maskmoe_experts_forward_train.restype = ctypes.c_int
+    lib.maskmoe_experts_backward_workspace_bytes.argtypes = [ctypes.POINTER(LayerDesc)]
+    lib.maskmoe_experts_backward_workspace_bytes.restype = _sz
+    lib.maskmoe_experts_backward.argtypes = [ctypes.POINTER(LayerDesc)] + [_vp] * 18 + [_sz, _vp]
+    lib.maskmoe_experts_backward.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -806,3 +827,242 @@ def maskmoe_experts_forward_mx4(x, topk_idx, topk_gate, experts: PackedMx4Expert
         ctypes.byref(desc), act, x.data_ptr(), topk_idx.data_ptr(), topk_gate.data_ptr(), ctypes.byref(experts.struct),
         y.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
     return y
+
+
+def maskmoe_mx8_quantize(x):
+    """8-bit blocks of x [..., cols] (bf16 or fp32, cols a multiple of 32) along its last dimension: codes [..., cols]
+    int8 and scales [..., cols/32] uint8; values are ``codes * 2**(scales - 133)``."""
+    lib = load()
+    shape, cols = _rows32(x, "x")
+    codes = x.new_empty(shape, dtype=_torch().int8)
+    scales = x.new_empty(shape[:-1] + (cols // 32,), dtype=_torch().uint8)
+    _check("maskmoe_mx8_quantize", lib.maskmoe_mx8_quantize(x.numel() // cols, cols, _dtype_code(x), x.data_ptr(),
+                                                            codes.data_ptr(), scales.data_ptr(), _stream()))
+    return codes, scales
+
+
+def maskmoe_mx8_dequantize(codes, scales, dtype):
+    """The values of codes [..., cols] int8 and scales [..., cols/32] uint8 as a bf16 or fp32 tensor [..., cols]."""
+    torch = _torch()
+    lib = load()
+    shape, cols = _rows32(codes, "codes")
+    here = torch.cuda.current_device()
+    _want(codes, "codes", shape, torch.int8, here)
+    _want(scales, "scales", shape[:-1] + (cols // 32,), torch.uint8, here)
+    out = codes.new_empty(shape, dtype=dtype)
+    _check("maskmoe_mx8_dequantize", lib.maskmoe_mx8_dequantize(codes.numel() // cols, cols, _dtype_code(out),
+                                                                codes.data_ptr(), scales.data_ptr(), out.data_ptr(),
+                                                                _stream()))
+    return out
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _rows32(t, name: str):
+    """Shape and row length of a contiguous tensor on the current device whose last dimension is whole blocks of 32."""
+    shape = t.shape
+    cols = shape[-1] if shape else 0
+    if cols == 0 or cols % 32:
+        raise ValueError(f"the last dimension of {name} must be a positive multiple of 32")
+    _fits(cols)
+    _want(t, name, shape, t.dtype, _torch().cuda.current_device())
+    return shape, cols
+
+
+def maskmoe_norm_forward(x, weight, residual=None, eps: float = 1e-5, with_y: bool = True, with_mx8: bool = False,
+                         hidden=None, y=None):
+    """Root-mean-square norm of the rows of x [..., d] (bf16 or fp32), after adding ``residual`` [..., d] when given:
+    ``s = x + residual; y = s / sqrt(mean(s**2) + eps) * weight``. weight [d]; all of one dtype.
+
+    Returns ``(y, hidden, codes, scales)``: y [..., d] (None without ``with_y``), hidden = s (None without a
+    residual unless a buffer is given), codes [..., d] int8 and scales [..., d/32] uint8, y's 8-bit blocks (None without
+    ``with_mx8``). ``hidden`` and ``y``: output buffers; hidden may be x or residual itself (in place), y too."""
+    torch = _torch()
+    lib = load()
+    shape = x.shape
+    if not shape or shape[-1] == 0:
+        raise ValueError("x must have rows of at least one element")
+    d = shape[-1]
+    T = x.numel() // d
+    _fits(T, d)
+    here = torch.cuda.current_device()
+    _want(x, "x", shape, x.dtype, here)
+    _want(weight, "weight", (d,), x.dtype, here)
+    if residual is not None:
+        _want(residual, "residual", shape, x.dtype, here)
+    if hidden is not None:
+        _want(hidden, "hidden", shape, x.dtype, here)
+    elif residual is not None:
+        hidden = torch.empty_like(x)
+    if y is not None:
+        _want(y, "y", shape, x.dtype, here)
+    elif with_y:
+        y = torch.empty_like(x)
+    codes = scales = None
+    if with_mx8:
+        codes = x.new_empty(shape, dtype=torch.int8)
+        scales = x.new_empty(shape[:-1] + (d // 32,), dtype=torch.uint8)
+    _check("maskmoe_norm_forward", lib.maskmoe_norm_forward(T, d, _dtype_code(x), eps, x.data_ptr(), _ptr(residual),
+                                                            weight.data_ptr(), _ptr(hidden), _ptr(y), _ptr(codes),
+                                                            _ptr(scales), _stream()))
+    return y, hidden, codes, scales
+
+
+def maskmoe_norm_backward_workspace_bytes(T: int, d: int) -> int:
+    _fits(T, d)
+    return int(load().maskmoe_norm_backward_workspace_bytes(T, d))
+
+
+def maskmoe_norm_backward(hidden, weight, dy, d_hidden=None, eps: float = 1e-5, with_d_weight: bool = True, d_x=None,
+                          workspace=None):
+    """Gradients of maskmoe_norm_forward from the ``hidden`` [..., d] it stored (x where there was no residual), for a
+    cotangent ``dy`` of y and ``d_hidden`` of hidden (None: nothing arrives along the stream). Returns ``(d_x [..., d],
+    d_weight [d] fp32 or None)``; d_x is the gradient of x and of the residual. ``d_x``: output buffer, which may be
+    dy, d_hidden or hidden itself."""
+    torch = _torch()
+    lib = load()
+    shape = hidden.shape
+    if not shape or shape[-1] == 0:
+        raise ValueError("hidden must have rows of at least one element")
+    d = shape[-1]
+    T = hidden.numel() // d
+    _fits(T, d)
+    here = torch.cuda.current_device()
+    _want(hidden, "hidden", shape, hidden.dtype, here)
+    _want(weight, "weight", (d,), hidden.dtype, here)
+    _want(dy, "dy", shape, hidden.dtype, here)
+    if d_hidden is not None:
+        _want(d_hidden, "d_hidden", shape, hidden.dtype, here)
+    if d_x is None:
+        d_x = torch.empty_like(hidden)
+    else:
+        _want(d_x, "d_x", shape, hidden.dtype, here)
+    d_weight, ws_bytes = None, 0
+    if with_d_weight:
+        d_weight = hidden.new_empty(d, dtype=torch.float32)
+        if workspace is None:
+            workspace = hidden.new_empty(max(int(lib.maskmoe_norm_backward_workspace_bytes(T, d)), 1), dtype=torch.uint8)
+        elif workspace.get_device() != here or not workspace.is_contiguous():
+            _refuse(workspace, "workspace")
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _check("maskmoe_norm_backward", lib.maskmoe_norm_backward(
+        T, d, _dtype_code(hidden), eps, hidden.data_ptr(), weight.data_ptr(), dy.data_ptr(), _ptr(d_hidden),
+        d_x.data_ptr(), _ptr(d_weight), _ptr(workspace) if with_d_weight else None, ws_bytes, _stream()))
+    return d_x, d_weight
+
+
+def maskmoe_experts_train_workspace_bytes(T: int, d: int, E: int, K: int, F: int, n_shared: int = 0) -> int:
+    _fits(T, d, E, K, F, n_shared)
+    return int(load().maskmoe_experts_train_workspace_bytes(ctypes.byref(make_desc(T, d, E, K, F, n_shared))))
+
+
+def maskmoe_experts_backward_workspace_bytes(T: int, d: int, E: int, K: int, F: int, n_shared: int = 0) -> int:
+    _fits(T, d, E, K, F, n_shared)
+    return int(load().maskmoe_experts_backward_workspace_bytes(ctypes.byref(make_desc(T, d, E, K, F, n_shared))))
+
+
+def _experts_train_desc(T, d, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down, here):
+    """Checks routing and weights of a training pass; its desc."""
+    torch = _torch()
+    if topk_idx.dim() != 2 or w_gate_up.dim() != 3:
+        raise ValueError("topk_idx must be 2-d and w_gate_up 3-d")
+    K, (E, F2, _) = topk_idx.shape[1], w_gate_up.shape
+    F = F2 // 2
+    ns = 0 if ws_gate_up is None else ws_gate_up.shape[0]
+    _fits(T, d, E, K, F2, ns)
+    _want(topk_idx, "topk_idx", (T, K), torch.int32, here)
+    _want(topk_gate, "topk_gate", (T, K), torch.float32, here)
+    if (ws_gate_up is None) != (ws_down is None):
+        raise ValueError("ws_gate_up and ws_down: both or neither")
+    for t, name, shape in ((w_gate_up, "w_gate_up", (E, 2 * F, d)), (w_down, "w_down", (E, d, F)),
+                           (ws_gate_up, "ws_gate_up", (ns, 2 * F, d)), (ws_down, "ws_down", (ns, d, F))):
+        if t is not None:
+            _want(t, name, shape, torch.bfloat16, here)
+    return make_desc(T, d, E, K, F, ns)
+
+
+def _train_workspace(workspace, need: int, like, here: int):
+    if workspace is None:
+        return like.new_empty(max(need, 1), dtype=_torch().uint8)
+    if workspace.get_device() != here or not workspace.is_contiguous():
+        _refuse(workspace, "workspace")
+    return workspace
+
+
+def maskmoe_experts_forward_train(x, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up=None, ws_down=None,
+                                  workspace=None, y=None, codes=None, scales=None):
+    """The routed and shared experts of a layer for a given routing (topk_idx [T,K] int32, entries outside the routed
+    experts add nothing; topk_gate [T,K] fp32), keeping the gate / up pre-activations in 8-bit blocks for
+    maskmoe_experts_backward. x [T,d] bf16, weights as maskmoe_layer_forward.
+
+    Returns ``(y [T,d], codes [T*(K+n_shared), 2F] int8, scales [T*(K+n_shared), 2F/32] uint8)``; rows by expert (shared
+    ones last), then token and slot; the last rows, one for each entry without an expert, are not written."""
+    torch = _torch()
+    lib = load()
+    if x.dim() != 2:
+        raise ValueError("x must be 2-d")
+    T, d = x.shape
+    here = torch.cuda.current_device()
+    _want(x, "x", (T, d), torch.bfloat16, here)
+    desc = _experts_train_desc(T, d, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down, here)
+    rows, F2 = T * (desc.K + desc.n_shared), 2 * desc.F
+    if codes is None:
+        codes = x.new_empty((rows, F2), dtype=torch.int8)
+    else:
+        _want(codes, "codes", (rows, F2), torch.int8, here)
+    if scales is None:
+        scales = x.new_empty((rows, F2 // 32), dtype=torch.uint8)
+    else:
+        _want(scales, "scales", (rows, F2 // 32), torch.uint8, here)
+    if y is None:
+        y = torch.empty_like(x)
+    else:
+        _want(y, "y", (T, d), torch.bfloat16, here)
+    workspace = _train_workspace(workspace, int(lib.maskmoe_experts_train_workspace_bytes(ctypes.byref(desc))), x, here)
+    _check("maskmoe_experts_forward_train", lib.maskmoe_experts_forward_train(
+        ctypes.byref(desc), x.data_ptr(), topk_idx.data_ptr(), topk_gate.data_ptr(), w_gate_up.data_ptr(),
+        w_down.data_ptr(), _ptr(ws_gate_up), _ptr(ws_down), y.data_ptr(), codes.data_ptr(), scales.data_ptr(),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+    return y, codes, scales
+
+
+def maskmoe_experts_backward(x, topk_idx, topk_gate, w_gate_up, w_down, codes, scales, dy, ws_gate_up=None,
+                             ws_down=None, x_scales=None, with_d_gate: bool = True, workspace=None):
+    """Gradients of maskmoe_experts_forward_train for a cotangent dy [T,d] bf16 of y, from the codes and scales it
+    returned. x [T,d] bf16 as in the forward, or its 8-bit blocks' codes [T,d] int8 with ``x_scales`` [T,d/32].
+
+    Returns a dict: d_x [T,d] bf16, d_gate [T,K] fp32 (None without ``with_d_gate``; it continues in
+    maskmoe_gate_backward), d_w_gate_up [E,2F,d], d_w_down [E,d,F], d_ws_gate_up, d_ws_down (None without shared experts),
+    bf16."""
+    torch = _torch()
+    lib = load()
+    if x.dim() != 2:
+        raise ValueError("x must be 2-d")
+    T, d = x.shape
+    here = torch.cuda.current_device()
+    if x_scales is None:
+        _want(x, "x", (T, d), torch.bfloat16, here)
+    else:
+        _want(x, "x", (T, d), torch.int8, here)
+        _want(x_scales, "x_scales", (T, d // 32), torch.uint8, here)
+    desc = _experts_train_desc(T, d, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down, here)
+    rows, F2 = T * (desc.K + desc.n_shared), 2 * desc.F
+    _want(codes, "codes", (rows, F2), torch.int8, here)
+    _want(scales, "scales", (rows, F2 // 32), torch.uint8, here)
+    _want(dy, "dy", (T, d), torch.bfloat16, here)
+    workspace = _train_workspace(workspace, int(lib.maskmoe_experts_backward_workspace_bytes(ctypes.byref(desc))), dy,
+                                 here)
+    out = dict(d_x=torch.empty_like(dy), d_gate=torch.empty_like(topk_gate) if with_d_gate else None,
+               d_w_gate_up=torch.empty_like(w_gate_up), d_w_down=torch.empty_like(w_down),
+               d_ws_gate_up=None if ws_gate_up is None else torch.empty_like(ws_gate_up),
+               d_ws_down=None if ws_down is None else torch.empty_like(ws_down))
+    _check("maskmoe_experts_backward", lib.maskmoe_experts_backward(
+        ctypes.byref(desc), x.data_ptr(), _ptr(x_scales), topk_idx.data_ptr(), topk_gate.data_ptr(),
+        w_gate_up.data_ptr(), w_down.data_ptr(), _ptr(ws_gate_up), _ptr(ws_down), codes.data_ptr(), scales.data_ptr(),
+        dy.data_ptr(), out["d_x"].data_ptr(), _ptr(out["d_gate"]), out["d_w_gate_up"].data_ptr(),
+        out["d_w_down"].data_ptr(), _ptr(out["d_ws_gate_up"]), _ptr(out["d_ws_down"]), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream()))
+    return out

@@ -1,0 +1,190 @@
+// C-ABI entry points of 8-bit blocks, the norm before a layer, and the experts' training pass at a given routing:
+// argument validation and launches. Nothing is enqueued before every argument has been checked.
+
+#include <math.h>
+#include <stdint.h>
+
+#include "maskmoe.h"
+#include "mx8.hpp"
+#include "norm.hpp"
+#include "train_experts.hpp"
+
+namespace {
+
+constexpr int64_t kLim = int64_t{1} << 31;
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+int hip_status(hipError_t e) { return e == hipSuccess ? MASKMOE_OK : MASKMOE_E_HIP; }
+bool known(int32_t dtype) { return dtype == MASKMOE_BF16 || dtype == MASKMOE_F32; }
+
+int check_mx8(int64_t rows, int32_t cols, int32_t dtype, const void* v, const void* codes, const void* scales) {
+  if (rows < 0 || cols < 1 || !known(dtype)) return MASKMOE_E_INVAL;
+  if (cols % 32 != 0 || rows > (int64_t{1} << 40) / cols) return MASKMOE_E_UNSUPPORTED;
+  if (rows > 0 && (!v || !codes || !scales)) return MASKMOE_E_INVAL;
+  if (!aligned(v, 16) || !aligned(codes, 16)) return MASKMOE_E_INVAL;
+  return MASKMOE_OK;
+}
+
+int check_norm(int32_t T, int32_t d, int32_t dtype, float eps) {
+  if (T < 0 || d < 1 || !known(dtype) || !(eps >= 0.0f) || !isfinite(eps)) return MASKMOE_E_INVAL;
+  return d > maskmoe::kNormMaxD ? MASKMOE_E_UNSUPPORTED : MASKMOE_OK;
+}
+
+int check_train(const maskmoe_layer_desc* d) {
+  if (!d || d->T < 0 || d->d < 1 || d->F < 1 || d->E < 1 || d->E > 256 || d->K < 1 || d->K > d->E || d->K > 16 ||
+      d->n_shared < 0 || d->n_shared > 8 || !known(d->dtype))
+    return MASKMOE_E_INVAL;
+  if (d->dtype != MASKMOE_BF16 || d->d % 64 != 0 || d->F % 64 != 0) return MASKMOE_E_UNSUPPORTED;
+  const int64_t rows = static_cast<int64_t>(d->T) * (d->K + d->n_shared);   // the products' 32-bit offsets
+  if (static_cast<int64_t>(d->T) * d->d >= kLim || rows * 2 * d->F >= kLim || rows * d->d >= kLim ||
+      int64_t{2} * d->F * d->d >= kLim)
+    return MASKMOE_E_UNSUPPORTED;
+  return MASKMOE_OK;
+}
+
+// What both directions read.
+int check_train_inputs(const maskmoe_layer_desc& d, const void* x, const int32_t* idx, const float* gate, const void* wg,
+                       const void* wd, const void* sg, const void* sd, const void* codes, const void* scales) {
+  if (!x || !idx || !gate || !wg || !wd || !codes || !scales) return MASKMOE_E_INVAL;
+  if (d.n_shared > 0 && (!sg || !sd)) return MASKMOE_E_INVAL;
+  for (const void* p : {x, wg, wd, sg, sd, codes})
+    if (!aligned(p, 16)) return MASKMOE_E_INVAL;
+  return aligned(idx, 4) && aligned(gate, 4) ? MASKMOE_OK : MASKMOE_E_INVAL;
+}
+
+maskmoe::ExpertsTrainArgs train_args(const maskmoe_layer_desc& d, const void* x, const int32_t* idx, const float* gate,
+                                     const void* wg, const void* wd, const void* sg, const void* sd) {
+  auto u16 = [](const void* p) { return static_cast<const uint16_t*>(p); };
+  maskmoe::ExpertsTrainArgs a{};
+  a.x = u16(x);
+  a.idx = idx;
+  a.gate = gate;
+  a.w_gate_up = u16(wg);
+  a.w_down = u16(wd);
+  a.ws_gate_up = u16(sg);
+  a.ws_down = u16(sd);
+  a.T = d.T; a.d = d.d; a.F = d.F; a.E = d.E; a.K = d.K; a.n_shared = d.n_shared;
+  return a;
+}
+
+maskmoe::ExpertsTrainLayout train_layout(const maskmoe_layer_desc& d) {
+  return maskmoe::experts_train_layout(d.T, d.d, d.F, d.E, d.K, d.n_shared);
+}
+
+}  // namespace
+
+extern "C" {
+
+int maskmoe_mx8_quantize(int64_t rows, int32_t cols, int32_t dtype, const void* src, int8_t* codes, uint8_t* scales,
+                         hipStream_t stream) {
+  const int st = check_mx8(rows, cols, dtype, src, codes, scales);
+  if (st != MASKMOE_OK || rows == 0) return st;
+  return hip_status(maskmoe::launch_mx8_quantize(dtype == MASKMOE_BF16, src, rows, cols, codes, scales, stream));
+}
+
+int maskmoe_mx8_dequantize(int64_t rows, int32_t cols, int32_t dtype, const int8_t* codes, const uint8_t* scales,
+                           void* dst, hipStream_t stream) {
+  const int st = check_mx8(rows, cols, dtype, dst, codes, scales);
+  if (st != MASKMOE_OK || rows == 0) return st;
+  return hip_status(maskmoe::launch_mx8_dequantize(dtype == MASKMOE_BF16, codes, scales, rows, cols, dst, stream));
+}
+
+int maskmoe_norm_forward(int32_t T, int32_t d, int32_t dtype, float eps, const void* x, const void* residual,
+                         const void* weight, void* hidden, void* y, int8_t* codes, uint8_t* scales, hipStream_t stream) {
+  const int st = check_norm(T, d, dtype, eps);
+  if (st != MASKMOE_OK) return st;
+  if (!codes != !scales) return MASKMOE_E_INVAL;
+  if (codes && d % 32 != 0) return MASKMOE_E_UNSUPPORTED;
+  if (T == 0) return MASKMOE_OK;
+  if (!x || !weight || (!hidden && !y && !codes) || (y && y == hidden)) return MASKMOE_E_INVAL;
+  for (const void* p : {x, residual, weight, static_cast<const void*>(hidden), static_cast<const void*>(y)})
+    if (!aligned(p, dtype == MASKMOE_BF16 ? 2 : 4)) return MASKMOE_E_INVAL;
+  const maskmoe::NormArgs a{x, residual, weight, hidden, y, codes, scales, T, d, eps, dtype == MASKMOE_BF16};
+  return hip_status(maskmoe::launch_norm_forward(a, stream));
+}
+
+size_t maskmoe_norm_backward_workspace_bytes(int32_t T, int32_t d) {
+  if (T < 0 || d < 1 || d > maskmoe::kNormMaxD) return 0;
+  return static_cast<size_t>(maskmoe::norm_backward_parts(T, d)) * d * 4;
+}
+
+int maskmoe_norm_backward(int32_t T, int32_t d, int32_t dtype, float eps, const void* hidden, const void* weight,
+                          const void* dy, const void* d_hidden, void* d_x, float* d_weight, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream) {
+  const int st = check_norm(T, d, dtype, eps);
+  if (st != MASKMOE_OK) return st;
+  if (T > 0 && (!hidden || !weight || !dy || !d_x)) return MASKMOE_E_INVAL;
+  for (const void* p : {hidden, weight, dy, d_hidden, static_cast<const void*>(d_x)})
+    if (!aligned(p, dtype == MASKMOE_BF16 ? 2 : 4)) return MASKMOE_E_INVAL;
+  if (!aligned(d_weight, 4)) return MASKMOE_E_INVAL;
+  const size_t need = maskmoe_norm_backward_workspace_bytes(T, d);
+  if (d_weight && need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return MASKMOE_E_WORKSPACE;
+  const maskmoe::NormBwdArgs a{hidden, weight, dy, d_hidden, d_x, d_weight, static_cast<float*>(workspace), T, d, eps,
+                               dtype == MASKMOE_BF16};
+  return hip_status(maskmoe::launch_norm_backward(a, stream));
+}
+
+size_t maskmoe_experts_train_workspace_bytes(const maskmoe_layer_desc* desc) {
+  return check_train(desc) == MASKMOE_OK ? train_layout(*desc).forward_total : 0;
+}
+
+int maskmoe_experts_forward_train(const maskmoe_layer_desc* desc, const void* x, const int32_t* topk_idx,
+                                  const float* topk_gate, const void* w_gate_up, const void* w_down,
+                                  const void* ws_gate_up, const void* ws_down, void* y, int8_t* codes, uint8_t* scales,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int st = check_train(desc);
+  if (st != MASKMOE_OK) return st;
+  const maskmoe_layer_desc& d = *desc;
+  if (d.T == 0) return MASKMOE_OK;
+  st = check_train_inputs(d, x, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down, codes, scales);
+  if (st != MASKMOE_OK) return st;
+  if (!y || !aligned(y, 16) || x == y) return MASKMOE_E_INVAL;
+  if (!workspace || workspace_bytes < train_layout(d).forward_total || !aligned(workspace, 256)) return MASKMOE_E_WORKSPACE;
+  maskmoe::ExpertsTrainArgs a = train_args(d, x, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down);
+  a.y = static_cast<uint16_t*>(y);
+  a.codes = codes;
+  a.scales = scales;
+  return hip_status(maskmoe::launch_experts_train(a, workspace, stream));
+}
+
+size_t maskmoe_experts_backward_workspace_bytes(const maskmoe_layer_desc* desc) {
+  return check_train(desc) == MASKMOE_OK ? train_layout(*desc).backward_total : 0;
+}
+
+int maskmoe_experts_backward(const maskmoe_layer_desc* desc, const void* x, const uint8_t* x_scales,
+                             const int32_t* topk_idx, const float* topk_gate, const void* w_gate_up, const void* w_down,
+                             const void* ws_gate_up, const void* ws_down, const int8_t* codes, const uint8_t* scales,
+                             const void* dy, void* d_x, float* d_gate, void* d_w_gate_up, void* d_w_down,
+                             void* d_ws_gate_up, void* d_ws_down, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream) {
+  int st = check_train(desc);
+  if (st != MASKMOE_OK) return st;
+  const maskmoe_layer_desc& d = *desc;
+  if (!d_w_gate_up || !d_w_down || (d.n_shared > 0 && (!d_ws_gate_up || !d_ws_down))) return MASKMOE_E_INVAL;
+  for (const void* p : {d_w_gate_up, d_w_down, d_ws_gate_up, d_ws_down})
+    if (!aligned(p, 16)) return MASKMOE_E_INVAL;
+  if (d.T > 0) {
+    st = check_train_inputs(d, x, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down, codes, scales);
+    if (st != MASKMOE_OK) return st;
+    if (!dy || !d_x || !aligned(dy, 16) || !aligned(d_x, 16) || !aligned(d_gate, 4) || d_x == dy || d_x == x)
+      return MASKMOE_E_INVAL;
+    if (!workspace || workspace_bytes < train_layout(d).backward_total || !aligned(workspace, 256))
+      return MASKMOE_E_WORKSPACE;
+  }
+  maskmoe::ExpertsBwdArgs b{};
+  b.f = train_args(d, x_scales ? nullptr : x, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down);
+  b.f.codes = const_cast<int8_t*>(codes);
+  b.f.scales = const_cast<uint8_t*>(scales);
+  b.x_codes = x_scales ? static_cast<const int8_t*>(x) : nullptr;
+  b.x_scales = x_scales;
+  b.dy = static_cast<const uint16_t*>(dy);
+  b.d_x = static_cast<uint16_t*>(d_x);
+  b.d_gate = d_gate;
+  b.d_w_gate_up = static_cast<uint16_t*>(d_w_gate_up);
+  b.d_w_down = static_cast<uint16_t*>(d_w_down);
+  b.d_ws_gate_up = static_cast<uint16_t*>(d_ws_gate_up);
+  b.d_ws_down = static_cast<uint16_t*>(d_ws_down);
+  return hip_status(maskmoe::launch_experts_backward(b, workspace, stream));
+}
+
+}  // extern "C"

@@ -20,10 +20,13 @@
 // accumulation is fp32; dX, dW are fp32.
 
 #include <mutex>
+#include <type_traits>
 
 #include "common.hpp"
 #include "gemm_tile.hpp"
 #include "kernels.hpp"
+#include "mx8.hpp"
+#include "train_experts.hpp"
 
 namespace maskmoe {
 namespace {
@@ -77,6 +80,11 @@ struct NtArgs {
   const int32_t* active;      // KSPLIT: the non-empty groups, n_active[0] of them
   const int32_t* n_active;
   const uint16_t* ab;         // SWIGLU_BWD: saved pre-activations [rows, 2N]
+  const int8_t* codes;        // SWIGLU_KEPT: 8-bit blocks of the pre-activations [rows, 2N]
+  const uint8_t* scales;      // SWIGLU_KEPT: [rows, 2N / 32]
+  const float* row_gate;      // SWIGLU_KEPT: gate of each row
+  uint16_t* gh;               // SWIGLU_KEPT: gate times SwiGLU activation [rows, N]
+  float* dgate_part;          // SWIGLU_KEPT: [rows, n_tiles] partial sums of u h
   void* c;                    // ROWS: [rows, ldc]; KSPLIT: routed groups' [M, N] matrices
   void* cs;                   // KSPLIT: shared groups' [M, N] matrices
   float* part;                // ROWS, fp32 output: partial tiles of split tail tiles (tile_job)
@@ -158,7 +166,7 @@ __device__ __forceinline__ void empty_groups(const int32_t* offsets, int G, uint
   }
 }
 
-// n: float4s of a matrix.
+// n: 16-byte pieces of a matrix.
 __device__ __forceinline__ void zero_slices(const uint64_t (&dead)[kDeadWords], int E, size_t n, int lid, int live,
                                             float* c, float* cs) {
   const size_t i0 = n * lid / live, i1 = n * (lid + 1) / live;
@@ -173,7 +181,128 @@ __device__ __forceinline__ void zero_slices(const uint64_t (&dead)[kDeadWords], 
 }
 
 enum { kNtRows = 0, kNtKSplit = 1 };
-enum { kEpiSwigluBwd = 0, kEpiF32 = 1 };
+enum { kEpiSwigluBwd = 0, kEpiF32 = 1, kEpiSwigluKept = 2, kEpiBf16 = 3 };
+
+// The finished tile (rows row0.., columns n0..) into out (row stride ld) as bf16, through LDS whole, so that it leaves in
+// 16-byte stores. ncol % 8 == 0.
+constexpr int kStgPitch16 = kTileN + 8;
+static_assert(kTileM * kStgPitch16 * 2 <= sizeof(TileLds), "a staged bf16 tile fits in LDS");
+__device__ __forceinline__ void nt_store_bf16(const f32x16 (&acc)[kTileTM][kTileTN], uint16_t* out, size_t ld, int row0,
+                                              int row_end, int n0, int ncol, TileLds& L) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 4, wn = wave % 4;
+  uint16_t* stg = reinterpret_cast<uint16_t*>(&L);
+  wait_lgkmcnt0();
+  tile_barrier();   // the k-loop's LDS reads are done
+#pragma unroll
+  for (int i = 0; i < kTileTM; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int j = 0; j < kTileTN; ++j)
+        stg[(wm * 128 + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kStgPitch16 + wn * 64 + j * 32 + (lane & 31)] =
+            f32_to_bf16(acc[i][j][r]);
+  wait_lgkmcnt0();
+  tile_barrier();
+#pragma unroll 4
+  for (int q = 0; q < 16; ++q) {   // 8192 pieces of eight columns: 32 per row
+    const int u = tid + kTileThreads * q;
+    const int pr = u >> 5, c = (u & 31) * 8, row = row0 + pr, col = n0 + c;
+    if (row < row_end && col < ncol)
+      *reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * ld + col) =
+          *reinterpret_cast<const u32x4*>(&stg[pr * kStgPitch16 + c]);
+  }
+}
+
+// Sum over each half of the wavefront, in its last lane.
+__device__ __forceinline__ float half_wave_sum(float v) {
+  auto add = [&](auto ctrl, auto rows) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value,
+                                                    0xF, false));
+  };
+  using std::integral_constant;
+  add(integral_constant<int, 0xB1>{}, integral_constant<int, 0xF>{});    // lanes 1 apart
+  add(integral_constant<int, 0x4E>{}, integral_constant<int, 0xF>{});    // 2 apart
+  add(integral_constant<int, 0x141>{}, integral_constant<int, 0xF>{});   // mirrored within 8
+  add(integral_constant<int, 0x140>{}, integral_constant<int, 0xF>{});   // mirrored within 16
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});   // lane 15 of rows 0, 2 to rows 1, 3
+  return v;
+}
+
+// Epilogue of u = dy W_down with the pre-activations in 8-bit blocks: da, db (bf16, [rows, 2N]), the gated SwiGLU
+// activation for the weight gradient (bf16, [rows, N]) and this tile's share of every row's d_gate = <u, h>. As
+// kEpiSwigluBwd's, the tile goes through LDS in two halves, a half's blocks loaded before it is staged.
+__device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x16 (&acc)[kTileTM][kTileTN], int row0,
+                                                     int row_end, int n0, int nt, TileLds& L) {
+  const int tid = threadIdx.x;
+  float* stg = reinterpret_cast<float*>(&L);
+  uint16_t* o = static_cast<uint16_t*>(p.c);
+  const size_t N = p.N;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint2 a8[8], b8[8];
+    uint32_t sa[8], sb[8];
+    float gate[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {   // 4096 pieces of 8 columns: 32 per staged row
+      const int u = tid + kTileThreads * q;
+      const int pr = u >> 5, col = n0 + (u & 31) * 8;
+      const int row = row0 + (pr >> 6) * 128 + 64 * h + (pr & 63);
+      a8[q] = b8[q] = make_uint2(0, 0);
+      sa[q] = sb[q] = 0;
+      gate[q] = 0.0f;
+      if (row < row_end && col < p.N) {
+        const size_t at = row * 2 * N + col;
+        a8[q] = *reinterpret_cast<const uint2*>(p.codes + at);
+        b8[q] = *reinterpret_cast<const uint2*>(p.codes + at + N);
+        sa[q] = p.scales[at / kMx8Block];
+        sb[q] = p.scales[(at + N) / kMx8Block];
+        gate[q] = p.row_gate[row];
+      }
+    }
+    wait_lgkmcnt0();
+    tile_barrier();   // the k-loop's (or the previous half's) LDS reads are done
+    stage_half(stg, acc, h);
+    wait_lgkmcnt0();
+    tile_barrier();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int u = tid + kTileThreads * q;
+      const int pr = u >> 5, cg = (u & 31) * 8, col = n0 + cg;
+      const int row = row0 + (pr >> 6) * 128 + 64 * h + (pr & 63);
+      const bool live = row < row_end && col < p.N;
+      float v[8], da[8], db[8], gh[8];
+      *reinterpret_cast<float4*>(&v[0]) = *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + cg]);
+      *reinterpret_cast<float4*>(&v[4]) = *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + cg + 4]);
+      const float s_a = mx8_step(sa[q]), s_b = mx8_step(sb[q]);
+      float dot = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float av = mx8_code_value(e < 4 ? a8[q].x : a8[q].y, e & 3) * s_a;
+        const float bv = mx8_code_value(e < 4 ? b8[q].x : b8[q].y, e & 3) * s_b;
+        const float s = sigmoid(av), hv = av * s * bv, gu = gate[q] * v[e];
+        dot += v[e] * hv;
+        da[e] = gu * bv * (s * (1.0f + av * (1.0f - s)));
+        db[e] = gu * av * s;
+        gh[e] = gate[q] * hv;
+      }
+      dot = half_wave_sum(live ? dot : 0.0f);   // 32 lanes hold a staged row
+      if ((u & 31) == 31 && row < row_end) p.dgate_part[static_cast<size_t>(row) * p.n_tiles + nt] = dot;
+      if (!live) continue;
+      uint16_t* dst = o + row * 2 * N + col;
+      u32x4 pa, pb, pg;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        pa[e] = f32x2_to_bf16x2(da[2 * e], da[2 * e + 1]);
+        pb[e] = f32x2_to_bf16x2(db[2 * e], db[2 * e + 1]);
+        pg[e] = f32x2_to_bf16x2(gh[2 * e], gh[2 * e + 1]);
+      }
+      *reinterpret_cast<u32x4*>(dst) = pa;
+      *reinterpret_cast<u32x4*>(dst + N) = pb;
+      *reinterpret_cast<u32x4*>(p.gh + row * N + col) = pg;
+    }
+  }
+}
+
 
 // ROWS (dgrad): group g's rows offsets[g]..offsets[g+1] of A (K-contiguous) times its own
 // K-major [K, N] matrix, row tiles enumerated by tile_off as in the forward. KSPLIT (wgrad): for
@@ -311,6 +440,17 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
         *reinterpret_cast<u32x4*>(dst + p.N) = *reinterpret_cast<const u32x4*>(db8);
       }
     }
+    return;
+  }
+  if constexpr (EPI == kEpiSwigluKept) {
+    swiglu_kept_epilogue(p, acc, row0, row_end, n0, nt, lds);
+    return;
+  }
+  if constexpr (EPI == kEpiBf16) {
+    const size_t mn = static_cast<size_t>(p.M) * p.N;
+    uint16_t* cb = g < p.E ? static_cast<uint16_t*>(p.c) + g * mn : static_cast<uint16_t*>(p.cs) + (g - p.E) * mn;
+    nt_store_bf16(acc, cb, p.N, row0, row_end, n0, p.N, lds);
+    zero_slices(dead, p.E, mn / 8, lid, live_tiles, static_cast<float*>(p.c), static_cast<float*>(p.cs));
     return;
   }
   float* cf = g < p.E ? static_cast<float*>(p.c) + static_cast<size_t>(g) * p.M * p.N
@@ -542,6 +682,62 @@ hipError_t launch_layer_backward(const BwdArgs& a, hipStream_t s) {
   (void)hipEventDestroy(fork);   // released once their waits are done
   (void)hipEventDestroy(join);
   return e;
+}
+
+// The five products of the gradient of experts whose pre-activations are kept in 8-bit blocks (train_experts.hip prepares
+// the rows and sums them up).
+hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s) {
+  const int G = a.G, d = a.d, F = a.F;
+  const size_t FD = static_cast<size_t>(F) * d;
+  NtArgs n{};
+  n.offsets = a.pb.offsets;
+  n.tile_off = a.pb.tile_off;
+  n.G = G; n.E = a.E;
+  n.mt_max = a.max_tiles;
+  n.cu_xcd = device_cus_per_xcd();
+  n.part = a.part;
+  // u = dy W_down and its epilogue
+  n.a = a.dyg; n.lda = d;
+  n.b = a.w_down; n.bs = a.ws_down; n.N = F; n.K = d; n.ldb = F;   // W_down [d, F]: K-major
+  n.codes = a.codes;
+  n.scales = a.scales;
+  n.row_gate = a.row_gate;
+  n.gh = a.gh;
+  n.dgate_part = a.dgate_part;
+  n.c = a.dab;
+  n.n_tiles = (F + kTileN - 1) / kTileN;
+  hipLaunchKernelGGL((gemm_nt_kernel<kNtRows, kEpiSwigluKept>), rows_grid(n.mt_max, n.n_tiles), dim3(kTileThreads), 0, s, n);
+  MASKMOE_TRY(hipGetLastError());
+  // rows of d_x = [da db] W_gate_up
+  n.a = a.dab; n.lda = 2 * F;
+  n.b = a.w_gate_up; n.bs = a.ws_gate_up; n.N = d; n.K = 2 * F; n.ldb = d;   // W_gate_up [2F, d]: K-major
+  n.c = a.dxr; n.ldc = d;
+  n.n_tiles = (d + kTileN - 1) / kTileN;
+  hipLaunchKernelGGL((gemm_nt_kernel<kNtRows, kEpiF32>), rows_grid(n.mt_max, n.n_tiles), dim3(kTileThreads), 0, s, n);
+  if (nt_tail_split(kNtRows, kEpiF32, n.K / kTileK))
+    hipLaunchKernelGGL(nt_tail_fixup, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(kTileThreads), 0, s, n);
+  MASKMOE_TRY(hipGetLastError());
+  // weight gradients over each expert's own rows; zeros for the others
+  NtArgs m{};
+  m.offsets = a.pb.offsets;
+  m.active = a.pb.active;
+  m.n_active = a.pb.n_active;
+  m.G = G; m.E = a.E;
+  m.a = a.dyg; m.lda = d; m.b = a.gh; m.ldb = F; m.M = d; m.N = F;   // dW_down [d, F] = dy^T (g h)
+  m.c = a.d_w_down; m.cs = a.d_ws_down;
+  m.mt_max = (d + kTileM - 1) / kTileM;
+  m.n_tiles = (F + kTileN - 1) / kTileN;
+  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dim3(G * m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
+  m.a = a.dab; m.lda = 2 * F; m.b = a.xg; m.ldb = d; m.M = 2 * F; m.N = d;   // dW_gate_up [2F, d] = [da db]^T x
+  m.c = a.d_w_gate_up; m.cs = a.d_ws_gate_up;
+  m.mt_max = (2 * F + kTileM - 1) / kTileM;
+  m.n_tiles = (d + kTileN - 1) / kTileN;
+  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dim3(G * m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
+  hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD / 2,
+                     static_cast<float*>(a.d_w_down), static_cast<float*>(a.d_ws_down));
+  hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD,
+                     static_cast<float*>(a.d_w_gate_up), static_cast<float*>(a.d_ws_gate_up));
+  return hipGetLastError();
 }
 
 }  // namespace maskmoe

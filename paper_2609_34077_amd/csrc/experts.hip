@@ -30,6 +30,8 @@
 #include "common.hpp"
 #include "gemm_tile.hpp"
 #include "kernels.hpp"
+#include "mx8.hpp"
+#include "train_experts.hpp"
 
 namespace maskmoe {
 namespace {
@@ -55,6 +57,8 @@ struct GemmArgs {
   int mt_max;               // bound on row tiles (the grid is sized for mt_max * n_tiles tiles)
   int n_tiles;              // column tiles
   int cu_xcd;               // workgroups an XCD runs at once (one per CU)
+  int8_t* codes;            // KEEP: 8-bit blocks of the gate / up pre-activations [rows, 2F]
+  uint8_t* scales;          // KEEP: [rows, 2F / 32]
   const int32_t* batch_off; // beside the batch path: its [G+1] tile offsets, and the launch runs only when
   int skew;                 // they are skewed (batch_skewed); else null
 };
@@ -148,12 +152,80 @@ __device__ __forceinline__ void gemm_epilogue(const GemmArgs& p, const f32x16 (&
   }
 }
 
+// Epilogue of a gate / up tile that keeps its pre-activations in 8-bit blocks: the fp32 tile goes through LDS in parts
+// of two fragment rows a wavefront (128 x 256 values), so that a thread then holds eight consecutive columns of a and
+// the same of b: the largest magnitude of a block comes from four lanes (in the accumulators' own layout a block lies
+// across 32 lanes, five exchanges for every value), and codes leave eight, H sixteen bytes at a time. F % 32 == 0, so
+// that a block is whole or past the matrix.
+constexpr int kKeptPitch = BN + 8;
+static_assert(128 * kKeptPitch * 4 <= sizeof(TileLds), "a staged part fits in LDS");
+template <int TM>
+__device__ __forceinline__ void gemm_epilogue_kept(const GemmArgs& p, const f32x16 (&acc)[TM][kTileTN], int row0,
+                                                   int row_end, int n0, TileLds& L) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave / 4, wn = wave % 4;
+  float* stg = reinterpret_cast<float*>(&L);
+  uint16_t* out = static_cast<uint16_t*>(p.out);
+  const size_t F = p.F;
+#pragma unroll
+  for (int part = 0; part < (TM + 1) / 2; ++part) {
+    wait_lgkmcnt0();
+    tile_barrier();   // the k-loop's (or the previous part's) LDS reads are done
+#pragma unroll
+    for (int ii = 0; ii < 2; ++ii)
+      if (2 * part + ii < TM)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int j = 0; j < kTileTN; ++j)
+            stg[(wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kKeptPitch + j * (BN / 2) + wn * 32 +
+                (lane & 31)] = acc[2 * part + ii < TM ? 2 * part + ii : 0][j][r];
+    wait_lgkmcnt0();
+    tile_barrier();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {   // 2048 pieces of eight columns: 16 per staged row
+      const int u = tid + GEMM_THREADS * q;
+      const int pr = u >> 4, cg = (u & 15) * 8, col = n0 + cg;
+      const int i = 2 * part + ((pr >> 5) & 1);
+      const int row = row0 + (pr >> 6) * 32 * TM + i * 32 + (pr & 31);
+      float a[8], b[8];
+      const float* src = stg + pr * kKeptPitch + cg;
+      *reinterpret_cast<f32x4*>(a) = *reinterpret_cast<const f32x4*>(src);
+      *reinterpret_cast<f32x4*>(a + 4) = *reinterpret_cast<const f32x4*>(src + 4);
+      *reinterpret_cast<f32x4*>(b) = *reinterpret_cast<const f32x4*>(src + BN / 2);
+      *reinterpret_cast<f32x4*>(b + 4) = *reinterpret_cast<const f32x4*>(src + BN / 2 + 4);
+      uint32_t ma = 0, mb = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ma = max(ma, __float_as_uint(a[e]) & 0x7fffffffu);
+        mb = max(mb, __float_as_uint(b[e]) & 0x7fffffffu);
+      }
+      const uint32_t ba = mx8_scale_byte(max_of_4_lanes(ma)), bb = mx8_scale_byte(max_of_4_lanes(mb));
+      if (i >= TM || row >= row_end || col >= p.F) continue;
+      u32x4 h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        h[e] = f32x2_to_bf16x2(silu(a[2 * e]) * b[2 * e], silu(a[2 * e + 1]) * b[2 * e + 1]);
+      *reinterpret_cast<u32x4*>(out + row * F + col) = h;
+      int8_t* c = p.codes + row * 2 * F + col;
+      *reinterpret_cast<uint2*>(c) = make_uint2(mx8_codes4(a[0], a[1], a[2], a[3], ba), mx8_codes4(a[4], a[5], a[6], a[7], ba));
+      *reinterpret_cast<uint2*>(c + F) = make_uint2(mx8_codes4(b[0], b[1], b[2], b[3], bb), mx8_codes4(b[4], b[5], b[6], b[7], bb));
+      if ((u & 3) == 0) {
+        uint8_t* sc = p.scales + (row * 2 * F + col) / kMx8Block;
+        sc[0] = static_cast<uint8_t>(ba);
+        sc[F / kMx8Block] = static_cast<uint8_t>(bb);
+      }
+    }
+  }
+}
+
 // A group's last row tile multiplies (and loads) only its 64-row pieces that hold rows, the two wave
 // groups sharing them evenly: 256-row tiles of a DeepSeek-shaped batch of 2000 tokens are a third
 // padding. Layers at 2000 tokens: DeepSeek-shaped, soft prior 488 -> 401 us (with adapters
 // 555 -> 489), 1000 tokens 386 -> 317; Mixtral-shaped, 400 tokens 664 -> 592.
 // PACKED: the expert matrices are in the packed layout (kPackRows x kPackCols blocks).
-template <int EPI, bool LORA = false, bool PACKED = false>
+// KEEP (EPI 0): the pre-activations are kept in 8-bit blocks.
+template <int EPI, bool LORA = false, bool PACKED = false, bool KEEP = false>
 __global__ __launch_bounds__(GEMM_THREADS) void grouped_gemm_bf16(const GemmArgs p) {
   constexpr int WN = 4;                 // waves: 2 along rows x 4 along columns
   constexpr int TN = kTileTN;
@@ -248,7 +320,8 @@ __global__ __launch_bounds__(GEMM_THREADS) void grouped_gemm_bf16(const GemmArgs
         return;
       }
     }
-    gemm_epilogue<EPI, TM>(p, acc, row0, row_end, n0, lds);
+    if constexpr (KEEP) gemm_epilogue_kept<TM>(p, acc, row0, row_end, n0, lds);
+    else gemm_epilogue<EPI, TM>(p, acc, row0, row_end, n0, lds);
   };
   if (tm == 4) tile(std::integral_constant<int, 4>{});
   else if (tm == 3) tile(std::integral_constant<int, 3>{});
@@ -951,6 +1024,24 @@ hipError_t launch_experts_bf16(const ExpertArgs& a, const PermBuffers& pb, uint1
   err = launch_combine(a, pb, O, true, 1, y, stream);
   record_mark(marks, 2, stream);
   return err;
+}
+
+hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, uint16_t* O, float* part,
+                               int8_t* codes, uint8_t* scales, int max_tiles, hipStream_t stream) {
+  GemmArgs g = gemm_args(0, a, pb, pb.tile_off, max_tiles, H, O, part, nullptr);
+  g.codes = codes;
+  g.scales = scales;
+  hipLaunchKernelGGL((grouped_gemm_bf16<0, false, false, true>), grouped_grid(max_tiles, g.n_tiles, false),
+                     dim3(GEMM_THREADS), 0, stream, g);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  g = gemm_args(1, a, pb, pb.tile_off, max_tiles, H, O, part, nullptr);
+  const bool tails = tail_can_split(1, a.F / BK);
+  launch_grouped<1>(false, false, grouped_grid(max_tiles, g.n_tiles, tails), g, stream);
+  err = hipGetLastError();
+  if (err != hipSuccess || !tails) return err;
+  hipLaunchKernelGGL(grouped_tail_fixup, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(GEMM_THREADS), 0, stream, g);
+  return hipGetLastError();
 }
 
 // Slices of the reduction dimension for the two streaming kernels. Measured on MI355X (a sweep

@@ -1,0 +1,353 @@
+// The root-mean-square norm before a layer, with the residual's addition, and its gradient (include/maskmoe.h,
+// maskmoe_norm_forward, maskmoe_norm_backward):
+//   s = x + residual,  h = s stored,  rstd = (mean_j s_j^2 + eps)^-1/2,  y_j = s_j rstd w_j  (in bf16 / fp32, 8-bit blocks)
+//   n = h rstd(h),  d_x = d_h + rstd (w dy - n mean_j(w dy n)),  d_w = sum_t dy n.
+//
+// Bound by HBM: a row is read once, kept in fp32 registers over its sum, and written once. N threads hold a row in V
+// pieces of 8 elements each; a workgroup has R = threads / N rows at a time and walks over the rest in steps of the
+// grid, its weights in registers. One barrier a step where a row spans wavefronts (the sums alternate between two LDS
+// buffers).
+
+#include <type_traits>
+
+#include "mx8.hpp"
+#include "norm.hpp"
+
+namespace maskmoe {
+namespace {
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_add(float v) {
+  const int o = __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xF, false);
+  return v + __int_as_float(o);
+}
+
+// Sum of the 64 lanes, in every lane.
+__device__ __forceinline__ float wave_sum(float v) {
+  v = dpp_add<0xB1, 0xF>(v);    // lanes 1 apart
+  v = dpp_add<0x4E, 0xF>(v);    // 2 apart
+  v = dpp_add<0x141, 0xF>(v);   // mirrored within 8
+  v = dpp_add<0x140, 0xF>(v);   // mirrored within 16
+  v = dpp_add<0x142, 0xA>(v);   // lane 15 of rows 0, 2 to rows 1, 3
+  v = dpp_add<0x143, 0xC>(v);   // lane 31 to rows 2, 3
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Sums of M values over the N threads of a row. red: M floats a wavefront of the workgroup, another buffer from one
+// call to the next.
+template <int N, int M>
+__device__ __forceinline__ void row_sum(float (&v)[M], float (*red)[M]) {
+#pragma unroll
+  for (int m = 0; m < M; ++m) v[m] = wave_sum(v[m]);
+  if constexpr (N > kWave) {
+    const int wave = threadIdx.x / kWave, first = wave & ~(N / kWave - 1);
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int m = 0; m < M; ++m) red[wave][m] = v[m];
+    lds_sync();
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      float s = red[first][m];
+#pragma unroll
+      for (int w = 1; w < N / kWave; ++w) s += red[first + w][m];
+      v[m] = s;
+    }
+  }
+}
+
+__device__ __forceinline__ float load1(bool bf16, const void* p, size_t i) {
+  return bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store1(bool bf16, void* p, size_t i, float v) {
+  if (bf16) static_cast<uint16_t*>(p)[i] = f32_to_bf16(v);
+  else static_cast<float*>(p)[i] = v;
+}
+
+// The 8 elements of a thread's piece p: columns 8 (p N + lane) .. of its row, in 16-byte accesses, or (VEC false: rows
+// or tensors that are not 16-byte aligned) columns p 8 N + lane + N j, element by element. Those at or past d are zero
+// and not stored.
+template <bool BF16, bool VEC, int N>
+struct Piece {
+  static __device__ __forceinline__ int col(int p, int lane, int j) {
+    return VEC ? 8 * (p * N + lane) + j : p * 8 * N + lane + N * j;
+  }
+  static __device__ __forceinline__ void load(const void* src, size_t row, int d, int p, int lane, float* v) {
+    if constexpr (VEC) {
+      if (col(p, lane, 0) < d) load_vec8<BF16>(src, row + col(p, lane, 0), v);
+      else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = col(p, lane, j) < d ? load1(BF16, src, row + col(p, lane, j)) : 0.0f;
+    }
+  }
+  static __device__ __forceinline__ void store(void* dst, size_t row, int d, int p, int lane, const float* v) {
+    if constexpr (VEC) {
+      if (col(p, lane, 0) < d) store_vec8<BF16>(dst, row + col(p, lane, 0), v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (col(p, lane, j) < d) store1(BF16, dst, row + col(p, lane, j), v[j]);
+    }
+  }
+};
+
+// 8-bit blocks of a piece; d % 32 == 0, so a block is whole or past the row. VEC: four lanes hold a block; else 32
+// lanes, one element each.
+template <bool VEC, int N>
+__device__ __forceinline__ void store_blocks(int8_t* codes, uint8_t* scales, size_t row, int d, int p, int lane,
+                                             const float* v) {
+  if constexpr (VEC) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+    const uint32_t byte = mx8_scale_byte(max_of_4_lanes(m));
+    const int c = 8 * (p * N + lane);
+    if (c >= d) return;
+    *reinterpret_cast<uint2*>(codes + row + c) =
+        make_uint2(mx8_codes4(v[0], v[1], v[2], v[3], byte), mx8_codes4(v[4], v[5], v[6], v[7], byte));
+    if ((lane & 3) == 0) scales[(row + c) / kMx8Block] = static_cast<uint8_t>(byte);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, kWave)));
+      const uint32_t byte = mx8_scale_byte(m);
+      const int c = p * 8 * N + lane + N * j;
+      if (c >= d) continue;
+      codes[row + c] = static_cast<int8_t>(byte == 255 ? 0u : mx8_code(v[j], byte));
+      if ((lane & 31) == 0) scales[(row + c) / kMx8Block] = static_cast<uint8_t>(byte);
+    }
+  }
+}
+
+template <int N>
+constexpr int kRowsOf = N >= 256 ? 1 : 256 / N;   // rows of a workgroup, forward
+
+template <bool BF16, bool VEC, int N, int V>
+__global__ __launch_bounds__(N* kRowsOf<N>) void norm_forward_kernel(const NormArgs a) {
+  using P = Piece<BF16, VEC, N>;
+  constexpr int R = kRowsOf<N>;
+  __shared__ float red[2][N * R / kWave][1];
+  const int lane = threadIdx.x % N, d = a.d;
+  float w[V][8];
+#pragma unroll
+  for (int p = 0; p < V; ++p) P::load(a.weight, 0, d, p, lane, w[p]);
+  const float inv_d = 1.0f / static_cast<float>(d);
+  int turn = 0;
+  for (int t0 = blockIdx.x * R; t0 < a.T; t0 += gridDim.x * R, turn ^= 1) {
+    const int t = t0 + threadIdx.x / N;
+    const bool live = t < a.T;
+    const size_t row = static_cast<size_t>(live ? t : a.T - 1) * d;   // past the end: the last row, not stored
+    const int dl = live ? d : 0;
+    float s[V][8];
+#pragma unroll
+    for (int p = 0; p < V; ++p) P::load(a.x, row, d, p, lane, s[p]);
+    if (a.residual) {
+      float r[V][8];
+#pragma unroll
+      for (int p = 0; p < V; ++p) P::load(a.residual, row, d, p, lane, r[p]);
+#pragma unroll
+      for (int p = 0; p < V; ++p)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[p][j] += r[p][j];
+    }
+    if (a.hidden)
+#pragma unroll
+      for (int p = 0; p < V; ++p) P::store(a.hidden, row, dl, p, lane, s[p]);
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int p = 0; p < V; ++p)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[0] += s[p][j] * s[p][j];
+    row_sum<N, 1>(sum, red[turn]);
+    const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
+#pragma unroll
+    for (int p = 0; p < V; ++p)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[p][j] = s[p][j] * rstd * w[p][j];
+    if (a.y)
+#pragma unroll
+      for (int p = 0; p < V; ++p) P::store(a.y, row, dl, p, lane, s[p]);
+    if (a.codes)
+#pragma unroll
+      for (int p = 0; p < V; ++p) store_blocks<VEC, N>(a.codes, a.scales, row, dl, p, lane, s[p]);
+  }
+}
+
+// Rows of a workgroup in the gradient: its sums over tokens leave the workgroup once, so fewer and larger ones.
+template <int N>
+constexpr int kBwdRowsOf = 1024 / N;
+
+template <bool BF16, bool VEC, int N, int V>
+__global__ __launch_bounds__(1024) void norm_backward_kernel(const NormBwdArgs a) {
+  using P = Piece<BF16, VEC, N>;
+  constexpr int R = kBwdRowsOf<N>;
+  __shared__ float red[2][1024 / kWave][2];
+  __shared__ float dws[R > 1 ? (R / 2) * N * 8 : 1];
+  const int lane = threadIdx.x % N, sub = threadIdx.x / N, d = a.d;
+  float w[V][8], dw[V][8];
+#pragma unroll
+  for (int p = 0; p < V; ++p) {
+    P::load(a.weight, 0, d, p, lane, w[p]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[p][j] = 0.0f;
+  }
+  const float inv_d = 1.0f / static_cast<float>(d);
+  int turn = 0;
+  for (int t0 = blockIdx.x * R; t0 < a.T; t0 += gridDim.x * R, turn ^= 1) {
+    const int t = t0 + sub;
+    const bool live = t < a.T;
+    const size_t row = static_cast<size_t>(live ? t : a.T - 1) * d;
+    const int dl = live ? d : 0;
+    float h[V][8], g[V][8], r[V][8];
+#pragma unroll
+    for (int p = 0; p < V; ++p) P::load(a.hidden, row, d, p, lane, h[p]);
+#pragma unroll
+    for (int p = 0; p < V; ++p) P::load(a.dy, row, d, p, lane, g[p]);
+    if (a.d_hidden)
+#pragma unroll
+      for (int p = 0; p < V; ++p) P::load(a.d_hidden, row, d, p, lane, r[p]);
+    float sum[2] = {0.0f, 0.0f};   // h^2 and w dy h
+#pragma unroll
+    for (int p = 0; p < V; ++p)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sum[0] += h[p][j] * h[p][j];
+        sum[1] += g[p][j] * w[p][j] * h[p][j];
+      }
+    row_sum<N, 2>(sum, red[turn]);
+    const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
+    const float c = sum[1] * rstd * inv_d;   // mean of w dy n
+#pragma unroll
+    for (int p = 0; p < V; ++p)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float n = h[p][j] * rstd;
+        if (live) dw[p][j] += g[p][j] * n;
+        const float dx = rstd * (w[p][j] * g[p][j] - n * c);
+        h[p][j] = a.d_hidden ? dx + r[p][j] : dx;
+      }
+#pragma unroll
+    for (int p = 0; p < V; ++p) P::store(a.d_x, row, dl, p, lane, h[p]);
+  }
+  if (!a.d_weight) return;
+  // the workgroup's rows together, halves at a time, then one row of partial sums
+#pragma unroll
+  for (int p = 0; p < V; ++p) {
+    if constexpr (R > 1)
+#pragma unroll
+      for (int half = R / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        if (sub >= half && sub < 2 * half)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dws[(j * (R / 2) + sub - half) * N + lane] = dw[p][j];
+        __syncthreads();
+        if (sub < half)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dw[p][j] += dws[(j * (R / 2) + sub) * N + lane];
+      }
+    if (sub == 0) Piece<false, VEC, N>::store(a.part, static_cast<size_t>(blockIdx.x) * d, d, p, lane, dw[p]);
+  }
+}
+
+// d_weight[j] = sum over the partial rows, in a fixed order: 64 columns a workgroup, 16 rows at a time.
+constexpr int kSumRows = 16;
+__global__ __launch_bounds__(kWave* kSumRows) void norm_weight_sum_kernel(const float* __restrict__ part, int parts, int d,
+                                                                          float* __restrict__ out) {
+  __shared__ float s[kSumRows][kWave];
+  const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, c = blockIdx.x * kWave + lane;
+  float v = 0.0f;
+  if (c < d)
+    for (int i = r; i < parts; i += kSumRows) v += part[static_cast<size_t>(i) * d + c];
+  s[r][lane] = v;
+  __syncthreads();
+  if (r != 0 || c >= d) return;
+  for (int i = 1; i < kSumRows; ++i) v += s[i][lane];
+  out[c] = v;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+using std::integral_constant;
+
+// f(N, V) with N threads of V pieces a row: the fewest threads that hold it, four pieces each at most.
+template <class F>
+hipError_t with_shape(int d, F f) {
+  const int n = (d + 7) / 8;
+  if (n <= 64) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (n <= 128) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (n <= 256) return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  if (n <= 512) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  if (n <= 1024) return f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  if (n <= 2048) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+}
+
+// The same for the gradient, which holds five values an element: two pieces, and four in the longest rows only (those
+// spill: 128 registers are what 1024 threads have).
+template <class F>
+hipError_t with_shape_backward(int d, F f) {
+  const int n = (d + 7) / 8;
+  if (n <= 64) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (n <= 128) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (n <= 256) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  if (n <= 512) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  if (n <= 1024) return f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+  if (n <= 2048) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+}
+
+}  // namespace
+
+hipError_t launch_norm_forward(const NormArgs& a, hipStream_t stream) {
+  if (a.T == 0) return hipSuccess;
+  const bool vec = a.d % 8 == 0 && aligned16(a.x) && aligned16(a.residual) && aligned16(a.weight) &&
+                   aligned16(a.hidden) && aligned16(a.y) && aligned16(a.codes);
+  return with_shape(a.d, [&](auto nc, auto vc) {
+    constexpr int N = decltype(nc)::value, V = decltype(vc)::value, R = kRowsOf<N>;
+    const int64_t need = (static_cast<int64_t>(a.T) + R - 1) / R;
+    const dim3 grid(static_cast<unsigned>(need < 2048 ? need : 2048)), block(N * R);
+    if (a.bf16 && vec) hipLaunchKernelGGL((norm_forward_kernel<true, true, N, V>), grid, block, 0, stream, a);
+    else if (a.bf16) hipLaunchKernelGGL((norm_forward_kernel<true, false, N, V>), grid, block, 0, stream, a);
+    else if (vec) hipLaunchKernelGGL((norm_forward_kernel<false, true, N, V>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((norm_forward_kernel<false, false, N, V>), grid, block, 0, stream, a);
+    return hipGetLastError();
+  });
+}
+
+int norm_backward_parts(int T, int d) {
+  int rows = 1;
+  (void)with_shape_backward(d, [&](auto nc, auto) {
+    rows = kBwdRowsOf<decltype(nc)::value>;
+    return hipSuccess;
+  });
+  const int64_t need = (static_cast<int64_t>(T) + rows - 1) / rows;
+  return static_cast<int>(need < 512 ? need : 512);
+}
+
+hipError_t launch_norm_backward(const NormBwdArgs& a, hipStream_t stream) {
+  const bool vec = a.d % 8 == 0 && aligned16(a.hidden) && aligned16(a.weight) && aligned16(a.dy) &&
+                   aligned16(a.d_hidden) && aligned16(a.d_x);
+  const int parts = norm_backward_parts(a.T, a.d);
+  if (a.T > 0) {
+    const hipError_t err = with_shape_backward(a.d, [&](auto nc, auto vc) {
+      constexpr int N = decltype(nc)::value, V = decltype(vc)::value;
+      const dim3 grid(static_cast<unsigned>(parts)), block(1024);
+      if (a.bf16 && vec) hipLaunchKernelGGL((norm_backward_kernel<true, true, N, V>), grid, block, 0, stream, a);
+      else if (a.bf16) hipLaunchKernelGGL((norm_backward_kernel<true, false, N, V>), grid, block, 0, stream, a);
+      else if (vec) hipLaunchKernelGGL((norm_backward_kernel<false, true, N, V>), grid, block, 0, stream, a);
+      else hipLaunchKernelGGL((norm_backward_kernel<false, false, N, V>), grid, block, 0, stream, a);
+      return hipGetLastError();
+    });
+    if (err != hipSuccess) return err;
+  }
+  if (!a.d_weight) return hipSuccess;
+  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((a.d + kWave - 1) / kWave), dim3(kWave * kSumRows), 0, stream, a.part,
+                     parts, a.d, a.d_weight);
+  return hipGetLastError();
+}
+
+}  // namespace maskmoe

@@ -1,0 +1,269 @@
+// The experts' training pass at a given routing (include/maskmoe.h, maskmoe_experts_forward_train, _backward). Entries
+// (token, slot) of routed experts and then of the shared ones are grouped by expert; the products run on those rows
+// (experts.hip, backward.hip); here: the entry list, the rows' gathering, the sums over a token's rows.
+
+#include <algorithm>
+
+#include "mx8.hpp"
+#include "train_experts.hpp"
+
+namespace maskmoe {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Entries of routed and shared experts in one list.
+__global__ __launch_bounds__(kThreads) void entries_kernel(const int32_t* __restrict__ idx, const float* __restrict__ gate,
+                                                          int T, int K, int E, int n_shared, int32_t* __restrict__ idx_all,
+                                                          float* __restrict__ gate_all) {
+  const int KS = K + n_shared;
+  const int j = blockIdx.x * kThreads + threadIdx.x;
+  if (j >= T * KS) return;
+  const int t = j / KS, k = j % KS;
+  const int e = k < K ? idx[t * K + k] : E + k - K;
+  idx_all[j] = k < K && (e < 0 || e >= E) ? -1 : e;
+  gate_all[j] = k < K ? gate[t * K + k] : 1.0f;
+}
+
+// Row of entry j, or -1 where it names no expert.
+__device__ __forceinline__ int entry_row(const int32_t* idx, const int32_t* inv, int j, int G) {
+  return static_cast<uint32_t>(idx[j]) < static_cast<uint32_t>(G) ? inv[j] : -1;
+}
+
+// Sum over a token's live entries of w v[row], in entry order, fp32, rounded once; a thread per eight columns, the loads
+// of U entries in flight. O16: v is bf16 and w the gate; else v is fp32 and w 1.
+template <bool O16>
+__global__ __launch_bounds__(kThreads) void token_sum_kernel(const void* __restrict__ v, const int32_t* __restrict__ idx,
+                                                            const float* __restrict__ gate, const int32_t* __restrict__ inv,
+                                                            int T, int KS, int G, int d, uint16_t* __restrict__ out) {
+  constexpr int U = 4;
+  const int c8 = d / 8;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+  if (i >= static_cast<int64_t>(T) * c8) return;
+  const int t = static_cast<int>(i / c8), c = static_cast<int>(i % c8) * 8;
+  float s[8] = {};
+  for (int k0 = 0; k0 < KS; k0 += U) {
+    int row[U];
+    float g[U], o[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = t * KS + min(k0 + u, KS - 1);
+      row[u] = k0 + u < KS ? entry_row(idx, inv, j, G) : -1;
+      g[u] = O16 ? gate[j] : 1.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (row[u] >= 0) load_vec8<O16>(v, static_cast<size_t>(row[u]) * d + c, o[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (row[u] >= 0)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += O16 ? g[u] * o[u][e] : o[u][e];
+  }
+  store_vec8<true>(out, 8 * i, s);
+}
+
+// dy and x (bf16, or the values of its blocks) of each row's token, and the row's gate. One workgroup per row.
+__global__ __launch_bounds__(kThreads) void gather_kernel(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ x,
+                                                         const int8_t* __restrict__ x_codes,
+                                                         const uint8_t* __restrict__ x_scales,
+                                                         const float* __restrict__ gate, const int32_t* __restrict__ rows,
+                                                         const int32_t* __restrict__ perm,
+                                                         const int32_t* __restrict__ row_tok, int d,
+                                                         uint16_t* __restrict__ dyg, uint16_t* __restrict__ xg,
+                                                         float* __restrict__ row_gate) {
+  const int r = blockIdx.x;
+  if (r >= rows[0]) return;
+  const size_t src = static_cast<size_t>(row_tok[r]) * d, dst = static_cast<size_t>(r) * d;
+  for (int c = threadIdx.x * 8; c < d; c += kThreads * 8) {
+    *reinterpret_cast<u32x4*>(dyg + dst + c) = *reinterpret_cast<const u32x4*>(dy + src + c);
+    if (x_codes) {
+      const uint2 q = *reinterpret_cast<const uint2*>(x_codes + src + c);
+      const float step = mx8_step(x_scales[(src + c) / kMx8Block]);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = mx8_code_value(e < 4 ? q.x : q.y, e & 3) * step;
+      store_vec8<true>(xg, dst + c, v);
+    } else {
+      *reinterpret_cast<u32x4*>(xg + dst + c) = *reinterpret_cast<const u32x4*>(x + src + c);
+    }
+  }
+  if (threadIdx.x == 0) row_gate[r] = gate[perm[r]];
+}
+
+// d_gate of the routed entries: the column tiles' shares in order.
+__global__ __launch_bounds__(kThreads) void d_gate_kernel(const float* __restrict__ part, const int32_t* __restrict__ idx,
+                                                         const int32_t* __restrict__ inv, int T, int K, int KS, int G,
+                                                         int parts, float* __restrict__ d_gate) {
+  const int i = blockIdx.x * kThreads + threadIdx.x;
+  if (i >= T * K) return;
+  const int row = entry_row(idx, inv, i / K * KS + i % K, G);
+  float s = 0.0f;
+  if (row >= 0)
+    for (int p = 0; p < parts; ++p) s += part[static_cast<size_t>(row) * parts + p];
+  d_gate[i] = s;
+}
+
+// n 16-byte pieces of zeros.
+__global__ __launch_bounds__(kThreads) void fill_zero_kernel(u32x4* __restrict__ p, size_t n) {
+  for (size_t i = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x; i < n;
+       i += static_cast<size_t>(gridDim.x) * kThreads)
+    p[i] = u32x4{0, 0, 0, 0};
+}
+
+struct Grouping {
+  const int32_t* idx;
+  const float* gate;
+  PermBuffers pb;
+  int G, KS, rows, max_tiles;
+};
+
+// Entry list and grouping; a.T > 0.
+hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, char* ws, Grouping& g, hipStream_t stream) {
+  g.G = a.E + a.n_shared;
+  g.KS = a.K + a.n_shared;
+  g.rows = a.T * g.KS;
+  g.idx = a.idx;
+  g.gate = a.gate;
+  g.pb.offsets = reinterpret_cast<int32_t*>(ws + w.offsets);
+  g.pb.tile_off = reinterpret_cast<int32_t*>(ws + w.tile_off);
+  g.pb.active = reinterpret_cast<int32_t*>(ws + w.active);
+  g.pb.n_active = reinterpret_cast<int32_t*>(ws + w.n_active);
+  g.pb.perm = reinterpret_cast<int32_t*>(ws + w.perm);
+  g.pb.inv = reinterpret_cast<int32_t*>(ws + w.inv);
+  g.pb.row_tok = reinterpret_cast<int32_t*>(ws + w.row_tok);
+  if (a.n_shared > 0) {
+    int32_t* idx = reinterpret_cast<int32_t*>(ws + w.idx);
+    float* gate = reinterpret_cast<float*>(ws + w.gate);
+    hipLaunchKernelGGL(entries_kernel, dim3((g.rows + kThreads - 1) / kThreads), dim3(kThreads), 0, stream, a.idx, a.gate,
+                       a.T, a.K, a.E, a.n_shared, idx, gate);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    g.idx = idx;
+    g.gate = gate;
+  }
+  g.max_tiles = std::min(g.rows, g.rows / kGemmBM + g.G);
+  return launch_permute(g.idx, a.T, g.KS, g.G, 0, kGemmBM, g.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
+}
+
+unsigned blocks(int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); }
+
+}  // namespace
+
+ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n_shared) {
+  ExpertsTrainLayout w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += (bytes + 255) & ~static_cast<size_t>(255);
+    return o;
+  };
+  const size_t rows = static_cast<size_t>(T) * (K + n_shared), G = static_cast<size_t>(E) + n_shared;
+  w.idx = take(rows * 4);
+  w.gate = take(rows * 4);
+  w.offsets = take((G + 1) * 4);
+  w.tile_off = take((G + 1) * 4);
+  w.active = take(G * 4);
+  w.n_active = take(4);
+  w.perm = take(rows * 4);
+  w.inv = take(rows * 4);
+  w.row_tok = take(rows * 4);
+  w.pcount = take(static_cast<size_t>(permute_chunks(T, K + n_shared)) * G * 4);
+  w.part = take(kTailPartBytes);
+  const size_t common = off;
+  w.H = take(rows * F * 2);
+  w.O = take(rows * d * 2);
+  w.forward_total = off;
+  off = common;
+  w.dyg = take(rows * d * 2);
+  w.xg = take(rows * d * 2);
+  w.row_gate = take(rows * 4);
+  w.gh = take(rows * F * 2);
+  w.dab = take(rows * 2 * F * 2);
+  w.dxr = take(rows * d * 4);
+  w.dgate_part = take(rows * dgate_parts(F) * 4);
+  w.backward_total = off;
+  return w;
+}
+
+hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipStream_t stream) {
+  const ExpertsTrainLayout w = experts_train_layout(a.T, a.d, a.F, a.E, a.K, a.n_shared);
+  char* ws = static_cast<char*>(workspace);
+  Grouping g;
+  hipError_t err = group_rows(a, w, ws, g, stream);
+  if (err != hipSuccess) return err;
+  ExpertArgs e{};
+  e.x = a.x;
+  e.w_gate_up = a.w_gate_up;
+  e.w_down = a.w_down;
+  e.ws_gate_up = a.ws_gate_up;
+  e.ws_down = a.ws_down;
+  e.T = a.T; e.d = a.d; e.F = a.F; e.E = a.E; e.K = g.KS; e.n_shared = a.n_shared;
+  uint16_t* O = reinterpret_cast<uint16_t*>(ws + w.O);
+  err = launch_experts_kept(e, g.pb, reinterpret_cast<uint16_t*>(ws + w.H), O, reinterpret_cast<float*>(ws + w.part),
+                            a.codes, a.scales, g.max_tiles, stream);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL(token_sum_kernel<true>, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
+                     O, g.idx, g.gate, g.pb.inv, a.T, g.KS, g.G, a.d, a.y);
+  return hipGetLastError();
+}
+
+hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hipStream_t stream) {
+  const ExpertsTrainArgs& a = b.f;
+  if (a.T == 0) {
+    const size_t n = static_cast<size_t>(a.F) * a.d / 8;
+    const struct { void* p; size_t n; } out[] = {{b.d_w_gate_up, 2 * n * a.E}, {b.d_w_down, n * a.E},
+                                                 {b.d_ws_gate_up, 2 * n * a.n_shared}, {b.d_ws_down, n * a.n_shared}};
+    for (const auto& o : out) {
+      if (o.n == 0) continue;
+      hipLaunchKernelGGL(fill_zero_kernel, dim3(static_cast<unsigned>(std::min<size_t>((o.n + kThreads - 1) / kThreads, 8192))),
+                         dim3(kThreads), 0, stream, static_cast<u32x4*>(o.p), o.n);
+      const hipError_t err = hipGetLastError();
+      if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
+  }
+  const ExpertsTrainLayout w = experts_train_layout(a.T, a.d, a.F, a.E, a.K, a.n_shared);
+  char* ws = static_cast<char*>(workspace);
+  Grouping g;
+  hipError_t err = group_rows(a, w, ws, g, stream);
+  if (err != hipSuccess) return err;
+  KeptBwdArgs k{};
+  k.w_gate_up = a.w_gate_up;
+  k.w_down = a.w_down;
+  k.ws_gate_up = a.ws_gate_up;
+  k.ws_down = a.ws_down;
+  k.pb = g.pb;
+  k.codes = a.codes;
+  k.scales = a.scales;
+  uint16_t* dyg = reinterpret_cast<uint16_t*>(ws + w.dyg);
+  uint16_t* xg = reinterpret_cast<uint16_t*>(ws + w.xg);
+  float* row_gate = reinterpret_cast<float*>(ws + w.row_gate);
+  k.dyg = dyg;
+  k.xg = xg;
+  k.row_gate = row_gate;
+  k.gh = reinterpret_cast<uint16_t*>(ws + w.gh);
+  k.dab = reinterpret_cast<uint16_t*>(ws + w.dab);
+  k.dxr = reinterpret_cast<float*>(ws + w.dxr);
+  k.dgate_part = reinterpret_cast<float*>(ws + w.dgate_part);
+  k.part = reinterpret_cast<float*>(ws + w.part);
+  k.d_w_gate_up = b.d_w_gate_up;
+  k.d_w_down = b.d_w_down;
+  k.d_ws_gate_up = b.d_ws_gate_up;
+  k.d_ws_down = b.d_ws_down;
+  k.d = a.d; k.F = a.F; k.E = a.E; k.G = g.G; k.max_tiles = g.max_tiles;
+  hipLaunchKernelGGL(gather_kernel, dim3(g.rows), dim3(kThreads), 0, stream, b.dy, a.x, b.x_codes, b.x_scales, g.gate,
+                     g.pb.offsets + g.G, g.pb.perm, g.pb.row_tok, a.d, dyg, xg, row_gate);
+  err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  err = launch_experts_backward_products(k, stream);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL(token_sum_kernel<false>, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
+                     k.dxr, g.idx, g.gate, g.pb.inv, a.T, g.KS, g.G, a.d, b.d_x);
+  if (b.d_gate)
+    hipLaunchKernelGGL(d_gate_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.K)), dim3(kThreads), 0, stream,
+                       k.dgate_part, g.idx, g.pb.inv, a.T, a.K, g.KS, g.G, dgate_parts(a.F), b.d_gate);
+  return hipGetLastError();
+}
+
+}  // namespace maskmoe

@@ -1,0 +1,372 @@
+"""The experts' training pass at a given routing, with its activations in 8-bit blocks, within the bounds that the oracle
+derives from every rounding on the way (oracle/mx8.py); the block of norm, gate, experts and their gradients together."""
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import say
+from oracle import mx8 as M
+from oracle import norm as N
+from paper_2609_34077_amd import _lib as L
+
+pytestmark = pytest.mark.gpu
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def make(T, d, F, E, K, ns, seed, pad=0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g)   # noqa: E731
+    v = dict(x=(r(T, d) * (1 + 5 * (torch.rand(d, generator=g) < 0.05))).bfloat16(), dy=(0.1 * r(T, d)).bfloat16(),
+             w_gate_up=(r(E, 2 * F, d) * d ** -0.5).bfloat16(), w_down=(r(E, d, F) * F ** -0.5).bfloat16(),
+             ws_gate_up=(r(ns, 2 * F, d) * d ** -0.5).bfloat16() if ns else None,
+             ws_down=(r(ns, d, F) * F ** -0.5).bfloat16() if ns else None,
+             idx=(r(T, E) + torch.linspace(0, 2, E)).topk(K, 1).indices.int(), gate=torch.rand((T, K), generator=g))
+    if pad:
+        v["idx"][T - pad:] = -1
+    return v
+
+
+def cuda(v):
+    return {k: None if t is None else t.cuda() for k, t in v.items()}
+
+
+def both(v, name):
+    w, s = v["w" + name], v["ws" + name]
+    return f64(w if s is None else torch.cat((w, s)))
+
+
+def forward(c, **kw):
+    return L.maskmoe_experts_forward_train(c["x"], c["idx"], c["gate"], c["w_gate_up"], c["w_down"],
+                                           ws_gate_up=c["ws_gate_up"], ws_down=c["ws_down"], **kw)
+
+
+def backward(c, codes, scales, **kw):
+    return L.maskmoe_experts_backward(kw.pop("x", c["x"]), c["idx"], c["gate"], c["w_gate_up"], c["w_down"], codes, scales,
+                                      c["dy"], ws_gate_up=c["ws_gate_up"], ws_down=c["ws_down"], **kw)
+
+
+def check(v, x8=False):
+    """Both directions against the oracle: the gradients from the codes that the forward left."""
+    c, ns = cuda(v), 0 if v["ws_down"] is None else len(v["ws_down"])
+    E, idx = len(v["w_down"]), f64(v["idx"]).astype(np.int64)
+    wg, wd = both(v, "_gate_up"), both(v, "_down")
+    x, gate = f64(v["x"]), f64(v["gate"])
+    rows = len(M.rows(idx, E, ns))
+    shape = (len(x) * (idx.shape[1] + ns), 2 * wd.shape[2])
+    codes = torch.full(shape, 77, dtype=torch.int8, device="cuda")
+    scales = torch.full((shape[0], shape[1] // 32), 201, dtype=torch.uint8, device="cuda")
+    y, codes, scales = forward(c, codes=codes, scales=scales)
+    want, bound, ab, e_ab = M.forward(x, idx, gate, wg, wd, ns)
+    assert (np.abs(f64(y) - want) <= bound).all()
+    kc, ks = codes.cpu().numpy().astype(np.int64), scales.cpu().numpy().astype(np.int64) - 127
+    worst, exps = M.off_by(ab, e_ab, kc[:rows], ks[:rows])
+    assert worst <= 0 and exps
+    assert (kc[rows:] == 77).all() and (ks[rows:] == 201 - 127).all()   # rows of entries without an expert
+    if x8:
+        xc, xs = L.maskmoe_mx8_quantize(c["x"])
+        grads = backward(c, codes, scales, x=xc, x_scales=xs)
+        x = M.rounded(x)
+    else:
+        grads = backward(c, codes, scales)
+    ref = M.backward(x, idx, gate, wg, wd, ns, M.values(kc[:rows], ks[:rows]), f64(v["dy"]))
+    got = {k: f64(t) for k, t in grads.items() if t is not None}
+    if ns:
+        for name in ("d_w_gate_up", "d_w_down"):
+            got[name] = np.concatenate((got[name], got.pop(name.replace("d_w", "d_ws"))))
+    for name, (value, room) in ref.items():
+        assert (np.abs(got[name] - value) <= room).all(), name
+    again = backward(c, codes, scales, **(dict(x=xc, x_scales=xs) if x8 else {}))
+    assert all(t is None or torch.equal(t, again[k]) for k, t in grads.items())
+    return y, codes, scales, grads
+
+
+# T, d, F, E, K, shared, empty slots at the end
+LAYERS = [(1, 64, 64, 1, 1, 0, 0), (1, 128, 192, 8, 2, 0, 0), (2, 192, 64, 4, 2, 1, 1), (5, 256, 320, 16, 6, 2, 0),
+          (16, 320, 128, 8, 2, 0, 3), (17, 64, 576, 3, 3, 0, 0), (33, 512, 256, 5, 2, 0, 2), (64, 128, 128, 2, 1, 1, 0),
+          (65, 192, 64, 2, 2, 0, 0), (100, 256, 512, 8, 2, 0, 7), (200, 384, 448, 4, 2, 2, 0), (300, 128, 1408, 4, 2, 1, 11),
+          (700, 640, 192, 3, 2, 0, 0), (520, 64, 128, 1, 1, 8, 100)]
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("T,d,F,E,K,ns,pad", LAYERS)
+def test_both_directions(T, d, F, E, K, ns, pad, x8):
+    say(f"experts training T={T} d={d} F={F} E={E} K={K} shared={ns} pad={pad} x8={x8}")
+    y, _, _, grads = check(make(T, d, F, E, K, ns, T + d + F, pad), x8)
+    if pad and not ns:
+        assert (y[T - pad:] == 0).all() and (grads["d_x"][T - pad:] == 0).all() and (grads["d_gate"][T - pad:] == 0).all()
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_uneven_and_odd_routing(T):
+    """All tokens to one expert; experts named twice; indices outside the experts; no expert at all."""
+    say(f"experts training, routing T={T}")
+    v = make(T, 128, 192, 6, 2, 0, T)
+    v["idx"][:] = 4
+    grads = check(v)[3]
+    assert (grads["d_w_down"][[0, 1, 2, 3, 5]] == 0).all() and (grads["d_w_gate_up"][[0, 1, 2, 3, 5]] == 0).all()
+    v["idx"][:, 0] = torch.arange(T) % 9 - 2
+    v["idx"][:, 1] = 2 ** 31 - 1 - torch.arange(T) % 3
+    check(v)
+    v["idx"][:] = torch.iinfo(torch.int32).min
+    y, _, _, grads = check(v)
+    assert (y == 0).all() and all((t == 0).all() for t in grads.values() if t is not None)
+    v = make(T, 128, 192, 4, 2, 2, T)
+    v["idx"][:] = -1
+    check(v)
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_most_experts_entries_and_shared_experts(T):
+    v = make(T, 64, 64, 256, 16, 8, T)
+    v["idx"] = torch.stack([torch.randperm(256, generator=torch.Generator().manual_seed(t))[:16] for t in range(T)]).int()
+    check(v)
+
+
+def plain(v, codes, scales, x, idx):
+    """Gradients by torch in float64, expert by expert, for sizes that the oracle's loop over rows is too slow for."""
+    ns = 0 if v["ws_down"] is None else len(v["ws_down"])
+    E, F = v["w_down"].shape[0], v["w_down"].shape[2]
+    dev = "cuda"
+    T, K = idx.shape
+    entries = torch.cat((idx.long(), torch.arange(E, E + ns, device=dev).expand(T, -1)), 1)
+    gates = torch.cat((v["gate"].double(), torch.ones((T, ns), device=dev, dtype=torch.float64)), 1)
+    dy, row = v["dy"].double(), 0
+    out = dict(d_x=torch.zeros_like(x), d_gate=torch.zeros_like(gates), w_gate_up=[], w_down=[])
+    for e in range(E + ns):
+        t, k = (entries == e).nonzero(as_tuple=True)
+        gu, dn = (v["w_gate_up"][e], v["w_down"][e]) if e < E else (v["ws_gate_up"][e - E], v["ws_down"][e - E])
+        gu, dn = gu.double(), dn.double()
+        ab = codes[row:row + len(t)].double() * torch.exp2(scales[row:row + len(t)].double() - 133).repeat_interleave(32, 1)
+        a, b, s = ab[:, :F], ab[:, F:], torch.sigmoid(ab[:, :F])
+        u, h, g = dy[t] @ dn, a * s * b, gates[t, k][:, None]
+        out["d_gate"][t, k] = (u * h).sum(1)
+        dab = torch.cat((g * u * b * s * (1 + a * (1 - s)), g * u * a * s), 1)
+        out["d_x"].index_add_(0, t, dab @ gu)
+        out["w_gate_up"].append(dab.t() @ x[t])
+        out["w_down"].append(dy[t].t() @ (g * h))
+        row += len(t)
+    out["d_gate"] = out["d_gate"][:, :K]
+    return out
+
+
+@pytest.mark.parametrize("T,d,F,E,K,ns,pad", [(3000, 2048, 1408, 64, 6, 2, 100), (700, 4096, 2048, 8, 2, 0, 0),
+                                              (5000, 1024, 4160, 4, 2, 1, 1)])
+def test_larger_layers(T, d, F, E, K, ns, pad):
+    """Many tiles, split tail tiles, experts of several row tiles. Independent roundings to bf16 are off by at most
+    2^-8 / sqrt(3) relative (RMS) each: two of them in a row in y's terms and its own, two in the gradients."""
+    say(f"experts training T={T} d={d} F={F}")
+    v = cuda(make(T, d, F, E, K, ns, 7, pad))
+    y, codes, scales = forward(v)
+    grads = backward(v, codes, scales)
+    ref = plain(v, codes, scales, v["x"].double(), v["idx"])
+    rel = lambda a, b: ((a.double() - b).norm() / b.norm()).item()   # noqa: E731
+    step = 2.0 ** -8 / 3 ** 0.5
+    assert rel(grads["d_x"], ref["d_x"]) <= step * 2 ** 0.5
+    assert rel(grads["d_gate"], ref["d_gate"]) <= 1e-5
+    for name in ("w_gate_up", "w_down"):
+        for e in range(E + ns):
+            got = grads["d_" + name][e] if e < E else grads["d_" + name.replace("w_", "ws_")][e - E]
+            assert rel(got, ref[name][e]) <= step * 2 ** 0.5, (name, e)
+    # the layer on the values: y's terms round h and the expert's output, y itself once more
+    x, entries = v["x"].double(), v["idx"].long()
+    want, row = torch.zeros_like(x), 0
+    for e in range(E + ns):
+        t, k = (entries == e).nonzero(as_tuple=True) if e < E else (torch.arange(T, device="cuda"), None)
+        gu, dn = (v["w_gate_up"][e], v["w_down"][e]) if e < E else (v["ws_gate_up"][e - E], v["ws_down"][e - E])
+        ab = x[t] @ gu.double().t()
+        h = ab[:, :F] * torch.sigmoid(ab[:, :F]) * ab[:, F:]
+        g = v["gate"][t, k].double()[:, None] if e < E else 1.0
+        want.index_add_(0, t, g * (h @ dn.double().t()))
+        if len(t):
+            kept = codes[row:row + len(t)].double() * torch.exp2(scales[row:row + len(t)].double() - 133).repeat_interleave(32, 1)
+            # half a step a value, 2^-7 of a block's largest; here relative to the whole
+            assert rel(kept, ab) <= 2.0 ** -6
+        row += len(t)
+    assert rel(y, want) <= step * 3 ** 0.5
+
+
+@pytest.mark.parametrize("T", [3, 90, 600])
+def test_nan_and_infinity_stay_in_their_token(T):
+    v = cuda(make(T, 192, 128, 4, 2, 1, T + 1))
+    y0, c0, s0 = forward(v)
+    g0 = backward(v, c0, s0)
+    x, dy = v["x"].clone(), v["dy"].clone()
+    v["x"][1, 7], v["x"][T - 1, 100] = float("nan"), float("inf")
+    y, c, s = forward(v)
+    rows = torch.ones(T, dtype=torch.bool)
+    rows[1] = rows[T - 1] = False
+    assert torch.equal(y[rows], y0[rows]) and y[1].isnan().all() and not y[T - 1].isfinite().any()
+    v["x"], v["dy"] = x, dy
+    v["dy"][1, 7] = float("nan")
+    g = backward(v, c0, s0)
+    rows[T - 1] = True
+    assert torch.equal(g["d_x"][rows], g0["d_x"][rows]) and g["d_x"][1].isnan().all()
+    assert torch.equal(g["d_gate"][rows], g0["d_gate"][rows]) and g["d_gate"][1].isnan().all()
+    left = torch.ones(4, dtype=torch.bool)
+    left[v["idx"][1].long().cpu()] = False
+    for name in ("d_w_gate_up", "d_w_down"):
+        assert torch.equal(g[name][left], g0[name][left])
+
+
+def test_no_tokens():
+    v = cuda(make(2, 64, 64, 3, 2, 1, 1))
+    for k in ("x", "dy", "idx", "gate"):
+        v[k] = v[k][:0]
+    y, codes, scales = forward(v)
+    assert y.shape == (0, 64) and codes.shape == (0, 128) and scales.shape == (0, 4)
+    for t in backward(v, codes, scales).values():
+        assert (t == 0).all()
+
+
+def test_without_d_gate_and_shared_experts_alone():
+    """A dense gated feed-forward: one shared expert, no entry that names a routed one."""
+    v = make(70, 128, 192, 1, 1, 1, 3)
+    v["idx"][:] = -1
+    c = cuda(v)
+    y, codes, scales = forward(c)
+    g = backward(c, codes, scales, with_d_gate=False)
+    assert g["d_gate"] is None
+    full = backward(c, codes, scales)
+    assert all(torch.equal(g[k], full[k]) for k in g if k != "d_gate")
+    check(v)
+
+
+@pytest.mark.parametrize("T,F", [(4, 320), (900, 320), (300, 2048)])
+def test_dirty_workspace_streams_and_graphs(T, F):
+    """The workspaces' contents do not matter; calls on two streams with workspaces each; captured and replayed with other
+    work between; the same bits every time."""
+    say(f"experts training graph T={T} F={F}")
+    E, K, ns, d = 8, 2, 1, 256
+    v = cuda(make(T, d, F, E, K, ns, T + 3, pad=1))
+    sizes = (L.maskmoe_experts_train_workspace_bytes(T, d, E, K, F, ns),
+             L.maskmoe_experts_backward_workspace_bytes(T, d, E, K, F, ns))
+    dirty = lambda fill: [torch.full((n,), fill, dtype=torch.uint8, device="cuda") for n in sizes]   # noqa: E731
+
+    def kept():
+        rows = T * (K + ns)
+        return dict(codes=torch.zeros((rows, 2 * F), dtype=torch.int8, device="cuda"),
+                    scales=torch.zeros((rows, 2 * F // 32), dtype=torch.uint8, device="cuda"))
+
+    def step(w, buf, **kw):
+        y, c, s = forward(buf, workspace=w[0], **(kw or kept()))
+        return [y, c, s] + list(backward(buf, c, s, workspace=w[1]).values())
+    ref = step((None, None), v)
+    for fill in (0xFF, 0x7F):
+        assert all(torch.equal(a, b) for a, b in zip(step(dirty(fill), v), ref))
+    streams, outs, works = [torch.cuda.Stream(), torch.cuda.Stream()], [], [dirty(1), dirty(2)]
+    torch.cuda.synchronize()
+    for s, w in zip(streams, works):
+        with torch.cuda.stream(s):
+            outs += [step(w, v) for _ in range(3)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for o in outs for a, b in zip(o, ref))
+    buf, keep, w = {k: t.clone() for k, t in v.items()}, kept(), dirty(3)
+    graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        got = step(w, buf, **keep)
+    for i in range(4):
+        for k in ("x", "dy", "gate", "idx"):
+            buf[k].copy_(v[k].roll(i, 0))
+        for t in keep.values():
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step((None, None), buf))), i
+
+
+def test_binding_refuses():
+    v = cuda(make(4, 64, 64, 3, 2, 1, 1))
+    y, codes, scales = forward(v)
+    bad = [dict(x=v["x"].float()), dict(x=v["x"][:3]), dict(idx=v["idx"].long()), dict(gate=v["gate"][:, :1]),
+           dict(w_down=v["w_down"][:2]), dict(ws_down=None), dict(w_gate_up=v["w_gate_up"].transpose(1, 2)),
+           dict(x=v["x"].cpu())]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            forward({**v, **kw})
+        with pytest.raises(ValueError):
+            backward({**v, **kw}, codes, scales)
+    for a, b in ((codes[:5], scales), (codes, scales[:, :2]), (codes.float(), scales)):
+        with pytest.raises(ValueError):
+            backward(v, a, b)
+    with pytest.raises(ValueError):
+        backward(v, codes, scales, x=v["x"], x_scales=scales)
+    with pytest.raises(ValueError):
+        forward(v, codes=codes[:5])
+    with pytest.raises(L.MaskMoEError):
+        forward(v, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+def test_block_of_norm_gate_and_experts():
+    """x + residual, norm, router, gate, experts and the whole way back, against autograd of the same block in float64
+    whose kept values are those of the blocks (straight through their rounding)."""
+    T, d, F, E, K, ns = 260, 192, 256, 8, 2, 1
+    v = cuda(make(T, d, F, E, K, ns, 11))
+    g = torch.Generator(device="cuda").manual_seed(5)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")   # noqa: E731
+    res, w, router = r(T, d).bfloat16(), (1 + 0.2 * r(d)).bfloat16(), (r(E, d) * d ** -0.5).bfloat16()
+    bias, x = 0.05 * r(E), v["x"]
+    dh_up = (0.1 * r(T, d)).bfloat16()   # the stream's own gradient from above
+    # forward
+    y, hidden, xc, xs = L.maskmoe_norm_forward(x, w, residual=res, with_mx8=True)
+    logits = y.float() @ router.float().t()
+    idx, gate, _ = L.maskmoe_gate_forward(logits, K, L.SCORE_SIGMOID, bias=bias, scale=2.5)
+    c = dict(v, x=y, idx=idx, gate=gate)
+    out, codes, scales = forward(c)
+    # backward
+    grads = backward(c, codes, scales, x=xc, x_scales=xs)
+    d_logits = L.maskmoe_gate_backward(logits, idx, grads["d_gate"], L.SCORE_SIGMOID, scale=2.5)
+    d_y = (grads["d_x"].float() + d_logits @ router.float()).bfloat16()
+    d_x, d_w = L.maskmoe_norm_backward(hidden, w, d_y, d_hidden=dh_up)
+    # the same in float64
+    leaf = lambda t: t.double().requires_grad_(True)   # noqa: E731
+    X, W, R = leaf(x), leaf(w), leaf(router)
+    mats = {k: leaf(v[k]) for k in ("w_gate_up", "w_down", "ws_gate_up", "ws_down")}
+    S = X + res.double()
+    Y = S / torch.sqrt((S * S).mean(-1, keepdim=True) + 1e-5) * W
+    P = torch.sigmoid(Y @ R.t()).gather(1, idx.long())
+    G = 2.5 * P / P.sum(-1, keepdim=True)
+    Y8 = Y + (L.maskmoe_mx8_dequantize(xc, xs, torch.float32).double() - Y).detach()   # what dW_gate_up reads
+    kept = L.maskmoe_mx8_dequantize(codes, scales, torch.float32).double()
+    O, row = torch.zeros_like(X), 0
+    for e in range(E + ns):
+        t, k = (idx == e).nonzero(as_tuple=True) if e < E else (torch.arange(T, device="cuda"), None)
+        gu, dn = (mats["w_gate_up"][e], mats["w_down"][e]) if e < E else (mats["ws_gate_up"][e - E], mats["ws_down"][e - E])
+        ab = Y[t] @ gu.detach().t() + (Y8[t].detach() @ gu.t() - (Y8[t] @ gu.t()).detach())
+        ab = ab + (kept[row:row + len(t)] - ab).detach()
+        h = torch.nn.functional.silu(ab[:, :F]) * ab[:, F:]
+        O = O.index_add(0, t, (G[t, k][:, None] if e < E else 1.0) * (h @ dn.t()))
+        row += len(t)
+    ((O * v["dy"].double()).sum() + (S * dh_up.double()).sum()).backward()
+    rel = lambda a, b: ((a.double() - b).norm() / b.norm()).item()   # noqa: E731
+    step = 2.0 ** -8 / 3 ** 0.5   # a rounding to bf16, RMS
+    assert rel(grads["d_w_gate_up"], mats["w_gate_up"].grad) <= 2 * step
+    assert rel(grads["d_w_down"], mats["w_down"].grad) <= 2 * step
+    assert rel(grads["d_ws_gate_up"], mats["ws_gate_up"].grad) <= 2 * step
+    assert rel(grads["d_ws_down"], mats["ws_down"].grad) <= 2 * step
+    # d_x: the terms of the experts' share (two roundings), d_y's, hidden's and its own
+    assert rel(d_x, X.grad) <= 5 ** 0.5 * step
+    assert rel(d_w, W.grad) <= 4 ** 0.5 * step
+
+
+def test_gradients_against_differences():
+    """The whole pass along a direction: central differences of the kernel's own fp32-accumulated loss, with steps large
+    enough that bf16's roundings of y (2^-8 of each value, independent) stay below the tolerance."""
+    T, d, F, E, K, ns = 64, 128, 128, 4, 2, 1
+    v = cuda(make(T, d, F, E, K, ns, 21))
+    y, codes, scales = forward(v)
+    g = backward(v, codes, scales)
+    # y is linear in the gates: exact differences but for y's rounding
+    u = torch.randn((T, K), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    loss = lambda c: (forward(c)[0].double() * v["dy"].double()).sum().item()   # noqa: E731
+    got = (loss({**v, "gate": v["gate"] + u}) - loss({**v, "gate": v["gate"] - u})) / 2
+    want = (g["d_gate"].double() * u.double()).sum().item()
+    # y's three roundings, independent over T d values, and the blocks' (half a step: 2^-7 of a block's largest, about
+    # 2^-6 / sqrt(12) of the values RMS) in d_gate's F terms, five standard deviations of each
+    noise = 5 * 2.0 ** -8 * (y.double() * v["dy"].double()).norm().item() * 3 ** 0.5 * 2
+    noise += 5 * 2.0 ** -6 * (g["d_gate"].double() * u.double()).norm().item()
+    assert abs(got - want) <= noise, (got, want, noise)

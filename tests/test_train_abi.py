@@ -1,0 +1,156 @@
+"""Refusals of the norm, the 8-bit blocks and the experts' training pass, without a GPU: every invalid argument is told
+before anything is enqueued."""
+
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2609_34077_amd import _lib as L
+
+pytestmark = pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="libmaskmoe.so not built")
+
+FAKE = 0x10000   # aligned, never read: only used where validation must fail
+
+
+@pytest.mark.parametrize("fn", ["maskmoe_mx8_quantize", "maskmoe_mx8_dequantize"])
+def test_mx8_conversion_rejects(fn):
+    f = getattr(L.load(), fn)
+    assert f(-1, 32, L.BF16, FAKE, FAKE, FAKE, None) == L.E_INVAL
+    assert f(1, 0, L.BF16, FAKE, FAKE, FAKE, None) == L.E_INVAL
+    assert f(1, 32, 2, FAKE, FAKE, FAKE, None) == L.E_INVAL
+    assert f(1, 48, L.F32, FAKE, FAKE, FAKE, None) == L.E_UNSUPPORTED
+    assert f(1 << 40, 32, L.F32, FAKE, FAKE, FAKE, None) == L.E_UNSUPPORTED
+    for i in range(3):
+        a = [FAKE] * 3
+        a[i] = None
+        assert f(1, 32, L.BF16, *a, None) == L.E_INVAL
+    vec, codes = (0, 1) if fn == "maskmoe_mx8_quantize" else (2, 0)
+    for i in (vec, codes):
+        a = [FAKE] * 3
+        a[i] = FAKE + 8
+        assert f(1, 32, L.BF16, *a, None) == L.E_INVAL
+    assert f(0, 32, L.BF16, None, None, None, None) == L.OK
+
+
+def norm(T=4, d=64, dtype=L.BF16, eps=1e-5, x=FAKE, r=FAKE, w=FAKE, h=FAKE + 4096, y=FAKE + 8192, c=FAKE, s=FAKE):
+    return L.load().maskmoe_norm_forward(T, d, dtype, eps, x, r, w, h, y, c, s, None)
+
+
+def norm_bwd(T=4, d=64, dtype=L.BF16, eps=1e-5, h=FAKE, w=FAKE, dy=FAKE, dh=FAKE, dx=FAKE, dw=FAKE, ws=FAKE,
+             ws_bytes=1 << 40):
+    return L.load().maskmoe_norm_backward(T, d, dtype, eps, h, w, dy, dh, dx, dw, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("f", [norm, norm_bwd])
+def test_norm_rejects_sizes(f):
+    for kw in (dict(T=-1), dict(d=0), dict(d=-8), dict(dtype=2), dict(eps=-1e-6), dict(eps=float("nan")),
+               dict(eps=float("inf"))):
+        assert f(**kw) == L.E_INVAL, kw
+    assert f(d=32769) == L.E_UNSUPPORTED
+    assert f(w=None) == L.E_INVAL and f(w=FAKE + 1) == L.E_INVAL and f(dtype=L.F32, w=FAKE + 2) == L.E_INVAL
+
+
+def test_norm_rejects_pointers():
+    for kw in (dict(x=None), dict(x=FAKE + 1), dict(r=FAKE + 1), dict(h=FAKE + 1), dict(y=FAKE + 1), dict(c=None),
+               dict(s=None), dict(h=None, y=None, c=None, s=None), dict(y=FAKE + 4096),
+               dict(dtype=L.F32, x=FAKE + 2)):
+        assert norm(**kw) == L.E_INVAL, kw
+    assert norm(d=48) == L.E_UNSUPPORTED
+    assert norm(T=0, x=None, w=None, h=None, y=None, c=None, s=None) == L.OK
+
+
+def test_norm_backward_rejects_pointers_and_workspaces():
+    lib = L.load()
+    for kw in (dict(h=None), dict(dy=None), dict(dx=None), dict(h=FAKE + 1), dict(dh=FAKE + 1), dict(dx=FAKE + 1),
+               dict(dw=FAKE + 2)):
+        assert norm_bwd(**kw) == L.E_INVAL, kw
+    need = lib.maskmoe_norm_backward_workspace_bytes(4, 64)
+    assert need > 0
+    for kw in (dict(ws=None), dict(ws=FAKE + 128), dict(ws_bytes=need - 1)):
+        assert norm_bwd(**kw) == L.E_WORKSPACE, kw
+    for T, d in ((-1, 64), (4, 0), (4, 32769)):
+        assert lib.maskmoe_norm_backward_workspace_bytes(T, d) == 0
+    assert norm_bwd(T=0, h=None, w=None, dy=None, dh=None, dx=None, dw=None, ws=None) == L.OK
+    sizes = [lib.maskmoe_norm_backward_workspace_bytes(T, 640) for T in (0, 1, 5, 100, 5000, 1 << 20)]
+    assert sizes == sorted(sizes)
+
+
+def fwd(desc, x=FAKE, idx=FAKE, gate=FAKE, wg=FAKE, wd=FAKE, sg=FAKE, sd=FAKE, y=FAKE + 65536, c=FAKE, s=FAKE, ws=FAKE,
+        ws_bytes=1 << 40):
+    return L.load().maskmoe_experts_forward_train(ctypes.byref(desc), x, idx, gate, wg, wd, sg, sd, y, c, s, ws, ws_bytes,
+                                                  None)
+
+
+def bwd(desc, x=FAKE, xs=None, idx=FAKE, gate=FAKE, wg=FAKE, wd=FAKE, sg=FAKE, sd=FAKE, c=FAKE, s=FAKE, dy=FAKE + 4096,
+        dx=FAKE + 65536, dg=FAKE, dwg=FAKE, dwd=FAKE, dsg=FAKE, dsd=FAKE, ws=FAKE, ws_bytes=1 << 40):
+    return L.load().maskmoe_experts_backward(ctypes.byref(desc), x, xs, idx, gate, wg, wd, sg, sd, c, s, dy, dx, dg, dwg,
+                                             dwd, dsg, dsd, ws, ws_bytes, None)
+
+
+OK = dict(T=4, d=64, E=8, K=2, F=64, n_shared=1)
+
+
+@pytest.mark.parametrize("call,query", [(fwd, "maskmoe_experts_train_workspace_bytes"),
+                                        (bwd, "maskmoe_experts_backward_workspace_bytes")])
+def test_experts_training_rejects(call, query):
+    query = getattr(L.load(), query)
+    for kw in (dict(T=-1), dict(E=0), dict(E=257), dict(K=0), dict(K=9), dict(E=32, K=17), dict(n_shared=9),
+               dict(n_shared=-1), dict(d=0), dict(F=0), dict(dtype=5)):
+        d = L.make_desc(**{**OK, **kw})
+        assert call(d) == L.E_INVAL and query(ctypes.byref(d)) == 0, kw
+    for kw in (dict(d=96), dict(F=96), dict(dtype=L.F32), dict(T=1 << 25, d=4096), dict(d=1 << 16, F=1 << 15),
+               dict(T=1 << 20, F=1024), dict(T=1 << 22, d=256, K=1)):
+        d = L.make_desc(**{**OK, **kw})
+        assert call(d) == L.E_UNSUPPORTED and query(ctypes.byref(d)) == 0, kw
+    d = L.make_desc(**OK)
+    for name in ("x", "wg", "wd", "sg", "sd", "c"):
+        assert call(d, **{name: None}) == L.E_INVAL and call(d, **{name: FAKE + 8}) == L.E_INVAL, name
+    for name in ("idx", "gate"):
+        assert call(d, **{name: None}) == L.E_INVAL and call(d, **{name: FAKE + 2}) == L.E_INVAL, name
+    assert call(d, s=None) == L.E_INVAL
+    need = query(ctypes.byref(d))
+    for kw in (dict(ws=None), dict(ws=FAKE + 128), dict(ws_bytes=need - 1)):
+        assert call(d, **kw) == L.E_WORKSPACE, kw
+    sizes = [query(ctypes.byref(L.make_desc(**{**OK, "T": T}))) for T in (0, 1, 16, 17, 100, 5000)]
+    assert sizes == sorted(sizes)
+
+
+def test_experts_training_rejects_outputs():
+    d = L.make_desc(**OK)
+    for kw in (dict(y=None), dict(y=FAKE), dict(y=FAKE + 8)):
+        assert fwd(d, **kw) == L.E_INVAL, kw
+    for kw in (dict(dy=None), dict(dy=FAKE + 8), dict(dx=None), dict(dx=FAKE), dict(dx=FAKE + 4096), dict(dx=FAKE + 8),
+               dict(dg=FAKE + 2), dict(dwg=None), dict(dwd=None), dict(dsg=None), dict(dsd=None), dict(dwg=FAKE + 8),
+               dict(dwd=FAKE + 8), dict(dsg=FAKE + 8), dict(dsd=FAKE + 8)):
+        assert bwd(d, **kw) == L.E_INVAL, kw
+    none = L.make_desc(**{**OK, "T": 0})
+    assert fwd(none, x=None, y=None, idx=None, gate=None, c=None, s=None, ws=None) == L.OK
+    assert bwd(none, dwg=None) == L.E_INVAL
+
+
+def test_sizes_that_int32_does_not_hold():
+    meta = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device="meta")
+    i32, f32, i8, u8 = torch.int32, torch.float32, torch.int8, torch.uint8
+    n = 2 ** 32 + 5
+    calls = [lambda: L.maskmoe_mx8_quantize(meta(2 ** 32 + 32)),
+             lambda: L.maskmoe_mx8_dequantize(meta(2 ** 32 + 32, dtype=i8), meta(2 ** 27 + 1, dtype=u8), torch.bfloat16),
+             lambda: L.maskmoe_norm_forward(meta(n, 32), meta(32)),
+             lambda: L.maskmoe_norm_forward(meta(1, n), meta(n)),
+             lambda: L.maskmoe_norm_backward(meta(n, 32), meta(32), meta(n, 32)),
+             lambda: L.maskmoe_norm_backward_workspace_bytes(n, 64),
+             lambda: L.maskmoe_experts_train_workspace_bytes(n, 64, 8, 2, 64),
+             lambda: L.maskmoe_experts_backward_workspace_bytes(4, 64, 8, 2, n * 64)]
+    for f in calls:
+        with pytest.raises(ValueError, match="below 2"):
+            f()
+
+
+def test_binding_refuses_host_tensors_and_empty_rows():
+    with pytest.raises(ValueError):
+        L.maskmoe_norm_forward(torch.zeros(3, 0), torch.zeros(0))
+    with pytest.raises(ValueError):
+        L.maskmoe_mx8_quantize(torch.zeros(3, 33))
+    with pytest.raises(ValueError):
+        L.maskmoe_mx8_dequantize(torch.zeros(3, 0, dtype=torch.int8), torch.zeros(3, 0, dtype=torch.uint8), torch.float32)
