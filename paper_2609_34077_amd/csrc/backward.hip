@@ -16,6 +16,8 @@
 // of the dgrads, and both operands of the weight gradients, whose contraction runs over each
 // expert's own rows of dO, h, [da db] and the gathered x (rows past the group's end read as
 // zeros; an expert no token chose gets zeros).
+// A row group's last tile multiplies and loads only its 64-row pieces that hold rows, as in the forward (but with
+// SwiGLU's backward on bf16 pre-activations, which keeps whole tiles).
 // Rounding (bf16 layers): dO = g dy and [da db] are rounded to bf16 before their GEMMs;
 // accumulation is fp32; dX, dW are fp32.
 
@@ -95,53 +97,6 @@ struct NtArgs {
 // ROWS with fp32 output may split each XCD's last-round tiles (see tile_job).
 __host__ __device__ constexpr bool nt_tail_split(int mode, int epi, int nk) {
   return mode == 0 && epi == 1 && tail_splittable(nk);
-}
-
-// Stores a finished ROWS tile of fp32 output: rows [row0, row_end), columns from n0.
-// Staged fp32 tiles: 128 rows x 256 columns at a pitch of 264 floats (the two 32-lane halves of
-// a wavefront, four rows apart, then write different banks).
-constexpr int kStgPitch = 264;
-static_assert(128 * kStgPitch * 4 <= sizeof(TileLds), "a staged half tile fits in LDS");
-
-// Half h (0, 1) of the tile into LDS: acc[2h + ii] of every wave, as staged row
-// wm*64 + ii*32 + (row within the 32-row block). Staged row pr is tile row
-// (pr >> 6) * 128 + 64 h + (pr & 63).
-__device__ __forceinline__ void stage_half(float* stg, const f32x16 (&acc)[kTileTM][kTileTN], int h) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave / 4, wn = wave % 4;
-#pragma unroll
-  for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int j = 0; j < kTileTN; ++j)
-        stg[(wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kStgPitch + wn * 64 + j * 32 +
-            (lane & 31)] = (h == 0 ? acc[ii][j][r] : acc[2 + ii][j][r]);
-}
-
-// The fp32 tile (rows row0.., columns n0..) into out (row stride ld), through LDS in two halves
-// so that it leaves in 16-byte stores: one 4-byte store per value and lane kept the
-// texture-address path busy for ~10 us at the end of every tile. ncol % 4 == 0.
-__device__ __forceinline__ void nt_store_staged(const f32x16 (&acc)[kTileTM][kTileTN], float* out, size_t ld, int row0,
-                                                int row_end, int n0, int ncol, TileLds& L) {
-  float* stg = reinterpret_cast<float*>(&L);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    wait_lgkmcnt0();
-    tile_barrier();   // the k-loop's (or the previous half's) LDS reads are done
-    stage_half(stg, acc, h);
-    wait_lgkmcnt0();
-    tile_barrier();
-#pragma unroll 4
-    for (int q = 0; q < 16; ++q) {   // 8192 float4 per half: 64 per staged row
-      const int u = static_cast<int>(threadIdx.x) + kTileThreads * q;
-      const int pr = u >> 6, c = (u & 63) * 4;
-      const int row = row0 + (pr >> 6) * 128 + 64 * h + (pr & 63), col = n0 + c;
-      if (row < row_end && col < ncol)
-        *reinterpret_cast<float4*>(out + static_cast<size_t>(row) * ld + col) =
-            *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + c]);
-    }
-  }
 }
 
 // The gradients of the groups that no row reached are zero. Where they are no more than the reached
@@ -230,15 +185,17 @@ __device__ __forceinline__ float half_wave_sum(float v) {
 
 // Epilogue of u = dy W_down with the pre-activations in 8-bit blocks: da, db (bf16, [rows, 2N]), the gated SwiGLU
 // activation for the weight gradient (bf16, [rows, N]) and this tile's share of every row's d_gate = <u, h>. As
-// kEpiSwigluBwd's, the tile goes through LDS in two halves, a half's blocks loaded before it is staged.
-__device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x16 (&acc)[kTileTM][kTileTN], int row0,
+// kEpiSwigluBwd's, the tile goes through LDS in parts of 128 rows, a part's blocks loaded before it is staged.
+template <int TM>
+__device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x16 (&acc)[TM][kTileTN], int row0,
                                                      int row_end, int n0, int nt, TileLds& L) {
   const int tid = threadIdx.x;
   float* stg = reinterpret_cast<float*>(&L);
   uint16_t* o = static_cast<uint16_t*>(p.c);
   const size_t N = p.N;
+  row_end = min(row_end, row0 + 64 * TM);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < (TM + 1) / 2; ++h) {
     uint2 a8[8], b8[8];
     uint32_t sa[8], sb[8];
     float gate[8];
@@ -246,7 +203,7 @@ __device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x
     for (int q = 0; q < 8; ++q) {   // 4096 pieces of 8 columns: 32 per staged row
       const int u = tid + kTileThreads * q;
       const int pr = u >> 5, col = n0 + (u & 31) * 8;
-      const int row = row0 + (pr >> 6) * 128 + 64 * h + (pr & 63);
+      const int row = row0 + staged_tile_row<TM>(pr, h);
       a8[q] = b8[q] = make_uint2(0, 0);
       sa[q] = sb[q] = 0;
       gate[q] = 0.0f;
@@ -260,29 +217,31 @@ __device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x
       }
     }
     wait_lgkmcnt0();
-    tile_barrier();   // the k-loop's (or the previous half's) LDS reads are done
-    stage_half(stg, acc, h);
+    tile_barrier();   // the k-loop's (or the previous part's) LDS reads are done
+    stage_part<TM>(stg, acc, h);
     wait_lgkmcnt0();
     tile_barrier();
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const int u = tid + kTileThreads * q;
       const int pr = u >> 5, cg = (u & 31) * 8, col = n0 + cg;
-      const int row = row0 + (pr >> 6) * 128 + 64 * h + (pr & 63);
+      const int row = row0 + staged_tile_row<TM>(pr, h);
       const bool live = row < row_end && col < p.N;
-      float v[8], da[8], db[8], gh[8];
+      float v[8], av[8], bv[8], da[8], db[8], gh[8];
       *reinterpret_cast<float4*>(&v[0]) = *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + cg]);
       *reinterpret_cast<float4*>(&v[4]) = *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + cg + 4]);
       const float s_a = mx8_step(sa[q]), s_b = mx8_step(sb[q]);
+      mx8_decode4(a8[q].x, s_a, av);
+      mx8_decode4(a8[q].y, s_a, av + 4);
+      mx8_decode4(b8[q].x, s_b, bv);
+      mx8_decode4(b8[q].y, s_b, bv + 4);
       float dot = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float av = mx8_code_value(e < 4 ? a8[q].x : a8[q].y, e & 3) * s_a;
-        const float bv = mx8_code_value(e < 4 ? b8[q].x : b8[q].y, e & 3) * s_b;
-        const float s = sigmoid(av), hv = av * s * bv, gu = gate[q] * v[e];
+        const float s = sigmoid(av[e]), l = av[e] * s, hv = l * bv[e], gu = gate[q] * v[e];
         dot += v[e] * hv;
-        da[e] = gu * bv * (s * (1.0f + av * (1.0f - s)));
-        db[e] = gu * av * s;
+        da[e] = gu * bv[e] * (s + l - l * s);   // SiLU' = s + a s (1 - s)
+        db[e] = gu * l;
         gh[e] = gate[q] * hv;
       }
       dot = half_wave_sum(live ? dot : 0.0f);   // 32 lanes hold a staged row
@@ -304,6 +263,21 @@ __device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x
 }
 
 
+// Tile of this workgroup where groups of `per` tiles each have reductions of their own lengths, longest group first: every
+// XCD takes an eighth of each group (pieces of per / 8 consecutive tiles, dealt in turn), so that all have the same
+// work and no long reduction starts late. In ranges of consecutive tiles for each XCD instead, as for products whose
+// tiles are all alike, the XCD with the shared experts' tiles decided: DeepSeek-shaped, 4096 tokens, the two
+// weight gradients 854 + 453 us.
+__host__ __device__ __forceinline__ int dealt_piece(int per) { return per < 8 ? 1 : per / 8; }
+__device__ __forceinline__ int dealt_tile_id(int per) {
+  const int c = dealt_piece(per), local = blockIdx.x >> 3;
+  return (local / c * 8 + static_cast<int>(blockIdx.x & 7)) * c + local % c;
+}
+static dim3 dealt_grid(int groups, int per) {
+  const int64_t c = dealt_piece(per), pieces = (static_cast<int64_t>(groups) * per + c - 1) / c;
+  return dim3(static_cast<unsigned>((pieces + 7) / 8 * 8 * c));
+}
+
 // ROWS (dgrad): group g's rows offsets[g]..offsets[g+1] of A (K-contiguous) times its own
 // K-major [K, N] matrix, row tiles enumerated by tile_off as in the forward. KSPLIT (wgrad): for
 // every non-empty group g the full [M, N] product over its rows offsets[g]..offsets[g+1] of the
@@ -317,6 +291,7 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   const int wn = wave % WN;
   int mt, nt, g, row0, row_end, nk;
   TileJob job{0, 0, 1, -1};
+  int tm = kTileTM;
   TileOps ops{};
   TileKm akm{}, bkm{};
   uint64_t dead[kDeadWords] = {};
@@ -339,9 +314,11 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
     const int k0 = job.z * nk * kTileK;
     const int n0 = nt * kTileN;
     ops.a = reinterpret_cast<const char*>(p.a + k0);
+    if (EPI != kEpiSwigluBwd && job.s == 1) tm = min((row_end - row0 + 63) / 64, kTileTM);
 #pragma unroll
     for (int i = 0; i < 4; ++i)   // element offsets < 2^31 (checked by the host)
-      ops.aoff[i] = static_cast<uint32_t>(min(row0 + tile_dma_row(i), row_end - 1) * p.lda + tile_dma_chunk(i) * 8) * 2u;
+      ops.aoff[i] =
+          static_cast<uint32_t>(min(row0 + tile_dma_row_a(tm, i), row_end - 1) * p.lda + tile_dma_chunk_a(tm, i) * 8) * 2u;
     const uint16_t* bm = g < p.E ? p.b + static_cast<size_t>(g) * p.N * p.K : p.bs + static_cast<size_t>(g - p.E) * p.N * p.K;
     bkm.base = reinterpret_cast<const char*>(bm + static_cast<size_t>(k0) * p.ldb + n0);
     bkm.ld = p.ldb * 2;
@@ -350,8 +327,13 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   } else {
     const int per = p.mt_max * p.n_tiles;
     live_tiles = p.n_active[0] * per;
-    if (static_cast<int>(blockIdx.x) >= live_tiles) return;
-    lid = xcd_tile_id(live_tiles);
+    if constexpr (EPI == kEpiBf16) {
+      lid = dealt_tile_id(per);
+      if (lid >= live_tiles) return;
+    } else {
+      if (static_cast<int>(blockIdx.x) >= live_tiles) return;
+      lid = xcd_tile_id(live_tiles);
+    }
     if (zeros_in_wgrad(p.G, p.n_active[0])) empty_groups(p.offsets, p.G, dead);
     g = p.active[lid / per];
     grouped_tile_coords(lid % per, p.mt_max, p.n_tiles, mt, nt);
@@ -372,6 +354,36 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   int bfrag[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j) bfrag[j] = wn * 64 + j * 32 + (lane & 31);
+  if constexpr (MODE == kNtRows && EPI != kEpiSwigluBwd) {
+    auto tile = [&](auto tm_c) {
+      constexpr int M = decltype(tm_c)::value;
+      f32x16 acc[M][TN];
+#pragma unroll
+      for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+      gemm_tile_mainloop<false, false, true, false, M>(ops, nk, bfrag, acc, lds, nullptr, &akm, &bkm);
+      if constexpr (EPI == kEpiSwigluKept) {
+        swiglu_kept_epilogue<M>(p, acc, row0, row_end, n0, nt, lds);
+      } else {
+        if constexpr (M == kTileTM) {
+          if (job.s > 1) {   // a slice of a split tail tile
+            tail_store_partial(p.part, job.slot, acc);
+            return;
+          }
+        }
+        tile_store_f32<M>(acc, static_cast<float*>(p.c), p.ldc, row0, row_end, n0, p.N, lds);
+      }
+    };
+    using std::integral_constant;
+    if (tm == 4) tile(integral_constant<int, 4>{});
+    else if (tm == 3) tile(integral_constant<int, 3>{});
+    else if (tm == 2) tile(integral_constant<int, 2>{});
+    else tile(integral_constant<int, 1>{});
+    return;
+  }
   f32x16 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -380,11 +392,6 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
   gemm_tile_mainloop<false, MODE == kNtKSplit, true>(ops, nk, bfrag, acc, lds, nullptr, &akm, &bkm);
-  if (MODE == kNtRows && EPI == kEpiF32) {
-    if (job.s > 1) tail_store_partial(p.part, job.slot, acc);   // a slice of a split tail tile
-    else nt_store_staged(acc, static_cast<float*>(p.c), p.ldc, row0, row_end, nt * kTileN, p.N, lds);
-    return;
-  }
 
   // acc[i][j][4 jj + ii] is row wm*128 + i*32 + 8 jj + 4 (lane >> 5) + ii, column
   // wn*64 + j*32 + (lane & 31) of the tile.
@@ -413,7 +420,7 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
       }
       wait_lgkmcnt0();
       tile_barrier();   // the k-loop's (or the previous half's) LDS reads are done
-      stage_half(stg, acc, h);
+      stage_part<kTileTM>(stg, acc, h);
       wait_lgkmcnt0();
       tile_barrier();
 #pragma unroll
@@ -442,10 +449,6 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
     }
     return;
   }
-  if constexpr (EPI == kEpiSwigluKept) {
-    swiglu_kept_epilogue(p, acc, row0, row_end, n0, nt, lds);
-    return;
-  }
   if constexpr (EPI == kEpiBf16) {
     const size_t mn = static_cast<size_t>(p.M) * p.N;
     uint16_t* cb = g < p.E ? static_cast<uint16_t*>(p.c) + g * mn : static_cast<uint16_t*>(p.cs) + (g - p.E) * mn;
@@ -455,7 +458,7 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   }
   float* cf = g < p.E ? static_cast<float*>(p.c) + static_cast<size_t>(g) * p.M * p.N
                       : static_cast<float*>(p.cs) + static_cast<size_t>(g - p.E) * p.M * p.N;
-  nt_store_staged(acc, cf, p.N, row0, row_end, n0, p.N, lds);
+  tile_store_f32<kTileTM>(acc, cf, p.N, row0, row_end, n0, p.N, lds);
   zero_slices(dead, p.E, static_cast<size_t>(p.M) * p.N / 4, lid, live_tiles, static_cast<float*>(p.c),
               static_cast<float*>(p.cs));
 }
@@ -720,19 +723,19 @@ hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s)
   // weight gradients over each expert's own rows; zeros for the others
   NtArgs m{};
   m.offsets = a.pb.offsets;
-  m.active = a.pb.active;
+  m.active = a.order;
   m.n_active = a.pb.n_active;
   m.G = G; m.E = a.E;
   m.a = a.dyg; m.lda = d; m.b = a.gh; m.ldb = F; m.M = d; m.N = F;   // dW_down [d, F] = dy^T (g h)
   m.c = a.d_w_down; m.cs = a.d_ws_down;
   m.mt_max = (d + kTileM - 1) / kTileM;
   m.n_tiles = (F + kTileN - 1) / kTileN;
-  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dim3(G * m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
+  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dealt_grid(G, m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
   m.a = a.dab; m.lda = 2 * F; m.b = a.xg; m.ldb = d; m.M = 2 * F; m.N = d;   // dW_gate_up [2F, d] = [da db]^T x
   m.c = a.d_w_gate_up; m.cs = a.d_ws_gate_up;
   m.mt_max = (2 * F + kTileM - 1) / kTileM;
   m.n_tiles = (d + kTileN - 1) / kTileN;
-  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dim3(G * m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
+  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dealt_grid(G, m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
   hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD / 2,
                      static_cast<float*>(a.d_w_down), static_cast<float*>(a.d_ws_down));
   hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD,

@@ -194,22 +194,20 @@ __device__ __forceinline__ void gemm_epilogue_kept(const GemmArgs& p, const f32x
       *reinterpret_cast<f32x4*>(a + 4) = *reinterpret_cast<const f32x4*>(src + 4);
       *reinterpret_cast<f32x4*>(b) = *reinterpret_cast<const f32x4*>(src + BN / 2);
       *reinterpret_cast<f32x4*>(b + 4) = *reinterpret_cast<const f32x4*>(src + BN / 2 + 4);
-      uint32_t ma = 0, mb = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        ma = max(ma, __float_as_uint(a[e]) & 0x7fffffffu);
-        mb = max(mb, __float_as_uint(b[e]) & 0x7fffffffu);
-      }
-      const uint32_t ba = mx8_scale_byte(max_of_4_lanes(ma)), bb = mx8_scale_byte(max_of_4_lanes(mb));
-      if (i >= TM || row >= row_end || col >= p.F) continue;
+      const uint32_t ba = mx8_scale_byte(max_of_4_lanes(max_magnitude<8>(a)));
+      const uint32_t bb = mx8_scale_byte(max_of_4_lanes(max_magnitude<8>(b)));
       u32x4 h;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         h[e] = f32x2_to_bf16x2(silu(a[2 * e]) * b[2 * e], silu(a[2 * e + 1]) * b[2 * e + 1]);
+      uint32_t ca[2], cb[2];
+      mx8_encode<8>(a, ba, ca);
+      mx8_encode<8>(b, bb, cb);
+      if (i >= TM || row >= row_end || col >= p.F) continue;
       *reinterpret_cast<u32x4*>(out + row * F + col) = h;
       int8_t* c = p.codes + row * 2 * F + col;
-      *reinterpret_cast<uint2*>(c) = make_uint2(mx8_codes4(a[0], a[1], a[2], a[3], ba), mx8_codes4(a[4], a[5], a[6], a[7], ba));
-      *reinterpret_cast<uint2*>(c + F) = make_uint2(mx8_codes4(b[0], b[1], b[2], b[3], bb), mx8_codes4(b[4], b[5], b[6], b[7], bb));
+      *reinterpret_cast<uint2*>(c) = make_uint2(ca[0], ca[1]);
+      *reinterpret_cast<uint2*>(c + F) = make_uint2(cb[0], cb[1]);
       if ((u & 3) == 0) {
         uint8_t* sc = p.scales + (row * 2 * F + col) / kMx8Block;
         sc[0] = static_cast<uint8_t>(ba);
@@ -224,7 +222,8 @@ __device__ __forceinline__ void gemm_epilogue_kept(const GemmArgs& p, const f32x
 // padding. Layers at 2000 tokens: DeepSeek-shaped, soft prior 488 -> 401 us (with adapters
 // 555 -> 489), 1000 tokens 386 -> 317; Mixtral-shaped, 400 tokens 664 -> 592.
 // PACKED: the expert matrices are in the packed layout (kPackRows x kPackCols blocks).
-// KEEP (EPI 0): the pre-activations are kept in 8-bit blocks.
+// KEEP: the training pass at a given routing. EPI 0: the pre-activations are kept in 8-bit blocks; EPI 1: O in fp32 (in
+// bf16 each term of y's sum would carry half a bf16 step more: y off by 2.9e-3 instead of 2.3e-3, relative RMS).
 template <int EPI, bool LORA = false, bool PACKED = false, bool KEEP = false>
 __global__ __launch_bounds__(GEMM_THREADS) void grouped_gemm_bf16(const GemmArgs p) {
   constexpr int WN = 4;                 // waves: 2 along rows x 4 along columns
@@ -320,7 +319,8 @@ __global__ __launch_bounds__(GEMM_THREADS) void grouped_gemm_bf16(const GemmArgs
         return;
       }
     }
-    if constexpr (KEEP) gemm_epilogue_kept<TM>(p, acc, row0, row_end, n0, lds);
+    if constexpr (KEEP && EPI == 0) gemm_epilogue_kept<TM>(p, acc, row0, row_end, n0, lds);
+    else if constexpr (KEEP) tile_store_f32<TM>(acc, static_cast<float*>(p.out), p.d, row0, row_end, n0, p.d, lds);
     else gemm_epilogue<EPI, TM>(p, acc, row0, row_end, n0, lds);
   };
   if (tm == 4) tile(std::integral_constant<int, 4>{});
@@ -332,6 +332,7 @@ __global__ __launch_bounds__(GEMM_THREADS) void grouped_gemm_bf16(const GemmArgs
 // Adds the slices of each split tail tile of the down GEMM (grouped_gemm_bf16<1>) in slice order
 // and stores its rows of O; kTailFixParts workgroups per possible tail tile, grid
 // 8 x kTailSlotsPerXcd x kTailFixParts.
+template <bool O32 = false>
 __global__ __launch_bounds__(GEMM_THREADS) void grouped_tail_fixup(const GemmArgs p) {
   const int mt_live = p.tile_off[p.G];
   const int live = mt_live * p.n_tiles;
@@ -345,7 +346,10 @@ __global__ __launch_bounds__(GEMM_THREADS) void grouped_tail_fixup(const GemmArg
   const int row0 = p.offsets[g] + (mt - p.tile_off[g]) * BM, row_end = p.offsets[g + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 4, wn = wave % 4;
   const int c0 = nt * BN + wn * 64 + (lane & 31);
-  uint16_t* out = static_cast<uint16_t*>(p.out);
+  auto put = [&](size_t o, float v) {
+    if (O32) static_cast<float*>(p.out)[o] = v;
+    else static_cast<uint16_t*>(p.out)[o] = f32_to_bf16(v);
+  };
   tail_fixup_part(p.part, xcd * kTailSlotsPerXcd + t * x.s, x.s, part, [&](int i, int q, float4 a0, float4 a1) {
     const float v0[4] = {a0.x, a0.y, a0.z, a0.w}, v1[4] = {a1.x, a1.y, a1.z, a1.w};
 #pragma unroll
@@ -353,8 +357,8 @@ __global__ __launch_bounds__(GEMM_THREADS) void grouped_tail_fixup(const GemmArg
       const int row = row0 + wm * 128 + i * 32 + 8 * q + 4 * (lane >> 5) + u;
       if (row >= row_end) continue;
       const size_t o = static_cast<size_t>(row) * p.d + c0;
-      if (c0 < p.d) out[o] = f32_to_bf16(v0[u]);
-      if (c0 + 32 < p.d) out[o + 32] = f32_to_bf16(v1[u]);
+      if (c0 < p.d) put(o, v0[u]);
+      if (c0 + 32 < p.d) put(o + 32, v1[u]);
     }
   });
 }
@@ -1015,7 +1019,7 @@ hipError_t launch_experts_bf16(const ExpertArgs& a, const PermBuffers& pb, uint1
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   if (tail_can_split(1, a.F / BK)) {
-    hipLaunchKernelGGL(grouped_tail_fixup, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(GEMM_THREADS), 0, stream, g);
+    hipLaunchKernelGGL(grouped_tail_fixup<false>, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(GEMM_THREADS), 0, stream, g);
     err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
@@ -1026,7 +1030,7 @@ hipError_t launch_experts_bf16(const ExpertArgs& a, const PermBuffers& pb, uint1
   return err;
 }
 
-hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, uint16_t* O, float* part,
+hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, float* O, float* part,
                                int8_t* codes, uint8_t* scales, int max_tiles, hipStream_t stream) {
   GemmArgs g = gemm_args(0, a, pb, pb.tile_off, max_tiles, H, O, part, nullptr);
   g.codes = codes;
@@ -1037,10 +1041,11 @@ hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint1
   if (err != hipSuccess) return err;
   g = gemm_args(1, a, pb, pb.tile_off, max_tiles, H, O, part, nullptr);
   const bool tails = tail_can_split(1, a.F / BK);
-  launch_grouped<1>(false, false, grouped_grid(max_tiles, g.n_tiles, tails), g, stream);
+  hipLaunchKernelGGL((grouped_gemm_bf16<1, false, false, true>), grouped_grid(max_tiles, g.n_tiles, tails),
+                     dim3(GEMM_THREADS), 0, stream, g);
   err = hipGetLastError();
   if (err != hipSuccess || !tails) return err;
-  hipLaunchKernelGGL(grouped_tail_fixup, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(GEMM_THREADS), 0, stream, g);
+  hipLaunchKernelGGL(grouped_tail_fixup<true>, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(GEMM_THREADS), 0, stream, g);
   return hipGetLastError();
 }
 

@@ -442,4 +442,60 @@ __device__ __forceinline__ void tail_fixup_part(const float* part, int slot0, in
   }
 }
 
+// Staged fp32 tiles: 128 rows x 256 columns at a pitch of 264 floats (the two 32-lane halves of
+// a wavefront, four rows apart, then write different banks).
+constexpr int kStgPitch = 264;
+static_assert(128 * kStgPitch * 4 <= sizeof(TileLds), "a staged half tile fits in LDS");
+
+// Part h of the tile of 64 TM rows into LDS: acc[2h + ii] of every wave (2h + ii < TM), as staged row
+// wm*64 + ii*32 + (row within the 32-row block).
+template <int TM>
+__device__ __forceinline__ void stage_part(float* stg, const f32x16 (&acc)[TM][kTileTN], int h) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / 4, wn = wave % 4;
+#pragma unroll
+  for (int ii = 0; ii < 2; ++ii) {
+    if (2 * h + ii >= TM) continue;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int j = 0; j < kTileTN; ++j)
+        stg[(wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kStgPitch + wn * 64 + j * 32 +
+            (lane & 31)] = acc[2 * h + ii < TM ? 2 * h + ii : 0][j][r];
+  }
+}
+// Tile row of staged row pr of part h; at least 64 TM where the part has no such row.
+template <int TM>
+__device__ __forceinline__ int staged_tile_row(int pr, int h) {
+  const int i = 2 * h + ((pr >> 5) & 1);
+  return i < TM ? (pr >> 6) * 32 * TM + i * 32 + (pr & 31) : 64 * TM;
+}
+
+// The fp32 tile (rows row0.., columns n0..) into out (row stride ld), through LDS in two halves
+// so that it leaves in 16-byte stores: one 4-byte store per value and lane kept the
+// texture-address path busy for ~10 us at the end of every tile. ncol % 4 == 0.
+template <int TM>
+__device__ __forceinline__ void tile_store_f32(const f32x16 (&acc)[TM][kTileTN], float* out, size_t ld, int row0,
+                                                int row_end, int n0, int ncol, TileLds& L) {
+  float* stg = reinterpret_cast<float*>(&L);
+  row_end = min(row_end, row0 + 64 * TM);
+#pragma unroll
+  for (int h = 0; h < (TM + 1) / 2; ++h) {
+    wait_lgkmcnt0();
+    tile_barrier();   // the k-loop's (or the previous part's) LDS reads are done
+    stage_part<TM>(stg, acc, h);
+    wait_lgkmcnt0();
+    tile_barrier();
+#pragma unroll 4
+    for (int q = 0; q < 16; ++q) {   // 8192 float4 per half: 64 per staged row
+      const int u = static_cast<int>(threadIdx.x) + kTileThreads * q;
+      const int pr = u >> 6, c = (u & 63) * 4;
+      const int row = row0 + staged_tile_row<TM>(pr, h), col = n0 + c;
+      if (row < row_end && col < ncol)
+        *reinterpret_cast<float4*>(out + static_cast<size_t>(row) * ld + col) =
+            *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + c]);
+    }
+  }
+}
+
 }  // namespace maskmoe

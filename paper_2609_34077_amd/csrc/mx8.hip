@@ -18,14 +18,10 @@ __global__ __launch_bounds__(kThreads) void mx8_quantize_kernel(const void* __re
     float v[16];
     load_vec8<BF16>(src, 16 * i, v);
     load_vec8<BF16>(src, 16 * i + 8, v + 8);
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
-    const uint32_t byte = mx8_scale_byte(max_of_2_lanes(m));   // n and the step are even: both lanes are here
-    u32x4 q;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = mx8_codes4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3], byte);
-    reinterpret_cast<u32x4*>(codes)[i] = q;
+    const uint32_t byte = mx8_scale_byte(max_of_2_lanes(max_magnitude<16>(v)));   // n and the step are even: both are here
+    uint32_t q[4];
+    mx8_encode<16>(v, byte, q);
+    reinterpret_cast<u32x4*>(codes)[i] = u32x4{q[0], q[1], q[2], q[3]};
     if ((i & 1) == 0) scales[i >> 1] = static_cast<uint8_t>(byte);
   }
 }
@@ -40,7 +36,7 @@ __global__ __launch_bounds__(kThreads) void mx8_dequantize_kernel(const int8_t* 
     const float s = mx8_step(scales[i >> 1]);
     float v[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = mx8_code_value(q[j >> 2], j & 3) * s;
+    for (int j = 0; j < 4; ++j) mx8_decode4(q[j], s, v + 4 * j);
     store_vec8<BF16>(dst, 16 * i, v);
     store_vec8<BF16>(dst, 16 * i + 8, v + 8);
   }

@@ -18,25 +18,59 @@ __device__ __forceinline__ float mx8_step(uint32_t byte) {
   return __uint_as_float(byte == 255 ? 0x7fc00000u : bits);
 }
 
+// 1 / step where that is a finite number (bytes from 6 on), else its largest power of two: mx8_lift takes the rest.
+__device__ __forceinline__ float mx8_inverse_step(uint32_t byte) {
+  return __uint_as_float(byte >= 6 ? (260 - byte) << 23 : 254u << 23);
+}
+
+// Multiplies the values of blocks below byte 6 (largest magnitude under 2^-121) by what mx8_inverse_step leaves out.
+template <int N>
+__device__ __forceinline__ void mx8_lift(float* v, uint32_t byte) {
+  if (__any(byte < 6)) {
+    const float f = __uint_as_float((127 + 6 - min(byte, 6u)) << 23);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= f;
+  }
+}
+
 // v / step as a code in the low byte of the result: nearest integer, ties to even, within -127..127. Adding 1.5 * 2^23
-// leaves the rounded integer in the low mantissa bits; v / step is exact (a power of two, |v / step| < 128) but where
-// it is far below one half.
-__device__ __forceinline__ uint32_t mx8_code(float v, uint32_t byte) {
+// leaves the rounded integer in the low mantissa bits; v / step is exact (a power of two).
+__device__ __forceinline__ uint32_t mx8_code(float v, float inverse_step) {
   constexpr float kMagic = 12582912.0f;
-  const float q = __builtin_amdgcn_ldexpf(v, 133 - static_cast<int>(byte)) + kMagic;
+  const float q = __builtin_fmaf(v, inverse_step, kMagic);
   return __float_as_uint(__builtin_amdgcn_fmed3f(q, kMagic - 127.0f, kMagic + 127.0f));
 }
 
-// Four values to four codes, the first in the lowest byte; 0 for a block of byte 255.
-__device__ __forceinline__ uint32_t mx8_codes4(float a, float b, float c, float d, uint32_t byte) {
-  const uint32_t lo = __builtin_amdgcn_perm(mx8_code(b, byte), mx8_code(a, byte), 0x0c0c0400u);
-  const uint32_t hi = __builtin_amdgcn_perm(mx8_code(d, byte), mx8_code(c, byte), 0x04000c0cu);
-  return byte == 255 ? 0u : lo | hi;
+// Four values to four codes, the first in the lowest byte.
+__device__ __forceinline__ uint32_t mx8_codes4(const float* v, float inverse_step) {
+  const uint32_t lo = __builtin_amdgcn_perm(mx8_code(v[1], inverse_step), mx8_code(v[0], inverse_step), 0x0c0c0400u);
+  const uint32_t hi = __builtin_amdgcn_perm(mx8_code(v[3], inverse_step), mx8_code(v[2], inverse_step), 0x04000c0cu);
+  return lo | hi;
 }
 
-// Code i (0..3) of a dword.
-__device__ __forceinline__ float mx8_code_value(uint32_t codes, int i) {
-  return static_cast<float>(static_cast<int32_t>(codes << (24 - 8 * i)) >> 24);
+// N values of one block (or more of it in other lanes, `byte` being the whole block's) to N / 4 dwords of codes; 0 for a
+// block of byte 255. The values are clobbered.
+template <int N>
+__device__ __forceinline__ void mx8_encode(float* v, uint32_t byte, uint32_t* codes) {
+  mx8_lift<N>(v, byte);
+  const float inv = mx8_inverse_step(byte);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) codes[i] = byte == 255 ? 0u : mx8_codes4(v + 4 * i, inv);
+}
+
+// The values of four codes (a byte's conversion is one instruction).
+__device__ __forceinline__ void mx8_decode4(uint32_t codes, float step, float* v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = static_cast<float>(static_cast<int8_t>(codes >> (8 * i))) * step;
+}
+
+// Bits of the largest magnitude of N values; a NaN counts as larger than any number.
+template <int N>
+__device__ __forceinline__ uint32_t max_magnitude(const float* v) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
 }
 
 template <int CTRL>

@@ -93,20 +93,18 @@ struct Piece {
   }
 };
 
-// 8-bit blocks of a piece; d % 32 == 0, so a block is whole or past the row. VEC: four lanes hold a block; else 32
+// 8-bit blocks of a piece, which is clobbered; d % 32 == 0, so a block is whole or past the row. VEC: four lanes hold a block; else 32
 // lanes, one element each.
 template <bool VEC, int N>
 __device__ __forceinline__ void store_blocks(int8_t* codes, uint8_t* scales, size_t row, int d, int p, int lane,
-                                             const float* v) {
+                                             float* v) {
   if constexpr (VEC) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
-    const uint32_t byte = mx8_scale_byte(max_of_4_lanes(m));
+    const uint32_t byte = mx8_scale_byte(max_of_4_lanes(max_magnitude<8>(v)));
     const int c = 8 * (p * N + lane);
+    uint32_t q[2];
+    mx8_encode<8>(v, byte, q);
     if (c >= d) return;
-    *reinterpret_cast<uint2*>(codes + row + c) =
-        make_uint2(mx8_codes4(v[0], v[1], v[2], v[3], byte), mx8_codes4(v[4], v[5], v[6], v[7], byte));
+    *reinterpret_cast<uint2*>(codes + row + c) = make_uint2(q[0], q[1]);
     if ((lane & 3) == 0) scales[(row + c) / kMx8Block] = static_cast<uint8_t>(byte);
   } else {
 #pragma unroll
@@ -116,8 +114,9 @@ __device__ __forceinline__ void store_blocks(int8_t* codes, uint8_t* scales, siz
       for (int o = 16; o >= 1; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, kWave)));
       const uint32_t byte = mx8_scale_byte(m);
       const int c = p * 8 * N + lane + N * j;
+      mx8_lift<1>(v + j, byte);
       if (c >= d) continue;
-      codes[row + c] = static_cast<int8_t>(byte == 255 ? 0u : mx8_code(v[j], byte));
+      codes[row + c] = static_cast<int8_t>(byte == 255 ? 0u : mx8_code(v[j], mx8_inverse_step(byte)));
       if ((lane & 31) == 0) scales[(row + c) / kMx8Block] = static_cast<uint8_t>(byte);
     }
   }

@@ -11,6 +11,7 @@ namespace maskmoe {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMaxGroups = 256 + 8;
 
 // Entries of routed and shared experts in one list.
 __global__ __launch_bounds__(kThreads) void entries_kernel(const int32_t* __restrict__ idx, const float* __restrict__ gate,
@@ -30,10 +31,9 @@ __device__ __forceinline__ int entry_row(const int32_t* idx, const int32_t* inv,
   return static_cast<uint32_t>(idx[j]) < static_cast<uint32_t>(G) ? inv[j] : -1;
 }
 
-// Sum over a token's live entries of w v[row], in entry order, fp32, rounded once; a thread per eight columns, the loads
-// of U entries in flight. O16: v is bf16 and w the gate; else v is fp32 and w 1.
-template <bool O16>
-__global__ __launch_bounds__(kThreads) void token_sum_kernel(const void* __restrict__ v, const int32_t* __restrict__ idx,
+// Sum over a token's live entries of gate v[row] (gate null: v[row]), in entry order, fp32, rounded once; a thread per
+// eight columns, the loads of U entries in flight. Bound by the rows' bytes.
+__global__ __launch_bounds__(kThreads) void token_sum_kernel(const float* __restrict__ v, const int32_t* __restrict__ idx,
                                                             const float* __restrict__ gate, const int32_t* __restrict__ inv,
                                                             int T, int KS, int G, int d, uint16_t* __restrict__ out) {
   constexpr int U = 4;
@@ -49,31 +49,44 @@ __global__ __launch_bounds__(kThreads) void token_sum_kernel(const void* __restr
     for (int u = 0; u < U; ++u) {
       const int j = t * KS + min(k0 + u, KS - 1);
       row[u] = k0 + u < KS ? entry_row(idx, inv, j, G) : -1;
-      g[u] = O16 ? gate[j] : 1.0f;
+      g[u] = gate ? gate[j] : 1.0f;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (row[u] >= 0) load_vec8<O16>(v, static_cast<size_t>(row[u]) * d + c, o[u]);
+      if (row[u] >= 0) load_vec8<false>(v, static_cast<size_t>(row[u]) * d + c, o[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (row[u] >= 0)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] += O16 ? g[u] * o[u][e] : o[u][e];
+        for (int e = 0; e < 8; ++e) s[e] += g[u] * o[u][e];
   }
   store_vec8<true>(out, 8 * i, s);
 }
 
-// dy and x (bf16, or the values of its blocks) of each row's token, and the row's gate. One workgroup per row.
+// dy and x (bf16, or the values of its blocks) of each row's token, and the row's gate: one workgroup per row. One more
+// lists the groups with rows, most rows first, then by number.
 __global__ __launch_bounds__(kThreads) void gather_kernel(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ x,
                                                          const int8_t* __restrict__ x_codes,
                                                          const uint8_t* __restrict__ x_scales,
-                                                         const float* __restrict__ gate, const int32_t* __restrict__ rows,
+                                                         const float* __restrict__ gate,
+                                                         const int32_t* __restrict__ offsets, int G,
                                                          const int32_t* __restrict__ perm,
                                                          const int32_t* __restrict__ row_tok, int d,
                                                          uint16_t* __restrict__ dyg, uint16_t* __restrict__ xg,
-                                                         float* __restrict__ row_gate) {
-  const int r = blockIdx.x;
-  if (r >= rows[0]) return;
+                                                         float* __restrict__ row_gate, int32_t* __restrict__ order) {
+  if (blockIdx.x == 0) {
+    __shared__ int count[kMaxGroups];
+    for (int g = threadIdx.x; g < G; g += kThreads) count[g] = offsets[g + 1] - offsets[g];
+    __syncthreads();
+    for (int g = threadIdx.x; g < G; g += kThreads) {
+      int rank = 0;
+      for (int o = 0; o < G; ++o) rank += count[o] > count[g] || (count[o] == count[g] && o < g) ? 1 : 0;
+      if (count[g] > 0) order[rank] = g;
+    }
+    return;
+  }
+  const int r = blockIdx.x - 1;
+  if (r >= offsets[G]) return;
   const size_t src = static_cast<size_t>(row_tok[r]) * d, dst = static_cast<size_t>(r) * d;
   for (int c = threadIdx.x * 8; c < d; c += kThreads * 8) {
     *reinterpret_cast<u32x4*>(dyg + dst + c) = *reinterpret_cast<const u32x4*>(dy + src + c);
@@ -81,8 +94,8 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(const uint16_t* __rest
       const uint2 q = *reinterpret_cast<const uint2*>(x_codes + src + c);
       const float step = mx8_step(x_scales[(src + c) / kMx8Block]);
       float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = mx8_code_value(e < 4 ? q.x : q.y, e & 3) * step;
+      mx8_decode4(q.x, step, v);
+      mx8_decode4(q.y, step, v + 4);
       store_vec8<true>(xg, dst + c, v);
     } else {
       *reinterpret_cast<u32x4*>(xg + dst + c) = *reinterpret_cast<const u32x4*>(x + src + c);
@@ -172,12 +185,13 @@ ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n
   w.part = take(kTailPartBytes);
   const size_t common = off;
   w.H = take(rows * F * 2);
-  w.O = take(rows * d * 2);
+  w.O = take(rows * d * 4);
   w.forward_total = off;
   off = common;
   w.dyg = take(rows * d * 2);
   w.xg = take(rows * d * 2);
   w.row_gate = take(rows * 4);
+  w.order = take(G * 4);
   w.gh = take(rows * F * 2);
   w.dab = take(rows * 2 * F * 2);
   w.dxr = take(rows * d * 4);
@@ -199,11 +213,11 @@ hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipS
   e.ws_gate_up = a.ws_gate_up;
   e.ws_down = a.ws_down;
   e.T = a.T; e.d = a.d; e.F = a.F; e.E = a.E; e.K = g.KS; e.n_shared = a.n_shared;
-  uint16_t* O = reinterpret_cast<uint16_t*>(ws + w.O);
+  float* O = reinterpret_cast<float*>(ws + w.O);
   err = launch_experts_kept(e, g.pb, reinterpret_cast<uint16_t*>(ws + w.H), O, reinterpret_cast<float*>(ws + w.part),
                             a.codes, a.scales, g.max_tiles, stream);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(token_sum_kernel<true>, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
+  hipLaunchKernelGGL(token_sum_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
                      O, g.idx, g.gate, g.pb.inv, a.T, g.KS, g.G, a.d, a.y);
   return hipGetLastError();
 }
@@ -239,6 +253,8 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   uint16_t* dyg = reinterpret_cast<uint16_t*>(ws + w.dyg);
   uint16_t* xg = reinterpret_cast<uint16_t*>(ws + w.xg);
   float* row_gate = reinterpret_cast<float*>(ws + w.row_gate);
+  int32_t* order = reinterpret_cast<int32_t*>(ws + w.order);
+  k.order = order;
   k.dyg = dyg;
   k.xg = xg;
   k.row_gate = row_gate;
@@ -252,14 +268,14 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   k.d_ws_gate_up = b.d_ws_gate_up;
   k.d_ws_down = b.d_ws_down;
   k.d = a.d; k.F = a.F; k.E = a.E; k.G = g.G; k.max_tiles = g.max_tiles;
-  hipLaunchKernelGGL(gather_kernel, dim3(g.rows), dim3(kThreads), 0, stream, b.dy, a.x, b.x_codes, b.x_scales, g.gate,
-                     g.pb.offsets + g.G, g.pb.perm, g.pb.row_tok, a.d, dyg, xg, row_gate);
+  hipLaunchKernelGGL(gather_kernel, dim3(g.rows + 1), dim3(kThreads), 0, stream, b.dy, a.x, b.x_codes, b.x_scales,
+                     g.gate, g.pb.offsets, g.G, g.pb.perm, g.pb.row_tok, a.d, dyg, xg, row_gate, order);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   err = launch_experts_backward_products(k, stream);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(token_sum_kernel<false>, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
-                     k.dxr, g.idx, g.gate, g.pb.inv, a.T, g.KS, g.G, a.d, b.d_x);
+  hipLaunchKernelGGL(token_sum_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
+                     k.dxr, g.idx, nullptr, g.pb.inv, a.T, g.KS, g.G, a.d, b.d_x);
   if (b.d_gate)
     hipLaunchKernelGGL(d_gate_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.K)), dim3(kThreads), 0, stream,
                        k.dgate_part, g.idx, g.pb.inv, a.T, a.K, g.KS, g.G, dgate_parts(a.F), b.d_gate);

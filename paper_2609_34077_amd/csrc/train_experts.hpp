@@ -33,21 +33,22 @@ struct ExpertsBwdArgs {
 struct ExpertsTrainLayout {   // byte offsets into the workspaces; the grouping is first in both
   size_t idx, gate, offsets, tile_off, active, n_active, perm, inv, row_tok, pcount;
   size_t H, O, part;                                            // forward
-  size_t dyg, xg, row_gate, gh, dab, dxr, dgate_part;           // gradient (with part)
+  size_t dyg, xg, row_gate, order, gh, dab, dxr, dgate_part;    // gradient (with part)
   size_t forward_total, backward_total;
 };
 ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n_shared);
 hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipStream_t stream);
 hipError_t launch_experts_backward(const ExpertsBwdArgs& a, void* workspace, hipStream_t stream);
 
-// H (bf16 [rows, F]) with codes and scales, then O (bf16 expert outputs [rows, d]), on row tiles of kGemmBM (experts.hip).
-hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, uint16_t* O, float* part,
+// H (bf16 [rows, F]) with codes and scales, then O (fp32 expert outputs [rows, d]), on row tiles of kGemmBM (experts.hip).
+hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, float* O, float* part,
                                int8_t* codes, uint8_t* scales, int max_tiles, hipStream_t stream);
 
 // The products of the gradient on rows grouped by expert (backward.hip).
 struct KeptBwdArgs {
   const uint16_t *w_gate_up, *w_down, *ws_gate_up, *ws_down;
   PermBuffers pb;
+  const int32_t* order;       // [pb.n_active[0]] the groups with rows, most rows first
   const int8_t* codes;        // [rows, 2F]
   const uint8_t* scales;
   const uint16_t* dyg;        // [rows, d] dy of each row's token
