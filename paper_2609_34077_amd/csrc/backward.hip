@@ -89,6 +89,7 @@ struct NtArgs {
   float* dgate_part;          // SWIGLU_KEPT: [rows, n_tiles] partial sums of u h
   void* c;                    // ROWS: [rows, ldc]; KSPLIT: routed groups' [M, N] matrices
   void* cs;                   // KSPLIT: shared groups' [M, N] matrices
+  int32_t* next;              // wgrad_kernel: [8] tiles that each XCD has handed out, 0 at the start
   float* part;                // ROWS, fp32 output: partial tiles of split tail tiles (tile_job)
   int G, E, M, N, K, lda, ldb, ldc, mt_max, n_tiles;
   int cu_xcd;                 // workgroups an XCD runs at once
@@ -136,37 +137,7 @@ __device__ __forceinline__ void zero_slices(const uint64_t (&dead)[kDeadWords], 
 }
 
 enum { kNtRows = 0, kNtKSplit = 1 };
-enum { kEpiSwigluBwd = 0, kEpiF32 = 1, kEpiSwigluKept = 2, kEpiBf16 = 3 };
-
-// The finished tile (rows row0.., columns n0..) into out (row stride ld) as bf16, through LDS whole, so that it leaves in
-// 16-byte stores. ncol % 8 == 0.
-constexpr int kStgPitch16 = kTileN + 8;
-static_assert(kTileM * kStgPitch16 * 2 <= sizeof(TileLds), "a staged bf16 tile fits in LDS");
-__device__ __forceinline__ void nt_store_bf16(const f32x16 (&acc)[kTileTM][kTileTN], uint16_t* out, size_t ld, int row0,
-                                              int row_end, int n0, int ncol, TileLds& L) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 4, wn = wave % 4;
-  uint16_t* stg = reinterpret_cast<uint16_t*>(&L);
-  wait_lgkmcnt0();
-  tile_barrier();   // the k-loop's LDS reads are done
-#pragma unroll
-  for (int i = 0; i < kTileTM; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int j = 0; j < kTileTN; ++j)
-        stg[(wm * 128 + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kStgPitch16 + wn * 64 + j * 32 + (lane & 31)] =
-            f32_to_bf16(acc[i][j][r]);
-  wait_lgkmcnt0();
-  tile_barrier();
-#pragma unroll 4
-  for (int q = 0; q < 16; ++q) {   // 8192 pieces of eight columns: 32 per row
-    const int u = tid + kTileThreads * q;
-    const int pr = u >> 5, c = (u & 31) * 8, row = row0 + pr, col = n0 + c;
-    if (row < row_end && col < ncol)
-      *reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * ld + col) =
-          *reinterpret_cast<const u32x4*>(&stg[pr * kStgPitch16 + c]);
-  }
-}
+enum { kEpiSwigluBwd = 0, kEpiF32 = 1, kEpiSwigluKept = 2 };
 
 // Sum over each half of the wavefront, in its last lane.
 __device__ __forceinline__ float half_wave_sum(float v) {
@@ -263,21 +234,6 @@ __device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x
 }
 
 
-// Tile of this workgroup where groups of `per` tiles each have reductions of their own lengths, longest group first: every
-// XCD takes an eighth of each group (pieces of per / 8 consecutive tiles, dealt in turn), so that all have the same
-// work and no long reduction starts late. In ranges of consecutive tiles for each XCD instead, as for products whose
-// tiles are all alike, the XCD with the shared experts' tiles decided: DeepSeek-shaped, 4096 tokens, the two
-// weight gradients 854 + 453 us.
-__host__ __device__ __forceinline__ int dealt_piece(int per) { return per < 8 ? 1 : per / 8; }
-__device__ __forceinline__ int dealt_tile_id(int per) {
-  const int c = dealt_piece(per), local = blockIdx.x >> 3;
-  return (local / c * 8 + static_cast<int>(blockIdx.x & 7)) * c + local % c;
-}
-static dim3 dealt_grid(int groups, int per) {
-  const int64_t c = dealt_piece(per), pieces = (static_cast<int64_t>(groups) * per + c - 1) / c;
-  return dim3(static_cast<unsigned>((pieces + 7) / 8 * 8 * c));
-}
-
 // ROWS (dgrad): group g's rows offsets[g]..offsets[g+1] of A (K-contiguous) times its own
 // K-major [K, N] matrix, row tiles enumerated by tile_off as in the forward. KSPLIT (wgrad): for
 // every non-empty group g the full [M, N] product over its rows offsets[g]..offsets[g+1] of the
@@ -327,13 +283,8 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   } else {
     const int per = p.mt_max * p.n_tiles;
     live_tiles = p.n_active[0] * per;
-    if constexpr (EPI == kEpiBf16) {
-      lid = dealt_tile_id(per);
-      if (lid >= live_tiles) return;
-    } else {
-      if (static_cast<int>(blockIdx.x) >= live_tiles) return;
-      lid = xcd_tile_id(live_tiles);
-    }
+    if (static_cast<int>(blockIdx.x) >= live_tiles) return;
+    lid = xcd_tile_id(live_tiles);
     if (zeros_in_wgrad(p.G, p.n_active[0])) empty_groups(p.offsets, p.G, dead);
     g = p.active[lid / per];
     grouped_tile_coords(lid % per, p.mt_max, p.n_tiles, mt, nt);
@@ -449,18 +400,122 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
     }
     return;
   }
-  if constexpr (EPI == kEpiBf16) {
-    const size_t mn = static_cast<size_t>(p.M) * p.N;
-    uint16_t* cb = g < p.E ? static_cast<uint16_t*>(p.c) + g * mn : static_cast<uint16_t*>(p.cs) + (g - p.E) * mn;
-    nt_store_bf16(acc, cb, p.N, row0, row_end, n0, p.N, lds);
-    zero_slices(dead, p.E, mn / 8, lid, live_tiles, static_cast<float*>(p.c), static_cast<float*>(p.cs));
-    return;
-  }
   float* cf = g < p.E ? static_cast<float*>(p.c) + static_cast<size_t>(g) * p.M * p.N
                       : static_cast<float*>(p.cs) + static_cast<size_t>(g - p.E) * p.M * p.N;
   tile_store_f32<kTileTM>(acc, cf, p.N, row0, row_end, n0, p.N, lds);
   zero_slices(dead, p.E, static_cast<size_t>(p.M) * p.N / 4, lid, live_tiles, static_cast<float*>(p.c),
               static_cast<float*>(p.cs));
+}
+
+// Weight gradients in bf16: for every group with rows the [M, N] product over its rows of the K-major A [rows, M] and
+// B [rows, N], p.active naming the groups by descending rows. One workgroup a CU takes tile after tile; the first k-tile
+// of the next tile is loaded while this one's results go through the other 64 KB of LDS (128 rows at a time, as bf16,
+// so that they leave in 16-byte stores), and the stores are not waited for. An expert's reduction is short where there
+// are many (DeepSeek-shaped, 4096 tokens: six k-tiles, 10 us, of which a workgroup per tile made 20).
+// After its first two tiles a workgroup takes them from its XCD's counter (which changes who computes a tile, not what
+// it holds): asked for at the start of a tile, handed round during its end, used for the loads at the next one's end.
+// Tile order: every XCD takes an eighth of each group (pieces of per / 8 consecutive tiles, dealt in turn), so that all
+// have the same work and no long reduction starts late. With a range of consecutive tiles for each XCD instead, as for
+// products whose tiles are all alike, the XCD with the shared experts' tiles decided: the two gradients of that layer
+// 854 + 453 us, dealt 520 + 270.
+__global__ __launch_bounds__(kTileThreads) void wgrad_kernel(const NtArgs p) {
+  __shared__ TileLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 4, wn = wave % 4;
+  const int per = p.mt_max * p.n_tiles, live_tiles = p.n_active[0] * per;
+  const int piece = per < 8 ? 1 : per / 8, xcd = blockIdx.x & 7, slots = gridDim.x >> 3;
+  uint64_t dead[kDeadWords] = {};
+  const bool zeros = zeros_in_wgrad(p.G, p.n_active[0]);
+  if (zeros) empty_groups(p.offsets, p.G, dead);
+  int bfrag[kTileTN];
+#pragma unroll
+  for (int j = 0; j < kTileTN; ++j) bfrag[j] = wn * 64 + j * 32 + (lane & 31);
+
+  struct Job {
+    int g, mt, nt, nk;
+    TileKm a, b;
+  };
+  auto tile_of = [&](int local) { return (local / piece * 8 + xcd) * piece + local % piece; };
+  auto job_of = [&](int lid) {
+    Job j;
+    j.g = p.active[lid / per];
+    grouped_tile_coords(lid % per, p.mt_max, p.n_tiles, j.mt, j.nt);
+    const int r0 = p.offsets[j.g], nrows = p.offsets[j.g + 1] - r0;
+    j.nk = (nrows + kTileK - 1) / kTileK;
+    j.a = TileKm{reinterpret_cast<const char*>(p.a + static_cast<size_t>(r0) * p.lda + j.mt * kTileM), p.lda * 2, nrows,
+                 p.M - j.mt * kTileM};
+    j.b = TileKm{reinterpret_cast<const char*>(p.b + static_cast<size_t>(r0) * p.ldb + j.nt * kTileN), p.ldb * 2, nrows,
+                 p.N - j.nt * kTileN};
+    return j;
+  };
+
+  int lid = tile_of(blockIdx.x >> 3), next = tile_of((blockIdx.x >> 3) + slots);
+  if (lid >= live_tiles) return;
+  Job job = job_of(lid);
+  gemm_tile_prefetch(job.a, job.b, lds);
+  wait_vmcnt<0>();
+  tile_barrier();
+  for (;;) {
+    f32x16 acc[kTileTM][kTileTN];
+#pragma unroll
+    for (int i = 0; i < kTileTM; ++i)
+#pragma unroll
+      for (int j = 0; j < kTileTN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    const bool more = next < live_tiles;
+    Job nj = job;
+    if (more) nj = job_of(next);
+    int taken = 0;
+    if (tid == 0 && more)
+      taken = __hip_atomic_fetch_add(p.next + xcd, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    gemm_tile_mainloop<false, true, true, false, kTileTM, true>(TileOps{}, job.nk, bfrag, acc, lds, nullptr, &job.a, &job.b);
+    wait_lgkmcnt0();
+    tile_barrier();   // every wave is past the k-loop's LDS reads, and its loads have arrived
+    if (more) gemm_tile_prefetch(nj.a, nj.b, lds);
+    int32_t* word = reinterpret_cast<int32_t*>(&lds.a[0][1][0]);   // A's second buffer is idle until the next mainloop
+    if (tid == 0) *word = taken;
+    const size_t mn = static_cast<size_t>(p.M) * p.N;
+    uint16_t* out = job.g < p.E ? static_cast<uint16_t*>(p.c) + job.g * mn
+                                : static_cast<uint16_t*>(p.cs) + (job.g - p.E) * mn;
+    // [128 rows][256 columns], 16-byte unit u of row r at u ^ 4 (r >> 2 & 1): the two halves of a wavefront, four rows
+    // apart, write different banks
+    uint16_t* stg = reinterpret_cast<uint16_t*>(&lds.b[1][0]);
+    int after = 0;
+    static_assert(128 * kTileN * 2 <= 2 * sizeof(lds.b[0]), "128 rows fit behind B's first buffer");
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int j = 0; j < kTileTN; ++j) {
+            const int row = wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+            const int col = wn * 64 + j * 32 + (lane & 31);
+            stg[row * kTileN + (col ^ (row >> 2 & 1) * 32)] = f32_to_bf16(acc[2 * h + ii][j][r]);
+          }
+      wait_lgkmcnt0();
+      if (h == 0) wait_vmcnt<0>();   // the next tile's first operands, before any store: stores are never waited for here
+      tile_barrier();
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {   // 4096 pieces of eight columns: 32 per row
+        const int u = tid + kTileThreads * q;
+        const int pr = u >> 5, c = (u & 31) * 8;
+        const int row = job.mt * kTileM + staged_tile_row<kTileTM>(pr, h), col = job.nt * kTileN + c;
+        if (row < p.M && col < p.N)
+          *reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * p.N + col) =
+              *reinterpret_cast<const u32x4*>(&stg[pr * kTileN + (c ^ (pr >> 2 & 1) * 32)]);
+      }
+      if (h == 0) after = __builtin_amdgcn_readfirstlane(*word);
+      wait_lgkmcnt0();
+      tile_barrier();   // the staged rows are read
+    }
+    if (zeros) zero_slices(dead, p.E, mn / 8, lid, live_tiles, static_cast<float*>(p.c), static_cast<float*>(p.cs));
+    if (!more) return;
+    lid = next;
+    job = nj;
+    next = tile_of(2 * slots + after);
+  }
 }
 
 // Adds the slices of each split tail tile of the ROWS fp32 product in slice order and stores
@@ -730,12 +785,14 @@ hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s)
   m.c = a.d_w_down; m.cs = a.d_ws_down;
   m.mt_max = (d + kTileM - 1) / kTileM;
   m.n_tiles = (F + kTileN - 1) / kTileN;
-  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dealt_grid(G, m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
+  m.next = a.next;
+  hipLaunchKernelGGL(wgrad_kernel, dim3(8 * n.cu_xcd), dim3(kTileThreads), 0, s, m);
   m.a = a.dab; m.lda = 2 * F; m.b = a.xg; m.ldb = d; m.M = 2 * F; m.N = d;   // dW_gate_up [2F, d] = [da db]^T x
   m.c = a.d_w_gate_up; m.cs = a.d_ws_gate_up;
   m.mt_max = (2 * F + kTileM - 1) / kTileM;
   m.n_tiles = (d + kTileN - 1) / kTileN;
-  hipLaunchKernelGGL((gemm_nt_kernel<kNtKSplit, kEpiBf16>), dealt_grid(G, m.mt_max * m.n_tiles), dim3(kTileThreads), 0, s, m);
+  m.next = a.next + 8;
+  hipLaunchKernelGGL(wgrad_kernel, dim3(8 * n.cu_xcd), dim3(kTileThreads), 0, s, m);
   hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD / 2,
                      static_cast<float*>(a.d_w_down), static_cast<float*>(a.d_ws_down));
   hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD,

@@ -144,13 +144,15 @@ __device__ __forceinline__ void tile_barrier() { asm volatile("s_barrier" ::: "m
 // STREAM: operand B is read by this workgroup alone: non-temporal loads.
 // TM: A fragments per wave; a tile of 64 TM rows, A fragment i then being tile row
 // 32 TM g + 32 i + (lane & 31) and o.aoff / o.x's following tile_dma_row_a(TM, i).
-template <bool EXTRA = false, bool AKM = false, bool BKM = false, bool STREAM = false, int TM = kTileTM>
+// PRE: the first k-tile's operands are in LDS (gemm_tile_prefetch, its loads waited for, and a barrier after that).
+template <bool EXTRA = false, bool AKM = false, bool BKM = false, bool STREAM = false, int TM = kTileTM, bool PRE = false>
 __device__ __forceinline__ void gemm_tile_mainloop(const TileOps& o, int nk, const int (&bfrag)[kTileTN],
                                                    f32x16 (&acc)[TM][kTileTN], TileLds& L,
                                                    const TileOps* x = nullptr, const TileKm* akm = nullptr,
                                                    const TileKm* bkm = nullptr) {
   static_assert(!(EXTRA && (AKM || BKM)), "the extra k-tile is K-contiguous");
   static_assert(!AKM || TM == kTileTM, "a K-major A operand fills the tile");
+  static_assert(!(EXTRA && PRE), "the extra k-tile is not prefetched");
   constexpr int X = EXTRA ? 1 : 0;
   if (nk <= 0) return;
   const int ntot = nk + X;
@@ -238,13 +240,15 @@ __device__ __forceinline__ void gemm_tile_mainloop(const TileOps& o, int nk, con
     for (int i = 0; i < TM; ++i) dma16(la0 + static_cast<uint32_t>(i * 1024), x->a, x->aoff[i]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) dma16(lb0 + static_cast<uint32_t>(i * 1024), x->b, x->boff[i]);
-  } else {
+  } else if (!PRE) {
     dma_a(0);
     dma_b(0);
   }
   dma_b(1);
-  wait_vmcnt<0>();
-  tile_barrier();
+  if (!PRE) {
+    wait_vmcnt<0>();
+    tile_barrier();
+  }
   // group 1 runs one phase behind group 0: one extra barrier first (group 0 adds it at the end)
   if (g == 1) tile_barrier();
   for (int m = 0; m < ntot; ++m) {
@@ -273,6 +277,25 @@ __device__ __forceinline__ void gemm_tile_mainloop(const TileOps& o, int nk, con
   }
   if (g == 0) tile_barrier();
   wait_vmcnt<0>();
+}
+
+// The first k-tile's loads of a product whose operands are both K-major, for a later mainloop of PRE: into buffer 0 of A
+// and of B, so the other buffers of B (64 KB) stay free until that mainloop. All waves are past the buffers' last use.
+__device__ __forceinline__ void gemm_tile_prefetch(const TileKm& akm, const TileKm& bkm, TileLds& L) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int g = wave >> 2, q = wave & 3;
+  const uint32_t la0 = lds_offset(&L.a[g][0][0]) + q * kTileTM * 1024;
+  const uint32_t lb0 = lds_offset(&L.b[0][0]) + (g * 16 + q * 4) * 1024;
+  const i32x4 ar = buffer_rsrc(akm.base, static_cast<uint32_t>(akm.krows) * static_cast<uint32_t>(akm.ld));
+  const i32x4 br = buffer_rsrc(bkm.base, static_cast<uint32_t>(bkm.krows) * static_cast<uint32_t>(bkm.ld));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int kr = 4 * (4 * q + i) + (lane >> 4);
+    const int col = g * 128 + 8 * km_unit(lane & 15, kr);
+    dma16b(la0 + static_cast<uint32_t>(i * 1024), ar, static_cast<uint32_t>(kr * akm.ld + min(col, akm.mcols - 8) * 2));
+    dma16b(lb0 + static_cast<uint32_t>(i * 1024), br, static_cast<uint32_t>(kr * bkm.ld + min(col, bkm.mcols - 8) * 2));
+  }
 }
 
 // XCD-aware tile order: the hardware deals workgroup ids round-robin over the 8 XCDs, so ids

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void token_sum_kernel(const float* __rest
 }
 
 // dy and x (bf16, or the values of its blocks) of each row's token, and the row's gate: one workgroup per row. One more
-// lists the groups with rows, most rows first, then by number.
+// lists the groups with rows, most rows first, then by number, and clears the counters of the weight gradients' tiles.
 __global__ __launch_bounds__(kThreads) void gather_kernel(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ x,
                                                          const int8_t* __restrict__ x_codes,
                                                          const uint8_t* __restrict__ x_scales,
@@ -73,9 +73,11 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(const uint16_t* __rest
                                                          const int32_t* __restrict__ perm,
                                                          const int32_t* __restrict__ row_tok, int d,
                                                          uint16_t* __restrict__ dyg, uint16_t* __restrict__ xg,
-                                                         float* __restrict__ row_gate, int32_t* __restrict__ order) {
+                                                         float* __restrict__ row_gate, int32_t* __restrict__ order,
+                                                         int32_t* __restrict__ next) {
   if (blockIdx.x == 0) {
     __shared__ int count[kMaxGroups];
+    if (threadIdx.x < 2 * 8) next[threadIdx.x] = 0;
     for (int g = threadIdx.x; g < G; g += kThreads) count[g] = offsets[g + 1] - offsets[g];
     __syncthreads();
     for (int g = threadIdx.x; g < G; g += kThreads) {
@@ -192,6 +194,7 @@ ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n
   w.xg = take(rows * d * 2);
   w.row_gate = take(rows * 4);
   w.order = take(G * 4);
+  w.next = take(2 * 8 * 4);
   w.gh = take(rows * F * 2);
   w.dab = take(rows * 2 * F * 2);
   w.dxr = take(rows * d * 4);
@@ -255,6 +258,7 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   float* row_gate = reinterpret_cast<float*>(ws + w.row_gate);
   int32_t* order = reinterpret_cast<int32_t*>(ws + w.order);
   k.order = order;
+  k.next = reinterpret_cast<int32_t*>(ws + w.next);
   k.dyg = dyg;
   k.xg = xg;
   k.row_gate = row_gate;
@@ -269,7 +273,7 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   k.d_ws_down = b.d_ws_down;
   k.d = a.d; k.F = a.F; k.E = a.E; k.G = g.G; k.max_tiles = g.max_tiles;
   hipLaunchKernelGGL(gather_kernel, dim3(g.rows + 1), dim3(kThreads), 0, stream, b.dy, a.x, b.x_codes, b.x_scales,
-                     g.gate, g.pb.offsets, g.G, g.pb.perm, g.pb.row_tok, a.d, dyg, xg, row_gate, order);
+                     g.gate, g.pb.offsets, g.G, g.pb.perm, g.pb.row_tok, a.d, dyg, xg, row_gate, order, k.next);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   err = launch_experts_backward_products(k, stream);

@@ -33,7 +33,7 @@ struct ExpertsBwdArgs {
 struct ExpertsTrainLayout {   // byte offsets into the workspaces; the grouping is first in both
   size_t idx, gate, offsets, tile_off, active, n_active, perm, inv, row_tok, pcount;
   size_t H, O, part;                                            // forward
-  size_t dyg, xg, row_gate, order, gh, dab, dxr, dgate_part;    // gradient (with part)
+  size_t dyg, xg, row_gate, order, next, gh, dab, dxr, dgate_part;    // gradient (with part)
   size_t forward_total, backward_total;
 };
 ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n_shared);
@@ -49,6 +49,7 @@ struct KeptBwdArgs {
   const uint16_t *w_gate_up, *w_down, *ws_gate_up, *ws_down;
   PermBuffers pb;
   const int32_t* order;       // [pb.n_active[0]] the groups with rows, most rows first
+  int32_t* next;              // [2][8] zeros: tiles that each XCD's workgroups have taken, of each weight gradient
   const int8_t* codes;        // [rows, 2F]
   const uint8_t* scales;
   const uint16_t* dyg;        // [rows, d] dy of each row's token
