@@ -829,47 +829,59 @@ def maskmoe_experts_forward_mx4(x, topk_idx, topk_gate, experts: PackedMx4Expert
     return y
 
 
+def _here(torch):
+    """Current device and the handle of its current stream."""
+    d = torch.cuda.current_device()
+    return d, torch._C._cuda_getCurrentRawStream(d)
+
+
+def _rows32(t, name: str):
+    """Row length of a tensor whose last dimension is whole blocks of 32."""
+    cols = t.shape[-1] if t.dim() else 0
+    if cols == 0 or cols % 32:
+        raise ValueError(f"the last dimension of {name} must be a positive multiple of 32")
+    _fits(cols)
+    return cols
+
+
 def maskmoe_mx8_quantize(x):
     """8-bit blocks of x [..., cols] (bf16 or fp32, cols a multiple of 32) along its last dimension: codes [..., cols]
     int8 and scales [..., cols/32] uint8; values are ``codes * 2**(scales - 133)``."""
-    lib = load()
-    shape, cols = _rows32(x, "x")
-    codes = x.new_empty(shape, dtype=_torch().int8)
-    scales = x.new_empty(shape[:-1] + (cols // 32,), dtype=_torch().uint8)
-    _check("maskmoe_mx8_quantize", lib.maskmoe_mx8_quantize(x.numel() // cols, cols, _dtype_code(x), x.data_ptr(),
-                                                            codes.data_ptr(), scales.data_ptr(), _stream()))
+    import torch
+    cols = _rows32(x, "x")
+    here, stream = _here(torch)
+    shape = x.shape
+    _want(x, "x", shape, x.dtype, here)
+    codes = torch.empty_like(x, dtype=torch.int8)
+    scales = x.new_empty((*shape[:-1], cols // 32), dtype=torch.uint8)
+    _check("maskmoe_mx8_quantize", load().maskmoe_mx8_quantize(x.numel() // cols, cols, _dtype_code(x), x.data_ptr(),
+                                                               codes.data_ptr(), scales.data_ptr(), stream))
     return codes, scales
 
 
 def maskmoe_mx8_dequantize(codes, scales, dtype):
     """The values of codes [..., cols] int8 and scales [..., cols/32] uint8 as a bf16 or fp32 tensor [..., cols]."""
-    torch = _torch()
-    lib = load()
-    shape, cols = _rows32(codes, "codes")
-    here = torch.cuda.current_device()
+    import torch
+    cols = _rows32(codes, "codes")
+    here, stream = _here(torch)
+    shape = codes.shape
     _want(codes, "codes", shape, torch.int8, here)
-    _want(scales, "scales", shape[:-1] + (cols // 32,), torch.uint8, here)
-    out = codes.new_empty(shape, dtype=dtype)
-    _check("maskmoe_mx8_dequantize", lib.maskmoe_mx8_dequantize(codes.numel() // cols, cols, _dtype_code(out),
-                                                                codes.data_ptr(), scales.data_ptr(), out.data_ptr(),
-                                                                _stream()))
+    _want(scales, "scales", (*shape[:-1], cols // 32), torch.uint8, here)
+    out = torch.empty_like(codes, dtype=dtype)
+    _check("maskmoe_mx8_dequantize", load().maskmoe_mx8_dequantize(codes.numel() // cols, cols, _dtype_code(out),
+                                                                   codes.data_ptr(), scales.data_ptr(), out.data_ptr(),
+                                                                   stream))
     return out
 
 
-def _torch():
-    import torch
-    return torch
-
-
-def _rows32(t, name: str):
-    """Shape and row length of a contiguous tensor on the current device whose last dimension is whole blocks of 32."""
-    shape = t.shape
-    cols = shape[-1] if shape else 0
-    if cols == 0 or cols % 32:
-        raise ValueError(f"the last dimension of {name} must be a positive multiple of 32")
-    _fits(cols)
-    _want(t, name, shape, t.dtype, _torch().cuda.current_device())
-    return shape, cols
+def _rows(t, name: str):
+    """Rows and row length of t [..., d]."""
+    d = t.shape[-1] if t.dim() else 0
+    if d == 0:
+        raise ValueError(f"{name} must have rows of at least one element")
+    T = t.numel() // d
+    _fits(T, d)
+    return T, d
 
 
 def maskmoe_norm_forward(x, weight, residual=None, eps: float = 1e-5, with_y: bool = True, with_mx8: bool = False,
@@ -880,34 +892,29 @@ def maskmoe_norm_forward(x, weight, residual=None, eps: float = 1e-5, with_y: bo
     Returns ``(y, hidden, codes, scales)``: y [..., d] (None without ``with_y``), hidden = s (None without a
     residual unless a buffer is given), codes [..., d] int8 and scales [..., d/32] uint8, y's 8-bit blocks (None without
     ``with_mx8``). ``hidden`` and ``y``: output buffers; hidden may be x or residual itself (in place), y too."""
-    torch = _torch()
-    lib = load()
-    shape = x.shape
-    if not shape or shape[-1] == 0:
-        raise ValueError("x must have rows of at least one element")
-    d = shape[-1]
-    T = x.numel() // d
-    _fits(T, d)
-    here = torch.cuda.current_device()
-    _want(x, "x", shape, x.dtype, here)
-    _want(weight, "weight", (d,), x.dtype, here)
+    import torch
+    T, d = _rows(x, "x")
+    here, stream = _here(torch)
+    shape, dtype = x.shape, x.dtype
+    _want(x, "x", shape, dtype, here)
+    _want(weight, "weight", (d,), dtype, here)
     if residual is not None:
-        _want(residual, "residual", shape, x.dtype, here)
+        _want(residual, "residual", shape, dtype, here)
     if hidden is not None:
-        _want(hidden, "hidden", shape, x.dtype, here)
+        _want(hidden, "hidden", shape, dtype, here)
     elif residual is not None:
         hidden = torch.empty_like(x)
     if y is not None:
-        _want(y, "y", shape, x.dtype, here)
+        _want(y, "y", shape, dtype, here)
     elif with_y:
         y = torch.empty_like(x)
     codes = scales = None
     if with_mx8:
-        codes = x.new_empty(shape, dtype=torch.int8)
-        scales = x.new_empty(shape[:-1] + (d // 32,), dtype=torch.uint8)
-    _check("maskmoe_norm_forward", lib.maskmoe_norm_forward(T, d, _dtype_code(x), eps, x.data_ptr(), _ptr(residual),
-                                                            weight.data_ptr(), _ptr(hidden), _ptr(y), _ptr(codes),
-                                                            _ptr(scales), _stream()))
+        codes = torch.empty_like(x, dtype=torch.int8)
+        scales = x.new_empty((*shape[:-1], d // 32), dtype=torch.uint8)
+    _check("maskmoe_norm_forward", load().maskmoe_norm_forward(
+        T, d, _dtype_code(x), eps, x.data_ptr(), _ptr(residual), weight.data_ptr(), _ptr(hidden), _ptr(y), _ptr(codes),
+        _ptr(scales), stream))
     return y, hidden, codes, scales
 
 
@@ -922,35 +929,31 @@ def maskmoe_norm_backward(hidden, weight, dy, d_hidden=None, eps: float = 1e-5, 
     cotangent ``dy`` of y and ``d_hidden`` of hidden (None: nothing arrives along the stream). Returns ``(d_x [..., d],
     d_weight [d] fp32 or None)``; d_x is the gradient of x and of the residual. ``d_x``: output buffer, which may be
     dy, d_hidden or hidden itself."""
-    torch = _torch()
-    lib = load()
-    shape = hidden.shape
-    if not shape or shape[-1] == 0:
-        raise ValueError("hidden must have rows of at least one element")
-    d = shape[-1]
-    T = hidden.numel() // d
-    _fits(T, d)
-    here = torch.cuda.current_device()
-    _want(hidden, "hidden", shape, hidden.dtype, here)
-    _want(weight, "weight", (d,), hidden.dtype, here)
-    _want(dy, "dy", shape, hidden.dtype, here)
+    import torch
+    T, d = _rows(hidden, "hidden")
+    here, stream = _here(torch)
+    shape, dtype = hidden.shape, hidden.dtype
+    _want(hidden, "hidden", shape, dtype, here)
+    _want(weight, "weight", (d,), dtype, here)
+    _want(dy, "dy", shape, dtype, here)
     if d_hidden is not None:
-        _want(d_hidden, "d_hidden", shape, hidden.dtype, here)
+        _want(d_hidden, "d_hidden", shape, dtype, here)
     if d_x is None:
         d_x = torch.empty_like(hidden)
     else:
-        _want(d_x, "d_x", shape, hidden.dtype, here)
+        _want(d_x, "d_x", shape, dtype, here)
+    lib = load()
     d_weight, ws_bytes = None, 0
     if with_d_weight:
-        d_weight = hidden.new_empty(d, dtype=torch.float32)
+        d_weight = torch.empty_like(weight, dtype=torch.float32)
         if workspace is None:
-            workspace = hidden.new_empty(max(int(lib.maskmoe_norm_backward_workspace_bytes(T, d)), 1), dtype=torch.uint8)
+            workspace = hidden.new_empty((max(lib.maskmoe_norm_backward_workspace_bytes(T, d), 1),), dtype=torch.uint8)
         elif workspace.get_device() != here or not workspace.is_contiguous():
             _refuse(workspace, "workspace")
         ws_bytes = workspace.numel() * workspace.element_size()
     _check("maskmoe_norm_backward", lib.maskmoe_norm_backward(
         T, d, _dtype_code(hidden), eps, hidden.data_ptr(), weight.data_ptr(), dy.data_ptr(), _ptr(d_hidden),
-        d_x.data_ptr(), _ptr(d_weight), _ptr(workspace) if with_d_weight else None, ws_bytes, _stream()))
+        d_x.data_ptr(), _ptr(d_weight), _ptr(workspace) if with_d_weight else None, ws_bytes, stream))
     return d_x, d_weight
 
 
@@ -966,7 +969,7 @@ def maskmoe_experts_backward_workspace_bytes(T: int, d: int, E: int, K: int, F: 
 
 def _experts_train_desc(T, d, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up, ws_down, here):
     """Checks routing and weights of a training pass; its desc."""
-    torch = _torch()
+    import torch
     if topk_idx.dim() != 2 or w_gate_up.dim() != 3:
         raise ValueError("topk_idx must be 2-d and w_gate_up 3-d")
     K, (E, F2, _) = topk_idx.shape[1], w_gate_up.shape
@@ -986,7 +989,8 @@ def _experts_train_desc(T, d, topk_idx, topk_gate, w_gate_up, w_down, ws_gate_up
 
 def _train_workspace(workspace, need: int, like, here: int):
     if workspace is None:
-        return like.new_empty(max(need, 1), dtype=_torch().uint8)
+        import torch
+        return like.new_empty(max(need, 1), dtype=torch.uint8)
     if workspace.get_device() != here or not workspace.is_contiguous():
         _refuse(workspace, "workspace")
     return workspace
@@ -1000,7 +1004,7 @@ def maskmoe_experts_forward_train(x, topk_idx, topk_gate, w_gate_up, w_down, ws_
 
     Returns ``(y [T,d], codes [T*(K+n_shared), 2F] int8, scales [T*(K+n_shared), 2F/32] uint8)``; rows by expert (shared
     ones last), then token and slot; the last rows, one for each entry without an expert, are not written."""
-    torch = _torch()
+    import torch
     lib = load()
     if x.dim() != 2:
         raise ValueError("x must be 2-d")
@@ -1037,7 +1041,7 @@ def maskmoe_experts_backward(x, topk_idx, topk_gate, w_gate_up, w_down, codes, s
     Returns a dict: d_x [T,d] bf16, d_gate [T,K] fp32 (None without ``with_d_gate``; it continues in
     maskmoe_gate_backward), d_w_gate_up [E,2F,d], d_w_down [E,d,F], d_ws_gate_up, d_ws_down (None without shared experts),
     bf16."""
-    torch = _torch()
+    import torch
     lib = load()
     if x.dim() != 2:
         raise ValueError("x must be 2-d")

@@ -16,6 +16,10 @@
 // 395 -> 267 (gate/up 189 -> 141, down 131 -> 78). Three or four chunks in flight changed nothing, and
 // 256 token rows (one workgroup per CU) lost 15-60%: its loads, LDS accesses and products no
 // longer overlap.
+// The training pass at a given routing (KEEP) keeps its pre-activations in 8-bit blocks: a wavefront's 32 gate (up) rows
+// are one block of each of its tokens, half of it in a lane and half in the lane 32 further. Its expert outputs stay
+// fp32. Against the 256-row tiles (row-major weights), gate/up and down: DeepSeek-shaped, 333 tokens, KEPT_DS;
+// Mixtral-shaped, 64 tokens, KEPT_MX.
 // Adapted experts (LORA) take the adapters' term as one more chunk, as the many-token path does.
 // Every sum is formed in the many-token path's order, so that a layer gives the same bits on either
 // (and as its training forward): chunks in ascending order, and a down projection whose 256 x 256
@@ -27,6 +31,7 @@
 #include "common.hpp"
 #include "gemm_tile.hpp"
 #include "kernels.hpp"
+#include "mx8.hpp"
 
 #include <algorithm>
 #include <type_traits>
@@ -47,7 +52,9 @@ struct BatchArgs {
   const uint16_t* ws;       // shared weights
   const int32_t* offsets;   // [G+1]
   const int32_t* tile_off;  // [G+1], tiles of BM rows
-  uint16_t* out;            // EPI 0: H [rows, F]; EPI 1: O [rows, d]
+  void* out;                // EPI 0: H bf16 [rows, F]; EPI 1: O [rows, d], bf16 or (KEEP) fp32
+  int8_t* codes;            // KEEP, EPI 0: 8-bit blocks of the pre-activations [rows, 2F]
+  uint8_t* scales;          // KEEP, EPI 0: [rows, 2F / 32]
   const int32_t* wide_off;  // [G+1], tiles of kGemmBM rows
   float* part;              // EPI 1: partial tiles, kTailSlots x [256 rows][256 columns] fp32
   int G, E, N, K, F, rows;  // N: output columns (F or d), K: reduction length
@@ -140,8 +147,26 @@ __device__ __forceinline__ void stream_tile(const void* w, uint32_t wbytes, uint
   }
 }
 
+// A lane's 16 values of a row's block, v[8 q + e] belonging to column 8 q + 4 (lane >> 5) + e, into codes (the block's
+// first column) and its scale.
+__device__ __forceinline__ void keep_block(const f32x16& acc, bool live, int8_t* codes, uint8_t* scale) {
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = acc[i];
+  uint32_t m = max_magnitude<16>(v);
+  m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32, kWave)));
+  const uint32_t byte = mx8_scale_byte(m);
+  uint32_t c[4];
+  mx8_encode<16>(v, byte, c);
+  if (!live) return;
+  const int hi = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) *reinterpret_cast<uint32_t*>(codes + 8 * q + 4 * hi) = c[q];
+  if (hi == 0) *scale = static_cast<uint8_t>(byte);
+}
+
 // EPI 0: gate/up with SwiGLU; EPI 1: down. PACKED: weights in the packed layout.
-template <int EPI, int BM, bool PACKED, bool LORA>
+template <int EPI, int BM, bool PACKED, bool LORA, bool KEEP = false>
 __global__ __launch_bounds__(kThreads, BM == 64 ? 3 : 2) void batch_gemm_kernel(const BatchArgs p) {
   constexpr int TN = BM / 64;                  // 32-token fragments per wavefront
   __shared__ u32x4 lds[2][(kW + BM) * 8];
@@ -247,9 +272,15 @@ __global__ __launch_bounds__(kThreads, BM == 64 ? 3 : 2) void batch_gemm_kernel(
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int row = row0 + wm * 32 * TN + 32 * j + l32;
+      if constexpr (KEEP && EPI == 0) {
+        const size_t at = static_cast<size_t>(row) * 2 * p.F + n0 + wn * 32;   // not written where row >= row_end
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          keep_block(acc[i][j], row < row_end, p.codes + at + i * p.F, p.scales + (at + i * p.F) / kMx8Block);
+      }
       if (row >= row_end) continue;
       if (EPI == 0) {
-        uint16_t* dsth = p.out + static_cast<size_t>(row) * p.F + n0 + wn * 32 + 4 * (lane >> 5);
+        uint16_t* dsth = static_cast<uint16_t*>(p.out) + static_cast<size_t>(row) * p.F + n0 + wn * 32 + 4 * (lane >> 5);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           float h[4];
@@ -273,11 +304,14 @@ __global__ __launch_bounds__(kThreads, BM == 64 ? 3 : 2) void batch_gemm_kernel(
             if (sl.s > 1) {
               *reinterpret_cast<float4*>(slot + wrow * kTileN + wcol + c) =
                   make_float4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
+            } else if (KEEP) {
+              *reinterpret_cast<float4*>(static_cast<float*>(p.out) + static_cast<size_t>(row) * p.N + n0 + c) =
+                  make_float4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
             } else {
               uint2 v;
               v.x = f32x2_to_bf16x2(a[4 * q], a[4 * q + 1]);
               v.y = f32x2_to_bf16x2(a[4 * q + 2], a[4 * q + 3]);
-              *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(row) * p.N + n0 + c) = v;
+              *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + static_cast<size_t>(row) * p.N + n0 + c) = v;
             }
           }
       }
@@ -288,6 +322,7 @@ __global__ __launch_bounds__(kThreads, BM == 64 ? 3 : 2) void batch_gemm_kernel(
 // Adds the slices of the down projection's split tiles in slice order and stores their rows of O:
 // kFixRows rows of one tile per workgroup, tail tile t of XCD xcd at workgroup 8 (t * parts + part) + xcd.
 constexpr int kFixRows = 16;
+template <bool O32 = false>
 __global__ __launch_bounds__(kThreads) void batch_fixup_kernel(const BatchArgs p, int parts) {
   const int b = blockIdx.x, xcd = b & 7, t = (b >> 3) / parts, part = (b >> 3) % parts;
   const int mt_live = p.wide_off[p.G], n_tiles = (p.N + kTileN - 1) / kTileN;
@@ -327,7 +362,11 @@ __global__ __launch_bounds__(kThreads) void batch_fixup_kernel(const BatchArgs p
       const float v[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (row0 + r + u < row_end) p.out[static_cast<size_t>(row0 + r + u) * p.N + col] = f32_to_bf16(v[u]);
+        if (row0 + r + u < row_end) {
+          const size_t o = static_cast<size_t>(row0 + r + u) * p.N + col;
+          if (O32) static_cast<float*>(p.out)[o] = v[u];
+          else static_cast<uint16_t*>(p.out)[o] = f32_to_bf16(v[u]);
+        }
     }
     return;
   }
@@ -338,17 +377,23 @@ __global__ __launch_bounds__(kThreads) void batch_fixup_kernel(const BatchArgs p
     const int r = part * kFixRows + 4 * i + (threadIdx.x >> 6);
     if (row0 + r >= row_end) break;
     const float4 a = sum(r * kTileN + c);
+    if (O32) {
+      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + static_cast<size_t>(row0 + r) * p.N + col) = a;
+      continue;
+    }
     uint2 o;
     o.x = f32x2_to_bf16x2(a.x, a.y);
     o.y = f32x2_to_bf16x2(a.z, a.w);
-    *reinterpret_cast<uint2*>(p.out + static_cast<size_t>(row0 + r) * p.N + col) = o;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + static_cast<size_t>(row0 + r) * p.N + col) = o;
   }
 }
 
 template <int EPI, int BM>
 void launch_bm(bool packed, int grid, const BatchArgs& p, hipStream_t s) {
   const dim3 g(grid), b(kThreads);
-  if (p.lora_b) {
+  if (p.codes) {
+    hipLaunchKernelGGL((batch_gemm_kernel<EPI, BM, false, false, true>), g, b, 0, s, p);
+  } else if (p.lora_b) {
     if (packed) hipLaunchKernelGGL((batch_gemm_kernel<EPI, BM, true, true>), g, b, 0, s, p);
     else hipLaunchKernelGGL((batch_gemm_kernel<EPI, BM, false, true>), g, b, 0, s, p);
   } else {
@@ -385,8 +430,9 @@ int batch_tile_rows(int T, int K, int pool, float peak) {
   return (pool >= 32 ? avg <= 75 : avg * peak <= 104) ? 128 : 0;
 }
 
-hipError_t launch_experts_batch(const ExpertArgs& a, const PermBuffers& pb, int bm, int pool, uint16_t* H, uint16_t* O,
-                                float* part, void* y, hipStream_t stream, hipEvent_t* marks, const LoraArgs* lora) {
+hipError_t launch_experts_batch(const ExpertArgs& a, const PermBuffers& pb, int bm, int pool, uint16_t* H, void* O,
+                                float* part, void* y, hipStream_t stream, hipEvent_t* marks, const LoraArgs* lora,
+                                const KeptOut* kept) {
   const int64_t TK = static_cast<int64_t>(a.T) * a.K;
   const int nonempty = static_cast<int>(std::min<int64_t>(TK, a.E));
   const int shared_tiles = a.n_shared * ((a.T + bm - 1) / bm);
@@ -414,6 +460,10 @@ hipError_t launch_experts_batch(const ExpertArgs& a, const PermBuffers& pb, int 
   p.cu_xcd = device_cus_per_xcd();
   p.G = a.E + a.n_shared; p.E = a.E; p.F = a.F;
   p.rows = a.T * (a.K + a.n_shared);
+  if (kept) {
+    p.codes = kept->codes;
+    p.scales = kept->scales;
+  }
 
   p.a = static_cast<const uint16_t*>(a.x);
   p.w = static_cast<const uint16_t*>(a.w_gate_up);
@@ -432,7 +482,7 @@ hipError_t launch_experts_batch(const ExpertArgs& a, const PermBuffers& pb, int 
   err = launch<0>(bm, a.packed, max_tiles * p.n_tiles, p, stream);
   if (err != hipSuccess) return err;
   if (may_skew) {
-    err = launch_grouped_skewed(0, a, pb, max_wide, p.skew, H, O, part, lora, stream);
+    err = launch_grouped_skewed(0, a, pb, max_wide, p.skew, H, O, part, lora, stream, kept);
     if (err != hipSuccess) return err;
   }
   record_mark(marks, 0, stream);
@@ -461,17 +511,21 @@ hipError_t launch_experts_batch(const ExpertArgs& a, const PermBuffers& pb, int 
   err = launch<1>(bm, a.packed, max_tiles * p.n_tiles * p.split, p, stream);
   if (err != hipSuccess) return err;
   if (may_skew) {
-    err = launch_grouped_skewed(1, a, pb, max_wide, p.skew, H, O, part, lora, stream);
+    err = launch_grouped_skewed(1, a, pb, max_wide, p.skew, H, O, part, lora, stream, kept);
     if (err != hipSuccess) return err;
   }
   if (sliced) {
     const int tails = static_cast<int>(std::min<int64_t>((static_cast<int64_t>(max_wide) * wide_tiles + 7) / 8, kTailSlotsPerXcd));
-    const int parts = (std::min(a.T, kTileM) + kFixRows - 1) / kFixRows;   // a group holds at most T rows
-    hipLaunchKernelGGL(batch_fixup_kernel, dim3(8 * tails * parts), dim3(kThreads), 0, stream, p, parts);
+    // a group holds at most T rows; all entries where an entry list may name an expert twice (kept)
+    const int most = static_cast<int>(std::min<int64_t>(kept ? TK : a.T, kTileM));
+    const int parts = (std::max(most, std::min(a.T, kTileM)) + kFixRows - 1) / kFixRows;
+    if (kept) hipLaunchKernelGGL(batch_fixup_kernel<true>, dim3(8 * tails * parts), dim3(kThreads), 0, stream, p, parts);
+    else hipLaunchKernelGGL(batch_fixup_kernel<false>, dim3(8 * tails * parts), dim3(kThreads), 0, stream, p, parts);
     err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
   record_mark(marks, 1, stream);
+  if (kept) return hipSuccess;
   err = launch_combine(a, pb, O, true, 1, y, stream);
   record_mark(marks, 2, stream);
   return err;

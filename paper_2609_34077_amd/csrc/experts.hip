@@ -985,13 +985,23 @@ static GemmArgs gemm_args(int epi, const ExpertArgs& a, const PermBuffers& pb, c
   return g;
 }
 
+template <int EPI>
+static void launch_grouped_kept(dim3 grid, const GemmArgs& g, hipStream_t stream) {
+  hipLaunchKernelGGL((grouped_gemm_bf16<EPI, false, false, true>), grid, dim3(GEMM_THREADS), 0, stream, g);
+}
+
 hipError_t launch_grouped_skewed(int epi, const ExpertArgs& a, const PermBuffers& pb, int max_tiles, int skew, uint16_t* H,
-                                 uint16_t* O, float* part, const LoraArgs* lora, hipStream_t stream) {
+                                 void* O, float* part, const LoraArgs* lora, hipStream_t stream, const KeptOut* kept) {
   GemmArgs g = gemm_args(epi, a, pb, pb.wide_off, max_tiles, H, O, part, lora);
   g.batch_off = pb.tile_off;
   g.skew = skew;
   const dim3 grid = grouped_grid(max_tiles, g.n_tiles, tail_can_split(epi, (epi == 0 ? a.d : a.F) / BK));
-  if (epi == 0) launch_grouped<0>(lora != nullptr, a.packed, grid, g, stream);
+  if (kept) {
+    g.codes = kept->codes;
+    g.scales = kept->scales;
+    if (epi == 0) launch_grouped_kept<0>(grid, g, stream);
+    else launch_grouped_kept<1>(grid, g, stream);
+  } else if (epi == 0) launch_grouped<0>(lora != nullptr, a.packed, grid, g, stream);
   else launch_grouped<1>(lora != nullptr, a.packed, grid, g, stream);
   return hipGetLastError();
 }
@@ -1031,18 +1041,16 @@ hipError_t launch_experts_bf16(const ExpertArgs& a, const PermBuffers& pb, uint1
 }
 
 hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, float* O, float* part,
-                               int8_t* codes, uint8_t* scales, int max_tiles, hipStream_t stream) {
+                               const KeptOut& kept, int max_tiles, hipStream_t stream) {
   GemmArgs g = gemm_args(0, a, pb, pb.tile_off, max_tiles, H, O, part, nullptr);
-  g.codes = codes;
-  g.scales = scales;
-  hipLaunchKernelGGL((grouped_gemm_bf16<0, false, false, true>), grouped_grid(max_tiles, g.n_tiles, false),
-                     dim3(GEMM_THREADS), 0, stream, g);
+  g.codes = kept.codes;
+  g.scales = kept.scales;
+  launch_grouped_kept<0>(grouped_grid(max_tiles, g.n_tiles, tail_can_split(0, a.d / BK)), g, stream);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   g = gemm_args(1, a, pb, pb.tile_off, max_tiles, H, O, part, nullptr);
   const bool tails = tail_can_split(1, a.F / BK);
-  hipLaunchKernelGGL((grouped_gemm_bf16<1, false, false, true>), grouped_grid(max_tiles, g.n_tiles, tails),
-                     dim3(GEMM_THREADS), 0, stream, g);
+  launch_grouped_kept<1>(grouped_grid(max_tiles, g.n_tiles, tails), g, stream);
   err = hipGetLastError();
   if (err != hipSuccess || !tails) return err;
   hipLaunchKernelGGL(grouped_tail_fixup<true>, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(GEMM_THREADS), 0, stream, g);

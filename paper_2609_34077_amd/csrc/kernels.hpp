@@ -151,18 +151,22 @@ hipError_t launch_experts_bf16_decode(const ExpertArgs& a, const PermBuffers& pb
 // GEMM `epi` (0 gate/up, 1 down) of that path on pb.wide_off's tiles, beside a batch launch: runs only when
 // the batch path's tiles (pb.tile_off) are skewed (batch_skewed); the down GEMM's partial tiles are left to
 // the batch path's fix-up.
+struct KeptOut {            // the training pass at a given routing: 8-bit blocks of the pre-activations, O in fp32
+  int8_t* codes;            // [rows, 2F]
+  uint8_t* scales;          // [rows, 2F / 32]
+};
 hipError_t launch_grouped_skewed(int epi, const ExpertArgs& a, const PermBuffers& pb, int max_tiles, int skew, uint16_t* H,
-                                 uint16_t* O, float* part, const LoraArgs* lora, hipStream_t stream);
+                                 void* O, float* part, const LoraArgs* lora, hipStream_t stream, const KeptOut* kept);
 // bf16, a serving-sized batch (batch.hip): few enough rows per expert that the weight stream bounds the
 // layer (with adapters for any number of tokens, else above kDecodeMaxT). batch_tile_rows: the row-tile size to permute
 // and launch with, 0 when the many-token path is faster; pool: experts the routing can select,
 // peak: 1, or with a soft prior its largest entry over a uniform one's.
 // O: bf16 expert outputs [rows, d]; part: kTailPartBytes for the down projection's slices; pb.wide_off
-// is needed. Bit-identical to launch_experts_bf16.
+// is needed. Bit-identical to launch_experts_bf16. kept (row-major weights, no adapters): O fp32, y is left to the caller.
 int batch_tile_rows(int T, int K, int pool, float peak);
-hipError_t launch_experts_batch(const ExpertArgs& a, const PermBuffers& pb, int bm, int pool, uint16_t* H, uint16_t* O,
+hipError_t launch_experts_batch(const ExpertArgs& a, const PermBuffers& pb, int bm, int pool, uint16_t* H, void* O,
                                 float* part, void* y, hipStream_t stream, hipEvent_t* marks,
-                                const LoraArgs* lora = nullptr);
+                                const LoraArgs* lora = nullptr, const KeptOut* kept = nullptr);
 // y = the gate-weighted combine of a bf16 layer's expert outputs: O [rows, d] bf16 (ob), or fp32
 // slices [split, rows, d].
 hipError_t launch_combine(const ExpertArgs& a, const PermBuffers& pb, const void* O, bool ob, int split, void* y,

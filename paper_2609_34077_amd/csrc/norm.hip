@@ -252,20 +252,25 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(const NormBwdArgs a
   }
 }
 
-// d_weight[j] = sum over the partial rows, in a fixed order: 64 columns a workgroup, 16 rows at a time.
-constexpr int kSumRows = 16;
-__global__ __launch_bounds__(kWave* kSumRows) void norm_weight_sum_kernel(const float* __restrict__ part, int parts, int d,
-                                                                          float* __restrict__ out) {
-  __shared__ float s[kSumRows][kWave];
-  const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, c = blockIdx.x * kWave + lane;
+// d_weight[j] = sum over the partial rows, in a fixed order: 16 columns a workgroup, 64 rows at a time, whose loads are
+// independent.
+constexpr int kSumCols = 16, kSumRows = 64;
+__global__ __launch_bounds__(kSumCols* kSumRows) void norm_weight_sum_kernel(const float* __restrict__ part, int parts,
+                                                                             int d, float* __restrict__ out) {
+  __shared__ float s[kSumRows][kSumCols];
+  const int r = threadIdx.x / kSumCols, j = threadIdx.x % kSumCols, c = blockIdx.x * kSumCols + j;
   float v = 0.0f;
-  if (c < d)
+  if (c < d) {
+#pragma unroll 8
     for (int i = r; i < parts; i += kSumRows) v += part[static_cast<size_t>(i) * d + c];
-  s[r][lane] = v;
-  __syncthreads();
-  if (r != 0 || c >= d) return;
-  for (int i = 1; i < kSumRows; ++i) v += s[i][lane];
-  out[c] = v;
+  }
+  s[r][j] = v;
+#pragma unroll
+  for (int half = kSumRows / 2; half >= 1; half /= 2) {
+    __syncthreads();
+    if (r < half) s[r][j] += s[r + half][j];
+  }
+  if (r == 0 && c < d) out[c] = s[0][j];
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -344,8 +349,8 @@ hipError_t launch_norm_backward(const NormBwdArgs& a, hipStream_t stream) {
     if (err != hipSuccess) return err;
   }
   if (!a.d_weight) return hipSuccess;
-  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((a.d + kWave - 1) / kWave), dim3(kWave * kSumRows), 0, stream, a.part,
-                     parts, a.d, a.d_weight);
+  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((a.d + kSumCols - 1) / kSumCols), dim3(kSumCols * kSumRows), 0, stream,
+                     a.part, parts, a.d, a.d_weight);
   return hipGetLastError();
 }
 

@@ -133,8 +133,9 @@ struct Grouping {
   int G, KS, rows, max_tiles;
 };
 
-// Entry list and grouping; a.T > 0.
-hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, char* ws, Grouping& g, hipStream_t stream) {
+// Entry list and grouping, in tiles of tile_rows rows; a.T > 0.
+hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, char* ws, int tile_rows, Grouping& g,
+                      hipStream_t stream) {
   g.G = a.E + a.n_shared;
   g.KS = a.K + a.n_shared;
   g.rows = a.T * g.KS;
@@ -157,8 +158,9 @@ hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, ch
     g.idx = idx;
     g.gate = gate;
   }
-  g.max_tiles = std::min(g.rows, g.rows / kGemmBM + g.G);
-  return launch_permute(g.idx, a.T, g.KS, g.G, 0, kGemmBM, g.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
+  if (tile_rows != kGemmBM) g.pb.wide_off = reinterpret_cast<int32_t*>(ws + w.wide_off);
+  g.max_tiles = std::min(g.rows, g.rows / tile_rows + g.G);
+  return launch_permute(g.idx, a.T, g.KS, g.G, 0, tile_rows, g.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
 }
 
 unsigned blocks(int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); }
@@ -178,6 +180,7 @@ ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n
   w.gate = take(rows * 4);
   w.offsets = take((G + 1) * 4);
   w.tile_off = take((G + 1) * 4);
+  w.wide_off = take((G + 1) * 4);
   w.active = take(G * 4);
   w.n_active = take(4);
   w.perm = take(rows * 4);
@@ -207,7 +210,9 @@ hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipS
   const ExpertsTrainLayout w = experts_train_layout(a.T, a.d, a.F, a.E, a.K, a.n_shared);
   char* ws = static_cast<char*>(workspace);
   Grouping g;
-  hipError_t err = group_rows(a, w, ws, g, stream);
+  // few rows an expert: the weights' stream decides, as in inference
+  const int batch_rows = batch_tile_rows(a.T, a.K, a.E, 1.0f);
+  hipError_t err = group_rows(a, w, ws, batch_rows ? batch_rows : kGemmBM, g, stream);
   if (err != hipSuccess) return err;
   ExpertArgs e{};
   e.x = a.x;
@@ -215,10 +220,13 @@ hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipS
   e.w_down = a.w_down;
   e.ws_gate_up = a.ws_gate_up;
   e.ws_down = a.ws_down;
-  e.T = a.T; e.d = a.d; e.F = a.F; e.E = a.E; e.K = g.KS; e.n_shared = a.n_shared;
+  e.T = a.T; e.d = a.d; e.F = a.F; e.E = a.E; e.K = a.K; e.n_shared = a.n_shared;
   float* O = reinterpret_cast<float*>(ws + w.O);
-  err = launch_experts_kept(e, g.pb, reinterpret_cast<uint16_t*>(ws + w.H), O, reinterpret_cast<float*>(ws + w.part),
-                            a.codes, a.scales, g.max_tiles, stream);
+  uint16_t* H = reinterpret_cast<uint16_t*>(ws + w.H);
+  float* part = reinterpret_cast<float*>(ws + w.part);
+  const KeptOut kept{a.codes, a.scales};
+  err = batch_rows ? launch_experts_batch(e, g.pb, batch_rows, a.E, H, O, part, nullptr, stream, nullptr, nullptr, &kept)
+                   : launch_experts_kept(e, g.pb, H, O, part, kept, g.max_tiles, stream);
   if (err != hipSuccess) return err;
   hipLaunchKernelGGL(token_sum_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
                      O, g.idx, g.gate, g.pb.inv, a.T, g.KS, g.G, a.d, a.y);
@@ -243,7 +251,7 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   const ExpertsTrainLayout w = experts_train_layout(a.T, a.d, a.F, a.E, a.K, a.n_shared);
   char* ws = static_cast<char*>(workspace);
   Grouping g;
-  hipError_t err = group_rows(a, w, ws, g, stream);
+  hipError_t err = group_rows(a, w, ws, kGemmBM, g, stream);
   if (err != hipSuccess) return err;
   KeptBwdArgs k{};
   k.w_gate_up = a.w_gate_up;

@@ -31,7 +31,7 @@ struct ExpertsBwdArgs {
 };
 
 struct ExpertsTrainLayout {   // byte offsets into the workspaces; the grouping is first in both
-  size_t idx, gate, offsets, tile_off, active, n_active, perm, inv, row_tok, pcount;
+  size_t idx, gate, offsets, tile_off, wide_off, active, n_active, perm, inv, row_tok, pcount;
   size_t H, O, part;                                            // forward
   size_t dyg, xg, row_gate, order, next, gh, dab, dxr, dgate_part;    // gradient (with part)
   size_t forward_total, backward_total;
@@ -40,9 +40,9 @@ ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n
 hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipStream_t stream);
 hipError_t launch_experts_backward(const ExpertsBwdArgs& a, void* workspace, hipStream_t stream);
 
-// H (bf16 [rows, F]) with codes and scales, then O (fp32 expert outputs [rows, d]), on row tiles of kGemmBM (experts.hip).
+// H (bf16 [rows, F]) with its blocks, then O (fp32 expert outputs [rows, d]), on row tiles of kGemmBM (experts.hip).
 hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, float* O, float* part,
-                               int8_t* codes, uint8_t* scales, int max_tiles, hipStream_t stream);
+                               const KeptOut& kept, int max_tiles, hipStream_t stream);
 
 // The products of the gradient on rows grouped by expert (backward.hip).
 struct KeptBwdArgs {
