@@ -16,19 +16,14 @@
 // of the dgrads, and both operands of the weight gradients, whose contraction runs over each
 // expert's own rows of dO, h, [da db] and the gathered x (rows past the group's end read as
 // zeros; an expert no token chose gets zeros).
-// A row group's last tile multiplies and loads only its 64-row pieces that hold rows, as in the forward (but with
-// SwiGLU's backward on bf16 pre-activations, which keeps whole tiles).
 // Rounding (bf16 layers): dO = g dy and [da db] are rounded to bf16 before their GEMMs;
 // accumulation is fp32; dX, dW are fp32.
 
 #include <mutex>
-#include <type_traits>
 
 #include "common.hpp"
 #include "gemm_tile.hpp"
 #include "kernels.hpp"
-#include "mx8.hpp"
-#include "train_experts.hpp"
 
 namespace maskmoe {
 namespace {
@@ -82,14 +77,8 @@ struct NtArgs {
   const int32_t* active;      // KSPLIT: the non-empty groups, n_active[0] of them
   const int32_t* n_active;
   const uint16_t* ab;         // SWIGLU_BWD: saved pre-activations [rows, 2N]
-  const int8_t* codes;        // SWIGLU_KEPT: 8-bit blocks of the pre-activations [rows, 2N]
-  const uint8_t* scales;      // SWIGLU_KEPT: [rows, 2N / 32]
-  const float* row_gate;      // SWIGLU_KEPT: gate of each row
-  uint16_t* gh;               // SWIGLU_KEPT: gate times SwiGLU activation [rows, N]
-  float* dgate_part;          // SWIGLU_KEPT: [rows, n_tiles] partial sums of u h
   void* c;                    // ROWS: [rows, ldc]; KSPLIT: routed groups' [M, N] matrices
   void* cs;                   // KSPLIT: shared groups' [M, N] matrices
-  int32_t* next;              // wgrad_kernel: [8] tiles that each XCD has handed out, 0 at the start
   float* part;                // ROWS, fp32 output: partial tiles of split tail tiles (tile_job)
   int G, E, M, N, K, lda, ldb, ldc, mt_max, n_tiles;
   int cu_xcd;                 // workgroups an XCD runs at once
@@ -98,6 +87,53 @@ struct NtArgs {
 // ROWS with fp32 output may split each XCD's last-round tiles (see tile_job).
 __host__ __device__ constexpr bool nt_tail_split(int mode, int epi, int nk) {
   return mode == 0 && epi == 1 && tail_splittable(nk);
+}
+
+// Stores a finished ROWS tile of fp32 output: rows [row0, row_end), columns from n0.
+// Staged fp32 tiles: 128 rows x 256 columns at a pitch of 264 floats (the two 32-lane halves of
+// a wavefront, four rows apart, then write different banks).
+constexpr int kStgPitch = 264;
+static_assert(128 * kStgPitch * 4 <= sizeof(TileLds), "a staged half tile fits in LDS");
+
+// Half h (0, 1) of the tile into LDS: acc[2h + ii] of every wave, as staged row
+// wm*64 + ii*32 + (row within the 32-row block). Staged row pr is tile row
+// (pr >> 6) * 128 + 64 h + (pr & 63).
+__device__ __forceinline__ void stage_half(float* stg, const f32x16 (&acc)[kTileTM][kTileTN], int h) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / 4, wn = wave % 4;
+#pragma unroll
+  for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int j = 0; j < kTileTN; ++j)
+        stg[(wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kStgPitch + wn * 64 + j * 32 +
+            (lane & 31)] = (h == 0 ? acc[ii][j][r] : acc[2 + ii][j][r]);
+}
+
+// The fp32 tile (rows row0.., columns n0..) into out (row stride ld), through LDS in two halves
+// so that it leaves in 16-byte stores: one 4-byte store per value and lane kept the
+// texture-address path busy for ~10 us at the end of every tile. ncol % 4 == 0.
+__device__ __forceinline__ void nt_store_staged(const f32x16 (&acc)[kTileTM][kTileTN], float* out, size_t ld, int row0,
+                                                int row_end, int n0, int ncol, TileLds& L) {
+  float* stg = reinterpret_cast<float*>(&L);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    wait_lgkmcnt0();
+    tile_barrier();   // the k-loop's (or the previous half's) LDS reads are done
+    stage_half(stg, acc, h);
+    wait_lgkmcnt0();
+    tile_barrier();
+#pragma unroll 4
+    for (int q = 0; q < 16; ++q) {   // 8192 float4 per half: 64 per staged row
+      const int u = static_cast<int>(threadIdx.x) + kTileThreads * q;
+      const int pr = u >> 6, c = (u & 63) * 4;
+      const int row = row0 + (pr >> 6) * 128 + 64 * h + (pr & 63), col = n0 + c;
+      if (row < row_end && col < ncol)
+        *reinterpret_cast<float4*>(out + static_cast<size_t>(row) * ld + col) =
+            *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + c]);
+    }
+  }
 }
 
 // The gradients of the groups that no row reached are zero. Where they are no more than the reached
@@ -122,7 +158,7 @@ __device__ __forceinline__ void empty_groups(const int32_t* offsets, int G, uint
   }
 }
 
-// n: 16-byte pieces of a matrix.
+// n: float4s of a matrix.
 __device__ __forceinline__ void zero_slices(const uint64_t (&dead)[kDeadWords], int E, size_t n, int lid, int live,
                                             float* c, float* cs) {
   const size_t i0 = n * lid / live, i1 = n * (lid + 1) / live;
@@ -137,102 +173,7 @@ __device__ __forceinline__ void zero_slices(const uint64_t (&dead)[kDeadWords], 
 }
 
 enum { kNtRows = 0, kNtKSplit = 1 };
-enum { kEpiSwigluBwd = 0, kEpiF32 = 1, kEpiSwigluKept = 2 };
-
-// Sum over each half of the wavefront, in its last lane.
-__device__ __forceinline__ float half_wave_sum(float v) {
-  auto add = [&](auto ctrl, auto rows) {
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value,
-                                                    0xF, false));
-  };
-  using std::integral_constant;
-  add(integral_constant<int, 0xB1>{}, integral_constant<int, 0xF>{});    // lanes 1 apart
-  add(integral_constant<int, 0x4E>{}, integral_constant<int, 0xF>{});    // 2 apart
-  add(integral_constant<int, 0x141>{}, integral_constant<int, 0xF>{});   // mirrored within 8
-  add(integral_constant<int, 0x140>{}, integral_constant<int, 0xF>{});   // mirrored within 16
-  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});   // lane 15 of rows 0, 2 to rows 1, 3
-  return v;
-}
-
-// Epilogue of u = dy W_down with the pre-activations in 8-bit blocks: da, db (bf16, [rows, 2N]), the gated SwiGLU
-// activation for the weight gradient (bf16, [rows, N]) and this tile's share of every row's d_gate = <u, h>. As
-// kEpiSwigluBwd's, the tile goes through LDS in parts of 128 rows, a part's blocks loaded before it is staged.
-template <int TM>
-__device__ __forceinline__ void swiglu_kept_epilogue(const NtArgs& p, const f32x16 (&acc)[TM][kTileTN], int row0,
-                                                     int row_end, int n0, int nt, TileLds& L) {
-  const int tid = threadIdx.x;
-  float* stg = reinterpret_cast<float*>(&L);
-  uint16_t* o = static_cast<uint16_t*>(p.c);
-  const size_t N = p.N;
-  row_end = min(row_end, row0 + 64 * TM);
-#pragma unroll
-  for (int h = 0; h < (TM + 1) / 2; ++h) {
-    uint2 a8[8], b8[8];
-    uint32_t sa[8], sb[8];
-    float gate[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {   // 4096 pieces of 8 columns: 32 per staged row
-      const int u = tid + kTileThreads * q;
-      const int pr = u >> 5, col = n0 + (u & 31) * 8;
-      const int row = row0 + staged_tile_row<TM>(pr, h);
-      a8[q] = b8[q] = make_uint2(0, 0);
-      sa[q] = sb[q] = 0;
-      gate[q] = 0.0f;
-      if (row < row_end && col < p.N) {
-        const size_t at = row * 2 * N + col;
-        a8[q] = *reinterpret_cast<const uint2*>(p.codes + at);
-        b8[q] = *reinterpret_cast<const uint2*>(p.codes + at + N);
-        sa[q] = p.scales[at / kMx8Block];
-        sb[q] = p.scales[(at + N) / kMx8Block];
-        gate[q] = p.row_gate[row];
-      }
-    }
-    wait_lgkmcnt0();
-    tile_barrier();   // the k-loop's (or the previous part's) LDS reads are done
-    stage_part<TM>(stg, acc, h);
-    wait_lgkmcnt0();
-    tile_barrier();
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int u = tid + kTileThreads * q;
-      const int pr = u >> 5, cg = (u & 31) * 8, col = n0 + cg;
-      const int row = row0 + staged_tile_row<TM>(pr, h);
-      const bool live = row < row_end && col < p.N;
-      float v[8], av[8], bv[8], da[8], db[8], gh[8];
-      *reinterpret_cast<float4*>(&v[0]) = *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + cg]);
-      *reinterpret_cast<float4*>(&v[4]) = *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + cg + 4]);
-      const float s_a = mx8_step(sa[q]), s_b = mx8_step(sb[q]);
-      mx8_decode4(a8[q].x, s_a, av);
-      mx8_decode4(a8[q].y, s_a, av + 4);
-      mx8_decode4(b8[q].x, s_b, bv);
-      mx8_decode4(b8[q].y, s_b, bv + 4);
-      float dot = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float s = sigmoid(av[e]), l = av[e] * s, hv = l * bv[e], gu = gate[q] * v[e];
-        dot += v[e] * hv;
-        da[e] = gu * bv[e] * (s + l - l * s);   // SiLU' = s + a s (1 - s)
-        db[e] = gu * l;
-        gh[e] = gate[q] * hv;
-      }
-      dot = half_wave_sum(live ? dot : 0.0f);   // 32 lanes hold a staged row
-      if ((u & 31) == 31 && row < row_end) p.dgate_part[static_cast<size_t>(row) * p.n_tiles + nt] = dot;
-      if (!live) continue;
-      uint16_t* dst = o + row * 2 * N + col;
-      u32x4 pa, pb, pg;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        pa[e] = f32x2_to_bf16x2(da[2 * e], da[2 * e + 1]);
-        pb[e] = f32x2_to_bf16x2(db[2 * e], db[2 * e + 1]);
-        pg[e] = f32x2_to_bf16x2(gh[2 * e], gh[2 * e + 1]);
-      }
-      *reinterpret_cast<u32x4*>(dst) = pa;
-      *reinterpret_cast<u32x4*>(dst + N) = pb;
-      *reinterpret_cast<u32x4*>(p.gh + row * N + col) = pg;
-    }
-  }
-}
-
+enum { kEpiSwigluBwd = 0, kEpiF32 = 1 };
 
 // ROWS (dgrad): group g's rows offsets[g]..offsets[g+1] of A (K-contiguous) times its own
 // K-major [K, N] matrix, row tiles enumerated by tile_off as in the forward. KSPLIT (wgrad): for
@@ -247,7 +188,6 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   const int wn = wave % WN;
   int mt, nt, g, row0, row_end, nk;
   TileJob job{0, 0, 1, -1};
-  int tm = kTileTM;
   TileOps ops{};
   TileKm akm{}, bkm{};
   uint64_t dead[kDeadWords] = {};
@@ -270,11 +210,9 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
     const int k0 = job.z * nk * kTileK;
     const int n0 = nt * kTileN;
     ops.a = reinterpret_cast<const char*>(p.a + k0);
-    if (EPI != kEpiSwigluBwd && job.s == 1) tm = min((row_end - row0 + 63) / 64, kTileTM);
 #pragma unroll
     for (int i = 0; i < 4; ++i)   // element offsets < 2^31 (checked by the host)
-      ops.aoff[i] =
-          static_cast<uint32_t>(min(row0 + tile_dma_row_a(tm, i), row_end - 1) * p.lda + tile_dma_chunk_a(tm, i) * 8) * 2u;
+      ops.aoff[i] = static_cast<uint32_t>(min(row0 + tile_dma_row(i), row_end - 1) * p.lda + tile_dma_chunk(i) * 8) * 2u;
     const uint16_t* bm = g < p.E ? p.b + static_cast<size_t>(g) * p.N * p.K : p.bs + static_cast<size_t>(g - p.E) * p.N * p.K;
     bkm.base = reinterpret_cast<const char*>(bm + static_cast<size_t>(k0) * p.ldb + n0);
     bkm.ld = p.ldb * 2;
@@ -305,36 +243,6 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   int bfrag[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j) bfrag[j] = wn * 64 + j * 32 + (lane & 31);
-  if constexpr (MODE == kNtRows && EPI != kEpiSwigluBwd) {
-    auto tile = [&](auto tm_c) {
-      constexpr int M = decltype(tm_c)::value;
-      f32x16 acc[M][TN];
-#pragma unroll
-      for (int i = 0; i < M; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-      gemm_tile_mainloop<false, false, true, false, M>(ops, nk, bfrag, acc, lds, nullptr, &akm, &bkm);
-      if constexpr (EPI == kEpiSwigluKept) {
-        swiglu_kept_epilogue<M>(p, acc, row0, row_end, n0, nt, lds);
-      } else {
-        if constexpr (M == kTileTM) {
-          if (job.s > 1) {   // a slice of a split tail tile
-            tail_store_partial(p.part, job.slot, acc);
-            return;
-          }
-        }
-        tile_store_f32<M>(acc, static_cast<float*>(p.c), p.ldc, row0, row_end, n0, p.N, lds);
-      }
-    };
-    using std::integral_constant;
-    if (tm == 4) tile(integral_constant<int, 4>{});
-    else if (tm == 3) tile(integral_constant<int, 3>{});
-    else if (tm == 2) tile(integral_constant<int, 2>{});
-    else tile(integral_constant<int, 1>{});
-    return;
-  }
   f32x16 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -343,6 +251,11 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
   gemm_tile_mainloop<false, MODE == kNtKSplit, true>(ops, nk, bfrag, acc, lds, nullptr, &akm, &bkm);
+  if (MODE == kNtRows && EPI == kEpiF32) {
+    if (job.s > 1) tail_store_partial(p.part, job.slot, acc);   // a slice of a split tail tile
+    else nt_store_staged(acc, static_cast<float*>(p.c), p.ldc, row0, row_end, nt * kTileN, p.N, lds);
+    return;
+  }
 
   // acc[i][j][4 jj + ii] is row wm*128 + i*32 + 8 jj + 4 (lane >> 5) + ii, column
   // wn*64 + j*32 + (lane & 31) of the tile.
@@ -371,7 +284,7 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
       }
       wait_lgkmcnt0();
       tile_barrier();   // the k-loop's (or the previous half's) LDS reads are done
-      stage_part<kTileTM>(stg, acc, h);
+      stage_half(stg, acc, h);
       wait_lgkmcnt0();
       tile_barrier();
 #pragma unroll
@@ -402,120 +315,9 @@ __global__ __launch_bounds__(kTileThreads) void gemm_nt_kernel(const NtArgs p) {
   }
   float* cf = g < p.E ? static_cast<float*>(p.c) + static_cast<size_t>(g) * p.M * p.N
                       : static_cast<float*>(p.cs) + static_cast<size_t>(g - p.E) * p.M * p.N;
-  tile_store_f32<kTileTM>(acc, cf, p.N, row0, row_end, n0, p.N, lds);
+  nt_store_staged(acc, cf, p.N, row0, row_end, n0, p.N, lds);
   zero_slices(dead, p.E, static_cast<size_t>(p.M) * p.N / 4, lid, live_tiles, static_cast<float*>(p.c),
               static_cast<float*>(p.cs));
-}
-
-// Weight gradients in bf16: for every group with rows the [M, N] product over its rows of the K-major A [rows, M] and
-// B [rows, N], p.active naming the groups by descending rows. One workgroup a CU takes tile after tile; the first k-tile
-// of the next tile is loaded while this one's results go through the other 64 KB of LDS (128 rows at a time, as bf16,
-// so that they leave in 16-byte stores), and the stores are not waited for. An expert's reduction is short where there
-// are many (DeepSeek-shaped, 4096 tokens: six k-tiles, 10 us, of which a workgroup per tile made 20).
-// After its first two tiles a workgroup takes them from its XCD's counter (which changes who computes a tile, not what
-// it holds): asked for at the start of a tile, handed round during its end, used for the loads at the next one's end.
-// Tile order: every XCD takes an eighth of each group (pieces of per / 8 consecutive tiles, dealt in turn), so that all
-// have the same work and no long reduction starts late. With a range of consecutive tiles for each XCD instead, as for
-// products whose tiles are all alike, the XCD with the shared experts' tiles decided: the two gradients of that layer
-// 854 + 453 us, dealt 520 + 270.
-__global__ __launch_bounds__(kTileThreads) void wgrad_kernel(const NtArgs p) {
-  __shared__ TileLds lds;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 4, wn = wave % 4;
-  const int per = p.mt_max * p.n_tiles, live_tiles = p.n_active[0] * per;
-  const int piece = per < 8 ? 1 : per / 8, xcd = blockIdx.x & 7, slots = gridDim.x >> 3;
-  uint64_t dead[kDeadWords] = {};
-  const bool zeros = zeros_in_wgrad(p.G, p.n_active[0]);
-  if (zeros) empty_groups(p.offsets, p.G, dead);
-  int bfrag[kTileTN];
-#pragma unroll
-  for (int j = 0; j < kTileTN; ++j) bfrag[j] = wn * 64 + j * 32 + (lane & 31);
-
-  struct Job {
-    int g, mt, nt, nk;
-    TileKm a, b;
-  };
-  auto tile_of = [&](int local) { return (local / piece * 8 + xcd) * piece + local % piece; };
-  auto job_of = [&](int lid) {
-    Job j;
-    j.g = p.active[lid / per];
-    grouped_tile_coords(lid % per, p.mt_max, p.n_tiles, j.mt, j.nt);
-    const int r0 = p.offsets[j.g], nrows = p.offsets[j.g + 1] - r0;
-    j.nk = (nrows + kTileK - 1) / kTileK;
-    j.a = TileKm{reinterpret_cast<const char*>(p.a + static_cast<size_t>(r0) * p.lda + j.mt * kTileM), p.lda * 2, nrows,
-                 p.M - j.mt * kTileM};
-    j.b = TileKm{reinterpret_cast<const char*>(p.b + static_cast<size_t>(r0) * p.ldb + j.nt * kTileN), p.ldb * 2, nrows,
-                 p.N - j.nt * kTileN};
-    return j;
-  };
-
-  int lid = tile_of(blockIdx.x >> 3), next = tile_of((blockIdx.x >> 3) + slots);
-  if (lid >= live_tiles) return;
-  Job job = job_of(lid);
-  gemm_tile_prefetch(job.a, job.b, lds);
-  wait_vmcnt<0>();
-  tile_barrier();
-  for (;;) {
-    f32x16 acc[kTileTM][kTileTN];
-#pragma unroll
-    for (int i = 0; i < kTileTM; ++i)
-#pragma unroll
-      for (int j = 0; j < kTileTN; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    const bool more = next < live_tiles;
-    Job nj = job;
-    if (more) nj = job_of(next);
-    int taken = 0;
-    if (tid == 0 && more)
-      taken = __hip_atomic_fetch_add(p.next + xcd, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    gemm_tile_mainloop<false, true, true, false, kTileTM, true>(TileOps{}, job.nk, bfrag, acc, lds, nullptr, &job.a, &job.b);
-    wait_lgkmcnt0();
-    tile_barrier();   // every wave is past the k-loop's LDS reads, and its loads have arrived
-    if (more) gemm_tile_prefetch(nj.a, nj.b, lds);
-    int32_t* word = reinterpret_cast<int32_t*>(&lds.a[0][1][0]);   // A's second buffer is idle until the next mainloop
-    if (tid == 0) *word = taken;
-    const size_t mn = static_cast<size_t>(p.M) * p.N;
-    uint16_t* out = job.g < p.E ? static_cast<uint16_t*>(p.c) + job.g * mn
-                                : static_cast<uint16_t*>(p.cs) + (job.g - p.E) * mn;
-    // [128 rows][256 columns], 16-byte unit u of row r at u ^ 4 (r >> 2 & 1): the two halves of a wavefront, four rows
-    // apart, write different banks
-    uint16_t* stg = reinterpret_cast<uint16_t*>(&lds.b[1][0]);
-    int after = 0;
-    static_assert(128 * kTileN * 2 <= 2 * sizeof(lds.b[0]), "128 rows fit behind B's first buffer");
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-#pragma unroll
-          for (int j = 0; j < kTileTN; ++j) {
-            const int row = wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-            const int col = wn * 64 + j * 32 + (lane & 31);
-            stg[row * kTileN + (col ^ (row >> 2 & 1) * 32)] = f32_to_bf16(acc[2 * h + ii][j][r]);
-          }
-      wait_lgkmcnt0();
-      if (h == 0) wait_vmcnt<0>();   // the next tile's first operands, before any store: stores are never waited for here
-      tile_barrier();
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {   // 4096 pieces of eight columns: 32 per row
-        const int u = tid + kTileThreads * q;
-        const int pr = u >> 5, c = (u & 31) * 8;
-        const int row = job.mt * kTileM + staged_tile_row<kTileTM>(pr, h), col = job.nt * kTileN + c;
-        if (row < p.M && col < p.N)
-          *reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * p.N + col) =
-              *reinterpret_cast<const u32x4*>(&stg[pr * kTileN + (c ^ (pr >> 2 & 1) * 32)]);
-      }
-      if (h == 0) after = __builtin_amdgcn_readfirstlane(*word);
-      wait_lgkmcnt0();
-      tile_barrier();   // the staged rows are read
-    }
-    if (zeros) zero_slices(dead, p.E, mn / 8, lid, live_tiles, static_cast<float*>(p.c), static_cast<float*>(p.cs));
-    if (!more) return;
-    lid = next;
-    job = nj;
-    next = tile_of(2 * slots + after);
-  }
 }
 
 // Adds the slices of each split tail tile of the ROWS fp32 product in slice order and stores
@@ -740,64 +542,6 @@ hipError_t launch_layer_backward(const BwdArgs& a, hipStream_t s) {
   (void)hipEventDestroy(fork);   // released once their waits are done
   (void)hipEventDestroy(join);
   return e;
-}
-
-// The five products of the gradient of experts whose pre-activations are kept in 8-bit blocks (train_experts.hip prepares
-// the rows and sums them up).
-hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s) {
-  const int G = a.G, d = a.d, F = a.F;
-  const size_t FD = static_cast<size_t>(F) * d;
-  NtArgs n{};
-  n.offsets = a.pb.offsets;
-  n.tile_off = a.pb.tile_off;
-  n.G = G; n.E = a.E;
-  n.mt_max = a.max_tiles;
-  n.cu_xcd = device_cus_per_xcd();
-  n.part = a.part;
-  // u = dy W_down and its epilogue
-  n.a = a.dyg; n.lda = d;
-  n.b = a.w_down; n.bs = a.ws_down; n.N = F; n.K = d; n.ldb = F;   // W_down [d, F]: K-major
-  n.codes = a.codes;
-  n.scales = a.scales;
-  n.row_gate = a.row_gate;
-  n.gh = a.gh;
-  n.dgate_part = a.dgate_part;
-  n.c = a.dab;
-  n.n_tiles = (F + kTileN - 1) / kTileN;
-  hipLaunchKernelGGL((gemm_nt_kernel<kNtRows, kEpiSwigluKept>), rows_grid(n.mt_max, n.n_tiles), dim3(kTileThreads), 0, s, n);
-  MASKMOE_TRY(hipGetLastError());
-  // rows of d_x = [da db] W_gate_up
-  n.a = a.dab; n.lda = 2 * F;
-  n.b = a.w_gate_up; n.bs = a.ws_gate_up; n.N = d; n.K = 2 * F; n.ldb = d;   // W_gate_up [2F, d]: K-major
-  n.c = a.dxr; n.ldc = d;
-  n.n_tiles = (d + kTileN - 1) / kTileN;
-  hipLaunchKernelGGL((gemm_nt_kernel<kNtRows, kEpiF32>), rows_grid(n.mt_max, n.n_tiles), dim3(kTileThreads), 0, s, n);
-  if (nt_tail_split(kNtRows, kEpiF32, n.K / kTileK))
-    hipLaunchKernelGGL(nt_tail_fixup, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(kTileThreads), 0, s, n);
-  MASKMOE_TRY(hipGetLastError());
-  // weight gradients over each expert's own rows; zeros for the others
-  NtArgs m{};
-  m.offsets = a.pb.offsets;
-  m.active = a.order;
-  m.n_active = a.pb.n_active;
-  m.G = G; m.E = a.E;
-  m.a = a.dyg; m.lda = d; m.b = a.gh; m.ldb = F; m.M = d; m.N = F;   // dW_down [d, F] = dy^T (g h)
-  m.c = a.d_w_down; m.cs = a.d_ws_down;
-  m.mt_max = (d + kTileM - 1) / kTileM;
-  m.n_tiles = (F + kTileN - 1) / kTileN;
-  m.next = a.next;
-  hipLaunchKernelGGL(wgrad_kernel, dim3(8 * n.cu_xcd), dim3(kTileThreads), 0, s, m);
-  m.a = a.dab; m.lda = 2 * F; m.b = a.xg; m.ldb = d; m.M = 2 * F; m.N = d;   // dW_gate_up [2F, d] = [da db]^T x
-  m.c = a.d_w_gate_up; m.cs = a.d_ws_gate_up;
-  m.mt_max = (2 * F + kTileM - 1) / kTileM;
-  m.n_tiles = (d + kTileN - 1) / kTileN;
-  m.next = a.next + 8;
-  hipLaunchKernelGGL(wgrad_kernel, dim3(8 * n.cu_xcd), dim3(kTileThreads), 0, s, m);
-  hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD / 2,
-                     static_cast<float*>(a.d_w_down), static_cast<float*>(a.d_ws_down));
-  hipLaunchKernelGGL(zero_unused_kernel, dim3(G, 512), dim3(kBwdThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E, FD,
-                     static_cast<float*>(a.d_w_gate_up), static_cast<float*>(a.d_ws_gate_up));
-  return hipGetLastError();
 }
 
 }  // namespace maskmoe

@@ -18,8 +18,8 @@
 // longer overlap.
 // The training pass at a given routing (KEEP) keeps its pre-activations in 8-bit blocks: a wavefront's 32 gate (up) rows
 // are one block of each of its tokens, half of it in a lane and half in the lane 32 further. Its expert outputs stay
-// fp32. Against the 256-row tiles (row-major weights), gate/up and down: DeepSeek-shaped, 333 tokens, KEPT_DS;
-// Mixtral-shaped, 64 tokens, KEPT_MX.
+// fp32. Against the 256-row tiles (row-major weights), gate/up and down: DeepSeek-shaped, 333 tokens,
+// 161 + 90 -> 151 + 78 us; Mixtral-shaped, 1 token, 92 + 71 -> 69 + 37, 64 tokens 347 + 185 -> 284 + 141.
 // Adapted experts (LORA) take the adapters' term as one more chunk, as the many-token path does.
 // Every sum is formed in the many-token path's order, so that a layer gives the same bits on either
 // (and as its training forward): chunks in ascending order, and a down projection whose 256 x 256

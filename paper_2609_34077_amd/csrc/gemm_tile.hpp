@@ -144,15 +144,13 @@ __device__ __forceinline__ void tile_barrier() { asm volatile("s_barrier" ::: "m
 // STREAM: operand B is read by this workgroup alone: non-temporal loads.
 // TM: A fragments per wave; a tile of 64 TM rows, A fragment i then being tile row
 // 32 TM g + 32 i + (lane & 31) and o.aoff / o.x's following tile_dma_row_a(TM, i).
-// PRE: the first k-tile's operands are in LDS (gemm_tile_prefetch, its loads waited for, and a barrier after that).
-template <bool EXTRA = false, bool AKM = false, bool BKM = false, bool STREAM = false, int TM = kTileTM, bool PRE = false>
+template <bool EXTRA = false, bool AKM = false, bool BKM = false, bool STREAM = false, int TM = kTileTM>
 __device__ __forceinline__ void gemm_tile_mainloop(const TileOps& o, int nk, const int (&bfrag)[kTileTN],
                                                    f32x16 (&acc)[TM][kTileTN], TileLds& L,
                                                    const TileOps* x = nullptr, const TileKm* akm = nullptr,
                                                    const TileKm* bkm = nullptr) {
   static_assert(!(EXTRA && (AKM || BKM)), "the extra k-tile is K-contiguous");
   static_assert(!AKM || TM == kTileTM, "a K-major A operand fills the tile");
-  static_assert(!(EXTRA && PRE), "the extra k-tile is not prefetched");
   constexpr int X = EXTRA ? 1 : 0;
   if (nk <= 0) return;
   const int ntot = nk + X;
@@ -240,15 +238,13 @@ __device__ __forceinline__ void gemm_tile_mainloop(const TileOps& o, int nk, con
     for (int i = 0; i < TM; ++i) dma16(la0 + static_cast<uint32_t>(i * 1024), x->a, x->aoff[i]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) dma16(lb0 + static_cast<uint32_t>(i * 1024), x->b, x->boff[i]);
-  } else if (!PRE) {
+  } else {
     dma_a(0);
     dma_b(0);
   }
   dma_b(1);
-  if (!PRE) {
-    wait_vmcnt<0>();
-    tile_barrier();
-  }
+  wait_vmcnt<0>();
+  tile_barrier();
   // group 1 runs one phase behind group 0: one extra barrier first (group 0 adds it at the end)
   if (g == 1) tile_barrier();
   for (int m = 0; m < ntot; ++m) {
@@ -277,25 +273,6 @@ __device__ __forceinline__ void gemm_tile_mainloop(const TileOps& o, int nk, con
   }
   if (g == 0) tile_barrier();
   wait_vmcnt<0>();
-}
-
-// The first k-tile's loads of a product whose operands are both K-major, for a later mainloop of PRE: into buffer 0 of A
-// and of B, so the other buffers of B (64 KB) stay free until that mainloop. All waves are past the buffers' last use.
-__device__ __forceinline__ void gemm_tile_prefetch(const TileKm& akm, const TileKm& bkm, TileLds& L) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int g = wave >> 2, q = wave & 3;
-  const uint32_t la0 = lds_offset(&L.a[g][0][0]) + q * kTileTM * 1024;
-  const uint32_t lb0 = lds_offset(&L.b[0][0]) + (g * 16 + q * 4) * 1024;
-  const i32x4 ar = buffer_rsrc(akm.base, static_cast<uint32_t>(akm.krows) * static_cast<uint32_t>(akm.ld));
-  const i32x4 br = buffer_rsrc(bkm.base, static_cast<uint32_t>(bkm.krows) * static_cast<uint32_t>(bkm.ld));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int kr = 4 * (4 * q + i) + (lane >> 4);
-    const int col = g * 128 + 8 * km_unit(lane & 15, kr);
-    dma16b(la0 + static_cast<uint32_t>(i * 1024), ar, static_cast<uint32_t>(kr * akm.ld + min(col, akm.mcols - 8) * 2));
-    dma16b(lb0 + static_cast<uint32_t>(i * 1024), br, static_cast<uint32_t>(kr * bkm.ld + min(col, bkm.mcols - 8) * 2));
-  }
 }
 
 // XCD-aware tile order: the hardware deals workgroup ids round-robin over the 8 XCDs, so ids
@@ -465,58 +442,39 @@ __device__ __forceinline__ void tail_fixup_part(const float* part, int slot0, in
   }
 }
 
-// Staged fp32 tiles: 128 rows x 256 columns at a pitch of 264 floats (the two 32-lane halves of
-// a wavefront, four rows apart, then write different banks).
-constexpr int kStgPitch = 264;
-static_assert(128 * kStgPitch * 4 <= sizeof(TileLds), "a staged half tile fits in LDS");
-
-// Part h of the tile of 64 TM rows into LDS: acc[2h + ii] of every wave (2h + ii < TM), as staged row
-// wm*64 + ii*32 + (row within the 32-row block).
+// The fp32 tile of 64 TM rows (rows row0.., columns n0..) into out (row stride ld), through LDS in parts of 128 rows (two
+// fragment rows a wavefront) at a pitch of 264 floats, so that it leaves in 16-byte stores. ncol % 4 == 0.
+constexpr int kStorePitch = kTileN + 8;
+static_assert(128 * kStorePitch * 4 <= sizeof(TileLds), "a staged part fits in LDS");
 template <int TM>
-__device__ __forceinline__ void stage_part(float* stg, const f32x16 (&acc)[TM][kTileTN], int h) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave / 4, wn = wave % 4;
-#pragma unroll
-  for (int ii = 0; ii < 2; ++ii) {
-    if (2 * h + ii >= TM) continue;
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int j = 0; j < kTileTN; ++j)
-        stg[(wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kStgPitch + wn * 64 + j * 32 +
-            (lane & 31)] = acc[2 * h + ii < TM ? 2 * h + ii : 0][j][r];
-  }
-}
-// Tile row of staged row pr of part h; at least 64 TM where the part has no such row.
-template <int TM>
-__device__ __forceinline__ int staged_tile_row(int pr, int h) {
-  const int i = 2 * h + ((pr >> 5) & 1);
-  return i < TM ? (pr >> 6) * 32 * TM + i * 32 + (pr & 31) : 64 * TM;
-}
-
-// The fp32 tile (rows row0.., columns n0..) into out (row stride ld), through LDS in two halves
-// so that it leaves in 16-byte stores: one 4-byte store per value and lane kept the
-// texture-address path busy for ~10 us at the end of every tile. ncol % 4 == 0.
-template <int TM>
-__device__ __forceinline__ void tile_store_f32(const f32x16 (&acc)[TM][kTileTN], float* out, size_t ld, int row0,
-                                                int row_end, int n0, int ncol, TileLds& L) {
+__device__ __forceinline__ void tile_store_f32(const f32x16 (&acc)[TM][kTileTN], float* out, size_t ld, int row0, int row_end,
+                                               int n0, int ncol, TileLds& L) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 4, wn = wave % 4;
   float* stg = reinterpret_cast<float*>(&L);
-  row_end = min(row_end, row0 + 64 * TM);
 #pragma unroll
   for (int h = 0; h < (TM + 1) / 2; ++h) {
     wait_lgkmcnt0();
     tile_barrier();   // the k-loop's (or the previous part's) LDS reads are done
-    stage_part<TM>(stg, acc, h);
+#pragma unroll
+    for (int ii = 0; ii < 2; ++ii) {
+      if (2 * h + ii >= TM) continue;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int j = 0; j < kTileTN; ++j)
+          stg[(wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kStorePitch + wn * 64 + j * 32 + (lane & 31)] =
+              acc[2 * h + ii < TM ? 2 * h + ii : 0][j][r];
+    }
     wait_lgkmcnt0();
     tile_barrier();
 #pragma unroll 4
-    for (int q = 0; q < 16; ++q) {   // 8192 float4 per half: 64 per staged row
+    for (int q = 0; q < 16; ++q) {   // 8192 float4: 64 per staged row
       const int u = static_cast<int>(threadIdx.x) + kTileThreads * q;
-      const int pr = u >> 6, c = (u & 63) * 4;
-      const int row = row0 + staged_tile_row<TM>(pr, h), col = n0 + c;
-      if (row < row_end && col < ncol)
+      const int pr = u >> 6, c = (u & 63) * 4, i = 2 * h + ((pr >> 5) & 1);
+      const int row = row0 + (pr >> 6) * 32 * TM + i * 32 + (pr & 31), col = n0 + c;
+      if (i < TM && row < row_end && col < ncol)
         *reinterpret_cast<float4*>(out + static_cast<size_t>(row) * ld + col) =
-            *reinterpret_cast<const float4*>(&stg[pr * kStgPitch + c]);
+            *reinterpret_cast<const float4*>(&stg[pr * kStorePitch + c]);
     }
   }
 }

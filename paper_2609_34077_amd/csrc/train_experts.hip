@@ -1,6 +1,6 @@
 // The experts' training pass at a given routing (include/maskmoe.h, maskmoe_experts_forward_train, _backward). Entries
 // (token, slot) of routed experts and then of the shared ones are grouped by expert; the products run on those rows
-// (experts.hip, backward.hip); here: the entry list, the rows' gathering, the sums over a token's rows.
+// (experts.hip, batch.hip, train_products.hip); here: the entry list, the grouping, the sums over a token's rows.
 
 #include <algorithm>
 
@@ -33,90 +33,86 @@ __device__ __forceinline__ int entry_row(const int32_t* idx, const int32_t* inv,
 
 // Sum over a token's live entries of gate v[row] (gate null: v[row]), in entry order, fp32, rounded once; a thread per
 // eight columns, the loads of U entries in flight. Bound by the rows' bytes.
-__global__ __launch_bounds__(kThreads) void token_sum_kernel(const float* __restrict__ v, const int32_t* __restrict__ idx,
-                                                            const float* __restrict__ gate, const int32_t* __restrict__ inv,
-                                                            int T, int KS, int G, int d, uint16_t* __restrict__ out) {
-  constexpr int U = 4;
-  const int c8 = d / 8;
+// With d_gate, workgroups behind the sums': d_gate of the routed entries, the column tiles' shares in order.
+struct TokenSumArgs {
+  const float* v;           // [rows, d]
+  const int32_t* idx;       // [T, KS]
+  const float* gate;        // [T, KS] or null
+  const int32_t* inv;       // [T, KS]
+  uint16_t* out;            // [T, d]
+  const float* dgate_part;  // [rows, parts]
+  float* d_gate;            // [T, K] or null
+  int T, K, KS, G, d, parts;
+  unsigned sum_blocks;
+};
+template <int U>
+__global__ __launch_bounds__(kThreads) void token_sum_kernel(const TokenSumArgs p) {
+  if (blockIdx.x >= p.sum_blocks) {
+    const int i = static_cast<int>(blockIdx.x - p.sum_blocks) * kThreads + threadIdx.x;
+    if (i >= p.T * p.K) return;
+    const int row = entry_row(p.idx, p.inv, i / p.K * p.KS + i % p.K, p.G);
+    float s = 0.0f;
+    if (row >= 0) {
+#pragma unroll 8
+      for (int q = 0; q < p.parts; ++q) s += p.dgate_part[static_cast<size_t>(row) * p.parts + q];
+    }
+    p.d_gate[i] = s;
+    return;
+  }
+  const int c8 = p.d / 8;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= static_cast<int64_t>(T) * c8) return;
+  if (i >= static_cast<int64_t>(p.T) * c8) return;
   const int t = static_cast<int>(i / c8), c = static_cast<int>(i % c8) * 8;
   float s[8] = {};
-  for (int k0 = 0; k0 < KS; k0 += U) {
+  for (int k0 = 0; k0 < p.KS; k0 += U) {
     int row[U];
     float g[U], o[U][8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int j = t * KS + min(k0 + u, KS - 1);
-      row[u] = k0 + u < KS ? entry_row(idx, inv, j, G) : -1;
-      g[u] = gate ? gate[j] : 1.0f;
+      const int j = t * p.KS + min(k0 + u, p.KS - 1);
+      row[u] = k0 + u < p.KS ? entry_row(p.idx, p.inv, j, p.G) : -1;
+      g[u] = p.gate ? p.gate[j] : 1.0f;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (row[u] >= 0) load_vec8<false>(v, static_cast<size_t>(row[u]) * d + c, o[u]);
+      if (row[u] >= 0) load_vec8<false>(p.v, static_cast<size_t>(row[u]) * p.d + c, o[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (row[u] >= 0)
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] += g[u] * o[u][e];
   }
-  store_vec8<true>(out, 8 * i, s);
+  store_vec8<true>(p.out, 8 * i, s);
 }
 
-// dy and x (bf16, or the values of its blocks) of each row's token, and the row's gate: one workgroup per row. One more
-// lists the groups with rows, most rows first, then by number, and clears the counters of the weight gradients' tiles.
-__global__ __launch_bounds__(kThreads) void gather_kernel(const uint16_t* __restrict__ dy, const uint16_t* __restrict__ x,
-                                                         const int8_t* __restrict__ x_codes,
-                                                         const uint8_t* __restrict__ x_scales,
-                                                         const float* __restrict__ gate,
-                                                         const int32_t* __restrict__ offsets, int G,
-                                                         const int32_t* __restrict__ perm,
-                                                         const int32_t* __restrict__ row_tok, int d,
-                                                         uint16_t* __restrict__ dyg, uint16_t* __restrict__ xg,
-                                                         float* __restrict__ row_gate, int32_t* __restrict__ order,
-                                                         int32_t* __restrict__ next) {
-  if (blockIdx.x == 0) {
-    __shared__ int count[kMaxGroups];
-    if (threadIdx.x < 2 * 8) next[threadIdx.x] = 0;
-    for (int g = threadIdx.x; g < G; g += kThreads) count[g] = offsets[g + 1] - offsets[g];
-    __syncthreads();
-    for (int g = threadIdx.x; g < G; g += kThreads) {
-      int rank = 0;
-      for (int o = 0; o < G; ++o) rank += count[o] > count[g] || (count[o] == count[g] && o < g) ? 1 : 0;
-      if (count[g] > 0) order[rank] = g;
-    }
-    return;
+// dy and x of each row's token. One workgroup per row.
+__global__ __launch_bounds__(kThreads) void gather_kernel(const u32x4* __restrict__ dy, const u32x4* __restrict__ x,
+                                                         const int32_t* __restrict__ rows, const int32_t* __restrict__ row_tok,
+                                                         int d8, u32x4* __restrict__ dyg, u32x4* __restrict__ xg) {
+  const int r = blockIdx.x;
+  if (r >= rows[0]) return;
+  const size_t src = static_cast<size_t>(row_tok[r]) * d8, dst = static_cast<size_t>(r) * d8;
+  for (int c = threadIdx.x; c < d8; c += kThreads) {
+    dyg[dst + c] = dy[src + c];
+    xg[dst + c] = x[src + c];
   }
-  const int r = blockIdx.x - 1;
-  if (r >= offsets[G]) return;
-  const size_t src = static_cast<size_t>(row_tok[r]) * d, dst = static_cast<size_t>(r) * d;
-  for (int c = threadIdx.x * 8; c < d; c += kThreads * 8) {
-    *reinterpret_cast<u32x4*>(dyg + dst + c) = *reinterpret_cast<const u32x4*>(dy + src + c);
-    if (x_codes) {
-      const uint2 q = *reinterpret_cast<const uint2*>(x_codes + src + c);
-      const float step = mx8_step(x_scales[(src + c) / kMx8Block]);
-      float v[8];
-      mx8_decode4(q.x, step, v);
-      mx8_decode4(q.y, step, v + 4);
-      store_vec8<true>(xg, dst + c, v);
-    } else {
-      *reinterpret_cast<u32x4*>(xg + dst + c) = *reinterpret_cast<const u32x4*>(x + src + c);
-    }
-  }
-  if (threadIdx.x == 0) row_gate[r] = gate[perm[r]];
 }
 
-// d_gate of the routed entries: the column tiles' shares in order.
-__global__ __launch_bounds__(kThreads) void d_gate_kernel(const float* __restrict__ part, const int32_t* __restrict__ idx,
-                                                         const int32_t* __restrict__ inv, int T, int K, int KS, int G,
-                                                         int parts, float* __restrict__ d_gate) {
-  const int i = blockIdx.x * kThreads + threadIdx.x;
-  if (i >= T * K) return;
-  const int row = entry_row(idx, inv, i / K * KS + i % K, G);
-  float s = 0.0f;
-  if (row >= 0)
-    for (int p = 0; p < parts; ++p) s += part[static_cast<size_t>(row) * parts + p];
-  d_gate[i] = s;
+// The gate of every row; the first workgroup lists the groups with rows, most rows first, then by number.
+__global__ __launch_bounds__(kThreads) void rows_kernel(const float* __restrict__ gate, const int32_t* __restrict__ offsets,
+                                                       int G, const int32_t* __restrict__ perm,
+                                                       float* __restrict__ row_gate, int32_t* __restrict__ order) {
+  const int r = blockIdx.x * kThreads + threadIdx.x;
+  if (r < offsets[G]) row_gate[r] = gate[perm[r]];
+  if (blockIdx.x > 0) return;
+  __shared__ int count[kMaxGroups];
+  for (int g = threadIdx.x; g < G; g += kThreads) count[g] = offsets[g + 1] - offsets[g];
+  __syncthreads();
+  for (int g = threadIdx.x; g < G; g += kThreads) {
+    int rank = 0;
+    for (int o = 0; o < G; ++o) rank += count[o] > count[g] || (count[o] == count[g] && o < g) ? 1 : 0;
+    if (count[g] > 0) order[rank] = g;
+  }
 }
 
 // n 16-byte pieces of zeros.
@@ -158,12 +154,21 @@ hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, ch
     g.idx = idx;
     g.gate = gate;
   }
-  if (tile_rows != kGemmBM) g.pb.wide_off = reinterpret_cast<int32_t*>(ws + w.wide_off);
+  if (tile_rows < kGemmBM) g.pb.wide_off = reinterpret_cast<int32_t*>(ws + w.wide_off);
   g.max_tiles = std::min(g.rows, g.rows / tile_rows + g.G);
   return launch_permute(g.idx, a.T, g.KS, g.G, 0, tile_rows, g.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
 }
 
 unsigned blocks(int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); }
+
+hipError_t launch_token_sum(TokenSumArgs p, hipStream_t stream) {
+  p.sum_blocks = blocks(static_cast<int64_t>(p.T) * p.d / 8);
+  const dim3 grid(p.sum_blocks + (p.d_gate ? blocks(static_cast<int64_t>(p.T) * p.K) : 0)), block(kThreads);
+  if (p.KS <= 2) hipLaunchKernelGGL(token_sum_kernel<2>, grid, block, 0, stream, p);
+  else if (p.KS <= 4) hipLaunchKernelGGL(token_sum_kernel<4>, grid, block, 0, stream, p);
+  else hipLaunchKernelGGL(token_sum_kernel<8>, grid, block, 0, stream, p);
+  return hipGetLastError();
+}
 
 }  // namespace
 
@@ -193,11 +198,11 @@ ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n
   w.O = take(rows * d * 4);
   w.forward_total = off;
   off = common;
-  w.dyg = take(rows * d * 2);
-  w.xg = take(rows * d * 2);
+  w.x = take(static_cast<size_t>(T) * d * 2);
+  w.dyg = take(gather_rows(F) ? rows * d * 2 : 0);
+  w.xg = take(gather_rows(F) ? rows * d * 2 : 0);
   w.row_gate = take(rows * 4);
   w.order = take(G * 4);
-  w.next = take(2 * 8 * 4);
   w.gh = take(rows * F * 2);
   w.dab = take(rows * 2 * F * 2);
   w.dxr = take(rows * d * 4);
@@ -228,9 +233,14 @@ hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipS
   err = batch_rows ? launch_experts_batch(e, g.pb, batch_rows, a.E, H, O, part, nullptr, stream, nullptr, nullptr, &kept)
                    : launch_experts_kept(e, g.pb, H, O, part, kept, g.max_tiles, stream);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(token_sum_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
-                     O, g.idx, g.gate, g.pb.inv, a.T, g.KS, g.G, a.d, a.y);
-  return hipGetLastError();
+  TokenSumArgs sum{};
+  sum.v = O;
+  sum.idx = g.idx;
+  sum.gate = g.gate;
+  sum.inv = g.pb.inv;
+  sum.out = a.y;
+  sum.T = a.T; sum.K = a.K; sum.KS = g.KS; sum.G = g.G; sum.d = a.d;
+  return launch_token_sum(sum, stream);
 }
 
 hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hipStream_t stream) {
@@ -261,14 +271,11 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   k.pb = g.pb;
   k.codes = a.codes;
   k.scales = a.scales;
-  uint16_t* dyg = reinterpret_cast<uint16_t*>(ws + w.dyg);
-  uint16_t* xg = reinterpret_cast<uint16_t*>(ws + w.xg);
   float* row_gate = reinterpret_cast<float*>(ws + w.row_gate);
   int32_t* order = reinterpret_cast<int32_t*>(ws + w.order);
   k.order = order;
-  k.next = reinterpret_cast<int32_t*>(ws + w.next);
-  k.dyg = dyg;
-  k.xg = xg;
+  k.dy = b.dy;
+  k.x = a.x;
   k.row_gate = row_gate;
   k.gh = reinterpret_cast<uint16_t*>(ws + w.gh);
   k.dab = reinterpret_cast<uint16_t*>(ws + w.dab);
@@ -279,19 +286,39 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   k.d_w_down = b.d_w_down;
   k.d_ws_gate_up = b.d_ws_gate_up;
   k.d_ws_down = b.d_ws_down;
-  k.d = a.d; k.F = a.F; k.E = a.E; k.G = g.G; k.max_tiles = g.max_tiles;
-  hipLaunchKernelGGL(gather_kernel, dim3(g.rows + 1), dim3(kThreads), 0, stream, b.dy, a.x, b.x_codes, b.x_scales,
-                     g.gate, g.pb.offsets, g.G, g.pb.perm, g.pb.row_tok, a.d, dyg, xg, row_gate, order, k.next);
+  k.T = a.T; k.d = a.d; k.F = a.F; k.E = a.E; k.G = g.G; k.max_tiles = g.max_tiles;
+  if (b.x_codes) {   // the values of x's blocks, which bf16 holds exactly
+    uint16_t* x = reinterpret_cast<uint16_t*>(ws + w.x);
+    err = launch_mx8_dequantize(true, b.x_codes, b.x_scales, a.T, a.d, x, stream);
+    if (err != hipSuccess) return err;
+    k.x = x;
+  }
+  hipLaunchKernelGGL(rows_kernel, dim3(blocks(g.rows)), dim3(kThreads), 0, stream, g.gate, g.pb.offsets, g.G, g.pb.perm,
+                     row_gate, order);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
+  if (gather_rows(a.F)) {
+    uint16_t* dyg = reinterpret_cast<uint16_t*>(ws + w.dyg);
+    uint16_t* xg = reinterpret_cast<uint16_t*>(ws + w.xg);
+    hipLaunchKernelGGL(gather_kernel, dim3(g.rows), dim3(kThreads), 0, stream, reinterpret_cast<const u32x4*>(k.dy),
+                       reinterpret_cast<const u32x4*>(k.x), g.pb.offsets + g.G, g.pb.row_tok, a.d / 8,
+                       reinterpret_cast<u32x4*>(dyg), reinterpret_cast<u32x4*>(xg));
+    err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    k.dyg = dyg;
+    k.xg = xg;
+  }
   err = launch_experts_backward_products(k, stream);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(token_sum_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.d / 8)), dim3(kThreads), 0, stream,
-                     k.dxr, g.idx, nullptr, g.pb.inv, a.T, g.KS, g.G, a.d, b.d_x);
-  if (b.d_gate)
-    hipLaunchKernelGGL(d_gate_kernel, dim3(blocks(static_cast<int64_t>(a.T) * a.K)), dim3(kThreads), 0, stream,
-                       k.dgate_part, g.idx, g.pb.inv, a.T, a.K, g.KS, g.G, dgate_parts(a.F), b.d_gate);
-  return hipGetLastError();
+  TokenSumArgs sum{};
+  sum.v = k.dxr;
+  sum.idx = g.idx;
+  sum.inv = g.pb.inv;
+  sum.out = b.d_x;
+  sum.dgate_part = k.dgate_part;
+  sum.d_gate = b.d_gate;
+  sum.T = a.T; sum.K = a.K; sum.KS = g.KS; sum.G = g.G; sum.d = a.d; sum.parts = dgate_parts(a.F);
+  return launch_token_sum(sum, stream);
 }
 
 }  // namespace maskmoe

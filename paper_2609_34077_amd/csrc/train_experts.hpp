@@ -32,8 +32,8 @@ struct ExpertsBwdArgs {
 
 struct ExpertsTrainLayout {   // byte offsets into the workspaces; the grouping is first in both
   size_t idx, gate, offsets, tile_off, wide_off, active, n_active, perm, inv, row_tok, pcount;
-  size_t H, O, part;                                            // forward
-  size_t dyg, xg, row_gate, order, next, gh, dab, dxr, dgate_part;    // gradient (with part)
+  size_t part, H, O;                                            // forward
+  size_t x, dyg, xg, row_gate, order, gh, dab, dxr, dgate_part;    // gradient (with part)
   size_t forward_total, backward_total;
 };
 ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n_shared);
@@ -44,25 +44,28 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& a, void* workspace, hip
 hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint16_t* H, float* O, float* part,
                                const KeptOut& kept, int max_tiles, hipStream_t stream);
 
-// The products of the gradient on rows grouped by expert (backward.hip).
+// The products of the gradient on rows grouped by expert, in row tiles of kGemmBM (train_products.hip).
 struct KeptBwdArgs {
   const uint16_t *w_gate_up, *w_down, *ws_gate_up, *ws_down;
   PermBuffers pb;
   const int32_t* order;       // [pb.n_active[0]] the groups with rows, most rows first
-  int32_t* next;              // [2][8] zeros: tiles that each XCD's workgroups have taken, of each weight gradient
   const int8_t* codes;        // [rows, 2F]
   const uint8_t* scales;
-  const uint16_t* dyg;        // [rows, d] dy of each row's token
-  const uint16_t* xg;         // [rows, d] x of each row's token
+  const uint16_t* dy;         // [T, d]
+  const uint16_t* x;          // [T, d]
+  const uint16_t *dyg, *xg;   // [rows, d] dy and x of each row's token, where gather_rows(F); else null
   const float* row_gate;      // [rows]
   uint16_t* gh;               // [rows, F]
   uint16_t* dab;              // [rows, 2F]
   float* dxr;                 // [rows, d]
   float* dgate_part;          // [rows, dgate_parts(F)]
-  float* part;                // kTailPartBytes
   void *d_w_gate_up, *d_w_down, *d_ws_gate_up, *d_ws_down;
-  int d, F, E, G, max_tiles;
+  float* part;                // kTailPartBytes
+  int T, d, F, E, G, max_tiles;
 };
+// Whether the weight gradients read dy and x from rows gathered for them. Reading them by token costs the products 4 %
+// (Mixtral-shaped, 8192 tokens, 4810 -> 5020 us; DeepSeek-shaped, 4096 tokens, 735 -> 755), the gathering 80 and 72 us there.
+inline bool gather_rows(int F) { return F >= 4096; }
 inline int dgate_parts(int F) { return (F + 255) / 256; }
 hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t stream);
 

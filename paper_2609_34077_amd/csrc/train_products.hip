@@ -1,0 +1,526 @@
+// The products of the experts' gradient (train_experts.hip): with rows grouped by expert,
+//   u = dy W_down  ->  da, db, g h, <u, h>   (rows_kernel<kSwiglu>)
+//   d_x rows = [da db] W_gate_up             (rows_kernel<kF32>)
+//   dW_down = dy^T (g h),  dW_gate_up = [da db]^T x   (wgrad_kernel)
+// on v_mfma_f32_32x32x16_bf16, fp32 sums. Operands whose reduction index is strided in memory (the weights; both of a
+// weight gradient) are loaded as they lie and turned by transposing LDS reads.
+//
+// Rows times weights run on the 256 x 256 pipeline of gemm_tile.hpp, whose A operand is read in pieces of 128 bytes a row; a
+// group's last row tile multiplies its 64-row pieces that hold rows only. On wgrad_kernel's form, which would read 64 bytes
+// of a row at a time, they were slower from about 1000 tokens on (Mixtral-shaped, 8192 tokens, 1820 -> 2160 and 2980 -> 5020 us).
+// Weight gradients, whose operands are both strided, run on tiles of their own, three workgroups a CU (wgrad_kernel).
+
+#include <type_traits>
+
+#include "common.hpp"
+#include "gemm_tile.hpp"
+#include "kernels.hpp"
+#include "mx8.hpp"
+#include "train_experts.hpp"
+
+namespace maskmoe {
+namespace {
+
+struct ProductArgs {
+  const uint16_t* a;          // rows: [.., lda], through row_tok if given; wgrad: K-major [rows, M]
+  const int32_t* row_tok;     // token of each row; null: a's own rows
+  const uint16_t* b;          // rows: the routed experts' K-major [K, N] matrices; wgrad: K-major [rows, N]
+  const uint16_t* bs;         // rows: the shared experts'
+  const int32_t* offsets;     // [G + 1] rows of each group
+  const int32_t* tile_off;    // [G + 1] row tiles (rows)
+  const int32_t* order;       // wgrad: the groups with rows, most rows first, n_active[0] of them
+  const int32_t* n_active;
+  void* c;                    // rows: [rows, N] fp32, or [da db] bf16 [rows, 2N]; wgrad: routed [M, N] matrices
+  void* cs;                   // wgrad: the shared experts'
+  const int8_t* codes;        // kSwiglu: 8-bit blocks of the pre-activations [rows, 2N]
+  const uint8_t* scales;      // [rows, 2N / 32]
+  const float* row_gate;      // [rows]
+  uint16_t* gh;               // [rows, N]
+  float* dgate_part;          // [rows, n_tiles] shares of <u, h>
+  float* part;                // kF32: partial tiles of split tail tiles (tile_job)
+  int G, E, M, N, K, lda, ldb, mt_max, n_tiles;
+  int cu_xcd;                 // rows: workgroups an XCD runs at once
+  int tokens;                 // wgrad: rows of the gathered operand
+};
+
+// ---------------------------------------------------------------- rows times a matrix of their expert
+
+enum { kSwiglu = 0, kF32 = 1 };
+
+// Part h of a tile of 64 TM rows into LDS as fp32 [128][kPitch]: acc[2h + ii] of every wavefront (2h + ii < TM) as staged
+// row 64 wm + 32 ii + (row within the 32-row block).
+constexpr int kPitch = kTileN + 8;
+static_assert(128 * kPitch * 4 <= sizeof(TileLds), "a staged part fits in LDS");
+template <int TM>
+__device__ __forceinline__ void stage_part(float* stg, const f32x16 (&acc)[TM][kTileTN], int h) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 4, wn = wave % 4;
+#pragma unroll
+  for (int ii = 0; ii < 2; ++ii) {
+    if (2 * h + ii >= TM) continue;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int j = 0; j < kTileTN; ++j)
+        stg[(wm * 64 + ii * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kPitch + wn * 64 + j * 32 + (lane & 31)] =
+            acc[2 * h + ii < TM ? 2 * h + ii : 0][j][r];
+  }
+}
+// Tile row of staged row pr of part h; 64 TM where the part has no such row.
+template <int TM>
+__device__ __forceinline__ int staged_tile_row(int pr, int h) {
+  const int i = 2 * h + ((pr >> 5) & 1);
+  return i < TM ? (pr >> 6) * 32 * TM + i * 32 + (pr & 31) : 64 * TM;
+}
+
+// Sum over each half of the wavefront, in its last lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float half_wave_sum(float v) {
+  v = dpp_add<0xB1, 0xF>(v);      // lanes 1 apart
+  v = dpp_add<0x4E, 0xF>(v);      // 2 apart
+  v = dpp_add<0x141, 0xF>(v);     // mirrored within 8
+  v = dpp_add<0x140, 0xF>(v);     // mirrored within 16
+  return dpp_add<0x142, 0xA>(v);  // lane 15 of rows 0, 2 to rows 1, 3
+}
+
+// End of u's tile: da = g u b SiLU'(a), db = g u SiLU(a), g h in bf16, and the tile's share of every row's <u, h>. The tile
+// goes through LDS in parts of 128 rows, so that a thread holds eight consecutive columns of a row (32 lanes a row); a
+// part's blocks are loaded before it is staged and waited for behind that (before it: 1910 instead of 1820 us, Mixtral-shaped,
+// 8192 tokens). Columns past the end read the last ones' and are not stored.
+template <int TM>
+__device__ __forceinline__ void swiglu_epilogue(const ProductArgs& p, const f32x16 (&acc)[TM][kTileTN], int row0, int row_end,
+                                                int nt, TileLds& L) {
+  constexpr int Q = 8;   // 4096 pieces of eight columns a part
+  const int tid = threadIdx.x, cg = (tid & 31) * 8, col = nt * kTileN + cg, cc = min(col, p.N - 8);
+  float* stg = reinterpret_cast<float*>(&L);
+  char* o = static_cast<char*>(p.c);
+  const uint32_t N = p.N;
+  const int end = min(row_end, row0 + 64 * TM);
+#pragma unroll
+  for (int h = 0; h < (TM + 1) / 2; ++h) {
+    uint2 a8[Q], b8[Q];
+    uint32_t sa[Q], sb[Q];
+    float gate[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int row = row0 + staged_tile_row<TM>((tid >> 5) + 16 * q, h);
+      a8[q] = b8[q] = make_uint2(0, 0);
+      sa[q] = sb[q] = 0;
+      gate[q] = 0.0f;
+      if (row >= end) continue;
+      const uint32_t at = static_cast<uint32_t>(row) * (2 * N) + cc;   // below 2^31
+      a8[q] = *reinterpret_cast<const uint2*>(p.codes + at);
+      b8[q] = *reinterpret_cast<const uint2*>(p.codes + at + N);
+      sa[q] = p.scales[at / kMx8Block];
+      sb[q] = p.scales[(at + N) / kMx8Block];
+      gate[q] = p.row_gate[row];
+    }
+    wait_lgkmcnt0();
+    tile_barrier();   // the k-loop's (or the previous part's) LDS reads are done
+    stage_part<TM>(stg, acc, h);
+    wait_lgkmcnt0();
+    tile_barrier();
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int pr = (tid >> 5) + 16 * q, row = row0 + staged_tile_row<TM>(pr, h);
+      float v[8], av[8], bv[8], da[8], db[8], gh[8];
+      *reinterpret_cast<f32x4*>(v) = *reinterpret_cast<const f32x4*>(stg + pr * kPitch + cg);
+      *reinterpret_cast<f32x4*>(v + 4) = *reinterpret_cast<const f32x4*>(stg + pr * kPitch + cg + 4);
+      const float s_a = mx8_step(sa[q]), s_b = mx8_step(sb[q]);
+      mx8_decode4(a8[q].x, s_a, av);
+      mx8_decode4(a8[q].y, s_a, av + 4);
+      mx8_decode4(b8[q].x, s_b, bv);
+      mx8_decode4(b8[q].y, s_b, bv + 4);
+      float dot = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float sg = sigmoid(av[e]), l = av[e] * sg, hv = l * bv[e], gu = gate[q] * v[e];
+        dot += v[e] * hv;
+        da[e] = gu * bv[e] * (sg + l - l * sg);   // SiLU' = s + a s (1 - s)
+        db[e] = gu * l;
+        gh[e] = gate[q] * hv;
+      }
+      const bool live = row < end && col < p.N;
+      dot = half_wave_sum(live ? dot : 0.0f);
+      if ((tid & 31) == 31 && row < end) p.dgate_part[static_cast<uint32_t>(row) * p.n_tiles + nt] = dot;
+      if (!live) continue;
+      u32x4 pa, pb, pg;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        pa[e] = f32x2_to_bf16x2(da[2 * e], da[2 * e + 1]);
+        pb[e] = f32x2_to_bf16x2(db[2 * e], db[2 * e + 1]);
+        pg[e] = f32x2_to_bf16x2(gh[2 * e], gh[2 * e + 1]);
+      }
+      const uint32_t at = (static_cast<uint32_t>(row) * (2 * N) + col) * 2;   // bytes, below 2^32
+      *reinterpret_cast<u32x4*>(o + at) = pa;
+      *reinterpret_cast<u32x4*>(o + (at + 2 * N)) = pb;
+      *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(p.gh) + (static_cast<uint32_t>(row) * N + col) * 2) = pg;
+    }
+  }
+}
+
+__device__ __forceinline__ int group_of(const int32_t* tile_off, int G, int mt) {
+  int lo = 0, hi = G;   // tile_off[lo] <= mt < tile_off[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (tile_off[mid] <= mt) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// kF32 splits the tiles of each XCD's last round over the reduction (tile_job); rows_fixup_kernel adds them.
+template <int EPI>
+__global__ __launch_bounds__(kTileThreads) void rows_kernel(const ProductArgs p) {
+  __shared__ TileLds lds;
+  const int lane = threadIdx.x & 63, wn = (threadIdx.x >> 6) % 4;
+  const int mt_live = p.tile_off[p.G], nkf = p.K / kTileK;
+  TileJob job;
+  if (!tile_job(static_cast<int>(blockIdx.x), mt_live * p.n_tiles, p.cu_xcd, nkf, EPI == kF32 && tail_splittable(nkf), job))
+    return;
+  int mt, nt;
+  grouped_tile_coords(job.lid, mt_live, p.n_tiles, mt, nt);
+  const int g = group_of(p.tile_off, p.G, mt);
+  const int row0 = p.offsets[g] + (mt - p.tile_off[g]) * kTileM, row_end = p.offsets[g + 1], n0 = nt * kTileN;
+  const int nk = nkf / job.s, k0 = job.z * nk * kTileK;
+  const int tm = job.s > 1 ? kTileTM : min((row_end - row0 + 63) / 64, kTileTM);
+  TileOps ops{};
+  ops.a = reinterpret_cast<const char*>(p.a + k0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {   // element offsets below 2^31
+    const int row = min(row0 + tile_dma_row_a(tm, i), row_end - 1);
+    ops.aoff[i] = static_cast<uint32_t>((p.row_tok ? p.row_tok[row] : row) * p.lda + tile_dma_chunk_a(tm, i) * 8) * 2u;
+  }
+  const uint16_t* w = g < p.E ? p.b + static_cast<size_t>(g) * p.N * p.K : p.bs + static_cast<size_t>(g - p.E) * p.N * p.K;
+  const TileKm bkm{reinterpret_cast<const char*>(w + static_cast<size_t>(k0) * p.ldb + n0), p.ldb * 2, nk * kTileK, p.N - n0};
+  int bfrag[kTileTN];
+#pragma unroll
+  for (int j = 0; j < kTileTN; ++j) bfrag[j] = wn * 64 + j * 32 + (lane & 31);
+  auto tile = [&](auto tm_c) {
+    constexpr int TM = decltype(tm_c)::value;
+    f32x16 acc[TM][kTileTN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < kTileTN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    gemm_tile_mainloop<false, false, true, false, TM>(ops, nk, bfrag, acc, lds, nullptr, nullptr, &bkm);
+    if constexpr (EPI == kSwiglu) {
+      swiglu_epilogue<TM>(p, acc, row0, row_end, nt, lds);
+    } else {
+      if constexpr (TM == kTileTM) {
+        if (job.s > 1) {   // a slice of a split tile
+          tail_store_partial(p.part, job.slot, acc);
+          return;
+        }
+      }
+      tile_store_f32<TM>(acc, static_cast<float*>(p.c), p.N, row0, min(row_end, row0 + 64 * TM), n0, p.N, lds);
+    }
+  };
+  using std::integral_constant;
+  if (tm == 4) tile(integral_constant<int, 4>{});
+  else if (tm == 3) tile(integral_constant<int, 3>{});
+  else if (tm == 2) tile(integral_constant<int, 2>{});
+  else tile(integral_constant<int, 1>{});
+}
+
+// Adds the slices of rows_kernel<kF32>'s split tiles in slice order; kTailFixParts workgroups per possible one, grid
+// 8 x kTailSlotsPerXcd x kTailFixParts.
+__global__ __launch_bounds__(kTileThreads) void rows_fixup_kernel(const ProductArgs p) {
+  const int mt_live = p.tile_off[p.G];
+  const int b = blockIdx.x, xcd = b & 7, t = (b >> 3) % kTailSlotsPerXcd, part = b / (8 * kTailSlotsPerXcd);
+  const XcdShare x = xcd_share(xcd, mt_live * p.n_tiles, p.cu_xcd, p.K / kTileK, true);
+  if (x.s == 1 || t >= x.r) return;
+  int mt, nt;
+  grouped_tile_coords(x.base + x.full + t, mt_live, p.n_tiles, mt, nt);
+  const int g = group_of(p.tile_off, p.G, mt);
+  const int row0 = p.offsets[g] + (mt - p.tile_off[g]) * kTileM, row_end = p.offsets[g + 1];
+  float* out = static_cast<float*>(p.c);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 4, wn = wave % 4;
+  const int c0 = nt * kTileN + wn * 64 + (lane & 31);
+  tail_fixup_part(p.part, xcd * kTailSlotsPerXcd + t * x.s, x.s, part, [&](int i, int q, float4 a0, float4 a1) {
+    const float v0[4] = {a0.x, a0.y, a0.z, a0.w}, v1[4] = {a1.x, a1.y, a1.z, a1.w};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int row = row0 + wm * 128 + i * 32 + 8 * q + 4 * (lane >> 5) + u;
+      if (row >= row_end) continue;
+      if (c0 < p.N) out[static_cast<size_t>(row) * p.N + c0] = v0[u];
+      if (c0 + 32 < p.N) out[static_cast<size_t>(row) * p.N + c0 + 32] = v1[u];
+    }
+  });
+}
+
+// ---------------------------------------------------------------- weight gradients
+
+constexpr int kThreads = 256, kM = 128, kN = 256, kChunk = 32;
+constexpr int kHalf = kChunk * 16;   // 16-byte units of a 128-column half of a chunk, [32 k][128]
+
+// Tiles of 128 x 256; a K-major operand's unit (eight columns) u of k-row kr sits at km_unit(u, kr) of its 128-column half.
+// Columns past the matrix are those of the next row, or past the buffer's end and zero: their products are stored nowhere.
+
+// 16 bytes per lane to LDS as dma16b, `step` (wave-uniform) added to the lane's offset; the buffer's end is checked against
+// their sum, so step must lie within the buffer.
+__device__ __forceinline__ void dma16s(uint32_t m0v, i32x4 rsrc, uint32_t voff, uint32_t step) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(m0v), "v"(voff), "s"(rsrc),
+               "s"(step)
+               : "memory", "m0");
+}
+
+// An offset behind any buffer: operands hold fewer than 2^31 elements in rows of whole 128 bytes.
+constexpr uint32_t kPast = 0xfffffff0u;
+
+// For every group with rows the [M, N] product over its rows of the K-major A [rows, M] and B [rows, N], in bf16; the
+// matrices of groups without rows are zeroed on the side, where these are not the most (zero_unused_kernel).
+// A workgroup of four wavefronts owns 128 x 256 results (64 x 128 a wavefront) and runs over chunks of 32 rows, the next
+// one on its way to LDS (48 KB, two buffers) while one is multiplied. Nothing within a workgroup hides a barrier, a first
+// load or the end of a tile; the two other workgroups of the CU do (168 registers each). Against the 256 x 256 pipeline of
+// gemm_tile.hpp, one workgroup a CU that loads its next tile's operands while it stores, both products: Mixtral-shaped, 64
+// tokens, 700 -> 500 us, 8192 tokens 4920 -> 4690 (1.23 PFLOP/s); DeepSeek-shaped, 64 tokens, 286 -> 235, 4096 tokens 735 ->
+// 700. Two workgroups a CU with three buffers and one barrier a chunk lost 10 to 20 % throughout. The compiler lets the
+// chunk's last products sink behind the barriers; held in place (a wavefront priority around them, a fence, the row
+// numbers' load at the chunk's end) the products took 1.4 to 1.9 times as long.
+// Tile order: every XCD takes an eighth of each group's tiles (pieces of per / 8 consecutive ones, dealt in turn), the groups
+// by descending rows, so that all XCDs have the same work and no long reduction starts late. With a range of consecutive
+// tiles for each XCD instead, the XCD with the shared experts' tiles decided (DeepSeek-shaped, 4096 tokens, two
+// products 1307 us instead of 790, on the 256 x 256 tiles of gemm_tile.hpp).
+__device__ __forceinline__ bool zeros_in_wgrad(int G, int n_active) { return G - n_active <= n_active; }
+
+__host__ __device__ __forceinline__ int dealt_piece(int per) { return per < 8 ? 1 : per / 8; }
+
+// The operand that is one row per token (kByTokenA: A, the cotangent; kByTokenB: B, the tokens) is read through row_tok, eight
+// row numbers a chunk and wavefront by one scalar load, or (kByRows) lies in rows gathered before (gather_rows, which
+// says when).
+enum { kByTokenA = 0, kByTokenB = 1, kByRows = 2 };
+template <int BY>
+__global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p) {
+  __shared__ u32x4 lds[2][3 * kHalf];   // [buffer][A, the two halves of B]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+  const int n_active = p.n_active[0], per = p.mt_max * p.n_tiles, live = n_active * per;
+  const int piece = dealt_piece(per), local = blockIdx.x >> 3;
+  const int lid = (local / piece * 8 + static_cast<int>(blockIdx.x & 7)) * piece + local % piece;
+  if (lid >= live) return;
+  const int g = p.order[lid / per];
+  int mt, nt;
+  grouped_tile_coords(lid % per, p.mt_max, p.n_tiles, mt, nt);
+  const int r0 = p.offsets[g], nrows = p.offsets[g + 1] - r0, m0 = mt * kM, n0 = nt * kN;
+  const int lda = 2 * p.lda, ldb = 2 * p.ldb;
+  // rows past the group's end read as zeros: they lie behind the buffer of the operand in rows, and are given an offset
+  // behind that of the gathered one (tokens ld: below 2^32 - 128)
+  auto rsrc = [&](const uint16_t* v, bool gather, int ld, int c0) {
+    const uint32_t rows = static_cast<uint32_t>(gather ? p.tokens : nrows);
+    return buffer_rsrc(v + (gather ? 0 : static_cast<size_t>(r0) * (ld / 2)) + c0, rows * static_cast<uint32_t>(ld) - 2u * static_cast<uint32_t>(c0));
+  };
+  const i32x4 ar = rsrc(p.a, BY == kByTokenA, lda, m0), br = rsrc(p.b, BY == kByTokenB, ldb, n0);
+  const int ld_tok = BY == kByTokenA ? lda : ldb;
+  const int s16 = lane >> 4, kr0 = 8 * wave + s16;   // k-row of this lane in the wavefront's first 1 KiB piece; 4 on in its second
+  const uint32_t unit = static_cast<uint32_t>(16 * km_unit(lane & 15, s16));
+  const uint32_t aoff = static_cast<uint32_t>(kr0 * lda) + unit, boff = static_cast<uint32_t>(kr0 * ldb) + unit;
+  const uint32_t base = lds_offset(&lds[0][0]), dst = base + static_cast<uint32_t>(2 * wave * 1024);
+  const int nc = (nrows + kChunk - 1) / kChunk;
+  const auto* tok = (const __attribute__((address_space(4))) int32_t*)(p.row_tok + r0 + 8 * wave);   // read by scalar loads
+  auto load = [&](int c, uint32_t buf) {   // six loads a wavefront, past the end of the last chunk again
+    const int k = min(c, nc - 1) * kChunk;
+    const uint32_t astep = static_cast<uint32_t>(k) * static_cast<uint32_t>(lda);
+    const uint32_t bstep = static_cast<uint32_t>(k) * static_cast<uint32_t>(ldb);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t la = dst + buf + static_cast<uint32_t>(i * 1024), lb = la + kHalf * 16;
+      const uint32_t at_a = aoff + static_cast<uint32_t>(4 * i * lda), at_b = boff + static_cast<uint32_t>(4 * i * ldb);
+      uint32_t token = kPast;
+      if constexpr (BY != kByRows) {
+        // up to 31 numbers past the group's last row are read (within the workspace) and not used
+        int t[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) t[q] = __builtin_amdgcn_readfirstlane(tok[k + 4 * i + q]) * ld_tok;
+        const int row = s16 & 2 ? (s16 & 1 ? t[3] : t[2]) : s16 & 1 ? t[1] : t[0];
+        if (k + kr0 + 4 * i < nrows) token = static_cast<uint32_t>(row) + unit;
+      }
+      if constexpr (BY == kByTokenA) dma16b(la, ar, token);
+      else dma16s(la, ar, at_a, astep);
+      if constexpr (BY == kByTokenB) {
+        dma16b(lb, br, token);
+        dma16b(lb + kHalf * 16, br, token == kPast ? kPast : token + 256);
+      } else {
+        dma16s(lb, br, at_b, bstep);
+        dma16s(lb + kHalf * 16, br, at_b + 256, bstep);
+      }
+    }
+  };
+  // Operands from LDS as read_km_operand does, by one address a fragment: k steps, halves and buffers are constants
+  uint32_t fa[2], fb[4];
+  {
+    const int G = lane >> 4, j = lane & 15;
+    const uint32_t row = static_cast<uint32_t>((8 * (G >> 1) + (j >> 2)) * 256 + (2 * (G & 1) + (j >> 1 & 1)) * 16 + (j & 1) * 8);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) fa[i] = base + row + static_cast<uint32_t>(((2 * wm + i) ^ (j >> 2)) * 64);
+#pragma unroll
+    for (int f = 0; f < 4; ++f) fb[f] = base + row + static_cast<uint32_t>((1 + wn) * kHalf * 16 + (f ^ (j >> 2)) * 64);
+  }
+  auto operand = [&](uint32_t at) {
+    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)(at)));
+    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)(at + 1024)));
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
+  };
+  f32x16 acc[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  constexpr uint32_t kBuf = 3 * kHalf * 16;
+  auto chunk = [&](int c, auto buf_c) {
+    constexpr uint32_t buf = decltype(buf_c)::value * kBuf;
+    load(c + 1, kBuf - buf);
+    wait_vmcnt<6>();
+    tile_barrier();
+#pragma unroll
+    for (int kk = 0; kk < kChunk / 16; ++kk) {
+      u32x4 a[2], b[4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) a[i] = operand(fa[i] + (buf + kk * 4096));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = operand(fb[j] + (buf + kk * 4096));
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = mfma_32x32x16(a[i], b[j], acc[i][j]);
+    }
+    wait_lgkmcnt0();
+    tile_barrier();   // the chunk is read: its buffer takes the one after the next
+  };
+  load(0, 0);
+  for (int c = 0; c < nc; c += 2) {
+    chunk(c, std::integral_constant<uint32_t, 0>{});
+    if (c + 1 < nc) chunk(c + 1, std::integral_constant<uint32_t, 1>{});
+  }
+  wait_vmcnt<0>();
+  tile_barrier();
+  const size_t mn = static_cast<size_t>(p.M) * p.N;
+  auto matrix = [&](int e) { return e < p.E ? static_cast<uint16_t*>(p.c) + e * mn : static_cast<uint16_t*>(p.cs) + (e - p.E) * mn; };
+  uint16_t* out = matrix(g);
+  // [64 rows][256 columns] as bf16, column c of row r at c ^ 32 (r >> 2 & 1): the two halves of a wavefront, four rows
+  // apart, write different banks. Staged row 32 wm + r: tile row 64 wm + 32 i + r.
+  uint16_t* stg = reinterpret_cast<uint16_t*>(&lds);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), col = wn * 128 + j * 32 + (lane & 31);
+        stg[row * kN + (col ^ (row >> 2 & 1) * 32)] = f32_to_bf16(acc[i][j][r]);
+      }
+    wait_lgkmcnt0();
+    tile_barrier();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {   // 2048 pieces of eight columns: 32 per row
+      const int pr = (tid >> 5) + 8 * q, c = (tid & 31) * 8, row = m0 + (pr >> 5) * 64 + i * 32 + (pr & 31), col = n0 + c;
+      if (row < p.M && col < p.N)
+        *reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * p.N + col) =
+            *reinterpret_cast<const u32x4*>(&stg[pr * kN + (c ^ (pr >> 2 & 1) * 32)]);
+    }
+    wait_lgkmcnt0();
+    tile_barrier();
+  }
+  if (n_active == p.G || !zeros_in_wgrad(p.G, n_active)) return;
+  const size_t n = mn / 8, i0 = n * lid / live, i1 = n * (lid + 1) / live;   // this tile's slice of every empty matrix
+  for (int e = 0; e < p.G; ++e) {
+    if (p.offsets[e + 1] > p.offsets[e]) continue;
+    f32x4* dst = reinterpret_cast<f32x4*>(matrix(e));
+    for (size_t i = i0 + tid; i < i1; i += kThreads) __builtin_nontemporal_store(f32x4{0.f, 0.f, 0.f, 0.f}, dst + i);
+  }
+}
+
+// Zeros the two gradients of the groups without rows (n: 16-byte pieces of a down matrix; gate / up has twice as many)
+// where they are more than those with. Grid (G, chunks).
+__global__ __launch_bounds__(kThreads) void zero_unused_kernel(const int32_t* __restrict__ offsets,
+                                                              const int32_t* __restrict__ n_active, int E, size_t n,
+                                                              u32x4* __restrict__ down, u32x4* __restrict__ s_down,
+                                                              u32x4* __restrict__ gate_up, u32x4* __restrict__ s_gate_up) {
+  const int g = blockIdx.x;
+  if (zeros_in_wgrad(gridDim.x, n_active[0]) || offsets[g + 1] > offsets[g]) return;
+  const u32x4 zero = {0, 0, 0, 0};
+  u32x4* dn = g < E ? down + g * n : s_down + (g - E) * n;
+  u32x4* gu = g < E ? gate_up + g * 2 * n : s_gate_up + (g - E) * 2 * n;
+  const size_t step = static_cast<size_t>(gridDim.y) * kThreads, first = static_cast<size_t>(blockIdx.y) * kThreads + threadIdx.x;
+  for (size_t i = first; i < n; i += step) dn[i] = zero;
+  for (size_t i = first; i < 2 * n; i += step) gu[i] = zero;
+}
+
+template <class T>
+T ceil_div(T a, T b) { return (a + b - 1) / b; }
+
+// 8 XCDs x (their largest share of the tiles + tail slices).
+dim3 rows_grid(int max_tiles, int n_tiles) {
+  return dim3(static_cast<unsigned>(8 * (ceil_div<int64_t>(static_cast<int64_t>(max_tiles) * n_tiles, 8) + kTailSlotsPerXcd)));
+}
+
+template <int BY>
+hipError_t launch_wgrad(ProductArgs p, const uint16_t* a, int M, const uint16_t* b, int N, void* c, void* cs, hipStream_t s) {
+  p.a = a; p.lda = M; p.M = M;
+  p.b = b; p.ldb = N; p.N = N;
+  p.c = c;
+  p.cs = cs;
+  p.mt_max = ceil_div(M, kM);
+  p.n_tiles = ceil_div(N, kN);
+  const int64_t per = static_cast<int64_t>(p.mt_max) * p.n_tiles, piece = dealt_piece(static_cast<int>(per));
+  const int64_t pieces = ceil_div(p.G * per, piece);
+  hipLaunchKernelGGL(wgrad_kernel<BY>, dim3(static_cast<unsigned>(ceil_div<int64_t>(pieces, 8) * 8 * piece)), dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s) {
+  ProductArgs p{};
+  p.offsets = a.pb.offsets;
+  p.tile_off = a.pb.tile_off;
+  p.order = a.order;
+  p.n_active = a.pb.n_active;
+  p.G = a.G; p.E = a.E;
+  p.cu_xcd = device_cus_per_xcd();
+  p.part = a.part;
+  // u = dy W_down and its end
+  p.a = a.dy; p.row_tok = a.pb.row_tok; p.lda = a.d;
+  p.b = a.w_down; p.bs = a.ws_down; p.K = a.d; p.N = a.F; p.ldb = a.F;   // W_down [d, F]: K-major
+  p.codes = a.codes;
+  p.scales = a.scales;
+  p.row_gate = a.row_gate;
+  p.gh = a.gh;
+  p.dgate_part = a.dgate_part;
+  p.c = a.dab;
+  p.n_tiles = ceil_div(p.N, kTileN);
+  hipLaunchKernelGGL(rows_kernel<kSwiglu>, rows_grid(a.max_tiles, p.n_tiles), dim3(kTileThreads), 0, s, p);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  // rows of d_x = [da db] W_gate_up
+  p.a = a.dab; p.row_tok = nullptr; p.lda = 2 * a.F;
+  p.b = a.w_gate_up; p.bs = a.ws_gate_up; p.K = 2 * a.F; p.N = a.d; p.ldb = a.d;   // W_gate_up [2F, d]: K-major
+  p.c = a.dxr;
+  p.n_tiles = ceil_div(p.N, kTileN);
+  hipLaunchKernelGGL(rows_kernel<kF32>, rows_grid(a.max_tiles, p.n_tiles), dim3(kTileThreads), 0, s, p);
+  if (tail_splittable(p.K / kTileK))
+    hipLaunchKernelGGL(rows_fixup_kernel, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(kTileThreads), 0, s, p);
+  err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  p.row_tok = a.pb.row_tok;
+  p.tokens = a.T;
+  // dW_down [d, F] = dy^T (g h), dW_gate_up [2F, d] = [da db]^T x
+  if (a.dyg) {
+    err = launch_wgrad<kByRows>(p, a.dyg, a.d, a.gh, a.F, a.d_w_down, a.d_ws_down, s);
+    if (err == hipSuccess) err = launch_wgrad<kByRows>(p, a.dab, 2 * a.F, a.xg, a.d, a.d_w_gate_up, a.d_ws_gate_up, s);
+  } else {
+    err = launch_wgrad<kByTokenA>(p, a.dy, a.d, a.gh, a.F, a.d_w_down, a.d_ws_down, s);
+    if (err == hipSuccess) err = launch_wgrad<kByTokenB>(p, a.dab, 2 * a.F, a.x, a.d, a.d_w_gate_up, a.d_ws_gate_up, s);
+  }
+  if (err != hipSuccess) return err;
+  auto u = [](void* q) { return static_cast<u32x4*>(q); };
+  hipLaunchKernelGGL(zero_unused_kernel, dim3(a.G, 64), dim3(kThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E,
+                     static_cast<size_t>(a.F) * a.d / 8, u(a.d_w_down), u(a.d_ws_down), u(a.d_w_gate_up), u(a.d_ws_gate_up));
+  return hipGetLastError();
+}
+
+}  // namespace maskmoe

@@ -153,16 +153,22 @@ def plain(v, codes, scales, x, idx):
     return out
 
 
+@pytest.mark.parametrize("x8", [False, True])
 @pytest.mark.parametrize("T,d,F,E,K,ns,pad", [(3000, 2048, 1408, 64, 6, 2, 100), (700, 4096, 2048, 8, 2, 0, 0),
                                               (5000, 1024, 4160, 4, 2, 1, 1)])
-def test_larger_layers(T, d, F, E, K, ns, pad):
+def test_larger_layers(T, d, F, E, K, ns, pad, x8):
     """Many tiles, split tail tiles, experts of several row tiles. Independent roundings to bf16 are off by at most
     2^-8 / sqrt(3) relative (RMS) each: two of them in a row in y's terms and its own, two in the gradients."""
-    say(f"experts training T={T} d={d} F={F}")
+    say(f"experts training T={T} d={d} F={F} x8={x8}")
     v = cuda(make(T, d, F, E, K, ns, 7, pad))
     y, codes, scales = forward(v)
-    grads = backward(v, codes, scales)
-    ref = plain(v, codes, scales, v["x"].double(), v["idx"])
+    if x8:
+        xc, xs = L.maskmoe_mx8_quantize(v["x"])
+        grads = backward(v, codes, scales, x=xc, x_scales=xs)
+        ref = plain(v, codes, scales, L.maskmoe_mx8_dequantize(xc, xs, torch.float32).double(), v["idx"])
+    else:
+        grads = backward(v, codes, scales)
+        ref = plain(v, codes, scales, v["x"].double(), v["idx"])
     rel = lambda a, b: ((a.double() - b).norm() / b.norm()).item()   # noqa: E731
     step = 2.0 ** -8 / 3 ** 0.5
     assert rel(grads["d_x"], ref["d_x"]) <= step * 2 ** 0.5
