@@ -33,10 +33,44 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// The same in fp64.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double v) {
+  const uint2 b = __builtin_bit_cast(uint2, v);
+  uint2 o;
+  o.x = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b.x), CTRL, ROWS, 0xF, false));
+  o.y = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b.y), CTRL, ROWS, 0xF, false));
+  return v + __builtin_bit_cast(double, o);
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  v = dpp_add<0xB1, 0xF>(v);
+  v = dpp_add<0x4E, 0xF>(v);
+  v = dpp_add<0x141, 0xF>(v);
+  v = dpp_add<0x140, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);
+  v = dpp_add<0x143, 0xC>(v);
+  uint2 b = __builtin_bit_cast(uint2, v);
+  b.x = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b.x), 63));
+  b.y = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b.y), 63));
+  return __builtin_bit_cast(double, b);
+}
+
+// m^-1/2 of a mean square as an fp32 number and its remainder: the hardware's, and one Newton step where m is in fp32's range.
+__device__ __forceinline__ void inverse_root(double m, float& hi, float& lo) {
+  const float mf = static_cast<float>(m);
+  hi = rsqrtf(mf);
+  lo = 0.0f;
+  if (mf >= 0x1p-126f && mf <= 0x1.fffffep127f) {
+    const double r = hi, full = r * (1.5 - 0.5 * m * r * r);
+    hi = static_cast<float>(full);
+    lo = static_cast<float>(full - hi);
+  }
+}
+
 // Sums of M values over the N threads of a row. red: M floats a wavefront of the workgroup, another buffer from one
 // call to the next.
-template <int N, int M>
-__device__ __forceinline__ void row_sum(float (&v)[M], float (*red)[M]) {
+template <int N, int M, class V>
+__device__ __forceinline__ void row_sum(V (&v)[M], V (*red)[M]) {
 #pragma unroll
   for (int m = 0; m < M; ++m) v[m] = wave_sum(v[m]);
   if constexpr (N > kWave) {
@@ -47,7 +81,7 @@ __device__ __forceinline__ void row_sum(float (&v)[M], float (*red)[M]) {
     lds_sync();
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      float s = red[first][m];
+      V s = red[first][m];
 #pragma unroll
       for (int w = 1; w < N / kWave; ++w) s += red[first + w][m];
       v[m] = s;
@@ -129,12 +163,12 @@ template <bool BF16, bool VEC, int N, int V>
 __global__ __launch_bounds__(N* kRowsOf<N>) void norm_forward_kernel(const NormArgs a) {
   using P = Piece<BF16, VEC, N>;
   constexpr int R = kRowsOf<N>;
-  __shared__ float red[2][N * R / kWave][1];
+  __shared__ double red[2][N * R / kWave][1];
   const int lane = threadIdx.x % N, d = a.d;
   float w[V][8];
 #pragma unroll
   for (int p = 0; p < V; ++p) P::load(a.weight, 0, d, p, lane, w[p]);
-  const float inv_d = 1.0f / static_cast<float>(d);
+  const double inv_d = 1.0 / d;
   int turn = 0;
   for (int t0 = blockIdx.x * R; t0 < a.T; t0 += gridDim.x * R, turn ^= 1) {
     const int t = t0 + threadIdx.x / N;
@@ -156,17 +190,25 @@ __global__ __launch_bounds__(N* kRowsOf<N>) void norm_forward_kernel(const NormA
     if (a.hidden)
 #pragma unroll
       for (int p = 0; p < V; ++p) P::store(a.hidden, row, dl, p, lane, s[p]);
-    float sum[1] = {0.0f};
+    // A thread's squares in fp32, their sum over the row in fp64, and the product with the inverse root and the weight by
+    // its fp32 value and remainder: y is off by little more than its rounding, so that 8-bit codes are those of the
+    // formula but within 2^-22 or so of a border.
+    float part = 0.0f;
 #pragma unroll
     for (int p = 0; p < V; ++p)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[0] += s[p][j] * s[p][j];
+      for (int j = 0; j < 8; ++j) part += s[p][j] * s[p][j];
+    double sum[1] = {part};
     row_sum<N, 1>(sum, red[turn]);
-    const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
+    float rstd, rest;
+    inverse_root(sum[0] * inv_d + a.eps, rstd, rest);
 #pragma unroll
     for (int p = 0; p < V; ++p)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[p][j] = s[p][j] * rstd * w[p][j];
+      for (int j = 0; j < 8; ++j) {
+        const float n = s[p][j] * rstd, e = __builtin_fmaf(s[p][j], rest, __builtin_fmaf(s[p][j], rstd, -n));
+        s[p][j] = __builtin_fmaf(n, w[p][j], e * w[p][j]);
+      }
     if (a.y)
 #pragma unroll
       for (int p = 0; p < V; ++p) P::store(a.y, row, dl, p, lane, s[p]);
@@ -277,21 +319,25 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 
 using std::integral_constant;
 
-// f(N, V) with N threads of V pieces a row: the fewest threads that hold it, four pieces each at most.
+// f(N, V) with N threads of V pieces a row: one piece each as long as a workgroup holds the row. Few registers a thread
+// then leave room for more rows at once (67 MB each of x, residual, hidden and y in bf16: d 2048 with 64 threads of four
+// pieces 50.2 us, 128 of two 47.2, 256 of one 44.5; d 4096 with 256 of two 50.0, 512 of one 42.7; d 8192 with 256 of four
+// 48.9, 1024 of one 42.5).
 template <class F>
 hipError_t with_shape(int d, F f) {
   const int n = (d + 7) / 8;
   if (n <= 64) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  if (n <= 128) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  if (n <= 256) return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-  if (n <= 512) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  if (n <= 1024) return f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  if (n <= 128) return f(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+  if (n <= 256) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  if (n <= 512) return f(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+  if (n <= 1024) return f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
   if (n <= 2048) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
   return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
 
-// The same for the gradient, which holds five values an element: two pieces, and four in the longest rows only (those
-// spill: 128 registers are what 1024 threads have).
+// The same for the gradient, whose rows' partial sums are bound less by registers than by their number (d 4096: 59.9 us
+// with 256 threads of two pieces, 60.0 with 512 of one; d 8192: 62.6 with 512 of two, 64.7 with 1024 of one). It holds five
+// values an element: four pieces, in the longest rows only, spill (128 registers are what 1024 threads have).
 template <class F>
 hipError_t with_shape_backward(int d, F f) {
   const int n = (d + 7) / 8;
@@ -299,7 +345,7 @@ hipError_t with_shape_backward(int d, F f) {
   if (n <= 128) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   if (n <= 256) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   if (n <= 512) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  if (n <= 1024) return f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+  if (n <= 1024) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
   if (n <= 2048) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
   return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
@@ -329,7 +375,8 @@ int norm_backward_parts(int T, int d) {
     return hipSuccess;
   });
   const int64_t need = (static_cast<int64_t>(T) + rows - 1) / rows;
-  return static_cast<int>(need < 512 ? need : 512);
+  const int most = d <= 8192 ? 512 : 256;   // of the longest rows, the partial sums' own bytes count
+  return static_cast<int>(need < most ? need : most);
 }
 
 hipError_t launch_norm_backward(const NormBwdArgs& a, hipStream_t stream) {
