@@ -170,8 +170,8 @@ __global__ __launch_bounds__(N* kRowsOf<N>) void norm_forward_kernel(const NormA
   for (int p = 0; p < V; ++p) P::load(a.weight, 0, d, p, lane, w[p]);
   const double inv_d = 1.0 / d;
   int turn = 0;
-  for (int t0 = blockIdx.x * R; t0 < a.T; t0 += gridDim.x * R, turn ^= 1) {
-    const int t = t0 + threadIdx.x / N;
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * R; t0 < a.T; t0 += gridDim.x * R, turn ^= 1) {
+    const int64_t t = t0 + threadIdx.x / N;
     const bool live = t < a.T;
     const size_t row = static_cast<size_t>(live ? t : a.T - 1) * d;   // past the end: the last row, not stored
     const int dl = live ? d : 0;
@@ -238,8 +238,8 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(const NormBwdArgs a
   }
   const float inv_d = 1.0f / static_cast<float>(d);
   int turn = 0;
-  for (int t0 = blockIdx.x * R; t0 < a.T; t0 += gridDim.x * R, turn ^= 1) {
-    const int t = t0 + sub;
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * R; t0 < a.T; t0 += gridDim.x * R, turn ^= 1) {
+    const int64_t t = t0 + sub;
     const bool live = t < a.T;
     const size_t row = static_cast<size_t>(live ? t : a.T - 1) * d;
     const int dl = live ? d : 0;

@@ -284,3 +284,21 @@ def test_past_32_bit_offsets():
     assert torch.equal(c2[-5:], c[-5:]) and torch.equal(s2[-5:], s[-5:])
     dx, _ = L.maskmoe_norm_backward(x, w, y)
     assert torch.equal(dx[-5:], L.maskmoe_norm_backward(x[-5:].clone(), w, y[-5:].clone())[0])
+
+
+def test_most_rows():
+    """2^31 - 1 rows: the walk over the rows ends, and the last ones are those of a call on them alone."""
+    T, last = 2 ** 31 - 1, 9000
+    say(f"norm {T} x 1")
+    x = torch.empty((T, 1), dtype=torch.bfloat16, device="cuda")
+    x.view(torch.int16).fill_(0x3F80)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x[-last:] = torch.randn((last, 1), generator=g, device="cuda").bfloat16()
+    w = torch.full((1,), 2.0, device="cuda").bfloat16()
+    y, _, _, _ = L.maskmoe_norm_forward(x, w, eps=0.5)
+    e, _, _, _ = L.maskmoe_norm_forward(x[-last:].clone(), w, eps=0.5)
+    assert torch.equal(y[-last:], e)
+    assert (y[:10].float() - 2 / 1.5 ** 0.5).abs().max() <= 2.0 ** -8 and torch.equal(y[:-last:4097], y[:1].expand(len(y[:-last:4097]), 1))
+    back = L.maskmoe_norm_backward(x, w, y, eps=0.5, with_d_weight=False)[0]
+    assert torch.equal(back[-last:], L.maskmoe_norm_backward(x[-last:].clone(), w, e, eps=0.5, with_d_weight=False)[0])
+    assert torch.equal(back[:-last:4097], back[:1].expand(len(back[:-last:4097]), 1))
