@@ -769,7 +769,7 @@ int maskmoe_norm_backward(int32_t T, int32_t d, int32_t dtype, float eps, const 
  *  Rounding: sums are fp32; h and each expert's output are rounded to bf16, y once; codes are those of the unrounded
  *  a and b.
  *  Errors: E_INVAL for a desc outside its ranges, NULL or misaligned pointers, x == y; E_WORKSPACE; E_UNSUPPORTED for
- *  MASKMOE_F32, d or F not multiples of 64, and T d, T (K + n_shared) 2F, T (K + n_shared) d or 2 F d at or above 2^31.
+ *  MASKMOE_F32, d or F not multiples of 64, and T d, R 2F, R d or 2 F d at or above 2^31, R = T (K + n_shared) + 64.
  *  T = 0 writes nothing.
  */
 size_t maskmoe_experts_train_workspace_bytes(const maskmoe_layer_desc* desc);

@@ -35,7 +35,8 @@ int check_train(const maskmoe_layer_desc* d) {
       d->n_shared < 0 || d->n_shared > 8 || !known(d->dtype))
     return MASKMOE_E_INVAL;
   if (d->dtype != MASKMOE_BF16 || d->d % 64 != 0 || d->F % 64 != 0) return MASKMOE_E_UNSUPPORTED;
-  const int64_t rows = static_cast<int64_t>(d->T) * (d->K + d->n_shared);   // the products' 32-bit offsets
+  // the products' 32-bit byte offsets; a weight gradient's last chunk reaches up to 31 rows and 512 bytes past the rows
+  const int64_t rows = static_cast<int64_t>(d->T) * (d->K + d->n_shared) + 64;
   if (static_cast<int64_t>(d->T) * d->d >= kLim || rows * 2 * d->F >= kLim || rows * d->d >= kLim ||
       int64_t{2} * d->F * d->d >= kLim)
     return MASKMOE_E_UNSUPPORTED;

@@ -331,11 +331,12 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
       uint32_t token = kPast;
       if constexpr (BY != kByRows) {
         // up to 31 numbers past the group's last row are read (within the workspace) and not used
-        int t[4];
+        uint32_t t[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) t[q] = __builtin_amdgcn_readfirstlane(tok[k + 4 * i + q]) * ld_tok;
-        const int row = s16 & 2 ? (s16 & 1 ? t[3] : t[2]) : s16 & 1 ? t[1] : t[0];
-        if (k + kr0 + 4 * i < nrows) token = static_cast<uint32_t>(row) + unit;
+        for (int q = 0; q < 4; ++q)
+          t[q] = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(tok[k + 4 * i + q])) * static_cast<uint32_t>(ld_tok);
+        const uint32_t row = s16 & 2 ? (s16 & 1 ? t[3] : t[2]) : s16 & 1 ? t[1] : t[0];
+        if (k + kr0 + 4 * i < nrows) token = row + unit;
       }
       if constexpr (BY == kByTokenA) dma16b(la, ar, token);
       else dma16s(la, ar, at_a, astep);

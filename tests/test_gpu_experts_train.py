@@ -195,6 +195,38 @@ def test_larger_layers(T, d, F, E, K, ns, pad, x8):
     assert rel(y, want) <= step * 3 ** 0.5
 
 
+@pytest.mark.parametrize("d,F", [(128, 512), (1024, 64), (2048, 1024), (8192, 4096)])
+def test_most_rows(d, F):
+    """As many rows as 32-bit offsets reach: the last tokens' outputs and gradients, and the weight gradients of a cotangent
+    that is zero but for them. Rounded as in test_larger_layers."""
+    E, K, n = 4, 2, 50
+    T = (2 ** 31 // max(2 * F, d) - 65) // K
+    say(f"experts training T={T} d={d} F={F}")
+    v = cuda(make(n, d, F, E, K, 0, 11))
+    g = torch.Generator(device="cuda").manual_seed(2)
+    big = dict(v, x=torch.zeros((T, d), dtype=torch.bfloat16, device="cuda"),
+               dy=torch.zeros((T, d), dtype=torch.bfloat16, device="cuda"), gate=torch.ones((T, K), device="cuda"),
+               idx=torch.randint(0, E, (T, K), generator=g, device="cuda", dtype=torch.int32))
+    big["x"].view(torch.int16).fill_(0x3D00)
+    for k in ("x", "dy", "idx", "gate"):
+        big[k][-n:] = v[k]
+    y, codes, scales = forward(big)
+    order = torch.argsort(big["idx"].flatten(), stable=True)
+    rows = (order >= (T - n) * K).nonzero()[:, 0]   # of the last tokens, in their order
+    grads = backward(big, codes, scales)
+    ref = plain(v, codes[rows], scales[rows], v["x"].double(), v["idx"])
+    rel = lambda a, b: ((a.double() - b).norm() / b.norm()).item()   # noqa: E731
+    step = 2.0 ** -8 / 3 ** 0.5
+    assert rel(grads["d_x"][-n:], ref["d_x"]) <= step * 2 ** 0.5 and not grads["d_x"][:-n].any()
+    assert rel(grads["d_gate"][-n:], ref["d_gate"]) <= 1e-5 and not grads["d_gate"][:-n].any()
+    for name in ("w_gate_up", "w_down"):
+        assert rel(grads["d_" + name], torch.stack(ref[name])) <= step * 2 ** 0.5, name
+    small, c, s = forward(v)
+    assert rel(y[-n:], small.double()) <= 2 * step * 3 ** 0.5
+    kept = lambda c, s: c.double() * torch.exp2(s.double() - 133).repeat_interleave(32, 1)   # noqa: E731
+    assert rel(kept(codes[rows], scales[rows]), kept(c, s)) <= 2.0 ** -6
+
+
 @pytest.mark.parametrize("T", [3, 90, 600])
 def test_nan_and_infinity_stay_in_their_token(T):
     v = cuda(make(T, 192, 128, 4, 2, 1, T + 1))

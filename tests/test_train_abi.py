@@ -117,6 +117,14 @@ def test_experts_training_rejects(call, query):
     assert sizes == sorted(sizes)
 
 
+@pytest.mark.parametrize("call", [fwd, bwd])
+def test_experts_training_rejects_rows_at_the_end_of_32_bits(call):
+    """A weight gradient's last chunk of 32 rows must not run past 2^32 bytes, where its offsets would start again."""
+    for kw, most in ((dict(F=512, K=1), 2 ** 21 - 65), (dict(d=1024, K=1), 2 ** 21 - 65), (dict(F=512, K=2), 2 ** 20 - 33)):
+        ok, over = (L.make_desc(**{**OK, "n_shared": 0, **kw, "T": T}) for T in (most, most + 1))
+        assert call(ok, ws=None) == L.E_WORKSPACE and call(over, ws=None) == L.E_UNSUPPORTED, kw
+
+
 def test_experts_training_rejects_outputs():
     d = L.make_desc(**OK)
     for kw in (dict(y=None), dict(y=FAKE), dict(y=FAKE + 8)):
