@@ -692,6 +692,7 @@ int maskmoe_experts_forward_mx4(const maskmoe_layer_desc* desc, int32_t act, con
  *  rows, cols   cols % 32 == 0.   dtype MASKMOE_BF16 or MASKMOE_F32: type of src / dst.
  *  src, dst     device [rows, cols].   codes device [rows, cols].   All three 16-byte aligned.
  *  scales       device [rows, cols / 32].
+ *  Buffers must not overlap.
  *  Errors: E_INVAL for negative rows, cols < 1, NULL or misaligned pointers or an unknown dtype; E_UNSUPPORTED for
  *  cols % 32 != 0 or more than 2^40 elements.
  */
@@ -716,9 +717,10 @@ int maskmoe_mx8_dequantize(int64_t rows, int32_t cols, int32_t dtype, const int8
  *  codes     device [T, d], scales device [T, d / 32]: both or neither; d % 32 == 0 then.
  *  Any alignment of the elements' own will do; rows of a multiple of 16 bytes in 16-byte aligned tensors are faster.
  *  Buffers other than those named above must not overlap.
- *  Rounding: s, the mean and y are fp32 (the norm is that of the unrounded s); hidden, y and the blocks are each rounded
- *  once from those. Rows whose squares pass fp32's range give 0, an infinity or NaN in a row NaN in all of it that an
- *  infinity or NaN reaches by the formula.
+ *  Rounding: s and y are fp32 (the norm is that of the unrounded s), the sum of squares and its root fp64; hidden, y and
+ *  the blocks are each rounded once from those. The squares are fp32: rows whose squares pass its range give 0, and below it
+ *  (elements under 2^-63 throughout) eps decides. An infinity gives NaN in its place and 0 elsewhere in its row, a NaN NaN
+ *  in the whole row.
  *  Errors: E_INVAL for sizes, eps or dtype outside their ranges, NULL required or misaligned pointers, no output at all,
  *  codes without scales (or the reverse), y == hidden; E_UNSUPPORTED for d > 32768 or codes with d % 32 != 0.
  */
@@ -766,8 +768,8 @@ int maskmoe_norm_backward(int32_t T, int32_t d, int32_t dtype, float eps, const 
  *  workspace   device, maskmoe_experts_train_workspace_bytes(desc) bytes, 256-byte aligned, free again once the call has
  *              run; contents on entry do not matter. Calls that may overlap, and graphs that may run at the same time,
  *              must not share it.
- *  Rounding: sums are fp32; h and each expert's output are rounded to bf16, y once; codes are those of the unrounded
- *  a and b.
+ *  Rounding: sums and the experts' outputs are fp32; h is rounded to bf16 before its product, y once; codes are those of
+ *  the unrounded a and b.
  *  Errors: E_INVAL for a desc outside its ranges, NULL or misaligned pointers, x == y; E_WORKSPACE; E_UNSUPPORTED for
  *  MASKMOE_F32, d or F not multiples of 64, and T d, R 2F, R d or 2 F d at or above 2^31, R = T (K + n_shared) + 64.
  *  T = 0 writes nothing.
@@ -796,6 +798,7 @@ int maskmoe_experts_forward_train(const maskmoe_layer_desc* desc, const void* x,
  *  d_w_gate_up device [E, 2F, d] bf16, d_w_down device [E, d, F] bf16: zero for experts that no entry names.
  *  d_ws_gate_up, d_ws_down: the shared experts', [n_shared, ...]; NULL when n_shared == 0.
  *  workspace   device, maskmoe_experts_backward_workspace_bytes(desc) bytes, as above.
+ *  Outputs must not overlap each other or what is read.
  *  Rounding: sums, d_gate and the rows' shares of d_x are fp32; da, db and g h are rounded to bf16 before their products;
  *  outputs are rounded once.
  *  Errors: as the forward's; E_INVAL for a missing gradient buffer too. T = 0 writes zero weight gradients.

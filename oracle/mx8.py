@@ -81,7 +81,6 @@ def forward(x, idx, gate, w_gate_up, w_down, n_shared):
         e_h = e_h + HALF * (np.abs(h) + e_h)
         o = w_down[e] @ h
         e_o = np.abs(w_down[e]) @ e_h + F * U32 * (np.abs(w_down[e]) @ (np.abs(h) + e_h))
-        e_o = e_o + HALF * (np.abs(o) + e_o)
         g = gate[t, k] if k < idx.shape[1] else 1.0
         y[t] += g * o
         b_y[t] += np.abs(g) * (e_o + 32 * U32 * np.abs(o))

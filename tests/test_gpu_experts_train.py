@@ -158,7 +158,7 @@ def plain(v, codes, scales, x, idx):
                                               (5000, 1024, 4160, 4, 2, 1, 1)])
 def test_larger_layers(T, d, F, E, K, ns, pad, x8):
     """Many tiles, split tail tiles, experts of several row tiles. Independent roundings to bf16 are off by at most
-    2^-8 / sqrt(3) relative (RMS) each: two of them in a row in y's terms and its own, two in the gradients."""
+    2^-8 / sqrt(3) relative (RMS) each: one in y's terms and its own, two in the gradients."""
     say(f"experts training T={T} d={d} F={F} x8={x8}")
     v = cuda(make(T, d, F, E, K, ns, 7, pad))
     y, codes, scales = forward(v)
@@ -177,7 +177,7 @@ def test_larger_layers(T, d, F, E, K, ns, pad, x8):
         for e in range(E + ns):
             got = grads["d_" + name][e] if e < E else grads["d_" + name.replace("w_", "ws_")][e - E]
             assert rel(got, ref[name][e]) <= step * 2 ** 0.5, (name, e)
-    # the layer on the values: y's terms round h and the expert's output, y itself once more
+    # the layer on the values: y's terms round h, y itself once more
     x, entries = v["x"].double(), v["idx"].long()
     want, row = torch.zeros_like(x), 0
     for e in range(E + ns):
@@ -192,7 +192,7 @@ def test_larger_layers(T, d, F, E, K, ns, pad, x8):
             # half a step a value, 2^-7 of a block's largest; here relative to the whole
             assert rel(kept, ab) <= 2.0 ** -6
         row += len(t)
-    assert rel(y, want) <= step * 3 ** 0.5
+    assert rel(y, want) <= step * 2 ** 0.5
 
 
 @pytest.mark.parametrize("d,F", [(128, 512), (1024, 64), (2048, 1024), (8192, 4096)])
@@ -222,7 +222,7 @@ def test_most_rows(d, F):
     for name in ("w_gate_up", "w_down"):
         assert rel(grads["d_" + name], torch.stack(ref[name])) <= step * 2 ** 0.5, name
     small, c, s = forward(v)
-    assert rel(y[-n:], small.double()) <= 2 * step * 3 ** 0.5
+    assert rel(y[-n:], small.double()) <= 2 * step * 2 ** 0.5
     kept = lambda c, s: c.double() * torch.exp2(s.double() - 133).repeat_interleave(32, 1)   # noqa: E731
     assert rel(kept(codes[rows], scales[rows]), kept(c, s)) <= 2.0 ** -6
 
