@@ -3,6 +3,7 @@
 // (experts.hip, batch.hip, train_products.hip); here: the entry list, the grouping, the sums over a token's rows.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "mx8.hpp"
 #include "train_experts.hpp"
@@ -32,7 +33,9 @@ __device__ __forceinline__ int entry_row(const int32_t* idx, const int32_t* inv,
 }
 
 // Sum over a token's live entries of gate v[row] (gate null: v[row]), in entry order, fp32, rounded once; a thread per
-// eight columns, the loads of U entries in flight. Bound by the rows' bytes.
+// C columns, the loads of U entries in flight. Bound by the rows' bytes: 268 MB of 8192 tokens with two entries each in 59
+// to 73 us, of 4096 with eight in 57. Few entries take eight columns and ordinary loads (four that bypass the caches: 72
+// to 78), many take four that bypass them (eight and ordinary: 86).
 // With d_gate, workgroups behind the sums': d_gate of the routed entries, the column tiles' shares in order.
 struct TokenSumArgs {
   const float* v;           // [rows, d]
@@ -45,8 +48,10 @@ struct TokenSumArgs {
   int T, K, KS, G, d, parts;
   unsigned sum_blocks;
 };
+constexpr int sum_columns(int U) { return U < 8 ? 8 : 4; }
 template <int U>
 __global__ __launch_bounds__(kThreads) void token_sum_kernel(const TokenSumArgs p) {
+  constexpr int C = sum_columns(U);
   if (blockIdx.x >= p.sum_blocks) {
     const int i = static_cast<int>(blockIdx.x - p.sum_blocks) * kThreads + threadIdx.x;
     if (i >= p.T * p.K) return;
@@ -59,14 +64,15 @@ __global__ __launch_bounds__(kThreads) void token_sum_kernel(const TokenSumArgs 
     p.d_gate[i] = s;
     return;
   }
-  const int c8 = p.d / 8;
+  const int pieces = p.d / C;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= static_cast<int64_t>(p.T) * c8) return;
-  const int t = static_cast<int>(i / c8), c = static_cast<int>(i % c8) * 8;
-  float s[8] = {};
+  if (i >= static_cast<int64_t>(p.T) * pieces) return;
+  const int t = static_cast<int>(i / pieces), c = static_cast<int>(i % pieces) * C;
+  float s[C] = {};
   for (int k0 = 0; k0 < p.KS; k0 += U) {
     int row[U];
-    float g[U], o[U][8];
+    float g[U];
+    f32x4 o[U][C / 4];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = t * p.KS + min(k0 + u, p.KS - 1);
@@ -74,15 +80,20 @@ __global__ __launch_bounds__(kThreads) void token_sum_kernel(const TokenSumArgs 
       g[u] = p.gate ? p.gate[j] : 1.0f;
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (row[u] >= 0) load_vec8<false>(p.v, static_cast<size_t>(row[u]) * p.d + c, o[u]);
+    for (int u = 0; u < U; ++u) {
+      if (row[u] < 0) continue;
+      const f32x4* v = reinterpret_cast<const f32x4*>(p.v + static_cast<size_t>(row[u]) * p.d + c);
+#pragma unroll
+      for (int q = 0; q < C / 4; ++q) o[u][q] = C == 4 ? __builtin_nontemporal_load(v + q) : v[q];
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (row[u] >= 0)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] += g[u] * o[u][e];
+        for (int e = 0; e < C; ++e) s[e] += g[u] * o[u][e / 4][e % 4];
   }
-  store_vec8<true>(p.out, 8 * i, s);
+  if constexpr (C == 8) store_vec8<true>(p.out, 8 * i, s);
+  else *reinterpret_cast<uint2*>(p.out + 4 * i) = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
 }
 
 // dy and x of each row's token. One workgroup per row.
@@ -162,12 +173,15 @@ hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, ch
 unsigned blocks(int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); }
 
 hipError_t launch_token_sum(TokenSumArgs p, hipStream_t stream) {
-  p.sum_blocks = blocks(static_cast<int64_t>(p.T) * p.d / 8);
-  const dim3 grid(p.sum_blocks + (p.d_gate ? blocks(static_cast<int64_t>(p.T) * p.K) : 0)), block(kThreads);
-  if (p.KS <= 2) hipLaunchKernelGGL(token_sum_kernel<2>, grid, block, 0, stream, p);
-  else if (p.KS <= 4) hipLaunchKernelGGL(token_sum_kernel<4>, grid, block, 0, stream, p);
-  else hipLaunchKernelGGL(token_sum_kernel<8>, grid, block, 0, stream, p);
-  return hipGetLastError();
+  auto launch = [&](auto u) {
+    constexpr int U = decltype(u)::value;
+    p.sum_blocks = blocks(static_cast<int64_t>(p.T) * p.d / sum_columns(U));
+    const dim3 grid(p.sum_blocks + (p.d_gate ? blocks(static_cast<int64_t>(p.T) * p.K) : 0));
+    hipLaunchKernelGGL(token_sum_kernel<U>, grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  return p.KS <= 2 ? launch(integral_constant<int, 2>{}) : p.KS <= 4 ? launch(integral_constant<int, 4>{}) : launch(integral_constant<int, 8>{});
 }
 
 }  // namespace
