@@ -34,7 +34,7 @@ __device__ __forceinline__ int entry_row(const int32_t* idx, const int32_t* inv,
 
 // Sum over a token's live entries of gate v[row] (gate null: v[row]), in entry order, fp32, rounded once; a thread per
 // C columns, the loads of U entries in flight. Bound by the rows' bytes: 268 MB of 8192 tokens with two entries each in 59
-// to 73 us, of 4096 with eight in 57. Few entries take eight columns and ordinary loads (four that bypass the caches: 72
+// to 62 us, of 4096 with eight in 55. Few entries take eight columns and ordinary loads (four that bypass the caches: 72
 // to 78), many take four that bypass them (eight and ordinary: 86).
 // With d_gate, workgroups behind the sums': d_gate of the routed entries, the column tiles' shares in order.
 struct TokenSumArgs {

@@ -88,7 +88,7 @@ __device__ __forceinline__ float half_wave_sum(float v) {
 // End of u's tile: da = g u b SiLU'(a), db = g u SiLU(a), g h in bf16, and the tile's share of every row's <u, h>. The tile
 // goes through LDS in parts of 128 rows, so that a thread holds eight consecutive columns of a row (32 lanes a row); a
 // part's blocks are loaded before it is staged and waited for behind that (before it: 1910 instead of 1820 us, Mixtral-shaped,
-// 8192 tokens). Columns past the end read the last ones' and are not stored.
+// 8192 tokens); they are read once, past the caches. Columns past the end read the last ones' and are not stored.
 template <int TM>
 __device__ __forceinline__ void swiglu_epilogue(const ProductArgs& p, const f32x16 (&acc)[TM][kTileTN], int row0, int row_end,
                                                 int nt, TileLds& L) {
@@ -111,8 +111,8 @@ __device__ __forceinline__ void swiglu_epilogue(const ProductArgs& p, const f32x
       gate[q] = 0.0f;
       if (row >= end) continue;
       const uint32_t at = static_cast<uint32_t>(row) * (2 * N) + cc;   // below 2^31
-      a8[q] = *reinterpret_cast<const uint2*>(p.codes + at);
-      b8[q] = *reinterpret_cast<const uint2*>(p.codes + at + N);
+      a8[q] = __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const uint64_t*>(p.codes + at)));
+      b8[q] = __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const uint64_t*>(p.codes + at + N)));
       sa[q] = p.scales[at / kMx8Block];
       sb[q] = p.scales[(at + N) / kMx8Block];
       gate[q] = p.row_gate[row];
@@ -280,7 +280,8 @@ constexpr uint32_t kPast = 0xfffffff0u;
 // tokens, 700 -> 500 us, 8192 tokens 4920 -> 4690 (1.23 PFLOP/s); DeepSeek-shaped, 64 tokens, 286 -> 235, 4096 tokens 735 ->
 // 700. Two workgroups a CU with three buffers and one barrier a chunk lost 10 to 20 % throughout. The compiler lets the
 // chunk's last products sink behind the barriers; held in place (a wavefront priority around them, a fence, the row
-// numbers' load at the chunk's end) the products took 1.4 to 1.9 times as long.
+// numbers' load at the chunk's end) the products took 1.4 to 1.9 times as long. Results bypass the caches, where d_x's
+// rows stay for the sum that follows (Mixtral-shaped, 8192 tokens, 74 -> 62 us there, the products as before).
 // Tile order: every XCD takes an eighth of each group's tiles (pieces of per / 8 consecutive ones, dealt in turn), the groups
 // by descending rows, so that all XCDs have the same work and no long reduction starts late. With a range of consecutive
 // tiles for each XCD instead, the XCD with the shared experts' tiles decided (DeepSeek-shaped, 4096 tokens, two
@@ -420,8 +421,8 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
     for (int q = 0; q < 8; ++q) {   // 2048 pieces of eight columns: 32 per row
       const int pr = (tid >> 5) + 8 * q, c = (tid & 31) * 8, row = m0 + (pr >> 5) * 64 + i * 32 + (pr & 31), col = n0 + c;
       if (row < p.M && col < p.N)
-        *reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * p.N + col) =
-            *reinterpret_cast<const u32x4*>(&stg[pr * kN + (c ^ (pr >> 2 & 1) * 32)]);
+        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&stg[pr * kN + (c ^ (pr >> 2 & 1) * 32)]),
+                                    reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * p.N + col));
     }
     wait_lgkmcnt0();
     tile_barrier();
