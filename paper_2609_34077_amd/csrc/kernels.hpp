@@ -24,6 +24,8 @@ struct PermBuffers {
   int32_t* inv;
   int32_t* row_tok;
   int32_t* wide_off = nullptr;
+  const float* gate = nullptr;   // [entries], with row_gate [rows]: the gate of each row's entry (the experts' gradient)
+  float* row_gate = nullptr;
 };
 // Router logits + softmax + mask/prior Top-K + gates for layers [0, L) of w_router
 // ([L, E, d]); host `mask` [L, E] (HARD_MASK) or `prior` [L, E] (SOFT_PRIOR), unused for

@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kPermThreads) void permute_scatter_kernel(const int
     pb.perm[pos] = j;
     pb.inv[j] = pos;
     pb.row_tok[pos] = j / K;
+    if (pb.row_gate) pb.row_gate[pos] = pb.gate[j];
   }
 }
 

@@ -165,6 +165,7 @@ __device__ inline void permute_block(const int32_t* idx, int T, int K, int E, in
       pb.perm[pos] = j;
       pb.inv[j] = pos;
       pb.row_tok[pos] = j / K;
+      if (pb.row_gate) pb.row_gate[pos] = pb.gate[j];
     }
   }
 }

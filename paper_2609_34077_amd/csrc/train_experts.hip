@@ -12,7 +12,6 @@ namespace maskmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxGroups = 256 + 8;
 
 // Entries of routed and shared experts in one list.
 __global__ __launch_bounds__(kThreads) void entries_kernel(const int32_t* __restrict__ idx, const float* __restrict__ gate,
@@ -109,23 +108,6 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(const u32x4* __restric
   }
 }
 
-// The gate of every row; the first workgroup lists the groups with rows, most rows first, then by number.
-__global__ __launch_bounds__(kThreads) void rows_kernel(const float* __restrict__ gate, const int32_t* __restrict__ offsets,
-                                                       int G, const int32_t* __restrict__ perm,
-                                                       float* __restrict__ row_gate, int32_t* __restrict__ order) {
-  const int r = blockIdx.x * kThreads + threadIdx.x;
-  if (r < offsets[G]) row_gate[r] = gate[perm[r]];
-  if (blockIdx.x > 0) return;
-  __shared__ int count[kMaxGroups];
-  for (int g = threadIdx.x; g < G; g += kThreads) count[g] = offsets[g + 1] - offsets[g];
-  __syncthreads();
-  for (int g = threadIdx.x; g < G; g += kThreads) {
-    int rank = 0;
-    for (int o = 0; o < G; ++o) rank += count[o] > count[g] || (count[o] == count[g] && o < g) ? 1 : 0;
-    if (count[g] > 0) order[rank] = g;
-  }
-}
-
 // n 16-byte pieces of zeros.
 __global__ __launch_bounds__(kThreads) void fill_zero_kernel(u32x4* __restrict__ p, size_t n) {
   for (size_t i = static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x; i < n;
@@ -140,9 +122,9 @@ struct Grouping {
   int G, KS, rows, max_tiles;
 };
 
-// Entry list and grouping, in tiles of tile_rows rows; a.T > 0.
-hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, char* ws, int tile_rows, Grouping& g,
-                      hipStream_t stream) {
+// Entry list and grouping, in tiles of tile_rows rows; row_gate: [rows] or null. a.T > 0.
+hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, char* ws, int tile_rows, float* row_gate,
+                      Grouping& g, hipStream_t stream) {
   g.G = a.E + a.n_shared;
   g.KS = a.K + a.n_shared;
   g.rows = a.T * g.KS;
@@ -165,6 +147,8 @@ hipError_t group_rows(const ExpertsTrainArgs& a, const ExpertsTrainLayout& w, ch
     g.idx = idx;
     g.gate = gate;
   }
+  g.pb.gate = g.gate;
+  g.pb.row_gate = row_gate;
   if (tile_rows < kGemmBM) g.pb.wide_off = reinterpret_cast<int32_t*>(ws + w.wide_off);
   g.max_tiles = std::min(g.rows, g.rows / tile_rows + g.G);
   return launch_permute(g.idx, a.T, g.KS, g.G, 0, tile_rows, g.pb, reinterpret_cast<int32_t*>(ws + w.pcount), stream);
@@ -231,7 +215,7 @@ hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipS
   Grouping g;
   // few rows an expert: the weights' stream decides, as in inference
   const int batch_rows = batch_tile_rows(a.T, a.K, a.E, 1.0f);
-  hipError_t err = group_rows(a, w, ws, batch_rows ? batch_rows : kGemmBM, g, stream);
+  hipError_t err = group_rows(a, w, ws, batch_rows ? batch_rows : kGemmBM, nullptr, g, stream);
   if (err != hipSuccess) return err;
   ExpertArgs e{};
   e.x = a.x;
@@ -275,7 +259,7 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   const ExpertsTrainLayout w = experts_train_layout(a.T, a.d, a.F, a.E, a.K, a.n_shared);
   char* ws = static_cast<char*>(workspace);
   Grouping g;
-  hipError_t err = group_rows(a, w, ws, kGemmBM, g, stream);
+  hipError_t err = group_rows(a, w, ws, kGemmBM, reinterpret_cast<float*>(ws + w.row_gate), g, stream);
   if (err != hipSuccess) return err;
   KeptBwdArgs k{};
   k.w_gate_up = a.w_gate_up;
@@ -285,12 +269,9 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   k.pb = g.pb;
   k.codes = a.codes;
   k.scales = a.scales;
-  float* row_gate = reinterpret_cast<float*>(ws + w.row_gate);
-  int32_t* order = reinterpret_cast<int32_t*>(ws + w.order);
-  k.order = order;
+  k.order = reinterpret_cast<int32_t*>(ws + w.order);
   k.dy = b.dy;
   k.x = a.x;
-  k.row_gate = row_gate;
   k.gh = reinterpret_cast<uint16_t*>(ws + w.gh);
   k.dab = reinterpret_cast<uint16_t*>(ws + w.dab);
   k.dxr = reinterpret_cast<float*>(ws + w.dxr);
@@ -307,10 +288,6 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
     if (err != hipSuccess) return err;
     k.x = x;
   }
-  hipLaunchKernelGGL(rows_kernel, dim3(blocks(g.rows)), dim3(kThreads), 0, stream, g.gate, g.pb.offsets, g.G, g.pb.perm,
-                     row_gate, order);
-  err = hipGetLastError();
-  if (err != hipSuccess) return err;
   if (gather_rows(a.F)) {
     uint16_t* dyg = reinterpret_cast<uint16_t*>(ws + w.dyg);
     uint16_t* xg = reinterpret_cast<uint16_t*>(ws + w.xg);

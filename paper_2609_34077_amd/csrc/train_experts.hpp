@@ -48,13 +48,12 @@ hipError_t launch_experts_kept(const ExpertArgs& a, const PermBuffers& pb, uint1
 struct KeptBwdArgs {
   const uint16_t *w_gate_up, *w_down, *ws_gate_up, *ws_down;
   PermBuffers pb;
-  const int32_t* order;       // [pb.n_active[0]] the groups with rows, most rows first
+  int32_t* order;             // [G] written: the groups, most rows first
   const int8_t* codes;        // [rows, 2F]
   const uint8_t* scales;
   const uint16_t* dy;         // [T, d]
   const uint16_t* x;          // [T, d]
   const uint16_t *dyg, *xg;   // [rows, d] dy and x of each row's token, where gather_rows(F); else null
-  const float* row_gate;      // [rows]
   uint16_t* gh;               // [rows, F]
   uint16_t* dab;              // [rows, 2F]
   float* dxr;                 // [rows, d]

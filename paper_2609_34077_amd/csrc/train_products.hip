@@ -28,7 +28,7 @@ struct ProductArgs {
   const uint16_t* bs;         // rows: the shared experts'
   const int32_t* offsets;     // [G + 1] rows of each group
   const int32_t* tile_off;    // [G + 1] row tiles (rows)
-  const int32_t* order;       // wgrad: the groups with rows, most rows first, n_active[0] of them
+  int32_t* order;             // the groups, most rows first; n_active[0] of them have rows. kSwiglu writes it, wgrad reads
   const int32_t* n_active;
   void* c;                    // rows: [rows, N] fp32, or [da db] bf16 [rows, 2N]; wgrad: routed [M, N] matrices
   void* cs;                   // wgrad: the shared experts'
@@ -170,12 +170,25 @@ __device__ __forceinline__ int group_of(const int32_t* tile_off, int G, int mt) 
   return lo;
 }
 
+// The groups by descending rows, equal ones by number. One workgroup; count: G numbers of LDS, free again after the call.
+__device__ __forceinline__ void order_groups(const ProductArgs& p, int* count) {
+  for (int g = threadIdx.x; g < p.G; g += kTileThreads) count[g] = p.offsets[g + 1] - p.offsets[g];
+  __syncthreads();
+  for (int g = threadIdx.x; g < p.G; g += kTileThreads) {
+    int rank = 0;
+    for (int o = 0; o < p.G; ++o) rank += count[o] > count[g] || (count[o] == count[g] && o < g) ? 1 : 0;
+    p.order[rank] = g;
+  }
+  __syncthreads();
+}
+
 // kF32 splits the tiles of each XCD's last round over the reduction (tile_job); rows_fixup_kernel adds them.
 template <int EPI>
 __global__ __launch_bounds__(kTileThreads) void rows_kernel(const ProductArgs p) {
   __shared__ TileLds lds;
   const int lane = threadIdx.x & 63, wn = (threadIdx.x >> 6) % 4;
   const int mt_live = p.tile_off[p.G], nkf = p.K / kTileK;
+  if (EPI == kSwiglu && blockIdx.x == gridDim.x - 1) order_groups(p, reinterpret_cast<int*>(&lds));   // (it has no tile)
   TileJob job;
   if (!tile_job(static_cast<int>(blockIdx.x), mt_live * p.n_tiles, p.cu_xcd, nkf, EPI == kF32 && tail_splittable(nkf), job))
     return;
@@ -271,8 +284,7 @@ __device__ __forceinline__ void dma16s(uint32_t m0v, i32x4 rsrc, uint32_t voff, 
 // An offset behind any buffer: operands hold fewer than 2^31 elements in rows of whole 128 bytes.
 constexpr uint32_t kPast = 0xfffffff0u;
 
-// For every group with rows the [M, N] product over its rows of the K-major A [rows, M] and B [rows, N], in bf16; the
-// matrices of groups without rows are zeroed on the side, where these are not the most (zero_unused_kernel).
+// For every group the [M, N] product over its rows of the K-major A [rows, M] and B [rows, N], in bf16; zeros without rows.
 // A workgroup of four wavefronts owns 128 x 256 results (64 x 128 a wavefront) and runs over chunks of 32 rows, the next
 // one on its way to LDS (48 KB, two buffers) while one is multiplied. Nothing within a workgroup hides a barrier, a first
 // load or the end of a tile; the two other workgroups of the CU do (168 registers each). Against the 256 x 256 pipeline of
@@ -286,8 +298,9 @@ constexpr uint32_t kPast = 0xfffffff0u;
 // by descending rows, so that all XCDs have the same work and no long reduction starts late. With a range of consecutive
 // tiles for each XCD instead, the XCD with the shared experts' tiles decided (DeepSeek-shaped, 4096 tokens, two
 // products 1307 us instead of 790, on the 256 x 256 tiles of gemm_tile.hpp).
-__device__ __forceinline__ bool zeros_in_wgrad(int G, int n_active) { return G - n_active <= n_active; }
-
+// The tiles of groups without rows are spread evenly among the others, so that their stores pass beside products
+// (DeepSeek-shaped, 8 tokens, about half the experts empty, both products 205 us; every tile with rows zeroing a slice of
+// every empty matrix: 290; a launch of its own behind them costs at least its start, 5).
 __host__ __device__ __forceinline__ int dealt_piece(int per) { return per < 8 ? 1 : per / 8; }
 
 // The operand that is one row per token (kByTokenA: A, the cotangent; kByTokenB: B, the tokens) is read through row_tok, eight
@@ -298,14 +311,34 @@ template <int BY>
 __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p) {
   __shared__ u32x4 lds[2][3 * kHalf];   // [buffer][A, the two halves of B]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
-  const int n_active = p.n_active[0], per = p.mt_max * p.n_tiles, live = n_active * per;
+  const int n_active = p.n_active[0], per = p.mt_max * p.n_tiles, total = p.G * per, empty = total - n_active * per;
   const int piece = dealt_piece(per), local = blockIdx.x >> 3;
   const int lid = (local / piece * 8 + static_cast<int>(blockIdx.x & 7)) * piece + local % piece;
-  if (lid >= live) return;
-  const int g = p.order[lid / per];
-  int mt, nt;
-  grouped_tile_coords(lid % per, p.mt_max, p.n_tiles, mt, nt);
-  const int r0 = p.offsets[g], nrows = p.offsets[g + 1] - r0, m0 = mt * kM, n0 = nt * kN;
+  if (lid >= total) return;
+  const size_t mn = static_cast<size_t>(p.M) * p.N;
+  auto matrix = [&](int e) { return e < p.E ? static_cast<uint16_t*>(p.c) + e * mn : static_cast<uint16_t*>(p.cs) + (e - p.E) * mn; };
+  int t = lid, mt, nt;
+  if (empty > 0) {
+    auto before = [&](int i) { return static_cast<int>(static_cast<uint64_t>(i) * static_cast<uint64_t>(empty) / static_cast<uint64_t>(total)); };
+    const int z = before(lid);
+    if (before(lid + 1) > z) {   // the z-th tile of groups without rows
+      grouped_tile_coords(z % per, p.mt_max, p.n_tiles, mt, nt);
+      uint16_t* out = matrix(p.order[n_active + z / per]);
+      const int col = nt * kN + (tid & 31) * 8;
+#pragma unroll
+      for (int q = 0; q < kM / 8; ++q) {
+        const int row = mt * kM + (tid >> 5) + 8 * q;
+        if (row < p.M && col < p.N)
+          __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>(out + static_cast<size_t>(row) * p.N + col));
+      }
+      return;
+    }
+    t -= z;
+  }
+  const int g = __builtin_amdgcn_readfirstlane(p.order[t / per]);   // (order is not const: a vector load)
+  grouped_tile_coords(t % per, p.mt_max, p.n_tiles, mt, nt);
+  const int r0 = __builtin_amdgcn_readfirstlane(p.offsets[g]), nrows = __builtin_amdgcn_readfirstlane(p.offsets[g + 1]) - r0;
+  const int m0 = mt * kM, n0 = nt * kN;
   const int lda = 2 * p.lda, ldb = 2 * p.ldb;
   // rows past the group's end read as zeros: they lie behind the buffer of the operand in rows, and are given an offset
   // behind that of the gathered one (tokens ld: below 2^32 - 128)
@@ -400,8 +433,6 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
   }
   wait_vmcnt<0>();
   tile_barrier();
-  const size_t mn = static_cast<size_t>(p.M) * p.N;
-  auto matrix = [&](int e) { return e < p.E ? static_cast<uint16_t*>(p.c) + e * mn : static_cast<uint16_t*>(p.cs) + (e - p.E) * mn; };
   uint16_t* out = matrix(g);
   // [64 rows][256 columns] as bf16, column c of row r at c ^ 32 (r >> 2 & 1): the two halves of a wavefront, four rows
   // apart, write different banks. Staged row 32 wm + r: tile row 64 wm + 32 i + r.
@@ -427,29 +458,6 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
     wait_lgkmcnt0();
     tile_barrier();
   }
-  if (n_active == p.G || !zeros_in_wgrad(p.G, n_active)) return;
-  const size_t n = mn / 8, i0 = n * lid / live, i1 = n * (lid + 1) / live;   // this tile's slice of every empty matrix
-  for (int e = 0; e < p.G; ++e) {
-    if (p.offsets[e + 1] > p.offsets[e]) continue;
-    f32x4* dst = reinterpret_cast<f32x4*>(matrix(e));
-    for (size_t i = i0 + tid; i < i1; i += kThreads) __builtin_nontemporal_store(f32x4{0.f, 0.f, 0.f, 0.f}, dst + i);
-  }
-}
-
-// Zeros the two gradients of the groups without rows (n: 16-byte pieces of a down matrix; gate / up has twice as many)
-// where they are more than those with. Grid (G, chunks).
-__global__ __launch_bounds__(kThreads) void zero_unused_kernel(const int32_t* __restrict__ offsets,
-                                                              const int32_t* __restrict__ n_active, int E, size_t n,
-                                                              u32x4* __restrict__ down, u32x4* __restrict__ s_down,
-                                                              u32x4* __restrict__ gate_up, u32x4* __restrict__ s_gate_up) {
-  const int g = blockIdx.x;
-  if (zeros_in_wgrad(gridDim.x, n_active[0]) || offsets[g + 1] > offsets[g]) return;
-  const u32x4 zero = {0, 0, 0, 0};
-  u32x4* dn = g < E ? down + g * n : s_down + (g - E) * n;
-  u32x4* gu = g < E ? gate_up + g * 2 * n : s_gate_up + (g - E) * 2 * n;
-  const size_t step = static_cast<size_t>(gridDim.y) * kThreads, first = static_cast<size_t>(blockIdx.y) * kThreads + threadIdx.x;
-  for (size_t i = first; i < n; i += step) dn[i] = zero;
-  for (size_t i = first; i < 2 * n; i += step) gu[i] = zero;
 }
 
 template <class T>
@@ -490,7 +498,7 @@ hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s)
   p.b = a.w_down; p.bs = a.ws_down; p.K = a.d; p.N = a.F; p.ldb = a.F;   // W_down [d, F]: K-major
   p.codes = a.codes;
   p.scales = a.scales;
-  p.row_gate = a.row_gate;
+  p.row_gate = a.pb.row_gate;
   p.gh = a.gh;
   p.dgate_part = a.dgate_part;
   p.c = a.dab;
@@ -518,11 +526,7 @@ hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s)
     err = launch_wgrad<kByTokenA>(p, a.dy, a.d, a.gh, a.F, a.d_w_down, a.d_ws_down, s);
     if (err == hipSuccess) err = launch_wgrad<kByTokenB>(p, a.dab, 2 * a.F, a.x, a.d, a.d_w_gate_up, a.d_ws_gate_up, s);
   }
-  if (err != hipSuccess) return err;
-  auto u = [](void* q) { return static_cast<u32x4*>(q); };
-  hipLaunchKernelGGL(zero_unused_kernel, dim3(a.G, 64), dim3(kThreads), 0, s, a.pb.offsets, a.pb.n_active, a.E,
-                     static_cast<size_t>(a.F) * a.d / 8, u(a.d_w_down), u(a.d_ws_down), u(a.d_w_gate_up), u(a.d_ws_gate_up));
-  return hipGetLastError();
+  return err;
 }
 
 }  // namespace maskmoe
