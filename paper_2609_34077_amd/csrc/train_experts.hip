@@ -45,6 +45,8 @@ struct TokenSumArgs {
   const float* dgate_part;  // [rows, parts]
   float* d_gate;            // [T, K] or null
   int T, K, KS, G, d, parts;
+  int split;                // v [split][rows, d]: parts of each row's values
+  size_t part_stride;
   unsigned sum_blocks;
 };
 constexpr int sum_columns(int U) { return U < 8 ? 8 : 4; }
@@ -71,25 +73,27 @@ __global__ __launch_bounds__(kThreads) void token_sum_kernel(const TokenSumArgs 
   for (int k0 = 0; k0 < p.KS; k0 += U) {
     int row[U];
     float g[U];
-    f32x4 o[U][C / 4];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = t * p.KS + min(k0 + u, p.KS - 1);
       row[u] = k0 + u < p.KS ? entry_row(p.idx, p.inv, j, p.G) : -1;
       g[u] = p.gate ? p.gate[j] : 1.0f;
     }
+    for (int z = 0; z < p.split; ++z) {
+      f32x4 o[U][C / 4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (row[u] < 0) continue;
-      const f32x4* v = reinterpret_cast<const f32x4*>(p.v + static_cast<size_t>(row[u]) * p.d + c);
+      for (int u = 0; u < U; ++u) {
+        if (row[u] < 0) continue;
+        const f32x4* v = reinterpret_cast<const f32x4*>(p.v + z * p.part_stride + static_cast<size_t>(row[u]) * p.d + c);
 #pragma unroll
-      for (int q = 0; q < C / 4; ++q) o[u][q] = C == 4 ? __builtin_nontemporal_load(v + q) : v[q];
+        for (int q = 0; q < C / 4; ++q) o[u][q] = C == 4 ? __builtin_nontemporal_load(v + q) : v[q];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (row[u] >= 0)
+#pragma unroll
+          for (int e = 0; e < C; ++e) s[e] += g[u] * o[u][e / 4][e % 4];
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (row[u] >= 0)
-#pragma unroll
-        for (int e = 0; e < C; ++e) s[e] += g[u] * o[u][e / 4][e % 4];
   }
   if constexpr (C == 8) store_vec8<true>(p.out, 8 * i, s);
   else *reinterpret_cast<uint2*>(p.out + 4 * i) = make_uint2(f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3]));
@@ -203,8 +207,9 @@ ExpertsTrainLayout experts_train_layout(int T, int d, int F, int E, int K, int n
   w.order = take(G * 4);
   w.gh = take(rows * F * 2);
   w.dab = take(rows * 2 * F * 2);
-  w.dxr = take(rows * d * 4);
-  w.dgate_part = take(rows * dgate_parts(F) * 4);
+  const bool thin = thin_rows(T, F, E, K, n_shared);
+  w.dxr = take(rows * d * 4 * (thin ? thin_split(T, d, F, E, K, n_shared) : 1));
+  w.dgate_part = take(rows * dgate_parts(F, thin) * 4);
   w.backward_total = off;
   return w;
 }
@@ -233,6 +238,7 @@ hipError_t launch_experts_train(const ExpertsTrainArgs& a, void* workspace, hipS
   if (err != hipSuccess) return err;
   TokenSumArgs sum{};
   sum.v = O;
+  sum.split = 1;
   sum.idx = g.idx;
   sum.gate = g.gate;
   sum.inv = g.pb.inv;
@@ -259,7 +265,8 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   const ExpertsTrainLayout w = experts_train_layout(a.T, a.d, a.F, a.E, a.K, a.n_shared);
   char* ws = static_cast<char*>(workspace);
   Grouping g;
-  hipError_t err = group_rows(a, w, ws, kGemmBM, reinterpret_cast<float*>(ws + w.row_gate), g, stream);
+  const bool thin = thin_rows(a.T, a.F, a.E, a.K, a.n_shared);
+  hipError_t err = group_rows(a, w, ws, thin ? 64 : kGemmBM, reinterpret_cast<float*>(ws + w.row_gate), g, stream);
   if (err != hipSuccess) return err;
   KeptBwdArgs k{};
   k.w_gate_up = a.w_gate_up;
@@ -281,7 +288,9 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   k.d_w_down = b.d_w_down;
   k.d_ws_gate_up = b.d_ws_gate_up;
   k.d_ws_down = b.d_ws_down;
-  k.T = a.T; k.d = a.d; k.F = a.F; k.E = a.E; k.G = g.G; k.max_tiles = g.max_tiles;
+  k.T = a.T; k.d = a.d; k.F = a.F; k.E = a.E; k.G = g.G; k.max_tiles = g.max_tiles; k.rows = g.rows;
+  k.thin = thin;
+  k.split = thin ? thin_split(a.T, a.d, a.F, a.E, a.K, a.n_shared) : 1;
   if (b.x_codes) {   // the values of x's blocks, which bf16 holds exactly
     uint16_t* x = reinterpret_cast<uint16_t*>(ws + w.x);
     err = launch_mx8_dequantize(true, b.x_codes, b.x_scales, a.T, a.d, x, stream);
@@ -308,7 +317,9 @@ hipError_t launch_experts_backward(const ExpertsBwdArgs& b, void* workspace, hip
   sum.out = b.d_x;
   sum.dgate_part = k.dgate_part;
   sum.d_gate = b.d_gate;
-  sum.T = a.T; sum.K = a.K; sum.KS = g.KS; sum.G = g.G; sum.d = a.d; sum.parts = dgate_parts(a.F);
+  sum.T = a.T; sum.K = a.K; sum.KS = g.KS; sum.G = g.G; sum.d = a.d; sum.parts = dgate_parts(a.F, thin);
+  sum.split = k.split;
+  sum.part_stride = static_cast<size_t>(g.rows) * a.d;
   return launch_token_sum(sum, stream);
 }
 

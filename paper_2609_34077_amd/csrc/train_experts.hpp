@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "kernels.hpp"
 
 namespace maskmoe {
@@ -60,12 +62,29 @@ struct KeptBwdArgs {
   float* dgate_part;          // [rows, dgate_parts(F)]
   void *d_w_gate_up, *d_w_down, *d_ws_gate_up, *d_ws_down;
   float* part;                // kTailPartBytes
-  int T, d, F, E, G, max_tiles;
+  int T, d, F, E, G, max_tiles, rows;
+  bool thin;                  // thin_rows: row tiles of 64, dxr in split parts
+  int split;
 };
+// Whether the products of rows and weights run on thin_rows_kernel's tiles: where an expert has few rows, the weights' bytes
+// decide; where the wide tiles are fewer than the CUs, their number. Kernels of the whole gradient in us, wide / thin tiles:
+// Mixtral-shaped 64 tokens 1363 / 1170, 160 (40 rows an expert) 1478 / 1255, 250 (63) 1574 / 1602, 333 1701 / 2027;
+// DeepSeek-shaped 8 tokens 391 / 332, 333 (31) 586 / 506, 600 (56) 703 / 662, 700 (66) 743 / 754; d 256, F 512, 8 experts of
+// 2 a token, 333 tokens (22 wide tiles in the first product) 58 / 39, 8000 (140) 204 / 183, 16000 (266) 319 / 322, 32000 541 / 606.
+inline bool thin_rows(int T, int F, int E, int K, int n_shared) {
+  const int64_t entries = static_cast<int64_t>(T) * K;
+  const int64_t wide = (entries / 256 + std::min<int64_t>(E, entries) + static_cast<int64_t>(n_shared) * ((T + 255) / 256)) * ((F + 255) / 256);
+  return entries <= int64_t{56} * E || wide < 256;
+}
+// Parts of d_x's reduction then: enough workgroups for a few rounds, 16 chunks of 32 each at least.
+inline int thin_split(int T, int d, int F, int E, int K, int n_shared) {
+  const int64_t tiles = (std::min<int64_t>(static_cast<int64_t>(T) * K, E) + static_cast<int64_t>(n_shared) * ((T + 63) / 64)) * ((d + 127) / 128);
+  return static_cast<int>(std::max<int64_t>(1, std::min({int64_t{8}, 4096 / std::max<int64_t>(tiles, 1), static_cast<int64_t>(2 * F / 512)})));
+}
 // Whether the weight gradients read dy and x from rows gathered for them. Reading them by token costs the products 4 %
 // (Mixtral-shaped, 8192 tokens, 4810 -> 5020 us; DeepSeek-shaped, 4096 tokens, 735 -> 755), the gathering 80 and 72 us there.
 inline bool gather_rows(int F) { return F >= 4096; }
-inline int dgate_parts(int F) { return (F + 255) / 256; }
+inline int dgate_parts(int F, bool thin) { return thin ? (F + 127) / 128 : (F + 255) / 256; }
 hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t stream);
 
 }  // namespace maskmoe

@@ -1,11 +1,12 @@
 // The products of the experts' gradient (train_experts.hip): with rows grouped by expert,
-//   u = dy W_down  ->  da, db, g h, <u, h>   (rows_kernel<kSwiglu>)
-//   d_x rows = [da db] W_gate_up             (rows_kernel<kF32>)
+//   u = dy W_down  ->  da, db, g h, <u, h>   (rows_kernel<kSwiglu>, thin_rows_kernel<kSwiglu>)
+//   d_x rows = [da db] W_gate_up             (rows_kernel<kF32>, thin_rows_kernel<kF32>)
 //   dW_down = dy^T (g h),  dW_gate_up = [da db]^T x   (wgrad_kernel)
 // on v_mfma_f32_32x32x16_bf16, fp32 sums. Operands whose reduction index is strided in memory (the weights; both of a
 // weight gradient) are loaded as they lie and turned by transposing LDS reads.
 //
-// Rows times weights run on the 256 x 256 pipeline of gemm_tile.hpp, whose A operand is read in pieces of 128 bytes a row; a
+// Rows times weights run on tiles of 64 x 128 where the weights' bytes bound them (thin_rows, which says when), else on the
+// 256 x 256 pipeline of gemm_tile.hpp, whose A operand is read in pieces of 128 bytes a row; a
 // group's last row tile multiplies its 64-row pieces that hold rows only. On wgrad_kernel's form, which would read 64 bytes
 // of a row at a time, they were slower from about 1000 tokens on (Mixtral-shaped, 8192 tokens, 1820 -> 2160 and 2980 -> 5020 us).
 // Weight gradients, whose operands are both strided, run on tiles of their own, three workgroups a CU (wgrad_kernel).
@@ -41,6 +42,9 @@ struct ProductArgs {
   int G, E, M, N, K, lda, ldb, mt_max, n_tiles;
   int cu_xcd;                 // rows: workgroups an XCD runs at once
   int tokens;                 // wgrad: rows of the gathered operand
+  int a_rows;                 // thin: rows of a
+  int split;                  // thin, kF32: parts of the reduction, c [split][rows, N]
+  size_t part_stride;         // thin, kF32: elements of a part of c
 };
 
 // ---------------------------------------------------------------- rows times a matrix of their expert
@@ -72,17 +76,57 @@ __device__ __forceinline__ int staged_tile_row(int pr, int h) {
   return i < TM ? (pr >> 6) * 32 * TM + i * 32 + (pr & 31) : 64 * TM;
 }
 
-// Sum over each half of the wavefront, in its last lane.
+// da, db and g h of eight columns and their share of <u, h>, from u's v and the blocks' codes and scales.
+struct SwigluPiece {
+  float dot;
+  u32x4 da, db, gh;
+};
+__device__ __forceinline__ SwigluPiece swiglu_piece(const float (&v)[8], uint2 a8, uint2 b8, uint32_t sa, uint32_t sb, float gate) {
+  SwigluPiece o;
+  float av[8], bv[8], da[8], db[8], gh[8];
+  const float s_a = mx8_step(sa), s_b = mx8_step(sb);
+  mx8_decode4(a8.x, s_a, av);
+  mx8_decode4(a8.y, s_a, av + 4);
+  mx8_decode4(b8.x, s_b, bv);
+  mx8_decode4(b8.y, s_b, bv + 4);
+  o.dot = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float sg = sigmoid(av[e]), l = av[e] * sg, hv = l * bv[e], gu = gate * v[e];
+    o.dot += v[e] * hv;
+    da[e] = gu * bv[e] * (sg + l - l * sg);   // SiLU' = s + a s (1 - s)
+    db[e] = gu * l;
+    gh[e] = gate * hv;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    o.da[e] = f32x2_to_bf16x2(da[2 * e], da[2 * e + 1]);
+    o.db[e] = f32x2_to_bf16x2(db[2 * e], db[2 * e + 1]);
+    o.gh[e] = f32x2_to_bf16x2(gh[2 * e], gh[2 * e + 1]);
+  }
+  return o;
+}
+__device__ __forceinline__ void store_piece(const ProductArgs& p, const SwigluPiece& o, int row, int col) {
+  const uint32_t N = p.N, at = (static_cast<uint32_t>(row) * (2 * N) + col) * 2;   // bytes, below 2^32
+  char* c = static_cast<char*>(p.c);
+  *reinterpret_cast<u32x4*>(c + at) = o.da;
+  *reinterpret_cast<u32x4*>(c + (at + 2 * N)) = o.db;
+  *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(p.gh) + (static_cast<uint32_t>(row) * N + col) * 2) = o.gh;
+}
+
+// Sum over 16 lanes, in each; over each half of the wavefront, in its last lane.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp_add(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xF, false));
 }
-__device__ __forceinline__ float half_wave_sum(float v) {
+__device__ __forceinline__ float sum_of_16(float v) {
   v = dpp_add<0xB1, 0xF>(v);      // lanes 1 apart
   v = dpp_add<0x4E, 0xF>(v);      // 2 apart
   v = dpp_add<0x141, 0xF>(v);     // mirrored within 8
-  v = dpp_add<0x140, 0xF>(v);     // mirrored within 16
-  return dpp_add<0x142, 0xA>(v);  // lane 15 of rows 0, 2 to rows 1, 3
+  return dpp_add<0x140, 0xF>(v);  // mirrored within 16
+}
+__device__ __forceinline__ float half_wave_sum(float v) {
+  return dpp_add<0x142, 0xA>(sum_of_16(v));   // lane 15 of rows 0, 2 to rows 1, 3
 }
 
 // End of u's tile: da = g u b SiLU'(a), db = g u SiLU(a), g h in bf16, and the tile's share of every row's <u, h>. The tile
@@ -95,7 +139,6 @@ __device__ __forceinline__ void swiglu_epilogue(const ProductArgs& p, const f32x
   constexpr int Q = 8;   // 4096 pieces of eight columns a part
   const int tid = threadIdx.x, cg = (tid & 31) * 8, col = nt * kTileN + cg, cc = min(col, p.N - 8);
   float* stg = reinterpret_cast<float*>(&L);
-  char* o = static_cast<char*>(p.c);
   const uint32_t N = p.N;
   const int end = min(row_end, row0 + 64 * TM);
 #pragma unroll
@@ -125,38 +168,14 @@ __device__ __forceinline__ void swiglu_epilogue(const ProductArgs& p, const f32x
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       const int pr = (tid >> 5) + 16 * q, row = row0 + staged_tile_row<TM>(pr, h);
-      float v[8], av[8], bv[8], da[8], db[8], gh[8];
+      float v[8];
       *reinterpret_cast<f32x4*>(v) = *reinterpret_cast<const f32x4*>(stg + pr * kPitch + cg);
       *reinterpret_cast<f32x4*>(v + 4) = *reinterpret_cast<const f32x4*>(stg + pr * kPitch + cg + 4);
-      const float s_a = mx8_step(sa[q]), s_b = mx8_step(sb[q]);
-      mx8_decode4(a8[q].x, s_a, av);
-      mx8_decode4(a8[q].y, s_a, av + 4);
-      mx8_decode4(b8[q].x, s_b, bv);
-      mx8_decode4(b8[q].y, s_b, bv + 4);
-      float dot = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float sg = sigmoid(av[e]), l = av[e] * sg, hv = l * bv[e], gu = gate[q] * v[e];
-        dot += v[e] * hv;
-        da[e] = gu * bv[e] * (sg + l - l * sg);   // SiLU' = s + a s (1 - s)
-        db[e] = gu * l;
-        gh[e] = gate[q] * hv;
-      }
+      const SwigluPiece o = swiglu_piece(v, a8[q], b8[q], sa[q], sb[q], gate[q]);
       const bool live = row < end && col < p.N;
-      dot = half_wave_sum(live ? dot : 0.0f);
+      const float dot = half_wave_sum(live ? o.dot : 0.0f);
       if ((tid & 31) == 31 && row < end) p.dgate_part[static_cast<uint32_t>(row) * p.n_tiles + nt] = dot;
-      if (!live) continue;
-      u32x4 pa, pb, pg;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        pa[e] = f32x2_to_bf16x2(da[2 * e], da[2 * e + 1]);
-        pb[e] = f32x2_to_bf16x2(db[2 * e], db[2 * e + 1]);
-        pg[e] = f32x2_to_bf16x2(gh[2 * e], gh[2 * e + 1]);
-      }
-      const uint32_t at = (static_cast<uint32_t>(row) * (2 * N) + col) * 2;   // bytes, below 2^32
-      *reinterpret_cast<u32x4*>(o + at) = pa;
-      *reinterpret_cast<u32x4*>(o + (at + 2 * N)) = pb;
-      *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(p.gh) + (static_cast<uint32_t>(row) * N + col) * 2) = pg;
+      if (live) store_piece(p, o, row, col);
     }
   }
 }
@@ -172,9 +191,9 @@ __device__ __forceinline__ int group_of(const int32_t* tile_off, int G, int mt) 
 
 // The groups by descending rows, equal ones by number. One workgroup; count: G numbers of LDS, free again after the call.
 __device__ __forceinline__ void order_groups(const ProductArgs& p, int* count) {
-  for (int g = threadIdx.x; g < p.G; g += kTileThreads) count[g] = p.offsets[g + 1] - p.offsets[g];
+  for (int g = threadIdx.x; g < p.G; g += blockDim.x) count[g] = p.offsets[g + 1] - p.offsets[g];
   __syncthreads();
-  for (int g = threadIdx.x; g < p.G; g += kTileThreads) {
+  for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
     int rank = 0;
     for (int o = 0; o < p.G; ++o) rank += count[o] > count[g] || (count[o] == count[g] && o < g) ? 1 : 0;
     p.order[rank] = g;
@@ -274,9 +293,15 @@ constexpr int kHalf = kChunk * 16;   // 16-byte units of a 128-column half of a 
 // Columns past the matrix are those of the next row, or past the buffer's end and zero: their products are stored nowhere.
 
 // 16 bytes per lane to LDS as dma16b, `step` (wave-uniform) added to the lane's offset; the buffer's end is checked against
-// their sum, so step must lie within the buffer.
+// their sum, so step must lie within the buffer. dma16s_once: for bytes that are read once, past the caches.
 __device__ __forceinline__ void dma16s(uint32_t m0v, i32x4 rsrc, uint32_t voff, uint32_t step) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(m0v), "v"(voff), "s"(rsrc),
+               "s"(step)
+               : "memory", "m0");
+}
+
+__device__ __forceinline__ void dma16s_once(uint32_t m0v, i32x4 rsrc, uint32_t voff, uint32_t step) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" ::"s"(m0v), "v"(voff), "s"(rsrc),
                "s"(step)
                : "memory", "m0");
 }
@@ -460,12 +485,173 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
   }
 }
 
+// ---------------------------------------------------------------- the same products of few rows an expert
+
+// Tiles of 64 x 128, three workgroups a CU, for products that the weights' bytes bound: what counts is how many of them are
+// on their way. A workgroup (four wavefronts of 64 x 32 results) runs over chunks of 32 of the reduction, the next three on
+// their way to LDS: the weights' [32][128] as in wgrad_kernel, the rows' [64][32] with 16-byte unit u of row r at
+// u ^ (r >> 2 & 3), so that 16 lanes of an operand read hit all banks. kF32 cuts the reduction into p.split parts, which the
+// sum over a token's rows adds.
+// Weights of Mixtral shape, 64 tokens: 940 MB in 185 us, 1880 in 328 (5.1 and 5.7 TB/s), on the wide tiles 200 and 448; of
+// DeepSeek shape 69 and 141, wide 89 and 165. With three buffers and four workgroups a CU 204 and 358. Weights that one row
+// tile reads bypass the caches (without that 203 and 345, and the weight gradients behind are slower too); with two row tiles
+// that costs (Mixtral-shaped, 333 tokens, 319 and 620 us; past the caches 421 and 805).
+// Tile order: a range of consecutive tiles for each XCD, the row tiles of one weight tile next to each other.
+constexpr int kThinM = 64, kThinN = 128, kThinBufs = 4;
+constexpr int kThinPitch = kThinN + 4;
+struct ThinLds {
+  u32x4 buf[kThinBufs][kHalf + kThinM * kChunk / 8];   // [buffer][weights, rows]
+};
+static_assert(kThinM * kThinPitch * 4 <= sizeof(ThinLds), "a staged tile fits in LDS");
+
+// swiglu_epilogue for a tile of 64 x 128: 16 lanes a row.
+__device__ __forceinline__ void thin_swiglu_epilogue(const ProductArgs& p, const f32x16 (&acc)[2], int row0, int row_end, int nt,
+                                                     ThinLds& L) {
+  constexpr int Q = 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int cg = (tid & 15) * 8, col = nt * kThinN + cg, cc = min(col, p.N - 8), end = min(row_end, row0 + kThinM);
+  const uint32_t N = p.N;
+  float* stg = reinterpret_cast<float*>(&L);
+  uint2 a8[Q], b8[Q];
+  uint32_t sa[Q], sb[Q];
+  float gate[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int row = min(row0 + (tid >> 4) + 16 * q, end - 1);
+    const uint32_t at = static_cast<uint32_t>(row) * (2 * N) + cc;
+    a8[q] = *reinterpret_cast<const uint2*>(p.codes + at);
+    b8[q] = *reinterpret_cast<const uint2*>(p.codes + at + N);
+    sa[q] = p.scales[at / kMx8Block];
+    sb[q] = p.scales[(at + N) / kMx8Block];
+    gate[q] = p.row_gate[row];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      stg[(32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kThinPitch + wave * 32 + (lane & 31)] = acc[i][r];
+  wait_lgkmcnt0();
+  tile_barrier();
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int pr = (tid >> 4) + 16 * q, row = row0 + pr;
+    float v[8];
+    *reinterpret_cast<f32x4*>(v) = *reinterpret_cast<const f32x4*>(stg + pr * kThinPitch + cg);
+    *reinterpret_cast<f32x4*>(v + 4) = *reinterpret_cast<const f32x4*>(stg + pr * kThinPitch + cg + 4);
+    const SwigluPiece o = swiglu_piece(v, a8[q], b8[q], sa[q], sb[q], gate[q]);
+    const bool live = row < end && col < p.N;
+    const float dot = sum_of_16(live ? o.dot : 0.0f);
+    if ((tid & 15) == 15 && row < end) p.dgate_part[static_cast<uint32_t>(row) * p.n_tiles + nt] = dot;
+    if (live) store_piece(p, o, row, col);
+  }
+}
+
+template <int EPI>
+__global__ __launch_bounds__(kThreads, 3) void thin_rows_kernel(const ProductArgs p) {
+  __shared__ ThinLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  if (EPI == kSwiglu && blockIdx.x == gridDim.x - 1) order_groups(p, reinterpret_cast<int*>(&lds));
+  const int per = p.n_tiles * p.split, live = uniform(p.tile_off[p.G]) * per, share = (live + 7) / 8;
+  const int local = blockIdx.x >> 3, lid = static_cast<int>(blockIdx.x & 7) * share + local;
+  if (local >= share || lid >= live) return;
+  const int g = uniform(group_of(p.tile_off, p.G, lid / per));
+  const int first = uniform(p.tile_off[g]), row_tiles = uniform(p.tile_off[g + 1]) - first, t = lid - first * per;
+  const int nt = t / row_tiles % p.n_tiles, z = t / row_tiles / p.n_tiles;
+  const int row0 = uniform(p.offsets[g]) + t % row_tiles * kThinM, row_end = uniform(p.offsets[g + 1]), n0 = nt * kThinN;
+  const int nk = p.K / kChunk, c0 = nk * z / p.split, nc = nk * (z + 1) / p.split - c0;
+  const int lda = 2 * p.lda, ldb = 2 * p.ldb;
+  const i32x4 ar = buffer_rsrc(p.a, static_cast<uint32_t>(p.a_rows) * static_cast<uint32_t>(lda));
+  const uint16_t* w = g < p.E ? p.b + static_cast<size_t>(g) * p.N * p.K : p.bs + static_cast<size_t>(g - p.E) * p.N * p.K;
+  const i32x4 br = buffer_rsrc(w + static_cast<size_t>(c0) * kChunk * p.ldb + n0,
+                               static_cast<uint32_t>(nc * kChunk) * static_cast<uint32_t>(ldb) - 2u * static_cast<uint32_t>(n0));
+  const int arow = min(row0 + 16 * wave + (lane >> 2), row_end - 1);
+  const uint32_t aoff = static_cast<uint32_t>(p.row_tok ? p.row_tok[arow] : arow) * static_cast<uint32_t>(lda) +
+                        static_cast<uint32_t>(((lane & 3) ^ (lane >> 4 & 3)) * 16 + c0 * kChunk * 2);
+  const int s16 = lane >> 4, kr0 = 8 * wave + s16;
+  const uint32_t boff = static_cast<uint32_t>(kr0 * ldb + 16 * km_unit(lane & 15, s16));
+  constexpr uint32_t kBuf = sizeof(ThinLds) / kThinBufs, kRowsAt = kHalf * 16;
+  const uint32_t base = lds_offset(&lds.buf[0][0]);
+  const bool once = row_tiles == 1;
+  auto load = [&](int c, uint32_t buf) {   // three loads a wavefront, past the end the last chunk again
+    const uint32_t k = static_cast<uint32_t>(min(c, nc - 1)), step = k * kChunk * static_cast<uint32_t>(ldb);
+    dma16s(base + buf + kRowsAt + static_cast<uint32_t>(wave * 1024), ar, aoff, k * kChunk * 2);
+    const uint32_t lb = base + buf + static_cast<uint32_t>(wave * 2048);
+    if (once) {
+      dma16s_once(lb, br, boff, step);
+      dma16s_once(lb + 1024, br, boff + static_cast<uint32_t>(4 * ldb), step);
+    } else {
+      dma16s(lb, br, boff, step);
+      dma16s(lb + 1024, br, boff + static_cast<uint32_t>(4 * ldb), step);
+    }
+  };
+  uint32_t fa[2][2], fb;
+  {
+    const int G = lane >> 4, j = lane & 15, m = lane & 31;
+    fb = base + static_cast<uint32_t>((8 * (G >> 1) + (j >> 2)) * 256 + (2 * (G & 1) + (j >> 1 & 1)) * 16 + (j & 1) * 8 + (wave ^ (j >> 2)) * 64);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        fa[i][kk] = base + kRowsAt + static_cast<uint32_t>((32 * i + m) * 64 + ((2 * kk + (lane >> 5)) ^ (m >> 2 & 3)) * 16);
+  }
+  f32x16 acc[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.0f;
+  load(0, 0);
+  load(1, kBuf);
+  load(2, 2 * kBuf);
+  uint32_t at = 0, next = 3 * kBuf;
+  for (int c = 0; c < nc; ++c) {
+    wait_vmcnt<6>();
+    tile_barrier();   // chunk c is here, and the buffer of the one before it read
+    load(c + 3, next);
+#pragma unroll
+    for (int kk = 0; kk < kChunk / 16; ++kk) {
+      const uint32_t bo = fb + at + kk * 4096;
+      const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)(bo)));
+      const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)(bo + 1024)));
+      const u32x4 b = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const u32x4 a = *(const lds_u32x4*)(size_t)(fa[i][kk] + at);
+        acc[i] = mfma_32x32x16(a, b, acc[i]);
+      }
+    }
+    wait_lgkmcnt0();
+    at = at == (kThinBufs - 1) * kBuf ? 0 : at + kBuf;
+    next = next == (kThinBufs - 1) * kBuf ? 0 : next + kBuf;
+  }
+  wait_vmcnt<0>();
+  tile_barrier();
+  if constexpr (EPI == kSwiglu) {
+    thin_swiglu_epilogue(p, acc, row0, row_end, nt, lds);
+  } else {
+    const int col = n0 + wave * 32 + (lane & 31);
+    float* out = static_cast<float*>(p.c) + static_cast<size_t>(z) * p.part_stride + col;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = row0 + 32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+        if (row < row_end && col < p.N) out[static_cast<size_t>(row) * p.N] = acc[i][r];
+      }
+  }
+}
+
 template <class T>
 T ceil_div(T a, T b) { return (a + b - 1) / b; }
 
 // 8 XCDs x (their largest share of the tiles + tail slices).
 dim3 rows_grid(int max_tiles, int n_tiles) {
   return dim3(static_cast<unsigned>(8 * (ceil_div<int64_t>(static_cast<int64_t>(max_tiles) * n_tiles, 8) + kTailSlotsPerXcd)));
+}
+
+// 8 XCDs x their largest share, and a workgroup without a tile.
+dim3 thin_grid(int max_tiles, int per) {
+  return dim3(static_cast<unsigned>(8 * (ceil_div<int64_t>(static_cast<int64_t>(max_tiles) * per, 8) + 1)));
 }
 
 template <int BY>
@@ -502,18 +688,33 @@ hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s)
   p.gh = a.gh;
   p.dgate_part = a.dgate_part;
   p.c = a.dab;
-  p.n_tiles = ceil_div(p.N, kTileN);
-  hipLaunchKernelGGL(rows_kernel<kSwiglu>, rows_grid(a.max_tiles, p.n_tiles), dim3(kTileThreads), 0, s, p);
+  p.a_rows = a.T;
+  p.split = 1;
+  if (a.thin) {
+    p.n_tiles = ceil_div(p.N, kThinN);
+    hipLaunchKernelGGL(thin_rows_kernel<kSwiglu>, thin_grid(a.max_tiles, p.n_tiles), dim3(kThreads), 0, s, p);
+  } else {
+    p.n_tiles = ceil_div(p.N, kTileN);
+    hipLaunchKernelGGL(rows_kernel<kSwiglu>, rows_grid(a.max_tiles, p.n_tiles), dim3(kTileThreads), 0, s, p);
+  }
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   // rows of d_x = [da db] W_gate_up
   p.a = a.dab; p.row_tok = nullptr; p.lda = 2 * a.F;
   p.b = a.w_gate_up; p.bs = a.ws_gate_up; p.K = 2 * a.F; p.N = a.d; p.ldb = a.d;   // W_gate_up [2F, d]: K-major
   p.c = a.dxr;
-  p.n_tiles = ceil_div(p.N, kTileN);
-  hipLaunchKernelGGL(rows_kernel<kF32>, rows_grid(a.max_tiles, p.n_tiles), dim3(kTileThreads), 0, s, p);
-  if (tail_splittable(p.K / kTileK))
-    hipLaunchKernelGGL(rows_fixup_kernel, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(kTileThreads), 0, s, p);
+  if (a.thin) {
+    p.a_rows = a.rows;
+    p.split = a.split;
+    p.part_stride = static_cast<size_t>(a.rows) * a.d;
+    p.n_tiles = ceil_div(p.N, kThinN);
+    hipLaunchKernelGGL(thin_rows_kernel<kF32>, thin_grid(a.max_tiles, p.n_tiles * p.split), dim3(kThreads), 0, s, p);
+  } else {
+    p.n_tiles = ceil_div(p.N, kTileN);
+    hipLaunchKernelGGL(rows_kernel<kF32>, rows_grid(a.max_tiles, p.n_tiles), dim3(kTileThreads), 0, s, p);
+    if (tail_splittable(p.K / kTileK))
+      hipLaunchKernelGGL(rows_fixup_kernel, dim3(8 * kTailSlotsPerXcd * kTailFixParts), dim3(kTileThreads), 0, s, p);
+  }
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   p.row_tok = a.pb.row_tok;

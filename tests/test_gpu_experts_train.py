@@ -88,7 +88,9 @@ def check(v, x8=False):
 LAYERS = [(1, 64, 64, 1, 1, 0, 0), (1, 128, 192, 8, 2, 0, 0), (2, 192, 64, 4, 2, 1, 1), (5, 256, 320, 16, 6, 2, 0),
           (16, 320, 128, 8, 2, 0, 3), (17, 64, 576, 3, 3, 0, 0), (33, 512, 256, 5, 2, 0, 2), (64, 128, 128, 2, 1, 1, 0),
           (65, 192, 64, 2, 2, 0, 0), (100, 256, 512, 8, 2, 0, 7), (200, 384, 448, 4, 2, 2, 0), (300, 128, 1408, 4, 2, 1, 11),
-          (700, 640, 192, 3, 2, 0, 0), (520, 64, 128, 1, 1, 8, 100)]
+          (700, 640, 192, 3, 2, 0, 0), (520, 64, 128, 1, 1, 8, 100),
+          # enough rows an expert and tiles for the wide ones
+          (400, 64, 8256, 2, 2, 2, 5), (300, 64, 6208, 5, 2, 2, 0)]
 
 
 @pytest.mark.parametrize("x8", [False, True])
@@ -154,7 +156,8 @@ def plain(v, codes, scales, x, idx):
 
 
 @pytest.mark.parametrize("x8", [False, True])
-@pytest.mark.parametrize("T,d,F,E,K,ns,pad", [(3000, 2048, 1408, 64, 6, 2, 100), (700, 4096, 2048, 8, 2, 0, 0),
+@pytest.mark.parametrize("T,d,F,E,K,ns,pad", [(3000, 2048, 1408, 64, 6, 2, 100), (500, 2048, 1408, 64, 6, 2, 3),
+                                              (700, 4096, 2048, 8, 2, 0, 0), (90, 4096, 6208, 8, 2, 0, 0),
                                               (5000, 1024, 4160, 4, 2, 1, 1)])
 def test_larger_layers(T, d, F, E, K, ns, pad, x8):
     """Many tiles, split tail tiles, experts of several row tiles. Independent roundings to bf16 are off by at most
@@ -227,9 +230,9 @@ def test_most_rows(d, F):
     assert rel(kept(codes[rows], scales[rows]), kept(c, s)) <= 2.0 ** -6
 
 
-@pytest.mark.parametrize("T", [3, 90, 600])
-def test_nan_and_infinity_stay_in_their_token(T):
-    v = cuda(make(T, 192, 128, 4, 2, 1, T + 1))
+@pytest.mark.parametrize("T,F", [(3, 128), (90, 128), (600, 128), (600, 8256)])
+def test_nan_and_infinity_stay_in_their_token(T, F):
+    v = cuda(make(T, 192, F, 4, 2, 1, T + 1))
     y0, c0, s0 = forward(v)
     g0 = backward(v, c0, s0)
     x, dy = v["x"].clone(), v["dy"].clone()
@@ -273,7 +276,7 @@ def test_without_d_gate_and_shared_experts_alone():
     check(v)
 
 
-@pytest.mark.parametrize("T,F", [(4, 320), (900, 320), (300, 2048)])
+@pytest.mark.parametrize("T,F", [(4, 320), (900, 320), (300, 2048), (900, 6208)])
 def test_dirty_workspace_streams_and_graphs(T, F):
     """The workspaces' contents do not matter; calls on two streams with workspaces each; captured and replayed with other
     work between; the same bits every time."""
