@@ -11,6 +11,7 @@
 // of a row at a time, they were slower from about 1000 tokens on (Mixtral-shaped, 8192 tokens, 1820 -> 2160 and 2980 -> 5020 us).
 // Weight gradients, whose operands are both strided, run on tiles of their own, three workgroups a CU (wgrad_kernel).
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.hpp"
@@ -38,12 +39,13 @@ struct ProductArgs {
   const float* row_gate;      // [rows]
   uint16_t* gh;               // [rows, N]
   float* dgate_part;          // [rows, n_tiles] shares of <u, h>
-  float* part;                // kF32: partial tiles of split tail tiles (tile_job)
+  float* part;                // kF32: partial tiles of split tail tiles (tile_job); wgrad: of split reductions
   int G, E, M, N, K, lda, ldb, mt_max, n_tiles;
   int cu_xcd;                 // rows: workgroups an XCD runs at once
   int tokens;                 // wgrad: rows of the gathered operand
   int a_rows;                 // thin: rows of a
-  int split;                  // thin, kF32: parts of the reduction, c [split][rows, N]
+  int split;                  // thin, kF32: parts of the reduction, c [split][rows, N]; wgrad: the same, into part from slot0
+  int slot0;
   size_t part_stride;         // thin, kF32: elements of a part of c
 };
 
@@ -328,6 +330,12 @@ constexpr uint32_t kPast = 0xfffffff0u;
 // every empty matrix: 290; a launch of its own behind them costs at least its start, 5).
 __host__ __device__ __forceinline__ int dealt_piece(int per) { return per < 8 ? 1 : per / 8; }
 
+// Where both products have few tiles with long reductions (wgrad_split) a tile's chunks go to p.split workgroups, whose fp32
+// results wgrad_fixup_kernel adds in order (d 256, F 512, 8 experts of 2 a token, 6000 tokens, 94 -> 49 us, 20000 284 -> 94;
+// d 320, F 192, 6 experts of 4 a token, 600 tokens 37 -> 32, 3000 141 -> 41). First chunk of part z:
+__device__ __forceinline__ int part_begin(int chunks, int z, int split) { return chunks * z / split; }
+constexpr int kMaxParts = 8;
+
 // The operand that is one row per token (kByTokenA: A, the cotangent; kByTokenB: B, the tokens) is read through row_tok, eight
 // row numbers a chunk and wavefront by one scalar load, or (kByRows) lies in rows gathered before (gather_rows, which
 // says when).
@@ -337,18 +345,19 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
   __shared__ u32x4 lds[2][3 * kHalf];   // [buffer][A, the two halves of B]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
   const int n_active = p.n_active[0], per = p.mt_max * p.n_tiles, total = p.G * per, empty = total - n_active * per;
-  const int piece = dealt_piece(per), local = blockIdx.x >> 3;
-  const int lid = (local / piece * 8 + static_cast<int>(blockIdx.x & 7)) * piece + local % piece;
+  const int piece = dealt_piece(per), block = blockIdx.x / p.split, z = blockIdx.x % p.split, local = block >> 3;
+  const int lid = (local / piece * 8 + (block & 7)) * piece + local % piece;
   if (lid >= total) return;
   const size_t mn = static_cast<size_t>(p.M) * p.N;
   auto matrix = [&](int e) { return e < p.E ? static_cast<uint16_t*>(p.c) + e * mn : static_cast<uint16_t*>(p.cs) + (e - p.E) * mn; };
   int t = lid, mt, nt;
   if (empty > 0) {
     auto before = [&](int i) { return static_cast<int>(static_cast<uint64_t>(i) * static_cast<uint64_t>(empty) / static_cast<uint64_t>(total)); };
-    const int z = before(lid);
-    if (before(lid + 1) > z) {   // the z-th tile of groups without rows
-      grouped_tile_coords(z % per, p.mt_max, p.n_tiles, mt, nt);
-      uint16_t* out = matrix(p.order[n_active + z / per]);
+    const int e = before(lid);
+    if (before(lid + 1) > e) {   // the e-th tile of groups without rows
+      if (z > 0) return;
+      grouped_tile_coords(e % per, p.mt_max, p.n_tiles, mt, nt);
+      uint16_t* out = matrix(p.order[n_active + e / per]);
       const int col = nt * kN + (tid & 31) * 8;
 #pragma unroll
       for (int q = 0; q < kM / 8; ++q) {
@@ -358,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
       }
       return;
     }
-    t -= z;
+    t -= e;
   }
   const int g = __builtin_amdgcn_readfirstlane(p.order[t / per]);   // (order is not const: a vector load)
   grouped_tile_coords(t % per, p.mt_max, p.n_tiles, mt, nt);
@@ -377,7 +386,8 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
   const uint32_t unit = static_cast<uint32_t>(16 * km_unit(lane & 15, s16));
   const uint32_t aoff = static_cast<uint32_t>(kr0 * lda) + unit, boff = static_cast<uint32_t>(kr0 * ldb) + unit;
   const uint32_t base = lds_offset(&lds[0][0]), dst = base + static_cast<uint32_t>(2 * wave * 1024);
-  const int nc = (nrows + kChunk - 1) / kChunk;
+  const int chunks = (nrows + kChunk - 1) / kChunk, first = part_begin(chunks, z, p.split), nc = part_begin(chunks, z + 1, p.split);
+  if (first == nc) return;   // fewer chunks than parts
   const auto* tok = (const __attribute__((address_space(4))) int32_t*)(p.row_tok + r0 + 8 * wave);   // read by scalar loads
   auto load = [&](int c, uint32_t buf) {   // six loads a wavefront, past the end of the last chunk again
     const int k = min(c, nc - 1) * kChunk;
@@ -451,12 +461,23 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
     wait_lgkmcnt0();
     tile_barrier();   // the chunk is read: its buffer takes the one after the next
   };
-  load(0, 0);
-  for (int c = 0; c < nc; c += 2) {
+  load(first, 0);
+  for (int c = first; c < nc; c += 2) {
     chunk(c, std::integral_constant<uint32_t, 0>{});
     if (c + 1 < nc) chunk(c + 1, std::integral_constant<uint32_t, 1>{});
   }
   wait_vmcnt<0>();
+  if (p.split > 1) {
+    f32x4* out = reinterpret_cast<f32x4*>(p.part) + static_cast<size_t>(p.slot0 + t * p.split + z) * (kM * kN / 4) + wave * 2048 + lane;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          out[((4 * i + j) * 4 + q) * kWave] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    return;
+  }
   tile_barrier();
   uint16_t* out = matrix(g);
   // [64 rows][256 columns] as bf16, column c of row r at c ^ 32 (r >> 2 & 1): the two halves of a wavefront, four rows
@@ -483,6 +504,40 @@ __global__ __launch_bounds__(kThreads, 3) void wgrad_kernel(const ProductArgs p)
     wait_lgkmcnt0();
     tile_barrier();
   }
+}
+
+// Adds the parts of split reductions of both products, in their order. Grid (tiles of a and of b, 8): an accumulator of every
+// wavefront each.
+__global__ __launch_bounds__(kThreads) void wgrad_fixup_kernel(const ProductArgs a, const ProductArgs b) {
+  const int tiles_a = a.G * a.mt_max * a.n_tiles, second = static_cast<int>(blockIdx.x) >= tiles_a;
+  const ProductArgs& p = second ? b : a;
+  const int t = static_cast<int>(blockIdx.x) - (second ? tiles_a : 0), per = p.mt_max * p.n_tiles;
+  if (t >= p.n_active[0] * per) return;
+  const int g = p.order[t / per], chunks = (p.offsets[g + 1] - p.offsets[g] + kChunk - 1) / kChunk;
+  int mt, nt;
+  grouped_tile_coords(t % per, p.mt_max, p.n_tiles, mt, nt);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ij = blockIdx.y;
+  f32x4 v[kMaxParts][4], sum[4] = {};
+#pragma unroll
+  for (int z = 0; z < kMaxParts; ++z) {
+    const bool live = z < p.split && part_begin(chunks, z, p.split) < part_begin(chunks, z + 1, p.split);
+    const f32x4* src = reinterpret_cast<const f32x4*>(p.part) + static_cast<size_t>(p.slot0 + t * p.split + z) * (kM * kN / 4) + wave * 2048 + lane;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[z][q] = live ? src[(ij * 4 + q) * kWave] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+#pragma unroll
+  for (int z = 0; z < kMaxParts; ++z)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] += v[z][q];
+  const size_t mn = static_cast<size_t>(p.M) * p.N;
+  uint16_t* out = g < p.E ? static_cast<uint16_t*>(p.c) + g * mn : static_cast<uint16_t*>(p.cs) + (g - p.E) * mn;
+  const int row0 = mt * kM + (wave >> 1) * 64 + (ij >> 2) * 32 + 4 * (lane >> 5), col = nt * kN + (wave & 1) * 128 + (ij & 3) * 32 + (lane & 31);
+  if (col >= p.N) return;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (row0 + 8 * q + u < p.M) out[static_cast<size_t>(row0 + 8 * q + u) * p.N + col] = f32_to_bf16(sum[q][u]);
 }
 
 // ---------------------------------------------------------------- the same products of few rows an expert
@@ -654,18 +709,28 @@ dim3 thin_grid(int max_tiles, int per) {
   return dim3(static_cast<unsigned>(8 * (ceil_div<int64_t>(static_cast<int64_t>(max_tiles) * per, 8) + 1)));
 }
 
-template <int BY>
-hipError_t launch_wgrad(ProductArgs p, const uint16_t* a, int M, const uint16_t* b, int N, void* c, void* cs, hipStream_t s) {
+void wgrad_args(ProductArgs& p, const uint16_t* a, int M, const uint16_t* b, int N, void* c, void* cs) {
   p.a = a; p.lda = M; p.M = M;
   p.b = b; p.ldb = N; p.N = N;
   p.c = c;
   p.cs = cs;
   p.mt_max = ceil_div(M, kM);
   p.n_tiles = ceil_div(N, kN);
+}
+template <int BY>
+hipError_t launch_wgrad(const ProductArgs& p, hipStream_t s) {
   const int64_t per = static_cast<int64_t>(p.mt_max) * p.n_tiles, piece = dealt_piece(static_cast<int>(per));
   const int64_t pieces = ceil_div(p.G * per, piece);
-  hipLaunchKernelGGL(wgrad_kernel<BY>, dim3(static_cast<unsigned>(ceil_div<int64_t>(pieces, 8) * 8 * piece)), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL(wgrad_kernel<BY>, dim3(static_cast<unsigned>(ceil_div<int64_t>(pieces, 8) * 8 * piece * p.split)), dim3(kThreads), 0, s, p);
   return hipGetLastError();
+}
+
+// Parts of the weight gradients' reductions for `tiles` of both products and groups of about `rows` rows: as the partial
+// tiles' room allows, eight chunks a part at least (four: d 320, F 192, 300 tokens, both products 27 us, with the
+// addition 28).
+int wgrad_split(int64_t tiles, int64_t rows) {
+  constexpr int64_t kSlots = kTailPartBytes / (kM * kN * 4);
+  return static_cast<int>(std::max<int64_t>(1, std::min({int64_t{kMaxParts}, kSlots / tiles, rows / (8 * kChunk)})));
 }
 
 }  // namespace
@@ -720,14 +785,22 @@ hipError_t launch_experts_backward_products(const KeptBwdArgs& a, hipStream_t s)
   p.row_tok = a.pb.row_tok;
   p.tokens = a.T;
   // dW_down [d, F] = dy^T (g h), dW_gate_up [2F, d] = [da db]^T x
+  ProductArgs down = p, up = p;
+  wgrad_args(down, a.dyg ? a.dyg : a.dy, a.d, a.gh, a.F, a.d_w_down, a.d_ws_down);
+  wgrad_args(up, a.dab, 2 * a.F, a.dyg ? a.xg : a.x, a.d, a.d_w_gate_up, a.d_ws_gate_up);
+  const int64_t down_tiles = static_cast<int64_t>(a.G) * down.mt_max * down.n_tiles, up_tiles = static_cast<int64_t>(a.G) * up.mt_max * up.n_tiles;
+  down.split = up.split = wgrad_split(down_tiles + up_tiles, a.G > a.E ? a.T : a.rows / a.E);
+  up.slot0 = static_cast<int>(down_tiles) * down.split;
   if (a.dyg) {
-    err = launch_wgrad<kByRows>(p, a.dyg, a.d, a.gh, a.F, a.d_w_down, a.d_ws_down, s);
-    if (err == hipSuccess) err = launch_wgrad<kByRows>(p, a.dab, 2 * a.F, a.xg, a.d, a.d_w_gate_up, a.d_ws_gate_up, s);
+    err = launch_wgrad<kByRows>(down, s);
+    if (err == hipSuccess) err = launch_wgrad<kByRows>(up, s);
   } else {
-    err = launch_wgrad<kByTokenA>(p, a.dy, a.d, a.gh, a.F, a.d_w_down, a.d_ws_down, s);
-    if (err == hipSuccess) err = launch_wgrad<kByTokenB>(p, a.dab, 2 * a.F, a.x, a.d, a.d_w_gate_up, a.d_ws_gate_up, s);
+    err = launch_wgrad<kByTokenA>(down, s);
+    if (err == hipSuccess) err = launch_wgrad<kByTokenB>(up, s);
   }
-  return err;
+  if (err != hipSuccess || down.split == 1) return err;
+  hipLaunchKernelGGL(wgrad_fixup_kernel, dim3(static_cast<unsigned>(down_tiles + up_tiles), 8), dim3(kThreads), 0, s, down, up);
+  return hipGetLastError();
 }
 
 }  // namespace maskmoe

@@ -89,6 +89,8 @@ LAYERS = [(1, 64, 64, 1, 1, 0, 0), (1, 128, 192, 8, 2, 0, 0), (2, 192, 64, 4, 2,
           (16, 320, 128, 8, 2, 0, 3), (17, 64, 576, 3, 3, 0, 0), (33, 512, 256, 5, 2, 0, 2), (64, 128, 128, 2, 1, 1, 0),
           (65, 192, 64, 2, 2, 0, 0), (100, 256, 512, 8, 2, 0, 7), (200, 384, 448, 4, 2, 2, 0), (300, 128, 1408, 4, 2, 1, 11),
           (700, 640, 192, 3, 2, 0, 0), (520, 64, 128, 1, 1, 8, 100),
+          # long reductions of few weight gradient tiles, with groups of fewer chunks than parts
+          (1500, 64, 64, 2, 2, 0, 200), (1200, 64, 128, 16, 1, 1, 7),
           # enough rows an expert and tiles for the wide ones
           (400, 64, 8256, 2, 2, 2, 5), (300, 64, 6208, 5, 2, 2, 0)]
 
