@@ -110,7 +110,10 @@ def check_forward(v, dtype, eps, residual, mx8, got):
 
 SHAPES = [(1, 1), (1, 4096), (2, 8), (3, 7), (5, 63), (4, 64), (9, 65), (1, 32), (7, 96), (3, 512), (6, 520), (5, 1000),
           (4, 1024), (3, 1025), (33, 2048), (3, 2056), (5, 4096), (4, 4104), (3, 8192), (2, 8193), (2, 16384), (2, 20000),
-          (1, 32768), (2500, 64), (9000, 24), (2100, 544)]
+          (1, 32768), (2500, 64), (9000, 24), (2100, 544),
+          # last pieces that are not whole, in every number of threads a row
+          (3, 9), (2, 15), (3, 511), (3, 513), (4, 1031), (600, 2047), (3, 2049), (3, 4095), (2, 4097), (2, 8191), (2, 16383),
+          (1, 16385), (1, 32767)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -207,6 +210,25 @@ def test_rows_of_zeros_infinities_and_nan():
         assert (y[3] == 0).all() and y[4:].isfinite().all()
         y0 = L.maskmoe_norm_forward(x.cuda(), w.cuda(), eps=0.0)[0].cpu()
         assert y0[0].isnan().all() and y0[4:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_infinities_and_nan_near_the_end_of_odd_rows(dtype):
+    """The last eight columns of a row are in two pieces: each counts once."""
+    x = torch.randn((5, 251), generator=torch.Generator().manual_seed(2)).to(dtype)
+    x[1, 245], x[2, 246], x[3, 250] = float("inf"), float("nan"), float("-inf")
+    w = torch.ones(251, dtype=dtype)
+    y = L.maskmoe_norm_forward(x.cuda(), w.cuda())[0].cpu()
+    assert y[2].isnan().all() and y[[0, 4]].isfinite().all()
+    for r, c in ((1, 245), (3, 250)):
+        rest = torch.arange(251) != c
+        assert y[r, c].isnan() and (y[r, rest] == 0).all()
+    dy = torch.randn((5, 251), generator=torch.Generator().manual_seed(3)).to(dtype)
+    dy[0, 244] = float("nan")
+    x[1:4] = 1
+    d_x, d_w = (t.cpu() for t in L.maskmoe_norm_backward(x.cuda(), w.cuda(), dy.cuda()))
+    assert d_x[0].isnan().all() and d_x[1:].isfinite().all()
+    assert d_w[244].isnan() and d_w[torch.arange(251) != 244].isfinite().all()
 
 
 def test_nothing_and_no_tokens():
