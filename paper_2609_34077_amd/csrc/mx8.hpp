@@ -48,6 +48,14 @@ __device__ __forceinline__ uint32_t mx8_codes4(const float* v, float inverse_ste
   return lo | hi;
 }
 
+// The same for v + rest, |rest| at most half a step of v's last bit: v's distance from its code (exact) and the rest say
+// whether the next code is nearer.
+__device__ __forceinline__ uint32_t mx8_code(float v, float rest, float inverse_step) {
+  constexpr float kMagic = 12582912.0f;
+  const float t = v * inverse_step, q = t + kMagic, off = __builtin_fmaf(rest, inverse_step, t - (q - kMagic));
+  return __float_as_uint(__builtin_amdgcn_fmed3f(q + ((off + kMagic) - kMagic), kMagic - 127.0f, kMagic + 127.0f));
+}
+
 // N values of one block (or more of it in other lanes, `byte` being the whole block's) to N / 4 dwords of codes; 0 for a
 // block of byte 255. The values are clobbered.
 template <int N>
@@ -56,6 +64,21 @@ __device__ __forceinline__ void mx8_encode(float* v, uint32_t byte, uint32_t* co
   const float inv = mx8_inverse_step(byte);
 #pragma unroll
   for (int i = 0; i < N / 4; ++i) codes[i] = byte == 255 ? 0u : mx8_codes4(v + 4 * i, inv);
+}
+
+// The same for v + rest.
+template <int N>
+__device__ __forceinline__ void mx8_encode(float* v, float* rest, uint32_t byte, uint32_t* codes) {
+  mx8_lift<N>(v, byte);
+  mx8_lift<N>(rest, byte);
+  const float inv = mx8_inverse_step(byte);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = mx8_code(v[4 * i + j], rest[4 * i + j], inv);
+    codes[i] = byte == 255 ? 0u : __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000c0cu);
+  }
 }
 
 // The values of four codes (a byte's conversion is one instruction).

@@ -172,14 +172,15 @@ struct Piece {
   }
 };
 
-// 8-bit blocks of a piece, which is clobbered; d % 32 == 0, so a block is whole or past the row: four lanes hold one.
+// 8-bit blocks of a piece v + rest, which is clobbered; d % 32 == 0, so a block is whole or past the row: four lanes hold one.
 template <bool VEC, int N>
-__device__ __forceinline__ void store_blocks(int8_t* codes, uint8_t* scales, size_t row, int d, int p, int lane, float* v) {
+__device__ __forceinline__ void store_blocks(int8_t* codes, uint8_t* scales, size_t row, int d, int p, int lane, float* v,
+                                             float* rest) {
   typedef uint64_t any64 __attribute__((aligned(1)));
   const uint32_t byte = mx8_scale_byte(max_of_4_lanes(max_magnitude<8>(v)));
   const int c = 8 * (p * N + lane);
   uint32_t q[2];
-  mx8_encode<8>(v, byte, q);
+  mx8_encode<8>(v, rest, byte, q);
   if (c >= d) return;
   if constexpr (VEC) *reinterpret_cast<uint2*>(codes + row + c) = make_uint2(q[0], q[1]);
   else *reinterpret_cast<any64*>(codes + row + c) = q[0] | static_cast<uint64_t>(q[1]) << 32;
@@ -220,9 +221,9 @@ __global__ __launch_bounds__(N* kRowsOf<N>) void norm_forward_kernel(const NormA
     if (a.hidden)
 #pragma unroll
       for (int p = 0; p < V; ++p) P::store(a.hidden, row, dl, p, lane, s[p]);
-    // A thread's squares in fp32, their sum over the row in fp64, and the product with the inverse root and the weight by
-    // its fp32 value and remainder: y is off by little more than its rounding, so that 8-bit codes are those of the
-    // formula but within 2^-22 or so of a border.
+    // A thread's squares in fp32, their sum over the row in fp64, the product with the inverse root and the weight by its
+    // fp32 value and remainder, and the blocks from y with its own remainder: codes are then the formula's but within 2^-26 or
+    // so of a border, however long the row. The fp32 value alone gave a code in 10^6 on the other side of its border.
     float part = 0.0f;
 #pragma unroll
     for (int p = 0; p < V; ++p)
@@ -233,18 +234,17 @@ __global__ __launch_bounds__(N* kRowsOf<N>) void norm_forward_kernel(const NormA
     float rstd, rest;
     inverse_root(sum[0] * inv_d + a.eps, rstd, rest);
 #pragma unroll
-    for (int p = 0; p < V; ++p)
+    for (int p = 0; p < V; ++p) {
+      float left[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float n = s[p][j] * rstd, e = __builtin_fmaf(s[p][j], rest, __builtin_fmaf(s[p][j], rstd, -n));
-        s[p][j] = __builtin_fmaf(n, w[p][j], e * w[p][j]);
+        const float n = s[p][j] * rstd, e = __builtin_fmaf(s[p][j], rest, __builtin_fmaf(s[p][j], rstd, -n)) * w[p][j];
+        s[p][j] = __builtin_fmaf(n, w[p][j], e);
+        left[j] = __builtin_fmaf(n, w[p][j], -s[p][j]) + e;
       }
-    if (a.y)
-#pragma unroll
-      for (int p = 0; p < V; ++p) P::store(a.y, row, dl, p, lane, s[p]);
-    if (a.codes)
-#pragma unroll
-      for (int p = 0; p < V; ++p) store_blocks<VEC, N>(a.codes, a.scales, row, dl, p, lane, s[p]);
+      if (a.y) P::store(a.y, row, dl, p, lane, s[p]);
+      if (a.codes) store_blocks<VEC, N>(a.codes, a.scales, row, dl, p, lane, s[p], left);
+    }
   }
 }
 
