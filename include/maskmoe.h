@@ -797,7 +797,7 @@ int maskmoe_experts_forward_train(const maskmoe_layer_desc* desc, const void* x,
  *  d_gate      device [T, K] float or NULL; 0 for entries without an expert.
  *  d_w_gate_up device [E, 2F, d] bf16, d_w_down device [E, d, F] bf16: zero for experts that no entry names.
  *  d_ws_gate_up, d_ws_down: the shared experts', [n_shared, ...]; NULL when n_shared == 0.
- *  workspace   device, maskmoe_experts_backward_workspace_bytes(desc) bytes, as above.
+ *  workspace   device, maskmoe_experts_backward_workspace_bytes(desc) bytes, as above. What T tokens need serves fewer too.
  *  Outputs must not overlap each other or what is read.
  *  Rounding: sums, d_gate and the rows' shares of d_x are fp32; da, db and g h are rounded to bf16 before their products;
  *  outputs are rounded once.

@@ -149,7 +149,24 @@ int maskmoe_experts_forward_train(const maskmoe_layer_desc* desc, const void* x,
 }
 
 size_t maskmoe_experts_backward_workspace_bytes(const maskmoe_layer_desc* desc) {
-  return check_train(desc) == MASKMOE_OK ? train_layout(*desc).backward_total : 0;
+  if (check_train(desc) != MASKMOE_OK) return 0;
+  const maskmoe_layer_desc& d = *desc;
+  // Fewer tokens may take more room (thin_rows, thin_split: both fall as T grows): the largest need of up to T tokens is at
+  // T or at the last one that has some number of parts.
+  size_t need = train_layout(d).backward_total;
+  for (int parts = 1; parts <= maskmoe::kThinMaxSplit; ++parts) {
+    int32_t lo = 0, hi = d.T;   // with 0 tokens nothing is needed
+    while (lo < hi) {
+      const int32_t t = hi - (hi - lo) / 2;
+      if (maskmoe::thin_rows(t, d.F, d.E, d.K, d.n_shared) && maskmoe::thin_split(t, d.d, d.F, d.E, d.K, d.n_shared) >= parts) lo = t;
+      else hi = t - 1;
+    }
+    maskmoe_layer_desc fewer = d;
+    fewer.T = lo;
+    const size_t n = train_layout(fewer).backward_total;
+    need = n > need ? n : need;
+  }
+  return need;
 }
 
 int maskmoe_experts_backward(const maskmoe_layer_desc* desc, const void* x, const uint8_t* x_scales,

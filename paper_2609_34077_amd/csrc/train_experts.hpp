@@ -76,10 +76,11 @@ inline bool thin_rows(int T, int F, int E, int K, int n_shared) {
   const int64_t wide = (entries / 256 + std::min<int64_t>(E, entries) + static_cast<int64_t>(n_shared) * ((T + 255) / 256)) * ((F + 255) / 256);
   return entries <= int64_t{56} * E || wide < 256;
 }
+constexpr int kThinMaxSplit = 8;
 // Parts of d_x's reduction then: enough workgroups for a few rounds, 16 chunks of 32 each at least.
 inline int thin_split(int T, int d, int F, int E, int K, int n_shared) {
   const int64_t tiles = (std::min<int64_t>(static_cast<int64_t>(T) * K, E) + static_cast<int64_t>(n_shared) * ((T + 63) / 64)) * ((d + 127) / 128);
-  return static_cast<int>(std::max<int64_t>(1, std::min({int64_t{8}, 4096 / std::max<int64_t>(tiles, 1), static_cast<int64_t>(2 * F / 512)})));
+  return static_cast<int>(std::max<int64_t>(1, std::min({int64_t{kThinMaxSplit}, 4096 / std::max<int64_t>(tiles, 1), static_cast<int64_t>(2 * F / 512)})));
 }
 // Whether the weight gradients read dy and x from rows gathered for them. Reading them by token costs the products 4 %
 // (Mixtral-shaped, 8192 tokens, 4810 -> 5020 us; DeepSeek-shaped, 4096 tokens, 735 -> 755), the gathering 80 and 72 us there.

@@ -125,6 +125,14 @@ def test_experts_training_rejects_rows_at_the_end_of_32_bits(call):
         assert call(ok, ws=None) == L.E_WORKSPACE and call(over, ws=None) == L.E_UNSUPPORTED, kw
 
 
+@pytest.mark.parametrize("shape", [dict(d=2048, E=64, K=6, F=1408, n_shared=2), dict(d=4096, E=8, K=2, F=14336, n_shared=0),
+                                   dict(d=256, E=8, K=2, F=512, n_shared=0), dict(d=320, E=5, K=3, F=192, n_shared=1)])
+def test_a_workspace_serves_fewer_tokens(shape):
+    for query in (L.maskmoe_experts_train_workspace_bytes, L.maskmoe_experts_backward_workspace_bytes):
+        sizes = [query(T, **shape) for T in [*range(1, 1500), *range(1500, 9000, 37)]]
+        assert sizes == sorted(sizes)
+
+
 def test_experts_training_rejects_outputs():
     d = L.make_desc(**OK)
     for kw in (dict(y=None), dict(y=FAKE), dict(y=FAKE + 8)):
