@@ -6,7 +6,7 @@
 // Bound by HBM: a row is read once, kept in fp32 registers over its sum, and written once. N threads hold a row in V
 // pieces of 8 elements each; a workgroup has R = threads / N rows at a time and walks over the rest in steps of the
 // grid, its weights in registers. One barrier a step where a row spans wavefronts (the sums alternate between two LDS
-// buffers). bf16, d 4096: 32768 tokens 195 us (5.5 TB/s; a copy moves 4.8), 8192 with blocks 58 (5.2), the gradient of
+// buffers). bf16, d 4096: 32768 tokens 195 us (5.5 TB/s; a copy moves 4.8), 8192 with blocks 59 (5.1), the gradient of
 // 8192 51 (5.3) and 4.9 for the weight's sum.
 
 #include <type_traits>
